@@ -58,7 +58,8 @@ typedef enum {
     FLOWMM_ERR_CUDA = 7,               /* a CUDA runtime call or launch failed */
     FLOWMM_ERR_TIMEOUT = 8,            /* device status: a bounded wait inside a kernel ran out */
     FLOWMM_ERR_UNSUPPORTED_DEVICE = 9,
-    FLOWMM_ERR_INDEX = 10              /* debug build only: an index list or a computed index was out of range */
+    FLOWMM_ERR_INDEX = 10,             /* an index was out of range (index lists: debug build only; pages, slots and rows of the paged cache: always) */
+    FLOWMM_ERR_POOL = 11               /* device status: the page pool, the block table or the slot map had no room for a unit's rows */
 } flowmm_status;
 
 typedef enum { FLOWMM_F32 = 0, FLOWMM_BF16 = 1 } flowmm_dtype;
@@ -283,6 +284,90 @@ typedef struct {
 flowmm_status flowmm_decode_workspace_bytes(const flowmm_decode_params *p, size_t *bytes);
 flowmm_status flowmm_decode_attention(const flowmm_decode_params *p, const void *q, const void *k, const void *v,
                                       float *out, void *ws, size_t ws_bytes, void *cuda_stream);
+
+/*
+ * The paged 8-bit cache: caches of units with lengths of their own, in pages of a common pool, with the decode attention that reads
+ * them.  After compression every sequence keeps its own number of rows, and a decode step is bound by reading K and V: a row is held
+ * in 8 bits instead of 16 or 32, and memory is given out by pages.  A cache is stored (flowmm_cache_store) from what
+ * flowmm_compress_layer wrote or from dense caches, grows by a row a step, is attended to (flowmm_cache_attention) and, when it has
+ * grown, is read back (flowmm_cache_load) for flowmm_recompress.
+ *
+ *   k_pages, v_pages [n_pages, Hkv, page_size, D] e4m3 codes (4 exponent bits of bias 7, 3 mantissa bits, 127 and 255 NaN, no
+ *                    infinity), dense
+ *   k_scale, v_scale [n_pages, Hkv] f32: a code stands for code * scale.  flowmm_cache_store writes powers of two from 2^-96 on;
+ *                    the readers take any positive scale.
+ *   block_table      [U, max_pages] int32: the pages of a unit, in order; entries behind its last page are not read
+ *   rows             [U] int32: rows that a unit holds, 0 to max_pages * page_size
+ *   slots            [U, n_rows] int32: where each new row of a unit goes, page * page_size + place in the page; -1: nowhere
+ *
+ * `ws` as everywhere (flowmm_cache_workspace_bytes, first 256 bytes zeroed once); calls that share one are kept in order.  Page
+ * numbers, slots and rows are checked before use in every build: a bad one sets the device status to FLOWMM_ERR_INDEX, nothing is
+ * read or written out of bounds for it, and the outputs of its unit are not valid.  Heads (at most
+ * 8 query heads a KV head), head_dim and dtype as in flowmm_decode_params.  n_pages * page_size, max_pages * page_size and
+ * n_units * n_rows are below 2^31.
+ */
+typedef struct {
+    int32_t n_units, n_q_heads, n_kv_heads, head_dim;
+    int32_t page_size;                  /* rows of a page: 16, 32, 64 or 128 */
+    int32_t n_pages;                    /* pages of the pool */
+    int32_t max_pages;                  /* entries of a unit in the block table */
+    int32_t n_rows;                     /* slots (plan), rows of k and v (store, load) of a unit */
+    int32_t dtype;                      /* flowmm_dtype of q and of the dense rows */
+    float softmax_scale;                /* 0 selects 1/sqrt(head_dim) */
+    int32_t path;                       /* flowmm_path of the attention */
+    int64_t k_stride[3], v_stride[3];   /* element strides (unit, head, row) of the dense rows */
+} flowmm_cache_params;
+
+flowmm_status flowmm_cache_workspace_bytes(const flowmm_cache_params *p, size_t *bytes);
+
+/*
+ * Block tables and slot maps from the lengths of the requests, on the GPU (a step can be captured in a graph).
+ * Unit u goes from rows[u] to max(0, rows[u] + grow[u]) rows: pages it needs more are taken from the ring of free pages, pages
+ * it needs no longer go back to it (grow = -rows ends a request), the first grow[u] slots say where its new rows go, the others are -1.
+ *   grow, rows [U] int32;  rows_out [U] out
+ *   free_pages [n_pages] int32 in and out, a ring;  free_state {head, count}: the free pages are free_pages[(head + i) % n_pages],
+ *              i < count;  free_state_out [2] out
+ *   block_table in and out: entries of pages taken are written, all others left as they were
+ *   slots [U, n_rows] out, or NULL: then any growth that the table has room for is planned, without slots
+ * Units are served in order, pages in the ring's order; pages given back in a call are not given out in it, and go behind the
+ * free ones, by unit and place.  A unit that asks for more than n_rows slots or max_pages pages, or that comes to need pages when
+ * all units so far have asked for more than are free, is left as it was (rows_out = rows, slots -1) and the status becomes
+ * FLOWMM_ERR_POOL; the others go on.  rows_out and free_state_out are arrays of their own: nothing that a call reads is changed
+ * by it (places of the ring and the table that it writes held nothing), so a step that is not carried out is planned again from
+ * the same rows and free_state.
+ */
+flowmm_status flowmm_cache_plan(const flowmm_cache_params *p, const int32_t *grow, const int32_t *rows, int32_t *rows_out,
+                                int32_t *free_pages, const int32_t *free_state, int32_t *free_state_out, int32_t *block_table,
+                                int32_t *slots, void *ws, size_t ws_bytes, void *cuda_stream);
+
+/*
+ * Rows into pages.  Row t of unit u goes to slots[u][t].  The rows of a unit go to consecutive places (the rest of a page, then
+ * whole pages from their first place on), as flowmm_cache_plan lays them out; -1 only behind the last row.  No page is written for
+ * two units.  Per page, KV head and tensor:
+ *   s = the smallest power of two, 2^-96 at least, with |x| <= 448 s for all finite new rows x of the page; where the page holds
+ *       rows already (the first new row is not at its first place), not below its scale s_old
+ *   new codes = e4m3(x / s), old codes = e4m3(code * s_old / s), round to nearest even; NaN and infinities become NaN
+ * Places behind the new rows are left as they were.  A single new row per unit (n_rows = 1) is the decode step's form.
+ *   k, v [U, Hkv, n_rows, D] with the element strides k_stride, v_stride
+ */
+flowmm_status flowmm_cache_store(const flowmm_cache_params *p, const void *k, const void *v, const int32_t *slots, void *k_pages,
+                                 void *v_pages, float *k_scale, float *v_scale, void *ws, size_t ws_bytes, void *cuda_stream);
+
+/* Pages into rows: k, v [U, Hkv, n_rows, D] out, code * scale rounded once, for the first min(rows[u], n_rows) rows of each unit;
+ * the others are left as they were. */
+flowmm_status flowmm_cache_load(const flowmm_cache_params *p, const void *k_pages, const void *v_pages, const float *k_scale,
+                                const float *v_scale, const int32_t *block_table, const int32_t *rows, void *k, void *v, void *ws,
+                                size_t ws_bytes, void *cuda_stream);
+
+/*
+ * flowmm_decode_attention over the paged cache: o = softmax(q . (k_scale K)^T * scale) (v_scale V) over the rows[u] rows of each
+ * unit, zero for a unit without rows.  What stands behind a unit's last row (codes of NaN too) has no influence.  Several new
+ * queries of a sequence are units that share a row of the block table and differ in rows.
+ *   q [U, Hq, D] dense, element type `dtype`;  out [U, Hq, D] f32
+ */
+flowmm_status flowmm_cache_attention(const flowmm_cache_params *p, const void *q, const void *k_pages, const void *v_pages,
+                                     const float *k_scale, const float *v_scale, const int32_t *block_table, const int32_t *rows,
+                                     float *out, void *ws, size_t ws_bytes, void *cuda_stream);
 
 /* Waits for `cuda_stream`, then returns the device status word at the start of `ws`
  * (FLOWMM_OK, or the first error a kernel recorded) and clears it. */

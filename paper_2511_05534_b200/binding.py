@@ -34,6 +34,7 @@ EXPORTS = (
     "flowmm_full_flow_workspace_bytes", "flowmm_full_flow",
     "flowmm_merge_static_status", "flowmm_merge_static_poke_status",
     "flowmm_recompress_workspace_bytes", "flowmm_recompress", "flowmm_debug_build",
+    "flowmm_cache_workspace_bytes", "flowmm_cache_plan", "flowmm_cache_store", "flowmm_cache_load", "flowmm_cache_attention",
 )
 
 
@@ -164,6 +165,9 @@ def load() -> ctypes.CDLL:
                             ("flowmm_match", [P] * 10 + [N, P]), ("flowmm_merge", [P] * 10 + [N, P]), ("flowmm_merge_static", [P] * 10),
                             ("flowmm_compress_layer", [P] * 15 + [N, P]), ("flowmm_recompress", [P] * 16 + [N, P]),
                             ("flowmm_full_flow", [P] * 9 + [N, P]), ("flowmm_decode_attention", [P] * 6 + [N, P]),
+                            ("flowmm_cache_workspace_bytes", [P] * 2), ("flowmm_cache_plan", [P] * 10 + [N, P]),
+                            ("flowmm_cache_store", [P] * 9 + [N, P]), ("flowmm_cache_load", [P] * 10 + [N, P]),
+                            ("flowmm_cache_attention", [P] * 10 + [N, P]),
                             ("flowmm_last_device_status", [P] * 2), ("flowmm_selftest_wait_timeout", [P] * 2),
                             ("flowmm_merge_static_status", [P]), ("flowmm_merge_static_poke_status", [ctypes.c_int32, P])):
             getattr(lib, name).argtypes = types
@@ -351,6 +355,140 @@ def flowmm_decode_attention(q, k, v, out, ws, softmax_scale: float = 0.0, path: 
                                                     torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()))
     if code != 0:
         raise FlowmmError(code, "flowmm_decode_attention")
+
+
+# ---- paged 8-bit cache ----------------------------------------------------------------------------
+
+class _CCacheParams(ctypes.Structure):
+    _fields_ = [
+        ("n_units", ctypes.c_int32), ("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32), ("page_size", ctypes.c_int32), ("n_pages", ctypes.c_int32),
+        ("max_pages", ctypes.c_int32), ("n_rows", ctypes.c_int32), ("dtype", ctypes.c_int32),
+        ("softmax_scale", ctypes.c_float), ("path", ctypes.c_int32),
+        ("k_stride", ctypes.c_int64 * 3), ("v_stride", ctypes.c_int64 * 3),
+    ]
+
+
+@dataclass
+class CacheParams:
+    """Mirror of flowmm_cache_params; the strides of the dense rows are taken from the tensors each call receives."""
+    n_units: int
+    n_q_heads: int
+    n_kv_heads: int
+    head_dim: int
+    page_size: int
+    n_pages: int
+    max_pages: int
+    n_rows: int = 1
+    dtype: int = BF16
+    softmax_scale: float = 0.0
+    path: int = PATH_AUTO
+
+    def c(self, k=None, v=None) -> _CCacheParams:
+        dense = (self.n_kv_heads * self.n_rows * self.head_dim, self.n_rows * self.head_dim, self.head_dim)
+        cp = _CCacheParams(*_CACHE_FIELDS(self))
+        cp.k_stride = (ctypes.c_int64 * 3)(*(dense if k is None else k.stride()[:3]))
+        cp.v_stride = (ctypes.c_int64 * 3)(*(dense if v is None else v.stride()[:3]))
+        return cp
+
+
+_CACHE_FIELDS = operator.attrgetter("n_units", "n_q_heads", "n_kv_heads", "head_dim", "page_size", "n_pages", "max_pages",
+                                    "n_rows", "dtype", "softmax_scale", "path")
+_CODE_TYPES = (torch.uint8, torch.float8_e4m3fn)
+
+
+def _cache_call(p: CacheParams, what: str, tensors, dense=()):
+    """The call's struct, after a look at what the C side cannot see: the tensors' shapes, types and devices.  `tensors` and `dense`
+    (the rows of K and V, by strides): (name, tensor, shape, types); a tensor may be None where the C entry point takes NULL.
+    Calls alike in all of that are looked at once."""
+    key = (what, _CACHE_FIELDS(p)) + tuple(None if t is None else (t.shape, t.stride(), t.dtype, t.get_device()) for _, t, _, _ in tensors + dense)
+    ref = _structs.get(key)
+    if ref is not None:
+        return ref
+    device = None
+    for name, t, shape, types in tensors + dense:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise ValueError("flowmm takes CUDA tensors")
+        if tuple(t.shape) != shape or t.dtype not in types:
+            raise ValueError("%s: %s must be a %s tensor of shape %s" % (what, name, " or ".join(str(x) for x in types), list(shape)))
+        if device is not None and t.get_device() != device:
+            raise ValueError("%s: %s is on another device than the other tensors" % (what, name))
+        device = t.get_device()
+    for name, t, _, _ in tensors:
+        if t is not None and not t.is_contiguous():
+            raise ValueError("%s: %s must be contiguous" % (what, name))
+    for name, t, _, _ in dense:
+        if t.stride(3) != 1:
+            raise ValueError("%s: %s must have contiguous head_dim" % (what, name))
+    if device != torch.cuda.current_device():
+        raise ValueError("%s: the tensors are not on the current device" % what)
+    return _keep_struct(key, p.c(*(t for _, t, _, _ in dense)))
+
+
+def _pool(p: CacheParams, k_pages, v_pages, k_scale, v_scale):
+    codes, scales = (p.n_pages, p.n_kv_heads, p.page_size, p.head_dim), (p.n_pages, p.n_kv_heads)
+    return (("k_pages", k_pages, codes, _CODE_TYPES), ("v_pages", v_pages, codes, _CODE_TYPES),
+            ("k_scale", k_scale, scales, (torch.float32,)), ("v_scale", v_scale, scales, (torch.float32,)))
+
+
+_INT32, _BYTES = (torch.int32,), (torch.uint8,)
+
+
+def flowmm_cache_workspace_bytes(p: CacheParams) -> int:
+    n = ctypes.c_size_t(0)
+    cp = p.c()
+    _check(load().flowmm_cache_workspace_bytes(ctypes.byref(cp), ctypes.byref(n)), "flowmm_cache_workspace_bytes")
+    return int(n.value)
+
+
+def alloc_cache_workspace(p: CacheParams, device="cuda") -> torch.Tensor:
+    """A workspace of the required size with its status word cleared."""
+    ws = torch.empty(flowmm_cache_workspace_bytes(p), dtype=torch.uint8, device=device)
+    ws[:256].zero_()
+    return ws
+
+
+def flowmm_cache_plan(p: CacheParams, grow, rows, rows_out, free_pages, free_state, free_state_out, block_table, slots, ws):
+    """Pages and slots for units that go from rows to rows + grow rows; slots may be None."""
+    U = p.n_units
+    cp = _cache_call(p, "flowmm_cache_plan", (
+        ("grow", grow, (U,), _INT32), ("rows", rows, (U,), _INT32), ("rows_out", rows_out, (U,), _INT32),
+        ("free_pages", free_pages, (p.n_pages,), _INT32), ("free_state", free_state, (2,), _INT32),
+        ("free_state_out", free_state_out, (2,), _INT32), ("block_table", block_table, (U, p.max_pages), _INT32),
+        ("slots", slots, (U, p.n_rows), _INT32), ("ws", ws, (ws.numel(),), _BYTES)))
+    _check(load().flowmm_cache_plan(cp, _p(grow), _p(rows), _p(rows_out), _p(free_pages), _p(free_state), _p(free_state_out),
+                                    _p(block_table), _p(slots), _p(ws), ws.numel(), _stream()), "flowmm_cache_plan")
+
+
+def flowmm_cache_store(p: CacheParams, k, v, slots, k_pages, v_pages, k_scale, v_scale, ws):
+    """Rows k, v [units, kv_heads, n_rows, head_dim] into pages (uint8 or float8_e4m3fn tensors), as slots says."""
+    rows, types = (p.n_units, p.n_kv_heads, p.n_rows, p.head_dim), (torch_dtype(p.dtype),)
+    cp = _cache_call(p, "flowmm_cache_store", (("slots", slots, (p.n_units, p.n_rows), _INT32),) + _pool(p, k_pages, v_pages, k_scale, v_scale) +
+                     (("ws", ws, (ws.numel(),), _BYTES),), (("k", k, rows, types), ("v", v, rows, types)))
+    _check(load().flowmm_cache_store(cp, _p(k), _p(v), _p(slots), _p(k_pages), _p(v_pages), _p(k_scale), _p(v_scale), _p(ws),
+                                     ws.numel(), _stream()), "flowmm_cache_store")
+
+
+def flowmm_cache_load(p: CacheParams, k_pages, v_pages, k_scale, v_scale, block_table, rows, k, v, ws):
+    """The first min(rows[u], n_rows) rows of every unit into k, v [units, kv_heads, n_rows, head_dim]."""
+    dense, types = (p.n_units, p.n_kv_heads, p.n_rows, p.head_dim), (torch_dtype(p.dtype),)
+    cp = _cache_call(p, "flowmm_cache_load", _pool(p, k_pages, v_pages, k_scale, v_scale) + (
+        ("block_table", block_table, (p.n_units, p.max_pages), _INT32), ("rows", rows, (p.n_units,), _INT32),
+        ("ws", ws, (ws.numel(),), _BYTES)), (("k", k, dense, types), ("v", v, dense, types)))
+    _check(load().flowmm_cache_load(cp, _p(k_pages), _p(v_pages), _p(k_scale), _p(v_scale), _p(block_table), _p(rows), _p(k), _p(v),
+                                    _p(ws), ws.numel(), _stream()), "flowmm_cache_load")
+
+
+def flowmm_cache_attention(p: CacheParams, q, k_pages, v_pages, k_scale, v_scale, block_table, rows, out, ws):
+    """Decode attention over the paged cache; q [units, q_heads, head_dim], out the same in float32."""
+    shape = (p.n_units, p.n_q_heads, p.head_dim)
+    cp = _cache_call(p, "flowmm_cache_attention", (("q", q, shape, (torch_dtype(p.dtype),)),) + _pool(p, k_pages, v_pages, k_scale, v_scale) + (
+        ("block_table", block_table, (p.n_units, p.max_pages), _INT32), ("rows", rows, (p.n_units,), _INT32),
+        ("out", out, shape, (torch.float32,)), ("ws", ws, (ws.numel(),), _BYTES)))
+    _check(load().flowmm_cache_attention(cp, _p(q), _p(k_pages), _p(v_pages), _p(k_scale), _p(v_scale), _p(block_table), _p(rows),
+                                         _p(out), _p(ws), ws.numel(), _stream()), "flowmm_cache_attention")
 
 
 def flowmm_selftest_wait_timeout(ws):

@@ -18,6 +18,8 @@
 #include "match_small_tc.cuh"
 #include "merge_rows.cuh"
 #include "merge_tc.cuh"
+#include "paged_attention.cuh"
+#include "paged_cache.cuh"
 #include "score_cluster_tc.cuh"
 #include "score_fused_tc.cuh"
 #include "match_tc.cuh"
@@ -1059,7 +1061,7 @@ flowmm_status flowmm_last_device_status(void *ws, void *cuda_stream) {
         if (cudaMemsetAsync(ws, 0, sizeof(word), st) != cudaSuccess) return FLOWMM_ERR_CUDA;
         if (cudaStreamSynchronize(st) != cudaSuccess) return FLOWMM_ERR_CUDA;
     }
-    return word >= 0 && word <= FLOWMM_ERR_INDEX ? static_cast<flowmm_status>(word) : FLOWMM_ERR_CUDA;
+    return word >= 0 && word <= FLOWMM_ERR_POOL ? static_cast<flowmm_status>(word) : FLOWMM_ERR_CUDA;
 }
 
 int32_t flowmm_last_launch_count(void) { return g_launches; }
@@ -1106,7 +1108,8 @@ const char *flowmm_status_string(flowmm_status s) {
         case FLOWMM_ERR_CUDA: return "CUDA error";
         case FLOWMM_ERR_TIMEOUT: return "device-side wait timed out";
         case FLOWMM_ERR_UNSUPPORTED_DEVICE: return "device is not compute capability 10.x";
-        case FLOWMM_ERR_INDEX: return "index out of range (debug build)";
+        case FLOWMM_ERR_INDEX: return "index out of range";
+        case FLOWMM_ERR_POOL: return "no room in the page pool, the block table or the slot map";
     }
     return "unknown status";
 }
@@ -1444,6 +1447,219 @@ extern "C" flowmm_status flowmm_decode_attention(const flowmm_decode_params *p, 
     if (p->dtype == FLOWMM_BF16)
         return p->head_dim == 128 ? launch_decode<__nv_bfloat16, 128>(a, uh, n_q, st) : launch_decode<__nv_bfloat16, 64>(a, uh, n_q, st);
     return p->head_dim == 128 ? launch_decode<float, 128>(a, uh, n_q, st) : launch_decode<float, 64>(a, uh, n_q, st);
+}
+
+// ---- paged 8-bit cache ----------------------------------------------------------------------------
+namespace {
+
+flowmm_status validate_cache(const flowmm_cache_params *p) {
+    if (!p) return FLOWMM_ERR_NULL;
+    if (p->n_units < 1 || p->n_q_heads < 1 || p->n_kv_heads < 1) return FLOWMM_ERR_SHAPE;
+    if (p->n_q_heads % p->n_kv_heads != 0 || p->n_q_heads / p->n_kv_heads > 8) return FLOWMM_ERR_SHAPE;
+    if (p->head_dim != 64 && p->head_dim != 128) return FLOWMM_ERR_SHAPE;
+    if (p->page_size != 16 && p->page_size != 32 && p->page_size != 64 && p->page_size != 128) return FLOWMM_ERR_SHAPE;
+    if (p->n_pages < 1 || p->max_pages < 1 || p->n_rows < 0) return FLOWMM_ERR_SHAPE;
+    constexpr int64_t limit = (int64_t)1 << 31;
+    if ((int64_t)p->n_pages * p->page_size >= limit || (int64_t)p->max_pages * p->page_size >= limit || (int64_t)p->n_units * p->n_rows >= limit)
+        return FLOWMM_ERR_SHAPE;
+    if ((int64_t)p->n_units * p->n_kv_heads > kMaxHeadsPerCall) return FLOWMM_ERR_SHAPE;
+    if (p->dtype != FLOWMM_F32 && p->dtype != FLOWMM_BF16) return FLOWMM_ERR_DTYPE;
+    if (!(p->softmax_scale >= 0.f)) return FLOWMM_ERR_SHAPE;
+    if (p->path != FLOWMM_PATH_AUTO && p->path != FLOWMM_PATH_SIMT) return FLOWMM_ERR_SHAPE;
+    return FLOWMM_OK;
+}
+
+int page_shift(int page) { return page == 16 ? 4 : page == 32 ? 5 : page == 64 ? 6 : 7; }
+
+// The attention's cut and scratch: [status word, 256 bytes][tickets][records].
+struct CachePlan {
+    int groups, gp, target;        // groups of query heads that are ranges of their own, heads of one, ranges aimed at
+    int64_t blocks;                // of the launch: no fewer than ranges can come out (paged_attention.cuh)
+    size_t part, total;            // where the records start; bytes
+};
+
+CachePlan cache_plan(const flowmm_cache_params &p) {
+    CachePlan c;
+    const int G = p.n_q_heads / p.n_kv_heads;
+    c.gp = G <= 1 ? 1 : G <= 2 ? 2 : 4;
+    c.groups = (G + c.gp - 1) / c.gp;
+    c.target = 4 * kScoreCtas;
+    const int64_t heads = (int64_t)p.n_units * p.n_kv_heads * c.groups, keys = (int64_t)p.max_pages * p.page_size;
+    c.blocks = std::min(heads * ((keys + paged::kSimtKeys - 1) / paged::kSimtKeys), c.target + heads);
+    c.part = 256 + align256((size_t)heads * sizeof(unsigned long long));
+    c.total = c.part + align256((size_t)c.blocks * c.gp * (p.head_dim + 2) * sizeof(float));
+    return c;
+}
+
+flowmm_status check_cache_ws(const flowmm_cache_params *p, const void *ws, size_t ws_bytes) {
+    if (!ws) return FLOWMM_ERR_NULL;
+    if (reinterpret_cast<uintptr_t>(ws) & 255) return FLOWMM_ERR_ALIGN;
+    return ws_bytes < cache_plan(*p).total ? FLOWMM_ERR_WORKSPACE : FLOWMM_OK;
+}
+
+bool aligned4(const void *ptr) { return (reinterpret_cast<uintptr_t>(ptr) & 3) == 0; }
+
+template <typename T, int D, int kTeam, int kVecs>
+flowmm_status launch_store(const paged::StoreArgs &a, cudaStream_t st) {
+    constexpr int block = kTeam < 128 ? 128 : kTeam, teams = block / kTeam;
+    launch(paged::cache_store_kernel<T, D, kTeam, kVecs>, (a.items + teams - 1) / teams, block, 0, st, a);
+    FLOWMM_LAUNCHED("cache_store");
+    return FLOWMM_OK;
+}
+
+// A team holds its page's rows in registers, 64 elements a thread; pages of 16 rows and calls of at most 16 rows take a warp.
+template <typename T>
+flowmm_status run_store(const flowmm_cache_params &p, const paged::StoreArgs &a, cudaStream_t st) {
+    const int rows = std::min(p.page_size, p.n_rows);
+    if (p.head_dim == 128) {
+        if (rows <= 16) return launch_store<T, 128, 32, 4>(a, st);
+        if (p.page_size == 32) return launch_store<T, 128, 64, 4>(a, st);
+        if (p.page_size == 64) return launch_store<T, 128, 128, 4>(a, st);
+        return launch_store<T, 128, 256, 4>(a, st);
+    }
+    if (rows <= 16) return launch_store<T, 64, 32, 2>(a, st);
+    if (p.page_size == 32) return launch_store<T, 64, 32, 4>(a, st);
+    if (p.page_size == 64) return launch_store<T, 64, 64, 4>(a, st);
+    return launch_store<T, 64, 128, 4>(a, st);
+}
+
+template <typename T>
+flowmm_status run_load(const flowmm_cache_params &p, const paged::LoadArgs &a, int64_t blocks, cudaStream_t st) {
+    if (p.head_dim == 128) launch(paged::cache_load_kernel<T, 128>, (unsigned)blocks, paged::kLoadThreads, 0, st, a);
+    else launch(paged::cache_load_kernel<T, 64>, (unsigned)blocks, paged::kLoadThreads, 0, st, a);
+    FLOWMM_LAUNCHED("cache_load");
+    return FLOWMM_OK;
+}
+
+template <int D>
+flowmm_status launch_cache_attention(const paged::AttnArgs &a, const CachePlan &c, cudaStream_t st) {
+    const unsigned blocks = (unsigned)c.blocks;
+    switch (c.gp) {
+        case 1: launch(paged::cache_attention_kernel<D, 1>, blocks, paged::kSimtThreads, 0, st, a); break;
+        case 2: launch(paged::cache_attention_kernel<D, 2>, blocks, paged::kSimtThreads, 0, st, a); break;
+        default: launch(paged::cache_attention_kernel<D, 4>, blocks, paged::kSimtThreads, 0, st, a); break;
+    }
+    FLOWMM_LAUNCHED("cache_attention");
+    return FLOWMM_OK;
+}
+
+}  // namespace
+
+extern "C" flowmm_status flowmm_cache_workspace_bytes(const flowmm_cache_params *p, size_t *bytes) {
+    if (!bytes) return FLOWMM_ERR_NULL;
+    FLOWMM_TRY(validate_cache(p));
+    *bytes = cache_plan(*p).total;
+    return FLOWMM_OK;
+}
+
+extern "C" flowmm_status flowmm_cache_plan(const flowmm_cache_params *p, const int32_t *grow, const int32_t *rows,
+                                           int32_t *rows_out, int32_t *free_pages, const int32_t *free_state,
+                                           int32_t *free_state_out, int32_t *block_table, int32_t *slots, void *ws,
+                                           size_t ws_bytes, void *cuda_stream) {
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    profile_begin(st);
+    FLOWMM_TRY(validate_cache(p));
+    if (!grow || !rows || !rows_out || !free_pages || !free_state || !free_state_out || !block_table) return FLOWMM_ERR_NULL;
+    if (rows_out == rows || free_state_out == free_state || (slots && p->n_rows < 1)) return FLOWMM_ERR_SHAPE;
+    if (!aligned4(grow) || !aligned4(rows) || !aligned4(rows_out) || !aligned4(free_pages) || !aligned4(free_state) ||
+        !aligned4(free_state_out) || !aligned4(block_table) || !aligned4(slots))
+        return FLOWMM_ERR_ALIGN;
+    FLOWMM_TRY(check_cache_ws(p, ws, ws_bytes));
+    FLOWMM_TRY(check_device());
+    paged::PlanArgs a;
+    a.grow = grow; a.rows = rows; a.rows_out = rows_out; a.ring = free_pages; a.state = free_state; a.state_out = free_state_out;
+    a.table = block_table; a.slots = slots; a.status = static_cast<int *>(ws);
+    a.U = p->n_units; a.T = p->n_rows; a.page = p->page_size; a.page_shift = page_shift(p->page_size);
+    a.n_pages = p->n_pages; a.max_pages = p->max_pages;
+    a.chunks = slots ? (p->n_rows + paged::kPlanChunk - 1) / paged::kPlanChunk : 1;
+    // a warp for every unit and chunk of slots, on as many blocks as there are SMs at most
+    const int64_t items = (int64_t)std::min(p->n_units, paged::kPlanThreads) * a.chunks;
+    const unsigned blocks = (unsigned)std::min<int64_t>(kScoreCtas, (items + paged::kPlanThreads / 32 - 1) / (paged::kPlanThreads / 32));
+    launch(paged::cache_plan_kernel, blocks, paged::kPlanThreads, 0, st, a);
+    FLOWMM_LAUNCHED("cache_plan");
+    return FLOWMM_OK;
+}
+
+extern "C" flowmm_status flowmm_cache_store(const flowmm_cache_params *p, const void *k, const void *v, const int32_t *slots,
+                                            void *k_pages, void *v_pages, float *k_scale, float *v_scale, void *ws,
+                                            size_t ws_bytes, void *cuda_stream) {
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    profile_begin(st);
+    FLOWMM_TRY(validate_cache(p));
+    if (p->n_rows < 1) return FLOWMM_ERR_SHAPE;
+    if (!k || !v || !slots || !k_pages || !v_pages || !k_scale || !v_scale) return FLOWMM_ERR_NULL;
+    if (!aligned16(k) || !aligned16(v) || !aligned16(k_pages) || !aligned16(v_pages) || !strides_ok(p->k_stride, p->head_dim) ||
+        !strides_ok(p->v_stride, p->head_dim) || !aligned4(slots) || !aligned4(k_scale) || !aligned4(v_scale))
+        return FLOWMM_ERR_ALIGN;
+    FLOWMM_TRY(check_cache_ws(p, ws, ws_bytes));
+    // pages that n_rows rows can reach, wherever in its page the first one goes
+    const int64_t runs = ((int64_t)p->n_rows + 2 * p->page_size - 2) / p->page_size, items = 2 * (int64_t)p->n_units * p->n_kv_heads * runs;
+    if (items >= (int64_t)1 << 31) return FLOWMM_ERR_SHAPE;
+    FLOWMM_TRY(check_device());
+    paged::StoreArgs a;
+    a.x[0] = k; a.x[1] = v; a.slots = slots;
+    a.pages[0] = static_cast<uint8_t *>(k_pages); a.pages[1] = static_cast<uint8_t *>(v_pages);
+    a.scale[0] = k_scale; a.scale[1] = v_scale; a.status = static_cast<int *>(ws);
+    a.Hkv = p->n_kv_heads; a.T = p->n_rows; a.page = p->page_size; a.page_shift = page_shift(p->page_size); a.n_pages = p->n_pages;
+    for (int i = 0; i < 3; ++i) { a.stride[0][i] = p->k_stride[i]; a.stride[1][i] = p->v_stride[i]; }
+    a.items = (uint32_t)items; a.by_heads = make_fastdiv(p->n_kv_heads); a.by_runs = make_fastdiv((uint32_t)runs);
+    return p->dtype == FLOWMM_BF16 ? run_store<__nv_bfloat16>(*p, a, st) : run_store<float>(*p, a, st);
+}
+
+extern "C" flowmm_status flowmm_cache_load(const flowmm_cache_params *p, const void *k_pages, const void *v_pages,
+                                           const float *k_scale, const float *v_scale, const int32_t *block_table,
+                                           const int32_t *rows, void *k, void *v, void *ws, size_t ws_bytes, void *cuda_stream) {
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    profile_begin(st);
+    FLOWMM_TRY(validate_cache(p));
+    if (p->n_rows < 1) return FLOWMM_ERR_SHAPE;
+    if (!k || !v || !k_pages || !v_pages || !k_scale || !v_scale || !block_table || !rows) return FLOWMM_ERR_NULL;
+    if (!aligned16(k) || !aligned16(v) || !aligned16(k_pages) || !aligned16(v_pages) || !strides_ok(p->k_stride, p->head_dim) ||
+        !strides_ok(p->v_stride, p->head_dim) || !aligned4(k_scale) || !aligned4(v_scale) || !aligned4(block_table) || !aligned4(rows))
+        return FLOWMM_ERR_ALIGN;
+    FLOWMM_TRY(check_cache_ws(p, ws, ws_bytes));
+    const int64_t pages = ((int64_t)p->n_rows + p->page_size - 1) / p->page_size, items = 2 * (int64_t)p->n_units * p->n_kv_heads * pages;
+    if (items >= (int64_t)1 << 31) return FLOWMM_ERR_SHAPE;
+    constexpr int block = paged::kLoadThreads * paged::kLoadVecs;
+    const int64_t blocks = (items * p->page_size * (p->head_dim / 16) + block - 1) / block;
+    if (blocks >= (int64_t)1 << 31) return FLOWMM_ERR_SHAPE;
+    FLOWMM_TRY(check_device());
+    paged::LoadArgs a;
+    a.pages[0] = static_cast<const uint8_t *>(k_pages); a.pages[1] = static_cast<const uint8_t *>(v_pages);
+    a.scale[0] = k_scale; a.scale[1] = v_scale; a.table = block_table; a.rows = rows; a.x[0] = k; a.x[1] = v;
+    a.status = static_cast<int *>(ws);
+    a.Hkv = p->n_kv_heads; a.n_rows = p->n_rows; a.page = p->page_size; a.page_shift = page_shift(p->page_size);
+    a.n_pages = p->n_pages; a.max_pages = p->max_pages;
+    for (int i = 0; i < 3; ++i) { a.stride[0][i] = p->k_stride[i]; a.stride[1][i] = p->v_stride[i]; }
+    a.items = (uint32_t)items; a.by_heads = make_fastdiv(p->n_kv_heads); a.by_pages = make_fastdiv((uint32_t)pages);
+    return p->dtype == FLOWMM_BF16 ? run_load<__nv_bfloat16>(*p, a, blocks, st) : run_load<float>(*p, a, blocks, st);
+}
+
+extern "C" flowmm_status flowmm_cache_attention(const flowmm_cache_params *p, const void *q, const void *k_pages,
+                                                const void *v_pages, const float *k_scale, const float *v_scale,
+                                                const int32_t *block_table, const int32_t *rows, float *out, void *ws,
+                                                size_t ws_bytes, void *cuda_stream) {
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    profile_begin(st);
+    FLOWMM_TRY(validate_cache(p));
+    if (!q || !k_pages || !v_pages || !k_scale || !v_scale || !block_table || !rows || !out) return FLOWMM_ERR_NULL;
+    if (!aligned16(q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned4(k_scale) || !aligned4(v_scale) ||
+        !aligned4(block_table) || !aligned4(rows) || !aligned4(out))
+        return FLOWMM_ERR_ALIGN;
+    FLOWMM_TRY(check_cache_ws(p, ws, ws_bytes));
+    FLOWMM_TRY(check_device());
+    const CachePlan c = cache_plan(*p);
+    paged::AttnArgs a;
+    a.q = q; a.k = static_cast<const uint8_t *>(k_pages); a.v = static_cast<const uint8_t *>(v_pages);
+    a.k_scale = k_scale; a.v_scale = v_scale; a.table = block_table; a.rows = rows; a.out = out;
+    a.ticket = at<unsigned long long>(ws, 256); a.part = at<float>(ws, c.part); a.status = static_cast<int *>(ws);
+    a.call = status_call_number();
+    a.U = p->n_units; a.Hq = p->n_q_heads; a.Hkv = p->n_kv_heads; a.G = p->n_q_heads / p->n_kv_heads; a.groups = c.groups;
+    a.page = p->page_size; a.page_shift = page_shift(p->page_size); a.n_pages = p->n_pages; a.max_pages = p->max_pages;
+    a.q_bf16 = p->dtype == FLOWMM_BF16; a.target = c.target;
+    const float scale = p->softmax_scale != 0.f ? p->softmax_scale : 1.f / sqrtf((float)p->head_dim);
+    a.scale_log2 = scale * kLog2e;
+    return p->head_dim == 128 ? launch_cache_attention<128>(a, c, st) : launch_cache_attention<64>(a, c, st);
 }
 
 // ---- re-compression of a cache that grew during decoding ----------------------------------------
