@@ -19,6 +19,7 @@
 #include "merge_rows.cuh"
 #include "merge_tc.cuh"
 #include "paged_attention.cuh"
+#include "paged_attention_tc.cuh"
 #include "paged_cache.cuh"
 #include "score_cluster_tc.cuh"
 #include "score_fused_tc.cuh"
@@ -1473,28 +1474,34 @@ int page_shift(int page) { return page == 16 ? 4 : page == 32 ? 5 : page == 64 ?
 
 // The attention's cut and scratch: [status word, 256 bytes][tickets][records].
 struct CachePlan {
+    bool tc;                       // the tensor-core kernel (bf16 queries, heads of 128) or the SIMT one
     int groups, gp, target;        // groups of query heads that are ranges of their own, heads of one, ranges aimed at
     int64_t blocks;                // of the launch: no fewer than ranges can come out (paged_attention.cuh)
     size_t part, total;            // where the records start; bytes
 };
 
-CachePlan cache_plan(const flowmm_cache_params &p) {
+CachePlan cache_plan(const flowmm_cache_params &p, int path) {
     CachePlan c;
     const int G = p.n_q_heads / p.n_kv_heads;
-    c.gp = G <= 1 ? 1 : G <= 2 ? 2 : 4;
+    c.tc = p.dtype == FLOWMM_BF16 && p.head_dim == 128 && path != FLOWMM_PATH_SIMT;
+    c.gp = c.tc ? G : G <= 1 ? 1 : G <= 2 ? 2 : 4;
     c.groups = (G + c.gp - 1) / c.gp;
-    c.target = 4 * kScoreCtas;
+    c.target = (c.tc ? 2 : 4) * kScoreCtas;
     const int64_t heads = (int64_t)p.n_units * p.n_kv_heads * c.groups, keys = (int64_t)p.max_pages * p.page_size;
-    c.blocks = std::min(heads * ((keys + paged::kSimtKeys - 1) / paged::kSimtKeys), c.target + heads);
+    const int tile = c.tc ? paged::ptc::kTile : paged::kSimtKeys;
+    c.blocks = std::min(heads * ((keys + tile - 1) / tile), c.target + heads);
     c.part = 256 + align256((size_t)heads * sizeof(unsigned long long));
     c.total = c.part + align256((size_t)c.blocks * c.gp * (p.head_dim + 2) * sizeof(float));
     return c;
 }
 
+// The same workspace serves both paths.
+size_t cache_bytes(const flowmm_cache_params &p) { return std::max(cache_plan(p, FLOWMM_PATH_AUTO).total, cache_plan(p, FLOWMM_PATH_SIMT).total); }
+
 flowmm_status check_cache_ws(const flowmm_cache_params *p, const void *ws, size_t ws_bytes) {
     if (!ws) return FLOWMM_ERR_NULL;
     if (reinterpret_cast<uintptr_t>(ws) & 255) return FLOWMM_ERR_ALIGN;
-    return ws_bytes < cache_plan(*p).total ? FLOWMM_ERR_WORKSPACE : FLOWMM_OK;
+    return ws_bytes < cache_bytes(*p) ? FLOWMM_ERR_WORKSPACE : FLOWMM_OK;
 }
 
 bool aligned4(const void *ptr) { return (reinterpret_cast<uintptr_t>(ptr) & 3) == 0; }
@@ -1531,6 +1538,20 @@ flowmm_status run_load(const flowmm_cache_params &p, const paged::LoadArgs &a, i
     return FLOWMM_OK;
 }
 
+flowmm_status launch_cache_attention_tc(const flowmm_cache_params &p, const paged::AttnArgs &a, const CachePlan &c, cudaStream_t st) {
+    CUtensorMap kmap, vmap;
+    const uint64_t head = (uint64_t)p.page_size * 128, dims[4] = {128, (uint64_t)p.page_size, (uint64_t)p.n_kv_heads, (uint64_t)p.n_pages};
+    const uint64_t strides[3] = {128, head, head * p.n_kv_heads};
+    const uint32_t box[4] = {128, (uint32_t)p.page_size, 1, 1};
+    if (!tc::make_byte_map(&kmap, a.k, 4, dims, strides, box) || !tc::make_byte_map(&vmap, a.v, 4, dims, strides, box)) return FLOWMM_ERR_CUDA;
+    if (!allow_smem(paged::ptc::cache_attention_tc_kernel) ||
+        cudaFuncSetAttribute(paged::ptc::cache_attention_tc_kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared) != cudaSuccess)
+        return FLOWMM_ERR_CUDA;
+    launch(paged::ptc::cache_attention_tc_kernel, (unsigned)c.blocks, paged::ptc::kThreads, paged::ptc::kSmemBytes, st, kmap, vmap, a);
+    FLOWMM_LAUNCHED("cache_attention_tc");
+    return FLOWMM_OK;
+}
+
 template <int D>
 flowmm_status launch_cache_attention(const paged::AttnArgs &a, const CachePlan &c, cudaStream_t st) {
     const unsigned blocks = (unsigned)c.blocks;
@@ -1548,7 +1569,7 @@ flowmm_status launch_cache_attention(const paged::AttnArgs &a, const CachePlan &
 extern "C" flowmm_status flowmm_cache_workspace_bytes(const flowmm_cache_params *p, size_t *bytes) {
     if (!bytes) return FLOWMM_ERR_NULL;
     FLOWMM_TRY(validate_cache(p));
-    *bytes = cache_plan(*p).total;
+    *bytes = cache_bytes(*p);
     return FLOWMM_OK;
 }
 
@@ -1648,7 +1669,7 @@ extern "C" flowmm_status flowmm_cache_attention(const flowmm_cache_params *p, co
         return FLOWMM_ERR_ALIGN;
     FLOWMM_TRY(check_cache_ws(p, ws, ws_bytes));
     FLOWMM_TRY(check_device());
-    const CachePlan c = cache_plan(*p);
+    const CachePlan c = cache_plan(*p, p->path);
     paged::AttnArgs a;
     a.q = q; a.k = static_cast<const uint8_t *>(k_pages); a.v = static_cast<const uint8_t *>(v_pages);
     a.k_scale = k_scale; a.v_scale = v_scale; a.table = block_table; a.rows = rows; a.out = out;
@@ -1659,6 +1680,7 @@ extern "C" flowmm_status flowmm_cache_attention(const flowmm_cache_params *p, co
     a.q_bf16 = p->dtype == FLOWMM_BF16; a.target = c.target;
     const float scale = p->softmax_scale != 0.f ? p->softmax_scale : 1.f / sqrtf((float)p->head_dim);
     a.scale_log2 = scale * kLog2e;
+    if (c.tc) return launch_cache_attention_tc(*p, a, c, st);
     return p->head_dim == 128 ? launch_cache_attention<128>(a, c, st) : launch_cache_attention<64>(a, c, st);
 }
 

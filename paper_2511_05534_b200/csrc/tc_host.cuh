@@ -24,11 +24,11 @@ inline EncodeTiledFn encode_fn() {
     return fn;
 }
 
-// bf16 tensor of `rank` dims (innermost first, contiguous innermost), box as given (box[0] = 64
-// elements = one 128-byte swizzle span), 128-byte swizzle, zero fill outside the tensor.
+// Tensor of `rank` dims (innermost first, contiguous innermost), box as given (box[0] = one 128-byte swizzle span, 64 elements of
+// bf16 or 128 bytes), 128-byte swizzle, zero fill outside the tensor.
 // strides_bytes[i] is the stride of dim i+1.  Returns false if the driver rejects the description.
-inline bool make_bf16_map(CUtensorMap *map, const void *base, int rank, const uint64_t *dims,
-                          const uint64_t *strides_bytes, const uint32_t *box_dims) {
+inline bool make_map(CUtensorMapDataType type, CUtensorMap *map, const void *base, int rank, const uint64_t *dims,
+                     const uint64_t *strides_bytes, const uint32_t *box_dims) {
     EncodeTiledFn fn = encode_fn();
     if (!fn) return false;
     cuuint64_t gdim[5], gstride[4];
@@ -36,7 +36,7 @@ inline bool make_bf16_map(CUtensorMap *map, const void *base, int rank, const ui
     for (int i = 0; i < rank; ++i) { gdim[i] = dims[i]; box[i] = box_dims[i]; estr[i] = 1; }
     for (int i = 0; i + 1 < rank; ++i) gstride[i] = strides_bytes[i];
     auto encode = [&]() {
-        return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void *>(base), gdim, gstride, box,
+        return fn(map, type, (cuuint32_t)rank, const_cast<void *>(base), gdim, gstride, box,
                   estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     };
@@ -45,6 +45,12 @@ inline bool make_bf16_map(CUtensorMap *map, const void *base, int rank, const ui
     if (r == CUDA_ERROR_INVALID_CONTEXT && cudaGetDevice(&dev) == cudaSuccess && cudaSetDevice(dev) == cudaSuccess)
         r = encode();                    // (the thread's first call: the driver wants a context, which the runtime binds as late as it can)
     return r == CUDA_SUCCESS;
+}
+inline bool make_bf16_map(CUtensorMap *map, const void *base, int rank, const uint64_t *dims, const uint64_t *strides_bytes, const uint32_t *box_dims) {
+    return make_map(CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, map, base, rank, dims, strides_bytes, box_dims);
+}
+inline bool make_byte_map(CUtensorMap *map, const void *base, int rank, const uint64_t *dims, const uint64_t *strides_bytes, const uint32_t *box_dims) {
+    return make_map(CU_TENSOR_MAP_DATA_TYPE_UINT8, map, base, rank, dims, strides_bytes, box_dims);
 }
 
 // SM count of the current device (a benign race: every thread would store the same value).
