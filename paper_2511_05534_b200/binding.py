@@ -397,43 +397,56 @@ _CACHE_FIELDS = operator.attrgetter("n_units", "n_q_heads", "n_kv_heads", "head_
 _CODE_TYPES = (torch.uint8, torch.float8_e4m3fn)
 
 
-def _cache_call(p: CacheParams, what: str, tensors, dense=()):
-    """The call's struct, after a look at what the C side cannot see: the tensors' shapes, types and devices.  `tensors` and `dense`
-    (the rows of K and V, by strides): (name, tensor, shape, types); a tensor may be None where the C entry point takes NULL.
-    Calls alike in all of that are looked at once."""
-    key = (what, _CACHE_FIELDS(p)) + tuple(None if t is None else (t.shape, t.stride(), t.dtype, t.get_device()) for _, t, _, _ in tensors + dense)
-    ref = _structs.get(key)
-    if ref is not None:
-        return ref
-    device = None
-    for name, t, shape, types in tensors + dense:
-        if t is None:
-            continue
-        if not t.is_cuda:
-            raise ValueError("flowmm takes CUDA tensors")
+# What a call's tensors look like, in C loops: ten tensors' shapes and strides by hand cost twice what the rest of a call does.  Strides and
+# numel together fix what memory a tensor covers.
+_strides, _numel, _device, _address = torch.Tensor.stride, torch.Tensor.numel, torch.Tensor.get_device, torch.Tensor.data_ptr
+_type = operator.attrgetter("dtype")
+_seen = {}
+
+
+def _cache_struct(p: CacheParams, what: str, tensors, expected, n_dense=0):
+    """The call's struct, after a look at what the C side cannot see: the tensors' shapes, types and devices.  expected(): (name, shape,
+    types) of each; the first n_dense, the rows of K and V, may have strides.  Calls alike in all of that are looked at once."""
+    if not tensors[0].is_cuda:
+        raise ValueError("flowmm takes CUDA tensors")
+    look = (*map(_strides, tensors), *map(_numel, tensors), *map(_type, tensors), *map(_device, tensors), torch._C._cuda_getDevice())
+    calls = _seen.get((what, _CACHE_FIELDS(p)))
+    if calls is not None:
+        for known, ref in calls:
+            if known == look:
+                return ref
+    for i, (t, (name, shape, types)) in enumerate(zip(tensors, expected())):
         if tuple(t.shape) != shape or t.dtype not in types:
             raise ValueError("%s: %s must be a %s tensor of shape %s" % (what, name, " or ".join(str(x) for x in types), list(shape)))
-        if device is not None and t.get_device() != device:
-            raise ValueError("%s: %s is on another device than the other tensors" % (what, name))
-        device = t.get_device()
-    for name, t, _, _ in tensors:
-        if t is not None and not t.is_contiguous():
-            raise ValueError("%s: %s must be contiguous" % (what, name))
-    for name, t, _, _ in dense:
-        if t.stride(3) != 1:
-            raise ValueError("%s: %s must have contiguous head_dim" % (what, name))
-    if device != torch.cuda.current_device():
-        raise ValueError("%s: the tensors are not on the current device" % what)
-    return _keep_struct(key, p.c(*(t for _, t, _, _ in dense)))
+        if t.get_device() != look[-1]:
+            raise ValueError("%s: %s is not on the current device" % (what, name))
+        if t.stride(3) != 1 if i < n_dense else not t.is_contiguous():
+            raise ValueError("%s: %s must %s" % (what, name, "have contiguous head_dim" if i < n_dense else "be contiguous"))
+    ref = ctypes.byref(p.c(*tensors[:n_dense]))                     # (holds on to the struct)
+    if len(_seen) >= _MAX_STRUCTS:
+        _seen.clear()
+    calls = _seen.setdefault((what, _CACHE_FIELDS(p)), [])
+    if len(calls) >= 8:
+        calls.clear()
+    calls.append((look, ref))
+    return ref
 
 
-def _pool(p: CacheParams, k_pages, v_pages, k_scale, v_scale):
+def _expect_pool(p: CacheParams):
     codes, scales = (p.n_pages, p.n_kv_heads, p.page_size, p.head_dim), (p.n_pages, p.n_kv_heads)
-    return (("k_pages", k_pages, codes, _CODE_TYPES), ("v_pages", v_pages, codes, _CODE_TYPES),
-            ("k_scale", k_scale, scales, (torch.float32,)), ("v_scale", v_scale, scales, (torch.float32,)))
+    return (("k_pages", codes, _CODE_TYPES), ("v_pages", codes, _CODE_TYPES), ("k_scale", scales, _FLOAT), ("v_scale", scales, _FLOAT))
 
 
-_INT32, _BYTES = (torch.int32,), (torch.uint8,)
+def _expect_rows(p: CacheParams):
+    shape, types = (p.n_units, p.n_kv_heads, p.n_rows, p.head_dim), (torch_dtype(p.dtype),)
+    return (("k", shape, types), ("v", shape, types))
+
+
+_INT32, _BYTES, _FLOAT = (torch.int32,), (torch.uint8,), (torch.float32,)
+
+
+def _cache_ws(ws):
+    return ("ws", (ws.numel(),), _BYTES)
 
 
 def flowmm_cache_workspace_bytes(p: CacheParams) -> int:
@@ -452,43 +465,40 @@ def alloc_cache_workspace(p: CacheParams, device="cuda") -> torch.Tensor:
 
 def flowmm_cache_plan(p: CacheParams, grow, rows, rows_out, free_pages, free_state, free_state_out, block_table, slots, ws):
     """Pages and slots for units that go from rows to rows + grow rows; slots may be None."""
-    U = p.n_units
-    cp = _cache_call(p, "flowmm_cache_plan", (
-        ("grow", grow, (U,), _INT32), ("rows", rows, (U,), _INT32), ("rows_out", rows_out, (U,), _INT32),
-        ("free_pages", free_pages, (p.n_pages,), _INT32), ("free_state", free_state, (2,), _INT32),
-        ("free_state_out", free_state_out, (2,), _INT32), ("block_table", block_table, (U, p.max_pages), _INT32),
-        ("slots", slots, (U, p.n_rows), _INT32), ("ws", ws, (ws.numel(),), _BYTES)))
-    _check(load().flowmm_cache_plan(cp, _p(grow), _p(rows), _p(rows_out), _p(free_pages), _p(free_state), _p(free_state_out),
-                                    _p(block_table), _p(slots), _p(ws), ws.numel(), _stream()), "flowmm_cache_plan")
+    tensors = (grow, rows, rows_out, free_pages, free_state, free_state_out, block_table, ws) + (() if slots is None else (slots,))
+    U = (p.n_units,)
+    ref = _cache_struct(p, "flowmm_cache_plan", tensors, lambda: (
+        ("grow", U, _INT32), ("rows", U, _INT32), ("rows_out", U, _INT32), ("free_pages", (p.n_pages,), _INT32), ("free_state", (2,), _INT32),
+        ("free_state_out", (2,), _INT32), ("block_table", (p.n_units, p.max_pages), _INT32), _cache_ws(ws), ("slots", (p.n_units, p.n_rows), _INT32)))
+    *at, ws_at = map(_address, tensors[:8])
+    _check((_lib or load()).flowmm_cache_plan(ref, *at, None if slots is None else slots.data_ptr(), ws_at, ws.numel(), torch._C._cuda_getCurrentRawStream(ws.get_device())), "flowmm_cache_plan")
 
 
 def flowmm_cache_store(p: CacheParams, k, v, slots, k_pages, v_pages, k_scale, v_scale, ws):
     """Rows k, v [units, kv_heads, n_rows, head_dim] into pages (uint8 or float8_e4m3fn tensors), as slots says."""
-    rows, types = (p.n_units, p.n_kv_heads, p.n_rows, p.head_dim), (torch_dtype(p.dtype),)
-    cp = _cache_call(p, "flowmm_cache_store", (("slots", slots, (p.n_units, p.n_rows), _INT32),) + _pool(p, k_pages, v_pages, k_scale, v_scale) +
-                     (("ws", ws, (ws.numel(),), _BYTES),), (("k", k, rows, types), ("v", v, rows, types)))
-    _check(load().flowmm_cache_store(cp, _p(k), _p(v), _p(slots), _p(k_pages), _p(v_pages), _p(k_scale), _p(v_scale), _p(ws),
-                                     ws.numel(), _stream()), "flowmm_cache_store")
+    tensors = (k, v, slots, k_pages, v_pages, k_scale, v_scale, ws)
+    ref = _cache_struct(p, "flowmm_cache_store", tensors, lambda: (
+        *_expect_rows(p), ("slots", (p.n_units, p.n_rows), _INT32), *_expect_pool(p), _cache_ws(ws)), 2)
+    _check((_lib or load()).flowmm_cache_store(ref, *map(_address, tensors), ws.numel(), torch._C._cuda_getCurrentRawStream(ws.get_device())), "flowmm_cache_store")
 
 
 def flowmm_cache_load(p: CacheParams, k_pages, v_pages, k_scale, v_scale, block_table, rows, k, v, ws):
     """The first min(rows[u], n_rows) rows of every unit into k, v [units, kv_heads, n_rows, head_dim]."""
-    dense, types = (p.n_units, p.n_kv_heads, p.n_rows, p.head_dim), (torch_dtype(p.dtype),)
-    cp = _cache_call(p, "flowmm_cache_load", _pool(p, k_pages, v_pages, k_scale, v_scale) + (
-        ("block_table", block_table, (p.n_units, p.max_pages), _INT32), ("rows", rows, (p.n_units,), _INT32),
-        ("ws", ws, (ws.numel(),), _BYTES)), (("k", k, dense, types), ("v", v, dense, types)))
-    _check(load().flowmm_cache_load(cp, _p(k_pages), _p(v_pages), _p(k_scale), _p(v_scale), _p(block_table), _p(rows), _p(k), _p(v),
-                                    _p(ws), ws.numel(), _stream()), "flowmm_cache_load")
+    tensors = (k, v, k_pages, v_pages, k_scale, v_scale, block_table, rows, ws)
+    ref = _cache_struct(p, "flowmm_cache_load", tensors, lambda: (
+        *_expect_rows(p), *_expect_pool(p), ("block_table", (p.n_units, p.max_pages), _INT32), ("rows", (p.n_units,), _INT32), _cache_ws(ws)), 2)
+    k_at, v_at, *at, ws_at = map(_address, tensors)
+    _check((_lib or load()).flowmm_cache_load(ref, *at, k_at, v_at, ws_at, ws.numel(), torch._C._cuda_getCurrentRawStream(ws.get_device())), "flowmm_cache_load")
 
 
 def flowmm_cache_attention(p: CacheParams, q, k_pages, v_pages, k_scale, v_scale, block_table, rows, out, ws):
     """Decode attention over the paged cache; q [units, q_heads, head_dim], out the same in float32."""
-    shape = (p.n_units, p.n_q_heads, p.head_dim)
-    cp = _cache_call(p, "flowmm_cache_attention", (("q", q, shape, (torch_dtype(p.dtype),)),) + _pool(p, k_pages, v_pages, k_scale, v_scale) + (
-        ("block_table", block_table, (p.n_units, p.max_pages), _INT32), ("rows", rows, (p.n_units,), _INT32),
-        ("out", out, shape, (torch.float32,)), ("ws", ws, (ws.numel(),), _BYTES)))
-    _check(load().flowmm_cache_attention(cp, _p(q), _p(k_pages), _p(v_pages), _p(k_scale), _p(v_scale), _p(block_table), _p(rows),
-                                         _p(out), _p(ws), ws.numel(), _stream()), "flowmm_cache_attention")
+    tensors = (q, k_pages, v_pages, k_scale, v_scale, block_table, rows, out, ws)
+    heads = (p.n_units, p.n_q_heads, p.head_dim)
+    ref = _cache_struct(p, "flowmm_cache_attention", tensors, lambda: (
+        ("q", heads, (torch_dtype(p.dtype),)), *_expect_pool(p), ("block_table", (p.n_units, p.max_pages), _INT32), ("rows", (p.n_units,), _INT32),
+        ("out", heads, _FLOAT), _cache_ws(ws)))
+    _check((_lib or load()).flowmm_cache_attention(ref, *map(_address, tensors), ws.numel(), torch._C._cuda_getCurrentRawStream(ws.get_device())), "flowmm_cache_attention")
 
 
 def flowmm_selftest_wait_timeout(ws):
