@@ -1491,7 +1491,7 @@ CachePlan cache_plan(const flowmm_cache_params &p, int path) {
     const int tile = c.tc ? paged::ptc::kTile : paged::kSimtKeys;
     c.blocks = std::min(heads * ((keys + tile - 1) / tile), c.target + heads);
     c.part = 256 + align256((size_t)heads * sizeof(unsigned long long));
-    c.total = c.part + align256((size_t)c.blocks * c.gp * (p.head_dim + 2) * sizeof(float));
+    c.total = c.part + align256((size_t)c.blocks * ((c.gp * (p.head_dim + 2) + 3) & ~3) * sizeof(float));
     return c;
 }
 
@@ -1544,10 +1544,10 @@ flowmm_status launch_cache_attention_tc(const flowmm_cache_params &p, const page
     const uint64_t strides[3] = {128, head, head * p.n_kv_heads};
     const uint32_t box[4] = {128, (uint32_t)p.page_size, 1, 1};
     if (!tc::make_byte_map(&kmap, a.k, 4, dims, strides, box) || !tc::make_byte_map(&vmap, a.v, 4, dims, strides, box)) return FLOWMM_ERR_CUDA;
-    if (!allow_smem(paged::ptc::cache_attention_tc_kernel) ||
-        cudaFuncSetAttribute(paged::ptc::cache_attention_tc_kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared) != cudaSuccess)
+    auto kernel = a.G <= paged::ptc::kHalf ? paged::ptc::cache_attention_tc_kernel<true> : paged::ptc::cache_attention_tc_kernel<false>;
+    if (!allow_smem(kernel) || cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared) != cudaSuccess)
         return FLOWMM_ERR_CUDA;
-    launch(paged::ptc::cache_attention_tc_kernel, (unsigned)c.blocks, paged::ptc::kThreads, paged::ptc::kSmemBytes, st, kmap, vmap, a);
+    launch(kernel, (unsigned)c.blocks, paged::ptc::kThreads, paged::ptc::kSmemBytes, st, kmap, vmap, a);
     FLOWMM_LAUNCHED("cache_attention_tc");
     return FLOWMM_OK;
 }
@@ -1677,7 +1677,7 @@ extern "C" flowmm_status flowmm_cache_attention(const flowmm_cache_params *p, co
     a.call = status_call_number();
     a.U = p->n_units; a.Hq = p->n_q_heads; a.Hkv = p->n_kv_heads; a.G = p->n_q_heads / p->n_kv_heads; a.groups = c.groups;
     a.page = p->page_size; a.page_shift = page_shift(p->page_size); a.n_pages = p->n_pages; a.max_pages = p->max_pages;
-    a.q_bf16 = p->dtype == FLOWMM_BF16; a.target = c.target;
+    a.q_bf16 = p->dtype == FLOWMM_BF16; a.target = c.target; a.by_heads = make_fastdiv(p->n_kv_heads * c.groups);
     const float scale = p->softmax_scale != 0.f ? p->softmax_scale : 1.f / sqrtf((float)p->head_dim);
     a.scale_log2 = scale * kLog2e;
     if (c.tc) return launch_cache_attention_tc(*p, a, c, st);

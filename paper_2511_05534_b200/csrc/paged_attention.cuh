@@ -16,12 +16,13 @@ struct AttnArgs {
     const float *k_scale, *v_scale;    // [n_pages, Hkv]
     const int *table, *rows;           // [U, max_pages], [U]
     float *out;                        // [U, Hq, D]
-    float *part;                       // [blocks][G][D + 2]: output relative to the maximum, maximum (log2), sum of weights
+    float *part;                       // [blocks] records (record_floats)
     unsigned long long *ticket;        // [U * Hkv * groups]: (call, ranges done)
     int *status;
     uint32_t call;
     int U, Hq, Hkv, G, groups, page, page_shift, n_pages, max_pages, q_bf16;
     int target;                        // ranges in all that the call is cut into, about
+    FastDiv by_heads;                  // by Hkv * groups
     float scale_log2;
 };
 
@@ -29,89 +30,141 @@ constexpr float kLowest = -3.402823466e38f;   // where maxima start: no logit is
 
 // ---- ranges --------------------------------------------------------------------------------------
 // The work of a call is cut by the lengths: tiles of kKeys keys, `per` of them to a range, so that all units together make about
-// `target` ranges of equal length (a unit's last one is what remains; a unit without rows has one, which writes zeros).  Every
-// block finds its own range: a sum over the units, then the prefix sum until its number falls into a unit.  Ranges are numbered
-// by unit, range, then head, so there are at most target + U * heads of them, the blocks of the launch.
+// `target` ranges of equal length (a unit's last one is what remains; a unit without rows has one, which writes zeros).  Where that would
+// cut the longest unit for a few tiles only, nothing is cut: joining costs as much as kJoinTiles tiles.  Every warp
+// finds its block's range by itself: a sum over the units, then a prefix sum (each lane some consecutive units) until the
+// block's number falls into a unit.  Ranges are numbered by unit, range, then head, so there are at most target + U * heads of
+// them, the blocks of the launch.  (With the whole block and its barriers 2.0 us for one unit, so 0.6.)
+constexpr int kJoinTiles = 4;
 struct Range { int u, h, split, n_split, tile0, tiles, rows; };
-template <int kThreads> struct RangeScratch { unsigned long long sums[kThreads / 32 + 1]; int scan[33]; Range found; int hit; };
 
 __device__ __forceinline__ int unit_rows(const AttnArgs &A, int u) {
     const int n = A.rows[u], most = A.max_pages << A.page_shift;
     return n < 0 ? 0 : min(n, most);
 }
 
-template <int kThreads, int kKeys>
-__device__ __forceinline__ bool find_range(const AttnArgs &A, int heads, uint32_t item, RangeScratch<kThreads> &s, Range &r) {
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    unsigned long long tiles = 0;
-    for (int u = tid; u < A.U; u += kThreads) {
-        const int n = A.rows[u];
-        if (blockIdx.x == 0 && (n < 0 || n > A.max_pages << A.page_shift)) report(A.status, kStatusIndex);
-        tiles += (unit_rows(A, u) + kKeys - 1) / kKeys;
+template <int kKeys>
+__device__ __forceinline__ bool find_range(const AttnArgs &A, uint32_t item, Range &r) {
+    const int lane = lane_id();
+    const uint32_t heads = A.by_heads.d, want = A.by_heads.div(item);
+    unsigned long long sum = 0;
+    int longest = 0;
+#pragma unroll 4
+    for (int u = lane; u < A.U; u += 32) {
+        const int t = (unit_rows(A, u) + kKeys - 1) / kKeys;
+        sum += t;
+        longest = max(longest, t);
     }
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) tiles += __shfl_xor_sync(0xFFFFFFFFu, tiles, o);
-    if (lane == 0) s.sums[warp] = tiles;
-    if (tid == 0) s.hit = 0;
-    __syncthreads();
-    tiles = 0;
+    for (int o = 16; o > 0; o >>= 1) {
+        sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+        longest = max(longest, __shfl_xor_sync(0xFFFFFFFFu, longest, o));
+    }
+    const unsigned long long tiles = sum * heads + A.target - 1;
+    const unsigned long long even = tiles >> 32 ? tiles / A.target : (uint32_t)tiles / (uint32_t)A.target;
+    const int per = longest <= (int)even + kJoinTiles ? max(1, longest) : max(1, (int)even);
+    const int each = (A.U + 31) >> 5, u0 = min(A.U, lane * each), u1 = min(A.U, u0 + each);
+    uint32_t mine = 0;
+#pragma unroll 4
+    for (int u = u0; u < u1; ++u) mine += max(1u, ((uint32_t)(unit_rows(A, u) + kKeys - 1) / kKeys + per - 1) / (uint32_t)per);
+    uint32_t upto = mine;
 #pragma unroll
-    for (int w = 0; w < kThreads / 32; ++w) tiles += s.sums[w];
-    const unsigned long long per_all = (tiles * heads + A.target - 1) / A.target;
-    const int per = per_all < 1 ? 1 : (int)per_all;
-    const uint32_t want = item / heads;
-    uint32_t before = 0;
-    for (int u0 = 0; u0 < A.U; u0 += kThreads) {
-        const int u = u0 + tid;
-        const int n = u < A.U ? unit_rows(A, u) : 0, t = (n + kKeys - 1) / kKeys;
-        const int mine = u < A.U ? max(1, (t + per - 1) / per) : 0;
-        int total;
-        const uint32_t at = before + block_exclusive_scan(mine, s.scan, total);
-        if (u < A.U && want >= at && want < at + mine) {
-            const int split = want - at;
-            s.found = {u, (int)(item % heads), split, mine, split * per, min(per, t - split * per), n};
-            s.hit = 1;
+    for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t x = __shfl_up_sync(0xFFFFFFFFu, upto, o);
+        if (lane >= o) upto += x;
+    }
+    const uint32_t hit = __ballot_sync(0xFFFFFFFFu, want < upto);      // the first lane whose units reach the number
+    if (hit == 0) return false;
+    const int owner = __ffs(hit) - 1;
+    int u = 0, split = 0, n_split = 0, t = 0, rows = 0;
+    if (lane == owner) {
+        uint32_t at = upto - mine;
+        for (u = u0; u < u1; ++u) {
+            rows = unit_rows(A, u);
+            t = (rows + kKeys - 1) / kKeys;
+            n_split = max(1u, ((uint32_t)t + per - 1) / (uint32_t)per);
+            if (want < at + n_split) break;
+            at += n_split;
         }
-        before += total;
-        if (want < before) break;                                     // (the same for the whole block)
+        split = want - at;
     }
-    __syncthreads();
-    if (!s.hit) return false;
-    r = s.found;
+    r.u = __shfl_sync(0xFFFFFFFFu, u, owner);
+    r.split = __shfl_sync(0xFFFFFFFFu, split, owner);
+    r.n_split = __shfl_sync(0xFFFFFFFFu, n_split, owner);
+    r.rows = __shfl_sync(0xFFFFFFFFu, rows, owner);
+    t = __shfl_sync(0xFFFFFFFFu, t, owner);
+    r.h = item - want * heads;
+    r.tile0 = r.split * per;
+    r.tiles = min(per, t - r.tile0);
     return true;
+}
+
+// Lengths out of range, reported once a call.
+__device__ __forceinline__ void check_lengths(const AttnArgs &A) {
+    if (blockIdx.x == 0)
+        for (int u = threadIdx.x; u < A.U; u += blockDim.x) {
+            const int n = A.rows[u];
+            if (n < 0 || n > A.max_pages << A.page_shift) report(A.status, kStatusIndex);
+        }
 }
 
 // ---- joining -------------------------------------------------------------------------------------
 // A block that has written its range's record takes a ticket of its head; the one that takes the last joins the records.  The
 // ticket carries the call's number, so the memory may hold anything before, and is back at zero after the last one.
-__device__ __forceinline__ bool take_ticket(unsigned long long *ticket, uint32_t call, int n) {
-    unsigned long long seen = *reinterpret_cast<volatile unsigned long long *>(ticket);
-    for (int tries = 0; tries < n; ++tries) {                         // (a lost exchange is another block's ticket: n - 1 at most)
+// `seen`: what the ticket was read as earlier on, to spare a read here.  One thread calls this, behind a barrier of the block.
+__device__ __forceinline__ bool take_ticket(unsigned long long *ticket, unsigned long long seen, uint32_t call, int n) {
+    __threadfence();                                                  // (the block's record, ordered before by the barrier)
+    bool last = false;
+    for (int tries = 0; tries <= n; ++tries) {                        // (a lost exchange is a read too early or another block's ticket: n at most)
         const uint32_t done = (uint32_t)(seen >> 32) == call ? (uint32_t)seen + 1u : 1u;
-        const bool last = done >= (uint32_t)n;
+        last = done >= (uint32_t)n;
         const unsigned long long prev = atomicCAS(ticket, seen, (unsigned long long)call << 32 | (last ? 0u : done));
-        if (prev == seen) return last;
+        if (prev == seen) break;
         seen = prev;
+        last = false;
     }
-    return false;
+    __threadfence();
+    return last;
 }
 
-// Joins the records of one head's ranges, `step` floats apart: by heads and dims over the block's threads.
+// A range's record: its G heads' outputs, relative to the maximum, then the maxima (log2) and the sums of weights.
+template <int D> __device__ __forceinline__ int record_floats(int G) { return (G * (D + 2) + 3) & ~3; }
+
+// Joins the records of one head group's ranges, `step` floats apart, in the ranges' order: a warp per query head, four or two dims a
+// lane.  The ranges' maxima and sums are read by the lanes, all of 32 ranges at once, the outputs sixteen ranges at a time.
 template <int kThreads, int D>
 __device__ __forceinline__ void join_ranges(const float *rec, int64_t step, int n, int G, float *out) {
-    for (int i = threadIdx.x; i < G * D; i += kThreads) {
-        const int g = i / D, d = i % D;
-        const float *p = rec + g * (D + 2);
-        float mx = kLowest, o = 0.f, l = 0.f;
-#pragma unroll 8
-        for (int s = 0; s < n; ++s) mx = fmaxf(mx, __ldcg(p + s * step + D));
-#pragma unroll 8
-        for (int s = 0; s < n; ++s) {
-            const float w = tc::ex2(__ldcg(p + s * step + D) - mx);
-            o = fmaf(__ldcg(p + s * step + d), w, o);
-            l = fmaf(__ldcg(p + s * step + D + 1), w, l);
+    constexpr int V = D / 32;
+    const int lane = lane_id();
+    for (int g = threadIdx.x >> 5; g < G; g += kThreads / 32) {
+        const float *top = rec + G * D + g;
+        float mx = kLowest, l = 0.f, o[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) o[i] = 0.f;
+        for (int s = lane; s < n; s += 32) mx = fmaxf(mx, __ldcg(top + s * step));
+#pragma unroll
+        for (int i = 16; i > 0; i >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, i));
+        for (int s0 = 0; s0 < n; s0 += 32) {
+            const bool on = s0 + lane < n;
+            const float w = on ? tc::ex2(__ldcg(top + (s0 + lane) * step) - mx) : 0.f;
+            if (on) l = fmaf(__ldcg(top + (s0 + lane) * step + G), w, l);
+            const int end = min(32, n - s0);
+            const float *at = rec + s0 * step + g * D + lane * V;
+#pragma unroll 16
+            for (int s = 0; s < end; ++s) {
+                const float c = __shfl_sync(0xFFFFFFFFu, w, s);
+                if (V == 4) {
+                    const float4 x = __ldcg(reinterpret_cast<const float4 *>(at + s * step));
+                    o[0] = fmaf(x.x, c, o[0]); o[1] = fmaf(x.y, c, o[1]); o[2] = fmaf(x.z, c, o[2]); o[3] = fmaf(x.w, c, o[3]);
+                } else {
+                    const float2 x = __ldcg(reinterpret_cast<const float2 *>(at + s * step));
+                    o[0] = fmaf(x.x, c, o[0]); o[1] = fmaf(x.y, c, o[1]);
+                }
+            }
         }
-        out[g * D + d] = o / l;
+        l = warp_sum(l);
+#pragma unroll
+        for (int i = 0; i < V; ++i) out[g * D + lane * V + i] = o[i] / l;
     }
 }
 
@@ -123,7 +176,6 @@ constexpr int kSimtThreads = 128, kSimtKeys = 64, kSimtPages = 256;
 template <int D, int GP>
 __global__ void __launch_bounds__(kSimtThreads) cache_attention_kernel(const AttnArgs A) {
     constexpr int kLanes = D / 16, kGroups = kSimtThreads / kLanes, kStep = 2;
-    __shared__ RangeScratch<kSimtThreads> scratch;
     __shared__ float rec[kGroups][GP][D + 2];
     __shared__ int ids[kSimtPages];
     __shared__ float ks[kSimtPages], vs[kSimtPages];
@@ -132,7 +184,8 @@ __global__ void __launch_bounds__(kSimtThreads) cache_attention_kernel(const Att
     successor_may_start();
     Range r;
     const int heads = A.Hkv * A.groups;
-    if (!find_range<kSimtThreads, kSimtKeys>(A, heads, blockIdx.x, scratch, r)) return;
+    check_lengths(A);
+    if (!find_range<kSimtKeys>(A, blockIdx.x, r)) return;
     const int tid = threadIdx.x, sub = tid % kLanes, grp = tid / kLanes;
     const int h = r.h / A.groups, g0 = (r.h % A.groups) * GP, G = min(GP, A.G - g0);
     float *out = A.out + ((int64_t)r.u * A.Hq + h * A.G + g0) * D;
@@ -235,7 +288,8 @@ __global__ void __launch_bounds__(kSimtThreads) cache_attention_kernel(const Att
         if (sub == 0) { rec[grp][g][D] = m[g]; rec[grp][g][D + 1] = l[g]; }
     }
     __syncthreads();
-    float *part = A.part + (int64_t)blockIdx.x * GP * (D + 2);
+    const int record = record_floats<D>(GP);
+    float *part = A.part + (int64_t)blockIdx.x * record;
     for (int i = tid; i < G * D; i += kSimtThreads) {
         const int g = i / D, d = i % D;
         float mx = kLowest, o = 0.f, ls = 0.f;
@@ -248,18 +302,19 @@ __global__ void __launch_bounds__(kSimtThreads) cache_attention_kernel(const Att
         if (r.n_split == 1) {
             out[i] = o / ls;
         } else {
-            part[g * (D + 2) + d] = o;
-            if (d == 0) { part[g * (D + 2) + D] = mx; part[g * (D + 2) + D + 1] = ls; }
+            part[i] = o;
+            if (d == 0) { part[G * D + g] = mx; part[G * D + G + g] = ls; }
         }
     }
     if (r.n_split == 1) return;
-    __threadfence();
     __syncthreads();
-    if (tid == 0) last = take_ticket(A.ticket + (int64_t)r.u * heads + r.h, A.call, r.n_split);
+    if (tid == 0) {
+        unsigned long long *ticket = A.ticket + (int64_t)r.u * heads + r.h;
+        last = take_ticket(ticket, *reinterpret_cast<volatile unsigned long long *>(ticket), A.call, r.n_split);
+    }
     __syncthreads();
     if (!last) return;
-    __threadfence();
-    join_ranges<kSimtThreads, D>(A.part + ((int64_t)blockIdx.x - (int64_t)r.split * heads) * GP * (D + 2), (int64_t)heads * GP * (D + 2), r.n_split, G, out);
+    join_ranges<kSimtThreads, D>(A.part + ((int64_t)blockIdx.x - (int64_t)r.split * heads) * record, (int64_t)heads * record, r.n_split, G, out);
 }
 
 }  // namespace paged
