@@ -1488,10 +1488,11 @@ CachePlan cache_plan(const flowmm_cache_params &p, int path) {
     c.groups = (G + c.gp - 1) / c.gp;
     c.target = (c.tc ? 2 : 4) * kScoreCtas;
     const int64_t heads = (int64_t)p.n_units * p.n_kv_heads * c.groups, keys = (int64_t)p.max_pages * p.page_size;
-    const int tile = c.tc ? paged::ptc::kTile : paged::kSimtKeys;
-    c.blocks = std::min(heads * ((keys + tile - 1) / tile), c.target + heads);
+    // tensor cores: equal shares, two records each; SIMT: a block and a record for each range
+    if (c.tc) c.blocks = std::min<int64_t>(heads * ((keys + paged::ptc::kTile - 1) / paged::ptc::kTile), c.target);
+    else c.blocks = std::min(heads * ((keys + paged::kSimtKeys - 1) / paged::kSimtKeys), c.target + heads);
     c.part = 256 + align256((size_t)heads * sizeof(unsigned long long));
-    c.total = c.part + align256((size_t)c.blocks * ((c.gp * (p.head_dim + 2) + 3) & ~3) * sizeof(float));
+    c.total = c.part + align256((size_t)c.blocks * (c.tc ? 2 : 1) * ((c.gp * (p.head_dim + 2) + 3) & ~3) * sizeof(float));
     return c;
 }
 
@@ -1668,6 +1669,9 @@ extern "C" flowmm_status flowmm_cache_attention(const flowmm_cache_params *p, co
         !aligned4(block_table) || !aligned4(rows) || !aligned4(out))
         return FLOWMM_ERR_ALIGN;
     FLOWMM_TRY(check_cache_ws(p, ws, ws_bytes));
+    // tiles of all heads are counted in 32 bits
+    if ((int64_t)p->n_units * p->n_q_heads * (((int64_t)p->max_pages * p->page_size + paged::kSimtKeys - 1) / paged::kSimtKeys) >= (int64_t)1 << 31)
+        return FLOWMM_ERR_SHAPE;
     FLOWMM_TRY(check_device());
     const CachePlan c = cache_plan(*p, p->path);
     paged::AttnArgs a;

@@ -130,10 +130,10 @@ __device__ __forceinline__ bool take_ticket(unsigned long long *ticket, unsigned
 // A range's record: its G heads' outputs, relative to the maximum, then the maxima (log2) and the sums of weights.
 template <int D> __device__ __forceinline__ int record_floats(int G) { return (G * (D + 2) + 3) & ~3; }
 
-// Joins the records of one head group's ranges, `step` floats apart, in the ranges' order: a warp per query head, four or two dims a
+// Joins the records of one head group's ranges, `step` floats apart (the first one `ahead` floats behind its place), in the ranges' order: a warp per query head, four or two dims a
 // lane.  The ranges' maxima and sums are read by the lanes, all of 32 ranges at once, the outputs sixteen ranges at a time.
 template <int kThreads, int D>
-__device__ __forceinline__ void join_ranges(const float *rec, int64_t step, int n, int G, float *out) {
+__device__ __forceinline__ void join_ranges(const float *rec, int64_t ahead, int64_t step, int n, int G, float *out) {
     constexpr int V = D / 32;
     const int lane = lane_id();
     for (int g = threadIdx.x >> 5; g < G; g += kThreads / 32) {
@@ -141,23 +141,24 @@ __device__ __forceinline__ void join_ranges(const float *rec, int64_t step, int 
         float mx = kLowest, l = 0.f, o[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) o[i] = 0.f;
-        for (int s = lane; s < n; s += 32) mx = fmaxf(mx, __ldcg(top + s * step));
+        for (int s = lane; s < n; s += 32) mx = fmaxf(mx, __ldcg(top + s * step + (s == 0 ? ahead : 0)));
 #pragma unroll
         for (int i = 16; i > 0; i >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, i));
         for (int s0 = 0; s0 < n; s0 += 32) {
             const bool on = s0 + lane < n;
-            const float w = on ? tc::ex2(__ldcg(top + (s0 + lane) * step) - mx) : 0.f;
-            if (on) l = fmaf(__ldcg(top + (s0 + lane) * step + G), w, l);
+            const float *mine = top + (s0 + lane) * step + (s0 + lane == 0 ? ahead : 0);
+            const float w = on ? tc::ex2(__ldcg(mine) - mx) : 0.f;
+            if (on) l = fmaf(__ldcg(mine + G), w, l);
             const int end = min(32, n - s0);
             const float *at = rec + s0 * step + g * D + lane * V;
 #pragma unroll 16
             for (int s = 0; s < end; ++s) {
                 const float c = __shfl_sync(0xFFFFFFFFu, w, s);
                 if (V == 4) {
-                    const float4 x = __ldcg(reinterpret_cast<const float4 *>(at + s * step));
+                    const float4 x = __ldcg(reinterpret_cast<const float4 *>(at + s * step + (s0 + s == 0 ? ahead : 0)));
                     o[0] = fmaf(x.x, c, o[0]); o[1] = fmaf(x.y, c, o[1]); o[2] = fmaf(x.z, c, o[2]); o[3] = fmaf(x.w, c, o[3]);
                 } else {
-                    const float2 x = __ldcg(reinterpret_cast<const float2 *>(at + s * step));
+                    const float2 x = __ldcg(reinterpret_cast<const float2 *>(at + s * step + (s0 + s == 0 ? ahead : 0)));
                     o[0] = fmaf(x.x, c, o[0]); o[1] = fmaf(x.y, c, o[1]);
                 }
             }
@@ -314,7 +315,7 @@ __global__ void __launch_bounds__(kSimtThreads) cache_attention_kernel(const Att
     }
     __syncthreads();
     if (!last) return;
-    join_ranges<kSimtThreads, D>(A.part + ((int64_t)blockIdx.x - (int64_t)r.split * heads) * record, (int64_t)heads * record, r.n_split, G, out);
+    join_ranges<kSimtThreads, D>(A.part + ((int64_t)blockIdx.x - (int64_t)r.split * heads) * record, 0, (int64_t)heads * record, r.n_split, G, out);
 }
 
 }  // namespace paged

@@ -9,13 +9,18 @@
 // The pages' scales join in fp32: K's on the logits; V's in the exponent of the weights, w_j = 2^(z_j + log2 sv_j - max), with a maximum of
 // its own, so that the largest weight is 1 whatever the scales are.  The sum of the softmax, sum_j 2^(z_j - max z), is apart.
 //
-// A block takes a range of tiles of 128 keys (paged_attention.cuh) of one (unit, KV head), in groups of seven tiles:
-//   warp 0     K tiles and V tiles by TMA, a box per page, into a ring of six stages of 16 KB: K of group c + 1 before V of group c
+// The tiles of 128 keys of all heads stand in a row, by unit, head and key, and every block of the launch (two to an SM) takes an
+// equal share of it: parts of heads, whole heads, as it comes (Walk).  A head that several blocks have part in is joined by the one that
+// comes last (paged_attention.cuh).  (Ranges of equal length of each head by itself, a block each, left a last round half empty: 16 sequences
+// of up to 33 792 rows, 8 heads, 352 ranges on 296 places, 174 us.)  A block goes through its tiles in groups of up to
+// seven of one head, the roles of its warps one or two groups apart, across the heads' borders too:
+//   warp 0     K tiles and V tiles by TMA, a box per page, into a ring of six stages of 16 KB: K of group c + 1 before V of group c;
+//              the next head's query operand; the scales of a group's pages
 //   warp 1     the products, in the same order; the logits of two groups stay in tensor memory
 //   warps 2-9  a thread per key of a tile: maxima of a group, then its weights; a thread per dim: the output, rescaled once a group.
 //              Two halves of four warps: for more than four query heads each has four of them, for fewer every other tile.  (One half
-//              alone took 1800 clocks for a tile of eight heads, and two such blocks to an SM longer than the memory.)
-// Two blocks share an SM (256 columns of tensor memory and 110 KB each).  Every wait is bounded.
+//              alone took 1800 clocks for a tile of eight heads, longer than its share of the memory's time.)
+// Every wait is bounded.
 #pragma once
 #include "paged_attention.cuh"
 
@@ -27,13 +32,16 @@ constexpr int kTile = 128, kStages = 6, kMaxHeads = 8, kHalf = 4, kGroup = 7, kT
 constexpr int kQCols = 2 * kMaxHeads, kPCols = 4 * kMaxHeads;            // N of the two products; by half, piece, head
 constexpr int kMostPages = kGroup * kTile / 16;                          // pages of a group
 constexpr uint32_t kStageBytes = kTile * 128;
-constexpr uint32_t kSmemQ = kStages * kStageBytes, kSmemP = kSmemQ + kQCols * 128, kSmemRed = kSmemP + 2 * kPCols * 128;
-constexpr uint32_t kSmemInfo = kSmemRed + 2 * 8 * 2 * kHalf * 4;          // red: [group parity][warp][maxima, with V's scales][head]
-constexpr uint32_t kSmemQInv = kSmemInfo + 3 * 2 * kMostPages * 4;        // info: [group mod 3][K's scale, log2 of V's][page]
-constexpr uint32_t kSmemBar = kSmemQInv + kMaxHeads * 4;
-constexpr int kBarFull = 0, kBarEmpty = kStages, kBarQ = 2 * kStages, kBarS = kBarQ + 1, kBarPFull = kBarS + 2 * kGroup,
-              kBarPEmpty = kBarPFull + 2, kBarO = kBarPEmpty + 2, kNumBars = kBarO + 1;
-constexpr uint32_t kSmemBytes = kSmemBar + 8 * kNumBars + 16;             // (+ TMEM address, abort flag, status, last)
+constexpr int kInfos = 4;                                                // groups whose scales are kept
+constexpr uint32_t kSmemQ = kStages * kStageBytes, kSmemP = kSmemQ + 2 * kQCols * 128, kSmemRed = kSmemP + 2 * kPCols * 128;
+constexpr uint32_t kSmemInfo = kSmemRed + 2 * 8 * 3 * kHalf * 4;          // red: [group parity][warp][maxima, with V's scales, sums][head]
+constexpr int kInfo = 2 * kMostPages + kMaxHeads;                         // [K's scale, log2 of V's][page], the queries' factors
+constexpr uint32_t kSmemFirst = kSmemInfo + kInfos * kInfo * 4;           // the factors of the first head's queries
+constexpr uint32_t kSmemBar = kSmemFirst + kMaxHeads * 4;
+constexpr int kBarFull = 0, kBarEmpty = kStages, kBarQFull = 2 * kStages, kBarQEmpty = kBarQFull + 2, kBarS = kBarQEmpty + 2,
+              kBarPFull = kBarS + 2 * kGroup /* a tile's logits, by its number in the share */, kBarPEmpty = kBarPFull + 2, kBarO = kBarPEmpty + 2, kBarIFull = kBarO + 1,
+              kBarIEmpty = kBarIFull + kInfos, kNumBars = kBarIEmpty + kInfos;
+constexpr uint32_t kSmemBytes = kSmemBar + 8 * kNumBars + 32;             // (+ TMEM address, abort flag, status, two "last" words)
 constexpr uint32_t kColS = kPCols;                                        // O in the first columns, then the two groups' logits
 static_assert(kColS + 2 * kGroup * kQCols <= kTmemCols, "tensor memory");
 static_assert(2 * (kSmemBytes + 1024) <= 227 * 1024, "two blocks to an SM");
@@ -81,11 +89,144 @@ __device__ __forceinline__ void four_pieces(float a, float b, uint32_t (&piece)[
     }
 }
 
+
+// ---- a block's share -----------------------------------------------------------------------------
+// Tiles [t0, t1) of the head (u, h), whose first tile has the number `head`; t0 has the number x, the share goes to `end`.
+struct Walk {
+    int u, h, rows, tiles, t0, t1;
+    uint32_t x, end, head, per;          // per: tiles of a share; 0: shares are whole heads
+};
+__device__ __forceinline__ int tiles_of(int rows) { return (rows + kTile - 1) / kTile; }
+
+// Where a block's share begins; every warp finds it by itself.  Where whole heads make the longest share no more than kJoinTiles
+// longer than an even one, heads are not cut: joining costs that much.
+__device__ __forceinline__ bool walk_begin(const AttnArgs &A, Walk &w) {
+    const int lane = lane_id(), H = A.Hkv, each = (A.U + 31) >> 5, u0 = min(A.U, lane * each), u1 = min(A.U, u0 + each);
+    uint32_t mine = 0;
+    int longest = 0;
+#pragma unroll 4
+    for (int u = u0; u < u1; ++u) {
+        const int t = tiles_of(unit_rows(A, u));
+        mine += t;
+        longest = max(longest, t);
+    }
+    uint32_t upto = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t x = __shfl_up_sync(0xFFFFFFFFu, upto, o);
+        if (lane >= o) upto += x;
+        longest = max(longest, __shfl_xor_sync(0xFFFFFFFFu, longest, o));
+    }
+    const uint32_t all = __shfl_sync(0xFFFFFFFFu, upto, 31) * H, blocks = gridDim.x;
+    const uint32_t heads = (uint32_t)A.U * H, share = (heads + blocks - 1) / blocks;
+    w.per = (all + blocks - 1) / blocks;
+    if (share * longest <= w.per + kJoinTiles) w.per = 0;
+    int find_u = 0, base = 0;                                         // a unit and the tiles of a head of each of those before it
+    if (w.per != 0) {
+        w.x = blockIdx.x * w.per;
+        w.end = min(all, w.x + w.per);
+        if (w.x >= w.end) return false;
+        const int owner = __ffs(__ballot_sync(0xFFFFFFFFu, w.x < upto * H)) - 1;
+        if (lane == owner) {
+            base = upto - mine;
+            for (find_u = u0; find_u < u1 - 1; ++find_u) {
+                const int t = tiles_of(unit_rows(A, find_u));
+                if (w.x < (uint32_t)(base + t) * H) break;
+                base += t;
+            }
+        }
+        w.u = __shfl_sync(0xFFFFFFFFu, find_u, owner);
+        base = __shfl_sync(0xFFFFFFFFu, base, owner);
+        w.rows = unit_rows(A, w.u);
+        w.tiles = tiles_of(w.rows);
+        const uint32_t in = w.x - (uint32_t)base * H;
+        w.h = in / w.tiles;
+        w.t0 = in - w.h * w.tiles;
+        w.head = w.x - w.t0;
+    } else {
+        const uint32_t from = blockIdx.x * share, to = min(heads, from + share);
+        if (from >= to) return false;
+        // numbers of the first tiles of the heads `from` and `to`
+        uint32_t number[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t head = i ? to : from;
+            const int v = head / H, g = head - v * H, owner = v < A.U ? v / each : 31;
+            uint32_t before = upto;
+            int t = 0;
+            if (lane == owner && v < A.U) {
+                before = upto - mine;
+                for (int u = u0; u < v; ++u) before += tiles_of(unit_rows(A, u));
+                t = tiles_of(unit_rows(A, v));
+            }
+            number[i] = __shfl_sync(0xFFFFFFFFu, before * H + g * t, owner);
+            if (i == 0) { w.u = v; w.h = g; }
+        }
+        w.x = w.head = number[0];
+        w.end = number[1];
+        if (w.x >= w.end) return false;
+        w.rows = unit_rows(A, w.u);
+        w.tiles = tiles_of(w.rows);
+        while (w.tiles == 0 && w.u < A.U - 1) { w.h = 0; ++w.u; w.rows = unit_rows(A, w.u); w.tiles = tiles_of(w.rows); }
+        w.t0 = 0;
+    }
+    w.t1 = min(w.tiles, w.t0 + (int)(w.end - w.x));
+    return true;
+}
+// On to the next head; false at the end of the share.
+__device__ __forceinline__ bool walk_next(const AttnArgs &A, Walk &w) {
+    w.x += w.t1 - w.t0;
+    if (w.x >= w.end) return false;
+    if (++w.h == A.Hkv) {
+        w.h = 0;
+        do { ++w.u; w.rows = unit_rows(A, w.u); w.tiles = tiles_of(w.rows); } while (w.tiles == 0 && w.u < A.U - 1);
+    }
+    w.head = w.x;
+    w.t0 = 0;
+    w.t1 = min(w.tiles, (int)(w.end - w.x));
+    return true;
+}
+// The blocks that have part in the head: the first one, and how many.
+__device__ __forceinline__ int walk_split(const Walk &w, uint32_t &first) {
+    if (w.per == 0 || (w.t0 == 0 && w.t1 == w.tiles)) return 1;
+    first = w.head / w.per;
+    return (w.head + w.tiles - 1) / w.per - first + 1;
+}
+
+// A query head's rows of the operand, by a warp: four elements a lane.  Rows by half, piece, head.  Returns the factor of its logits:
+// the queries' power of two and the softmax's scale; NaN for a query that is not finite.
+__device__ __forceinline__ float put_query(uint32_t operand, int g, uint2 v, float scale_log2) {
+    const int lane = lane_id();
+    const float x[4] = {__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xFFFF0000u), __uint_as_float(v.y << 16), __uint_as_float(v.y & 0xFFFF0000u)};
+    float size = 0.f;
+    bool fine = true;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { size = fmaxf(size, fabsf(x[i])); fine = fine && is_finite(x[i]); }
+    if (!fine) size = __uint_as_float(0x7F800000u);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) size = fmaxf(size, __shfl_xor_sync(0xFFFFFFFFu, size, o));
+    const int ex = is_finite(size) ? max(-100, (int)(__float_as_uint(size) >> 23) - 127) - 7 : 0;   // the largest element to [128, 256)
+    const float f = power_of_two(-ex);
+    uint32_t lo[2], hi[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const float a = x[2 * i] * f, b = x[2 * i + 1] * f;
+        hi[i] = to_e4m3x2(a, b);
+        const float2 h = from_e4m3x2(hi[i]);
+        lo[i] = to_e4m3x2((a - h.x) * 16.f, (b - h.y) * 16.f);
+    }
+    const int n = (g >> 2) * 8 + (g & 3);
+    const uint32_t at = operand + (lane & 3) * 4;
+    sts32(at + n * 128 + (((lane >> 2) ^ (n & 7)) << 4), hi[0] | hi[1] << 16);
+    sts32(at + (n + 4) * 128 + (((lane >> 2) ^ ((n + 4) & 7)) << 4), lo[0] | lo[1] << 16);
+    return is_finite(size) ? power_of_two(ex) * scale_log2 : __uint_as_float(0x7FC00000u);
+}
+
 // kByTiles: at most four query heads, the halves take every other tile; else the halves have four heads each.
 template <bool kByTiles>
 __global__ void __launch_bounds__(kThreads, 2)
 cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap, const AttnArgs A) {
-    constexpr int kCols = kByTiles ? kPCols / 2 : kPCols;            // N of the second product
+    constexpr int kCols = kByTiles ? kPCols / 2 : kPCols, kHeads = kByTiles ? kHalf : kMaxHeads;    // N of the second product; heads served
     constexpr uint32_t kPv = kIdescPV | idesc_e4m3(128, kCols);
     extern __shared__ __align__(1024) uint8_t ptc_smem[];
     const uint32_t base = tc::smem_u32(ptc_smem), bars = base + kSmemBar;
@@ -94,6 +235,7 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
     int *cta_status = reinterpret_cast<int *>(tmem_slot + 2);
     volatile int *last = reinterpret_cast<volatile int *>(tmem_slot + 3);
+    float *info = reinterpret_cast<float *>(ptc_smem + kSmemInfo), *first_factors = reinterpret_cast<float *>(ptc_smem + kSmemFirst);
     if ((base & 1023u) != 0) {                       // the swizzled tiles need a 1024-byte aligned base
         predecessor_done();
         if (threadIdx.x == 0) report(A.status, 6);
@@ -102,7 +244,7 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
     auto bar = [&](int i) { return bars + 8u * i; };
     if (threadIdx.x == 0) {
         for (int i = 0; i < kNumBars; ++i)
-            tc::mbar_init(bar(i), i == kBarQ ? 256 : i == kBarPFull || i == kBarPFull + 1 ? (kByTiles ? 128 : 256) : 1);
+            tc::mbar_init(bar(i), i == kBarPFull || i == kBarPFull + 1 ? (kByTiles ? 128 : 256) : i >= kBarIEmpty ? 256 : 1);
         *abort_flag = 0;
         *cta_status = 0;
         tc::mbar_init_fence();
@@ -117,87 +259,132 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
     predecessor_done();
     successor_may_start();
 
-    Range r;
-    check_lengths(A);
-    const bool work = find_range<kTile>(A, blockIdx.x, r);
-    const int nt = work ? r.tiles : 0, groups = (nt + kGroup - 1) / kGroup;
-    const int key0 = work ? r.tile0 * kTile : 0, G = A.G;
-    const int *table = A.table + (int64_t)(work ? r.u : 0) * A.max_pages;
-    const int page_at = key0 >> A.page_shift, pages = work ? (r.rows + A.page - 1) >> A.page_shift : 0;   // first page of the range; the unit's
-    const int tile_pages = kTile >> A.page_shift, record = record_floats<128>(G);
-    unsigned long long *ticket = A.ticket + (work ? (int64_t)r.u * A.Hkv + r.h : 0), seen = 0;
-    if (threadIdx.x == 32 && work && r.n_split > 1) seen = *reinterpret_cast<volatile unsigned long long *>(ticket);
-
-    if (!work || r.rows == 0) {
-        if (work) {
-            float *out = A.out + ((int64_t)r.u * A.Hq + r.h * G) * 128;
-            for (int i = threadIdx.x; i < G * 128; i += kThreads) out[i] = 0.f;
-        }
+    Walk begin;
+    const bool work = walk_begin(A, begin);
+    const int G = A.G, tile_pages = kTile >> A.page_shift, record = record_floats<128>(G);
+    auto query = [&](const Walk &w, int g) {
+        return g < G ? *reinterpret_cast<const uint2 *>(static_cast<const __nv_bfloat16 *>(A.q) + ((int64_t)w.u * A.Hq + w.h * G + g) * 128 + lane * 4)
+                     : make_uint2(0, 0);
+    };
+    if (!work) {
     } else if (warp == 0) {
-        // numbers of a group's pages, two a lane: of the group before, of this one and of the next
-        auto numbers = [&](int c, int &a, int &b) {
-            const int j = page_at + c * kGroup * tile_pages + lane, end = min(pages, page_at + (c + 1) * kGroup * tile_pages);
-            a = j < end ? table[j] : 0;
-            b = j + 32 < end ? table[j + 32] : 0;
-            if ((unsigned)a >= (unsigned)A.n_pages) { report(A.status, kStatusIndex); a = 0; }
-            if ((unsigned)b >= (unsigned)A.n_pages) { report(A.status, kStatusIndex); b = 0; }
+        // A group's pages, two a lane: their numbers, and their scales.
+        struct Pages { int a, b; float ka, kb, va, vb; };
+        auto numbers = [&](const Walk &w, int t, Pages &p) {
+            const int j = (t << (7 - A.page_shift)) + lane, end = min((w.rows + A.page - 1) >> A.page_shift, min(t + kGroup, w.t1) << (7 - A.page_shift));
+            const int *table = A.table + (int64_t)w.u * A.max_pages;
+            p.a = j < end ? table[j] : 0;
+            p.b = j + 32 < end ? table[j + 32] : 0;
+            if ((unsigned)p.a >= (unsigned)A.n_pages) { report(A.status, kStatusIndex); p.a = 0; }
+            if ((unsigned)p.b >= (unsigned)A.n_pages) { report(A.status, kStatusIndex); p.b = 0; }
+        };
+        auto scales = [&](int h, Pages &p) {
+            const int64_t a = (int64_t)p.a * A.Hkv + h, b = (int64_t)p.b * A.Hkv + h;
+            p.ka = A.k_scale[a]; p.va = A.v_scale[a];
+            if (lane + 32 < kGroup * tile_pages) { p.kb = A.k_scale[b]; p.vb = A.v_scale[b]; }
         };
         int st = 0, phase = 0;
-        auto tiles = [&](const CUtensorMap *m, int c, int a, int b) {
-            const int n = min(kGroup, nt - c * kGroup);
-            for (int t = 0; t < n; ++t) {
+        auto tiles = [&](const CUtensorMap *m, const Pages &p, int h, int t, int n, int pages) {      // n tiles from t on of a unit of so many pages
+            for (int i = 0; i < n; ++i) {
                 if (!tc::mbar_wait_warp(bar(kBarEmpty + st), phase ^ 1, abort_flag, cta_status)) return false;
-                const int slot = t * tile_pages + lane;
-                const int x = __shfl_sync(0xFFFFFFFFu, a, slot & 31), y = __shfl_sync(0xFFFFFFFFu, b, slot & 31), id = slot < 32 ? x : y;
-                const int here = min(tile_pages, pages - page_at - (c * kGroup + t) * tile_pages);      // pages of the tile that there are
+                const int slot = i * tile_pages + lane;
+                const int x = __shfl_sync(0xFFFFFFFFu, p.a, slot & 31), y = __shfl_sync(0xFFFFFFFFu, p.b, slot & 31), id = slot < 32 ? x : y;
+                const int here = min(tile_pages, pages - (t + i) * tile_pages);      // pages of the tile that there are
                 if (tc::elect_one()) tc::mbar_expect_tx(bar(kBarFull + st), (uint32_t)here << (A.page_shift + 7));
                 __syncwarp();
-                if (lane < here) tc::tma_load_4d(base + st * kStageBytes + ((uint32_t)lane << (A.page_shift + 7)), m, bar(kBarFull + st), 0, 0, r.h, id);
+                if (lane < here) tc::tma_load_4d(base + st * kStageBytes + ((uint32_t)lane << (A.page_shift + 7)), m, bar(kBarFull + st), 0, 0, h, id);
                 __syncwarp();
                 if (++st == kStages) { st = 0; phase ^= 1; }
             }
             return true;
         };
-        int before_a = 0, before_b = 0, a, b, next_a = 0, next_b = 0;
-        numbers(0, a, b);
-        bool ok = true;
-        for (int c = 0; ok && c < groups; ++c) {
-            if (c + 1 < groups) numbers(c + 1, next_a, next_b);
-            ok = tiles(&kmap, c, a, b);
-            if (ok && c > 0) ok = tiles(&vmap, c - 1, before_a, before_b);
-            before_a = a; before_b = b; a = next_a; b = next_b;
+        Walk w = begin, ahead = begin;                               // `ahead`, `ahead_t`: the group after this one
+        int t = w.t0, ahead_t = w.t0, before_t = 0, before_n = 0, before_h = 0, before_pages = 0, group = 0, head = 0;
+        bool ok = true, more = true;
+        float factor = 0.f;                                          // of query head `lane` (from the second head on)
+        Pages now, next, before;
+        before.a = before.b = 0;
+        uint2 q[kHeads];                                             // the next head's query
+        numbers(w, t, now);
+        scales(w.h, now);
+        while (true) {
+            const int n = min(kGroup, w.t1 - t), pages = (w.rows + A.page - 1) >> A.page_shift;
+            // the group after this one: its pages' numbers, and its head's query, on their way
+            ahead_t = t + n;
+            const bool same = ahead_t < w.t1;
+            if (!same) { more = walk_next(A, ahead); ahead_t = ahead.t0; }
+            if (more) {
+                numbers(ahead, ahead_t, next);
+                if (!same) {
+#pragma unroll
+                    for (int g = 0; g < kHeads; ++g) q[g] = query(ahead, g);
+                }
+            }
+            ok = tiles(&kmap, now, w.h, t, n, pages);
+            if (!ok) break;
+            const int buffer = group % kInfos;
+            ok = tc::mbar_wait_warp(bar(kBarIEmpty + buffer), (group / kInfos & 1) ^ 1, abort_flag, cta_status);
+            if (!ok) break;
+            float *to = info + buffer * kInfo;
+            if (lane < kMaxHeads) to[2 * kMostPages + lane] = factor;
+            to[lane] = now.ka; to[kMostPages + lane] = log2_of(now.va);
+            if (lane + 32 < kMostPages) { to[lane + 32] = now.kb; to[kMostPages + lane + 32] = log2_of(now.vb); }
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(bar(kBarIFull + buffer));
+            if (more) scales(ahead.h, next);
+            if (group > 0) ok = tiles(&vmap, before, before_h, before_t, before_n, before_pages);
+            if (!ok) break;
+            before = now; before_h = w.h; before_t = t; before_n = n; before_pages = pages;
+            if (!more) break;
+            if (!same) {                                             // the next head's operand (the first one's is made below)
+                ++head;
+                ok = tc::mbar_wait_warp(bar(kBarQEmpty + (head & 1)), (head >> 1 & 1) ^ 1, abort_flag, cta_status);
+                if (!ok) break;
+#pragma unroll
+                for (int g = 0; g < kHeads; ++g) {
+                    const float f = put_query(base + kSmemQ + (head & 1) * kQCols * 128, g, q[g], A.scale_log2);
+                    factor = lane == g ? f : factor;
+                }
+                fence_proxy_async();
+                __syncwarp();
+                if (lane == 0) tc::mbar_arrive(bar(kBarQFull + (head & 1)));
+            }
+            w = ahead; t = ahead_t; now = next; ++group;
         }
-        if (ok) ok = tiles(&vmap, groups - 1, before_a, before_b);
+        if (ok) ok = tiles(&vmap, before, before_h, before_t, before_n, before_pages);
         if (!ok)         // winding down after a timeout: give copies already issued a moment to land
             for (int i = 0; i < kStages; ++i)
                 for (int s = 0; s < (1 << 16) && !tc::mbar_try_wait(bar(kBarFull + i), 0) && !tc::mbar_try_wait(bar(kBarFull + i), 1); ++s) {}
     } else if (warp == 1) {
-        const uint32_t q_lo = tc::desc_lo(base + kSmemQ);
-        int st = 0, phase = 0;
+        int st = 0, phase = 0, tile = 0, made = 0;                   // made: the logits' bars, in turn
         auto next = [&]() { if (++st == kStages) { st = 0; phase ^= 1; } };
-        auto logits = [&](int c) {
-            const int n = min(kGroup, nt - c * kGroup);
+        auto logits = [&](int group, int n, uint32_t q_lo) {
             for (int t = 0; t < n; ++t, next()) {
                 if (!tc::mbar_wait_warp(bar(kBarFull + st), phase, abort_flag, cta_status)) return false;
                 tc::tc_fence_after();
-                const uint32_t a_lo = tc::desc_lo(base + st * kStageBytes), at = tmem + kColS + ((c & 1) * kGroup + t) * kQCols;
+                const uint32_t a_lo = tc::desc_lo(base + st * kStageBytes), at = tmem + kColS + ((group & 1) * kGroup + t) * kQCols;
                 if (tc::elect_one()) {
 #pragma unroll
                     for (int j = 0; j < 4; ++j) umma_e4m3(at, a_lo + 2 * j, q_lo + 2 * j, kIdescQK, j > 0);
                     tc::umma_commit(bar(kBarEmpty + st));
-                    tc::umma_commit(bar(kBarS + (c & 1) * kGroup + t));
+                    tc::umma_commit(bar(kBarS + made));
                 }
                 __syncwarp();
+                if (++made == 2 * kGroup) made = 0;
             }
             return true;
         };
-        auto output = [&](int c) {
-            const int n = min(kGroup, nt - c * kGroup);
-            for (int t = 0; t < n; ++t, next()) {
-                const int i = c * kGroup + t, pb = i & 1;
-                if (!tc::mbar_wait_warp(bar(kBarFull + st), phase, abort_flag, cta_status) ||
-                    !tc::mbar_wait_warp(bar(kBarPFull + pb), (i >> 1) & 1, abort_flag, cta_status))
-                    return false;
+        auto output = [&](int n, int valid) {                        // valid: rows of the last tile that the unit has
+            for (int t = 0; t < n; ++t, ++tile, next()) {
+                const int pb = tile & 1;
+                if (!tc::mbar_wait_warp(bar(kBarFull + st), phase, abort_flag, cta_status)) return false;
+                if (t == n - 1 && valid < kTile) {
+                    // rows of V behind the unit's last one: zeros, since a weight of zero times a NaN would not be nothing
+                    for (int i = valid * 8 + lane; i < kTile * 8; i += 32) tc::sts128(base + st * kStageBytes + i * 16, 0.f, 0.f, 0.f, 0.f);
+                    fence_proxy_async();
+                    __syncwarp();
+                }
+                if (!tc::mbar_wait_warp(bar(kBarPFull + pb), (tile >> 1) & 1, abort_flag, cta_status)) return false;
                 tc::tc_fence_after();
                 const uint32_t a_lo = tc::desc_lo(base + st * kStageBytes), p_lo = tc::desc_lo(base + kSmemP + pb * kPCols * 128);
                 if (tc::elect_one()) {
@@ -211,79 +398,47 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
             }
             return true;
         };
-        bool ok = tc::mbar_wait_warp(bar(kBarQ), 0, abort_flag, cta_status);
-        for (int c = 0; ok && c < groups; ++c) {
-            ok = logits(c);
-            if (ok && c > 0) ok = output(c - 1);
-        }
-        if (ok) output(groups - 1);
+        Walk w = begin;
+        bool ok = true;
+        int group = 0, head = 0, before_n = 0, before_valid = 0;
+        do {
+            const uint32_t q_lo = tc::desc_lo(base + kSmemQ + (head & 1) * kQCols * 128);
+            ok = tc::mbar_wait_warp(bar(kBarQFull + (head & 1)), head >> 1 & 1, abort_flag, cta_status);
+            for (int t = w.t0; ok && t < w.t1; t += kGroup, ++group) {
+                const int n = min(kGroup, w.t1 - t);
+                ok = logits(group, n, q_lo);
+                if (ok && t + n == w.t1) {
+                    if (tc::elect_one()) tc::umma_commit(bar(kBarQEmpty + (head & 1)));
+                    __syncwarp();
+                }
+                if (ok && group > 0) ok = output(before_n, before_valid);
+                before_n = n;
+                before_valid = min(kTile, w.rows - (t + n - 1) * kTile);
+            }
+            ++head;
+        } while (ok && walk_next(A, w));
+        if (ok) output(before_n, before_valid);
     } else {
         const int e = threadIdx.x - 64, half = e >> 7;               // 0 .. 255
         const int row = 32 * (warp & 3) + lane;                      // TMEM lane this thread reads: key of a tile / output dim
         const uint32_t trow = tmem + ((uint32_t)(32 * (warp & 3)) << 16);
         const int set = kByTiles ? 0 : half, g0 = kHalf * set;       // this half's heads
-        const int part_of = kByTiles ? half : 0, parts = kByTiles ? 2 : 1;   // ... and tiles: those with i % parts == part_of
+        constexpr int parts = kByTiles ? 2 : 1;                      // ... and tiles: all, or those with the number of the half
         const uint32_t tcols = trow + set * 8;                       // columns of their logits within a tile's
-        float *red = reinterpret_cast<float *>(ptc_smem + kSmemRed), *info = reinterpret_cast<float *>(ptc_smem + kSmemInfo);
-        float *qinv = reinterpret_cast<float *>(ptc_smem + kSmemQInv);
-        // scales of a group's pages, one a thread
-        auto scales = [&](int c, float &k, float &lv) {
-            const int j = page_at + c * kGroup * tile_pages + e;
-            k = 0.f; lv = 0.f;
-            if (e < kGroup * tile_pages && j < pages) {
-                int id = table[j];
-                if ((unsigned)id >= (unsigned)A.n_pages) id = 0;    // (the loader has reported it)
-                k = A.k_scale[(int64_t)id * A.Hkv + r.h];
-                lv = log2_of(A.v_scale[(int64_t)id * A.Hkv + r.h]);
-            }
-        };
-        float next_k, next_lv;
-        scales(0, next_k, next_lv);
-        {   // the query operand: a warp per head (zero beyond G), four elements a lane
-            const int g = e >> 5;
-            float x[4] = {0.f, 0.f, 0.f, 0.f};
-            if (g < G) {
-                const uint2 v = *reinterpret_cast<const uint2 *>(static_cast<const __nv_bfloat16 *>(A.q) + ((int64_t)r.u * A.Hq + r.h * G + g) * 128 + lane * 4);
-                x[0] = __uint_as_float(v.x << 16); x[1] = __uint_as_float(v.x & 0xFFFF0000u);
-                x[2] = __uint_as_float(v.y << 16); x[3] = __uint_as_float(v.y & 0xFFFF0000u);
-            }
-            float size = 0.f;
-            bool fine = true;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) { size = fmaxf(size, fabsf(x[i])); fine = fine && is_finite(x[i]); }
-            if (!fine) size = __uint_as_float(0x7F800000u);
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) size = fmaxf(size, __shfl_xor_sync(0xFFFFFFFFu, size, o));
-            const int ex = is_finite(size) ? max(-100, (int)(__float_as_uint(size) >> 23) - 127) - 7 : 0;   // the largest element to [128, 256)
-            const float f = power_of_two(-ex);
-            uint32_t lo[2], hi[2];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const float a = x[2 * i] * f, b = x[2 * i + 1] * f;
-                hi[i] = to_e4m3x2(a, b);
-                const float2 h = from_e4m3x2(hi[i]);
-                lo[i] = to_e4m3x2((a - h.x) * 16.f, (b - h.y) * 16.f);
-            }
-            // rows of the operand: by half, piece, head
-            const int n = (g >> 2) * 8 + (g & 3);
-            const uint32_t at = base + kSmemQ + (lane & 3) * 4;
-            sts32(at + n * 128 + (((lane >> 2) ^ (n & 7)) << 4), hi[0] | hi[1] << 16);
-            sts32(at + (n + 4) * 128 + (((lane >> 2) ^ ((n + 4) & 7)) << 4), lo[0] | lo[1] << 16);
-            // a query that is not finite: its logits become NaN by this factor
-            if (lane == 0) qinv[g] = is_finite(size) ? power_of_two(ex) * A.scale_log2 : __uint_as_float(0x7FC00000u);
+        float *red = reinterpret_cast<float *>(ptc_smem + kSmemRed);
+        if ((e >> 5) < kHeads) {                                     // the first head's operand, a warp per query head
+            const float f = put_query(base + kSmemQ, e >> 5, query(begin, e >> 5), A.scale_log2);
+            if (lane == 0) first_factors[e >> 5] = f;
         }
         fence_proxy_async();
-        tc::mbar_arrive(bar(kBarQ));
-        if (e < kMostPages) { info[e] = next_k; info[kMostPages + e] = next_lv; }
         epi_sync();
+        if (e == 0) tc::mbar_arrive(bar(kBarQFull));
 
         float cq[kHalf], m[kHalf], mv[kHalf], l[kHalf], acc[kHalf];
-#pragma unroll
-        for (int g = 0; g < kHalf; ++g) { cq[g] = qinv[g0 + g]; m[g] = kLowest; mv[g] = kLowest; l[g] = 0.f; acc[g] = 0.f; }
         bool ok = true;
-        auto add_output = [&](int c) {                               // group c's product into acc
+        auto add_output = [&](int group) {                           // a group's product into acc
             if (kByTiles && half != 0) return;                       // (one thread a dim is enough)
-            ok = ok && tc::mbar_wait_warp(bar(kBarO), c & 1, abort_flag, cta_status);
+            ok = ok && tc::mbar_wait_warp(bar(kBarO), group & 1, abort_flag, cta_status);
             if (!ok) return;
             tc::tc_fence_after();
             float o[8], o2[8];
@@ -292,129 +447,28 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
 #pragma unroll
             for (int g = 0; g < kHalf; ++g) acc[g] += fmaf(fmaf(fmaf(o2[4 + g], 0.0625f, o2[g]), 0.0625f, o[4 + g]), 0.0625f, o[g]);
         };
-        for (int c = 0; c < groups; ++c) {
-            const int n = min(kGroup, nt - c * kGroup), first_key = key0 + c * kGroup * kTile;
-            const int t0 = kByTiles ? (c * kGroup + part_of) & 1 : 0;  // this half's first tile of the group
-            const float *in = info + (c % 3) * 2 * kMostPages;
-            if (c + 1 < groups) scales(c + 1, next_k, next_lv);
-            float top[kHalf], topv[kHalf];
-#pragma unroll
-            for (int g = 0; g < kHalf; ++g) { top[g] = kLowest; topv[g] = kLowest; }
-            for (int t = t0; t < n; t += parts) {
-                ok = ok && tc::mbar_wait_warp(bar(kBarS + (c & 1) * kGroup + t), (c >> 1) & 1, abort_flag, cta_status);
-                if (!ok) continue;
-                tc::tc_fence_after();
-                float s[8];
-                tmem_ld8(tcols + kColS + ((c & 1) * kGroup + t) * kQCols, s);
-                if (first_key + t * kTile + row < r.rows) {
-                    const int j = (t * kTile + row) >> A.page_shift;
-                    const float ks = in[j], lv = in[kMostPages + j];
-#pragma unroll
-                    for (int g = 0; g < kHalf; ++g) {
-                        const float z = fmaf(s[4 + g], 0.0625f, s[g]) * (ks * cq[g]);
-                        top[g] = fmaxf(top[g], z);
-                        topv[g] = fmaxf(topv[g], z + lv);
-                    }
-                }
-            }
-            float *all = red + (c & 1) * 8 * 2 * kHalf;
+        // A head is finished behind the barrier of the group after it: its sums of weights have been left in `all` before.
+        auto leave_sums = [&](float *all) {
 #pragma unroll
             for (int g = 0; g < kHalf; ++g) {
-#pragma unroll
-                for (int o = 16; o > 0; o >>= 1) {
-                    top[g] = fmaxf(top[g], __shfl_xor_sync(0xFFFFFFFFu, top[g], o));
-                    topv[g] = fmaxf(topv[g], __shfl_xor_sync(0xFFFFFFFFu, topv[g], o));
-                }
-                if (lane == 0) { all[(e >> 5) * 2 * kHalf + g] = top[g]; all[(e >> 5) * 2 * kHalf + kHalf + g] = topv[g]; }
+                const float sum = warp_sum(l[g]);
+                if (lane == 0) all[(e >> 5) * 3 * kHalf + 2 * kHalf + g] = sum;
             }
-            // (three buffers: a slower thread may still read the scales of the group before, and nobody those before it)
-            if (c + 1 < groups && e < kMostPages) {
-                float *to = info + ((c + 1) % 3) * 2 * kMostPages;
-                to[e] = next_k; to[kMostPages + e] = next_lv;
-            }
-            if (c > 0) {                                             // (before the barrier: behind it this group's product may begin)
-                add_output(c - 1);
-                tc::tc_fence_before();
-            }
-            epi_sync();
+        };
+        auto finish = [&](const Walk &w, const float *all) {
+            if ((kByTiles && half != 0) || !ok) return;
+            uint32_t first = 0;
+            const int n_split = walk_split(w, first);
+            float *out = A.out + ((int64_t)w.u * A.Hq + w.h * G) * 128 + row;
+            float *part = A.part + ((int64_t)2 * blockIdx.x + (w.t0 == 0)) * record;
 #pragma unroll
             for (int g = 0; g < kHalf; ++g) {
-                float a = m[g], b = mv[g];
-#pragma unroll
-                for (int w = 0; w < 4 * parts; ++w) {
-                    const float *of = all + (4 * (kByTiles ? 0 : half) + w) * 2 * kHalf;
-                    a = fmaxf(a, of[g]);
-                    b = fmaxf(b, of[kHalf + g]);
-                }
-                l[g] *= tc::ex2(m[g] - a);
-                acc[g] *= tc::ex2(mv[g] - b);
-                m[g] = a; mv[g] = b;
-            }
-            for (int t = t0; t < n; t += parts) {
-                const int i = c * kGroup + t, pb = i & 1;
-                ok = ok && tc::mbar_wait_warp(bar(kBarPEmpty + pb), ((i >> 1) & 1) ^ 1, abort_flag, cta_status);
-                if (!ok) continue;
-                float s[8];
-                tmem_ld8(tcols + kColS + ((c & 1) * kGroup + t) * kQCols, s);
-                const bool valid = first_key + t * kTile + row < r.rows;
-                const int j = (t * kTile + row) >> A.page_shift;
-                const float ks = in[j], lv = in[kMostPages + j] + 8.f;                  // (weights times 256)
-                // rows of the operand by half, piece, head: their number's last three bits, which the swizzle takes, are those of 4 piece + head
-                const uint32_t at = base + kSmemP + pb * kPCols * 128 + set * 16 * 128 + (row & 15);
-#pragma unroll
-                for (int g = 0; g < kHalf; g += 2) {
-                    if (g0 + g < G) {
-                        float w[2];
-#pragma unroll
-                        for (int k = 0; k < 2; ++k) {
-                            const float z = fmaf(s[4 + g + k], 0.0625f, s[g + k]) * (ks * cq[g + k]);
-                            l[g + k] += valid ? tc::ex2(z - m[g + k]) : 0.f;
-                            w[k] = valid ? tc::ex2(z + lv - mv[g + k]) : 0.f;
-                        }
-                        uint32_t piece[4];
-                        four_pieces(w[0], w[1], piece);
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            const int n0 = 4 * k + g, n1 = n0 + 1;
-                            sts8(at + n0 * 128 + (((row >> 4) ^ (n0 & 7)) << 4), piece[k]);
-                            sts8(at + n1 * 128 + (((row >> 4) ^ (n1 & 7)) << 4), piece[k] >> 8);
-                        }
-                    }
-                }
-                if (i == nt - 1 && first_key + (t + 1) * kTile > r.rows) {
-                    // Rows of V behind the unit's last one: zeros, since a weight of zero times a NaN would not be nothing.  The range's last
-                    // tile is the last one the loader sends; the stage's load before it has been waited for (it is a K tile of this group, or a V tile
-                    // whose product is done: of the group before, or four and more tiles back in this one).
-                    const int load = 2 * nt - 1, at_stage = load % kStages;
-                    ok = ok && tc::mbar_wait_warp(bar(kBarFull + at_stage), (load / kStages) & 1, abort_flag, cta_status);
-                    if (!ok) continue;
-                    if (!valid)
-                        for (int k = half * (2 - parts) * 4; k < (kByTiles ? 8 : half * 4 + 4); ++k)
-                            tc::sts128(base + at_stage * kStageBytes + row * 128 + k * 16, 0.f, 0.f, 0.f, 0.f);
-                }
-                fence_proxy_async();
-                tc::tc_fence_before();
-                tc::mbar_arrive(bar(kBarPFull + pb));
-            }
-        }
-        add_output(groups - 1);
-        float *sums = red + (groups & 1) * 8 * 2 * kHalf;              // (not what the last group's maxima are read from)
-#pragma unroll
-        for (int g = 0; g < kHalf; ++g) {
-            l[g] = warp_sum(l[g]);
-            if (lane == 0) sums[(e >> 5) * 2 * kHalf + g] = l[g];
-        }
-        epi_sync();
-        float *out = A.out + ((int64_t)r.u * A.Hq + r.h * G) * 128 + row, *part = A.part + (int64_t)blockIdx.x * record;
-        if (!kByTiles || half == 0) {
-#pragma unroll
-            for (int g = 0; g < kHalf; ++g) {
-                if (g0 + g < G && ok) {
+                if (g0 + g < G) {
                     float sum = 0.f;
 #pragma unroll
-                    for (int w = 0; w < 4 * parts; ++w) sum += sums[(4 * (kByTiles ? 0 : half) + w) * 2 * kHalf + g];
+                    for (int i = 0; i < 4 * parts; ++i) sum += all[(4 * (kByTiles ? 0 : half) + i) * 3 * kHalf + 2 * kHalf + g];
                     const float o = acc[g] * tc::ex2(mv[g] - m[g] - 8.f);       // relative to the logits' maximum
-                    if (r.n_split == 1) {
+                    if (n_split == 1) {
                         out[(g0 + g) * 128] = o / sum;
                     } else {
                         part[(g0 + g) * 128 + row] = o;
@@ -422,19 +476,150 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
                     }
                 }
             }
+        };
+        Walk w = begin, done = begin;
+        int group = 0, head = 0, tile = 0;
+        while (true) {
+            for (int t1 = w.t0; t1 < w.t1; t1 += kGroup, ++group) {
+                const int n = min(kGroup, w.t1 - t1), first_key = t1 * kTile, buffer = group % kInfos;
+                const int from = kByTiles ? (tile + half) & 1 : 0;   // this half's first tile of the group
+                const float *in = info + buffer * kInfo, *factors = (head == 0 ? first_factors : in + 2 * kMostPages) + g0;
+                ok = ok && tc::mbar_wait_warp(bar(kBarIFull + buffer), group / kInfos & 1, abort_flag, cta_status);
+                float top[kHalf], topv[kHalf];
+#pragma unroll
+                for (int g = 0; g < kHalf; ++g) { top[g] = kLowest; topv[g] = kLowest; cq[g] = ok ? factors[g] : 0.f; }
+                for (int t = from; t < n; t += parts) {
+                    const int turn = (tile + t) / (2 * kGroup);
+                    ok = ok && tc::mbar_wait_warp(bar(kBarS + tile + t - turn * 2 * kGroup), turn & 1, abort_flag, cta_status);
+                    if (!ok) continue;
+                    tc::tc_fence_after();
+                    float s[8];
+                    tmem_ld8(tcols + kColS + ((group & 1) * kGroup + t) * kQCols, s);
+                    if (first_key + t * kTile + row < w.rows) {
+                        const int j = (t * kTile + row) >> A.page_shift;
+                        const float ks = in[j], lv = in[kMostPages + j];
+#pragma unroll
+                        for (int g = 0; g < kHalf; ++g) {
+                            const float z = fmaf(s[4 + g], 0.0625f, s[g]) * (ks * cq[g]);
+                            top[g] = fmaxf(top[g], z);
+                            topv[g] = fmaxf(topv[g], z + lv);
+                        }
+                    }
+                }
+                float *all = red + (group & 1) * 8 * 3 * kHalf;
+#pragma unroll
+                for (int g = 0; g < kHalf; ++g) {
+#pragma unroll
+                    for (int o = 16; o > 0; o >>= 1) {
+                        top[g] = fmaxf(top[g], __shfl_xor_sync(0xFFFFFFFFu, top[g], o));
+                        topv[g] = fmaxf(topv[g], __shfl_xor_sync(0xFFFFFFFFu, topv[g], o));
+                    }
+                    if (lane == 0) { all[(e >> 5) * 3 * kHalf + g] = top[g]; all[(e >> 5) * 3 * kHalf + kHalf + g] = topv[g]; }
+                }
+                const bool first = t1 == w.t0;
+                if (group > 0) {                                     // (before the barrier: behind it this group's product may begin)
+                    add_output(group - 1);
+                    tc::tc_fence_before();
+                    if (first) leave_sums(all);
+                }
+                epi_sync();
+                if (first) {
+                    if (group > 0) finish(done, all);
+#pragma unroll
+                    for (int g = 0; g < kHalf; ++g) { m[g] = kLowest; mv[g] = kLowest; l[g] = 0.f; acc[g] = 0.f; }
+                    done = w;
+                }
+#pragma unroll
+                for (int g = 0; g < kHalf; ++g) {
+                    float a = m[g], b = mv[g];
+#pragma unroll
+                    for (int i = 0; i < 4 * parts; ++i) {
+                        const float *of = all + (4 * (kByTiles ? 0 : half) + i) * 3 * kHalf;
+                        a = fmaxf(a, of[g]);
+                        b = fmaxf(b, of[kHalf + g]);
+                    }
+                    l[g] *= tc::ex2(m[g] - a);
+                    acc[g] *= tc::ex2(mv[g] - b);
+                    m[g] = a; mv[g] = b;
+                }
+                for (int t = from; t < n; t += parts) {
+                    const int i = tile + t, pb = i & 1;
+                    ok = ok && tc::mbar_wait_warp(bar(kBarPEmpty + pb), ((i >> 1) & 1) ^ 1, abort_flag, cta_status);
+                    if (!ok) continue;
+                    float s[8];
+                    tmem_ld8(tcols + kColS + ((group & 1) * kGroup + t) * kQCols, s);
+                    const bool valid = first_key + t * kTile + row < w.rows;
+                    const int j = (t * kTile + row) >> A.page_shift;
+                    const float ks = in[j], lv = in[kMostPages + j] + 8.f;                  // (weights times 256)
+                    // rows of the operand by half, piece, head: their number's last three bits, which the swizzle takes, are those of 4 piece + head
+                    const uint32_t at = base + kSmemP + pb * kPCols * 128 + set * 16 * 128 + (row & 15);
+#pragma unroll
+                    for (int g = 0; g < kHalf; g += 2) {
+                        if (g0 + g < G) {
+                            float x[2];
+#pragma unroll
+                            for (int k = 0; k < 2; ++k) {
+                                const float z = fmaf(s[4 + g + k], 0.0625f, s[g + k]) * (ks * cq[g + k]);
+                                l[g + k] += valid ? tc::ex2(z - m[g + k]) : 0.f;
+                                x[k] = valid ? tc::ex2(z + lv - mv[g + k]) : 0.f;
+                            }
+                            uint32_t piece[4];
+                            four_pieces(x[0], x[1], piece);
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                const int n0 = 4 * k + g, n1 = n0 + 1;
+                                sts8(at + n0 * 128 + (((row >> 4) ^ (n0 & 7)) << 4), piece[k]);
+                                sts8(at + n1 * 128 + (((row >> 4) ^ (n1 & 7)) << 4), piece[k] >> 8);
+                            }
+                        }
+                    }
+                    fence_proxy_async();
+                    tc::tc_fence_before();
+                    tc::mbar_arrive(bar(kBarPFull + pb));
+                }
+                tc::mbar_arrive(bar(kBarIEmpty + buffer));
+                tile += n;
+            }
+            ++head;
+            if (!walk_next(A, w)) break;
         }
+        add_output(group - 1);
+        float *all = red + (group & 1) * 8 * 3 * kHalf;
+        leave_sums(all);
+        epi_sync();
+        finish(done, all);
+    }
+    // units without rows, shared out over the blocks
+    for (int u = blockIdx.x; u < A.U; u += gridDim.x) {
+        const int n = A.rows[u];
+        if (n < 0 || n > A.max_pages << A.page_shift) { if (threadIdx.x == 0) report(A.status, kStatusIndex); }
+        if (n <= 0)
+            for (int i = threadIdx.x; i < A.Hq * 128; i += kThreads) A.out[(int64_t)u * A.Hq * 128 + i] = 0.f;
     }
     tc::tc_fence_before();
     __syncthreads();
     tc::tc_fence_after();
     if (warp == 1) tc::tmem_dealloc(tmem, kTmemCols);
     if (threadIdx.x == 0 && *abort_flag != 0) report(A.status, *cta_status);
-    if (!work || r.n_split == 1) return;
-    if (threadIdx.x == 32) *last = take_ticket(ticket, seen, A.call, r.n_split);
-    __syncthreads();
-    if (!*last) return;
-    join_ranges<kThreads, 128>(A.part + ((int64_t)blockIdx.x - (int64_t)r.split * A.Hkv) * record, (int64_t)A.Hkv * record, r.n_split, G,
-                               A.out + ((int64_t)r.u * A.Hq + r.h * G) * 128);
+    if (!work || begin.per == 0) return;
+    // the first and the last head of the share may be others' too
+    Walk w = begin;
+    do {
+        uint32_t first = 0;
+        const int n = walk_split(w, first);
+        if (n > 1) {
+            if (threadIdx.x == 0) {
+                unsigned long long *ticket = A.ticket + (int64_t)w.u * A.Hkv + w.h;
+                *last = take_ticket(ticket, *reinterpret_cast<volatile unsigned long long *>(ticket), A.call, n);
+            }
+            __syncthreads();
+            if (*last) {
+                // (the first block's record is its last head's, in the second place, the others' their first head's)
+                join_ranges<kThreads, 128>(A.part + (int64_t)2 * first * record, record, (int64_t)2 * record, n, G, A.out + ((int64_t)w.u * A.Hq + w.h * G) * 128);
+            }
+            __syncthreads();
+        }
+    } while (walk_next(A, w));
 }
 
 }  // namespace ptc
