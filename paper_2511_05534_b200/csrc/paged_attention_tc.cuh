@@ -14,8 +14,8 @@
 // comes last (paged_attention.cuh).  (Ranges of equal length of each head by itself, a block each, left a last round half empty: 16 sequences
 // of up to 33 792 rows, 8 heads, 352 ranges on 296 places, 174 us.)  A block goes through its tiles in groups of up to
 // seven of one head, the roles of its warps one or two groups apart, across the heads' borders too:
-//   warp 0     K tiles and V tiles by TMA, a box per page, into a ring of six stages of 16 KB: K of group c + 1 before V of group c;
-//              the next head's query operand; the scales of a group's pages
+//   warp 0     K tiles and V tiles by TMA, a box per page, into a ring of six stages of 16 KB: a tile of K of group c + 1 and one of V of
+//              group c in turn; the next head's query operand; the scales of a group's pages
 //   warp 1     the products, in the same order; the logits of two groups stay in tensor memory
 //   warps 2-9  a thread per key of a tile: maxima of a group, then its weights; a thread per dim: the output, rescaled once a group.
 //              Two halves of four warps: for more than four query heads each has four of them, for fewer every other tile.  (One half
@@ -284,58 +284,65 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
             if (lane + 32 < kGroup * tile_pages) { p.kb = A.k_scale[b]; p.vb = A.v_scale[b]; }
         };
         int st = 0, phase = 0;
-        auto tiles = [&](const CUtensorMap *m, const Pages &p, int h, int t, int n, int pages) {      // n tiles from t on of a unit of so many pages
-            for (int i = 0; i < n; ++i) {
-                if (!tc::mbar_wait_warp(bar(kBarEmpty + st), phase ^ 1, abort_flag, cta_status)) return false;
-                const int slot = i * tile_pages + lane;
-                const int x = __shfl_sync(0xFFFFFFFFu, p.a, slot & 31), y = __shfl_sync(0xFFFFFFFFu, p.b, slot & 31), id = slot < 32 ? x : y;
-                const int here = min(tile_pages, pages - (t + i) * tile_pages);      // pages of the tile that there are
-                if (tc::elect_one()) tc::mbar_expect_tx(bar(kBarFull + st), (uint32_t)here << (A.page_shift + 7));
-                __syncwarp();
-                if (lane < here) tc::tma_load_4d(base + st * kStageBytes + ((uint32_t)lane << (A.page_shift + 7)), m, bar(kBarFull + st), 0, 0, h, id);
-                __syncwarp();
-                if (++st == kStages) { st = 0; phase ^= 1; }
-            }
+        struct Group { Pages p; int h, t, n, pages; };               // n tiles from t on of a unit of so many pages
+        auto load_tile = [&](const CUtensorMap *m, const Group &g, int i) {
+            if (!tc::mbar_wait_warp(bar(kBarEmpty + st), phase ^ 1, abort_flag, cta_status)) return false;
+            const int slot = i * tile_pages + lane;
+            const int x = __shfl_sync(0xFFFFFFFFu, g.p.a, slot & 31), y = __shfl_sync(0xFFFFFFFFu, g.p.b, slot & 31), id = slot < 32 ? x : y;
+            const int here = min(tile_pages, g.pages - (g.t + i) * tile_pages);      // pages of the tile that there are
+            if (tc::elect_one()) tc::mbar_expect_tx(bar(kBarFull + st), (uint32_t)here << (A.page_shift + 7));
+            __syncwarp();
+            if (lane < here) tc::tma_load_4d(base + st * kStageBytes + ((uint32_t)lane << (A.page_shift + 7)), m, bar(kBarFull + st), 0, 0, g.h, id);
+            __syncwarp();
+            if (++st == kStages) { st = 0; phase ^= 1; }
             return true;
         };
-        Walk w = begin, ahead = begin;                               // `ahead`, `ahead_t`: the group after this one
-        int t = w.t0, ahead_t = w.t0, before_t = 0, before_n = 0, before_h = 0, before_pages = 0, group = 0, head = 0;
+        auto load_tiles = [&](const Group &k, const Group &v) {
+            bool ok = true;
+            for (int i = 0; ok && i < max(k.n, v.n); ++i) {
+                if (i < k.n) ok = load_tile(&kmap, k, i);
+                if (ok && i < v.n) ok = load_tile(&vmap, v, i);
+            }
+            return ok;
+        };
+        Walk ahead = begin;                                          // the head of the group after this one
+        int group = 0, head = 0, end = begin.t1;
         bool ok = true, more = true;
         float factor = 0.f;                                          // of query head `lane` (from the second head on)
-        Pages now, next, before;
-        before.a = before.b = 0;
+        Group now, next, before;
         uint2 q[kHeads];                                             // the next head's query
-        numbers(w, t, now);
-        scales(w.h, now);
+        before.n = 0; before.h = before.t = before.pages = before.p.a = before.p.b = 0;
+        auto set = [&](Group &g, const Walk &w, int t) {
+            g.h = w.h; g.t = t; g.n = min(kGroup, w.t1 - t); g.pages = (w.rows + A.page - 1) >> A.page_shift;
+            numbers(w, t, g.p);
+        };
+        set(now, begin, begin.t0);
+        scales(now.h, now.p);
         while (true) {
-            const int n = min(kGroup, w.t1 - t), pages = (w.rows + A.page - 1) >> A.page_shift;
             // the group after this one: its pages' numbers, and its head's query, on their way
-            ahead_t = t + n;
-            const bool same = ahead_t < w.t1;
-            if (!same) { more = walk_next(A, ahead); ahead_t = ahead.t0; }
+            const bool same = now.t + now.n < end;
+            if (!same) { more = walk_next(A, ahead); end = ahead.t1; }
             if (more) {
-                numbers(ahead, ahead_t, next);
+                set(next, ahead, same ? now.t + now.n : ahead.t0);
                 if (!same) {
 #pragma unroll
                     for (int g = 0; g < kHeads; ++g) q[g] = query(ahead, g);
                 }
             }
-            ok = tiles(&kmap, now, w.h, t, n, pages);
+            ok = load_tiles(now, before);
             if (!ok) break;
             const int buffer = group % kInfos;
             ok = tc::mbar_wait_warp(bar(kBarIEmpty + buffer), (group / kInfos & 1) ^ 1, abort_flag, cta_status);
             if (!ok) break;
             float *to = info + buffer * kInfo;
             if (lane < kMaxHeads) to[2 * kMostPages + lane] = factor;
-            to[lane] = now.ka; to[kMostPages + lane] = log2_of(now.va);
-            if (lane + 32 < kMostPages) { to[lane + 32] = now.kb; to[kMostPages + lane + 32] = log2_of(now.vb); }
+            to[lane] = now.p.ka; to[kMostPages + lane] = log2_of(now.p.va);
+            if (lane + 32 < kMostPages) { to[lane + 32] = now.p.kb; to[kMostPages + lane + 32] = log2_of(now.p.vb); }
             __syncwarp();
             if (lane == 0) tc::mbar_arrive(bar(kBarIFull + buffer));
-            if (more) scales(ahead.h, next);
-            if (group > 0) ok = tiles(&vmap, before, before_h, before_t, before_n, before_pages);
-            if (!ok) break;
-            before = now; before_h = w.h; before_t = t; before_n = n; before_pages = pages;
+            before = now;
             if (!more) break;
+            scales(next.h, next.p);
             if (!same) {                                             // the next head's operand (the first one's is made below)
                 ++head;
                 ok = tc::mbar_wait_warp(bar(kBarQEmpty + (head & 1)), (head >> 1 & 1) ^ 1, abort_flag, cta_status);
@@ -349,53 +356,55 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
                 __syncwarp();
                 if (lane == 0) tc::mbar_arrive(bar(kBarQFull + (head & 1)));
             }
-            w = ahead; t = ahead_t; now = next; ++group;
+            now = next; ++group;
         }
-        if (ok) ok = tiles(&vmap, before, before_h, before_t, before_n, before_pages);
+        if (ok) {
+            now.n = 0;
+            ok = load_tiles(now, before);
+        }
         if (!ok)         // winding down after a timeout: give copies already issued a moment to land
             for (int i = 0; i < kStages; ++i)
                 for (int s = 0; s < (1 << 16) && !tc::mbar_try_wait(bar(kBarFull + i), 0) && !tc::mbar_try_wait(bar(kBarFull + i), 1); ++s) {}
     } else if (warp == 1) {
         int st = 0, phase = 0, tile = 0, made = 0;                   // made: the logits' bars, in turn
         auto next = [&]() { if (++st == kStages) { st = 0; phase ^= 1; } };
-        auto logits = [&](int group, int n, uint32_t q_lo) {
-            for (int t = 0; t < n; ++t, next()) {
-                if (!tc::mbar_wait_warp(bar(kBarFull + st), phase, abort_flag, cta_status)) return false;
-                tc::tc_fence_after();
-                const uint32_t a_lo = tc::desc_lo(base + st * kStageBytes), at = tmem + kColS + ((group & 1) * kGroup + t) * kQCols;
-                if (tc::elect_one()) {
+        auto logits = [&](int group, int t, uint32_t q_lo) {
+            if (!tc::mbar_wait_warp(bar(kBarFull + st), phase, abort_flag, cta_status)) return false;
+            tc::tc_fence_after();
+            const uint32_t a_lo = tc::desc_lo(base + st * kStageBytes), at = tmem + kColS + ((group & 1) * kGroup + t) * kQCols;
+            if (tc::elect_one()) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) umma_e4m3(at, a_lo + 2 * j, q_lo + 2 * j, kIdescQK, j > 0);
-                    tc::umma_commit(bar(kBarEmpty + st));
-                    tc::umma_commit(bar(kBarS + made));
-                }
-                __syncwarp();
-                if (++made == 2 * kGroup) made = 0;
+                for (int j = 0; j < 4; ++j) umma_e4m3(at, a_lo + 2 * j, q_lo + 2 * j, kIdescQK, j > 0);
+                tc::umma_commit(bar(kBarEmpty + st));
+                tc::umma_commit(bar(kBarS + made));
             }
+            __syncwarp();
+            if (++made == 2 * kGroup) made = 0;
+            next();
             return true;
         };
-        auto output = [&](int n, int valid) {                        // valid: rows of the last tile that the unit has
-            for (int t = 0; t < n; ++t, ++tile, next()) {
-                const int pb = tile & 1;
-                if (!tc::mbar_wait_warp(bar(kBarFull + st), phase, abort_flag, cta_status)) return false;
-                if (t == n - 1 && valid < kTile) {
-                    // rows of V behind the unit's last one: zeros, since a weight of zero times a NaN would not be nothing
-                    for (int i = valid * 8 + lane; i < kTile * 8; i += 32) tc::sts128(base + st * kStageBytes + i * 16, 0.f, 0.f, 0.f, 0.f);
-                    fence_proxy_async();
-                    __syncwarp();
-                }
-                if (!tc::mbar_wait_warp(bar(kBarPFull + pb), (tile >> 1) & 1, abort_flag, cta_status)) return false;
-                tc::tc_fence_after();
-                const uint32_t a_lo = tc::desc_lo(base + st * kStageBytes), p_lo = tc::desc_lo(base + kSmemP + pb * kPCols * 128);
-                if (tc::elect_one()) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) umma_e4m3(tmem, a_lo + 256 * j, p_lo + 2 * j, kPv, (t | j) != 0);
-                    tc::umma_commit(bar(kBarEmpty + st));
-                    tc::umma_commit(bar(kBarPEmpty + pb));
-                    if (t == n - 1) tc::umma_commit(bar(kBarO));
-                }
+        auto output = [&](int t, int n, int valid) {                 // valid: rows of the last tile that the unit has
+            const int pb = tile & 1;
+            if (!tc::mbar_wait_warp(bar(kBarFull + st), phase, abort_flag, cta_status)) return false;
+            if (t == n - 1 && valid < kTile) {
+                // rows of V behind the unit's last one: zeros, since a weight of zero times a NaN would not be nothing
+                for (int i = valid * 8 + lane; i < kTile * 8; i += 32) tc::sts128(base + st * kStageBytes + i * 16, 0.f, 0.f, 0.f, 0.f);
+                fence_proxy_async();
                 __syncwarp();
             }
+            if (!tc::mbar_wait_warp(bar(kBarPFull + pb), (tile >> 1) & 1, abort_flag, cta_status)) return false;
+            tc::tc_fence_after();
+            const uint32_t a_lo = tc::desc_lo(base + st * kStageBytes), p_lo = tc::desc_lo(base + kSmemP + pb * kPCols * 128);
+            if (tc::elect_one()) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) umma_e4m3(tmem, a_lo + 256 * j, p_lo + 2 * j, kPv, (t | j) != 0);
+                tc::umma_commit(bar(kBarEmpty + st));
+                tc::umma_commit(bar(kBarPEmpty + pb));
+                if (t == n - 1) tc::umma_commit(bar(kBarO));
+            }
+            __syncwarp();
+            ++tile;
+            next();
             return true;
         };
         Walk w = begin;
@@ -406,18 +415,20 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
             ok = tc::mbar_wait_warp(bar(kBarQFull + (head & 1)), head >> 1 & 1, abort_flag, cta_status);
             for (int t = w.t0; ok && t < w.t1; t += kGroup, ++group) {
                 const int n = min(kGroup, w.t1 - t);
-                ok = logits(group, n, q_lo);
+                for (int i = 0; ok && i < max(n, before_n); ++i) {   // (as the loader sends them)
+                    if (i < n) ok = logits(group, i, q_lo);
+                    if (ok && i < before_n) ok = output(i, before_n, before_valid);
+                }
                 if (ok && t + n == w.t1) {
                     if (tc::elect_one()) tc::umma_commit(bar(kBarQEmpty + (head & 1)));
                     __syncwarp();
                 }
-                if (ok && group > 0) ok = output(before_n, before_valid);
                 before_n = n;
                 before_valid = min(kTile, w.rows - (t + n - 1) * kTile);
             }
             ++head;
         } while (ok && walk_next(A, w));
-        if (ok) output(before_n, before_valid);
+        for (int i = 0; ok && i < before_n; ++i) ok = output(i, before_n, before_valid);
     } else {
         const int e = threadIdx.x - 64, half = e >> 7;               // 0 .. 255
         const int row = 32 * (warp & 3) + lane;                      // TMEM lane this thread reads: key of a tile / output dim
