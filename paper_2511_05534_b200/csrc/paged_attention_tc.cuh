@@ -9,10 +9,12 @@
 // The pages' scales join in fp32: K's on the logits; V's in the exponent of the weights, w_j = 2^(z_j + log2 sv_j - max), with a maximum of
 // its own, so that the largest weight is 1 whatever the scales are.  The sum of the softmax, sum_j 2^(z_j - max z), is apart.
 //
-// The tiles of 128 keys of all heads stand in a row, by unit, head and key, and every block of the launch (two to an SM) takes an
-// equal share of it: parts of heads, whole heads, as it comes (Walk).  A head that several blocks have part in is joined by the one that
-// comes last (paged_attention.cuh).  (Ranges of equal length of each head by itself, a block each, left a last round half empty: 16 sequences
-// of up to 33 792 rows, 8 heads, 352 ranges on 296 places, 174 us.)  A block goes through its tiles in groups of up to
+// The tiles of 128 keys of all heads stand in a row, by unit, head and key, and are cut into pieces: a long one for every block of the launch
+// (two to an SM), three quarters of its even share, and short ones that the blocks draw from a counter when they are
+// done.  (Even shares alone left the SMs done between 85 and 125 us after the start, 16 sequences of up to 33 792 rows, 8 heads: they do not all get
+// the same of the memory.  Ranges of equal length of each head by itself, a block each, left a last round half empty: 174 us.)
+// A head that several pieces have part in leaves a record for each, and cache_join_kernel joins them in order, so that results do not
+// depend on who drew what.  A block goes through its tiles in groups of up to
 // seven of one head, the roles of its warps one or two groups apart, across the heads' borders too:
 //   warp 0     K tiles and V tiles by TMA, a box per page, into a ring of six stages of 16 KB: a tile of K of group c + 1 and one of V of
 //              group c in turn; the next head's query operand; the scales of a group's pages
@@ -37,11 +39,12 @@ constexpr uint32_t kSmemQ = kStages * kStageBytes, kSmemP = kSmemQ + 2 * kQCols 
 constexpr uint32_t kSmemInfo = kSmemRed + 2 * 8 * 3 * kHalf * 4;          // red: [group parity][warp][maxima, with V's scales, sums][head]
 constexpr int kInfo = 2 * kMostPages + kMaxHeads;                         // [K's scale, log2 of V's][page], the queries' factors
 constexpr uint32_t kSmemFirst = kSmemInfo + kInfos * kInfo * 4;           // the factors of the first head's queries
-constexpr uint32_t kSmemBar = kSmemFirst + kMaxHeads * 4;
+constexpr uint32_t kSmemTask = kSmemFirst + kMaxHeads * 4;                // tasks: [group mod 4]
+constexpr uint32_t kSmemBar = kSmemTask + kInfos * 32;
 constexpr int kBarFull = 0, kBarEmpty = kStages, kBarQFull = 2 * kStages, kBarQEmpty = kBarQFull + 2, kBarS = kBarQEmpty + 2,
-              kBarPFull = kBarS + 2 * kGroup /* a tile's logits, by its number in the share */, kBarPEmpty = kBarPFull + 2, kBarO = kBarPEmpty + 2, kBarIFull = kBarO + 1,
-              kBarIEmpty = kBarIFull + kInfos, kNumBars = kBarIEmpty + kInfos;
-constexpr uint32_t kSmemBytes = kSmemBar + 8 * kNumBars + 32;             // (+ TMEM address, abort flag, status, two "last" words)
+              kBarPFull = kBarS + 2 * kGroup /* a tile's logits, by its number in the block */, kBarPEmpty = kBarPFull + 2, kBarO = kBarPEmpty + 2, kBarTask = kBarO + 1,
+              kBarIFull = kBarTask + kInfos, kBarIEmpty = kBarIFull + kInfos, kNumBars = kBarIEmpty + kInfos;
+constexpr uint32_t kSmemBytes = kSmemBar + 8 * kNumBars + 16;             // (+ TMEM address, abort flag, status)
 constexpr uint32_t kColS = kPCols;                                        // O in the first columns, then the two groups' logits
 static_assert(kColS + 2 * kGroup * kQCols <= kTmemCols, "tensor memory");
 static_assert(2 * (kSmemBytes + 1024) <= 227 * 1024, "two blocks to an SM");
@@ -90,90 +93,119 @@ __device__ __forceinline__ void four_pieces(float a, float b, uint32_t (&piece)[
 }
 
 
-// ---- a block's share -----------------------------------------------------------------------------
-// Tiles [t0, t1) of the head (u, h), whose first tile has the number `head`; t0 has the number x, the share goes to `end`.
-struct Walk {
-    int u, h, rows, tiles, t0, t1;
-    uint32_t x, end, head, per;          // per: tiles of a share; 0: shares are whole heads
-};
+// ---- pieces --------------------------------------------------------------------------------------
+constexpr int kMostPieces = 1184, kLeastPiece = 3;      // short pieces of a call; tiles of one
+
 __device__ __forceinline__ int tiles_of(int rows) { return (rows + kTile - 1) / kTile; }
 
-// Where a block's share begins; every warp finds it by itself.  Where whole heads make the longest share no more than kJoinTiles
-// longer than an even one, heads are not cut: joining costs that much.
-__device__ __forceinline__ bool walk_begin(const AttnArgs &A, Walk &w) {
-    const int lane = lane_id(), H = A.Hkv, each = (A.U + 31) >> 5, u0 = min(A.U, lane * each), u1 = min(A.U, u0 + each);
-    uint32_t mine = 0;
+// How a call is cut; every warp that asks finds it by itself, each lane from some consecutive units.
+struct Cut {
+    int each, u0, u1;                    // this lane's units
+    uint32_t mine, upto;                 // their tiles, of one head; with all units before
+    uint32_t all, blocks, share, piece;  // tiles of all heads; long pieces and their tiles; tiles of a short piece.  share 0: whole heads
+    uint32_t heads;                      // ... so many a block
+};
+// Where whole heads make the longest piece no more than kJoinTiles longer than an even one, heads are not cut: joining costs that much.
+__device__ __forceinline__ Cut make_cut(const AttnArgs &A, uint32_t blocks) {
+    Cut c;
+    const int lane = lane_id();
+    c.each = (A.U + 31) >> 5;
+    c.u0 = min(A.U, lane * c.each);
+    c.u1 = min(A.U, c.u0 + c.each);
+    c.mine = 0;
     int longest = 0;
 #pragma unroll 4
-    for (int u = u0; u < u1; ++u) {
+    for (int u = c.u0; u < c.u1; ++u) {
         const int t = tiles_of(unit_rows(A, u));
-        mine += t;
+        c.mine += t;
         longest = max(longest, t);
     }
-    uint32_t upto = mine;
+    c.upto = c.mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const uint32_t x = __shfl_up_sync(0xFFFFFFFFu, upto, o);
-        if (lane >= o) upto += x;
+        const uint32_t x = __shfl_up_sync(0xFFFFFFFFu, c.upto, o);
+        if (lane >= o) c.upto += x;
         longest = max(longest, __shfl_xor_sync(0xFFFFFFFFu, longest, o));
     }
-    const uint32_t all = __shfl_sync(0xFFFFFFFFu, upto, 31) * H, blocks = gridDim.x;
-    const uint32_t heads = (uint32_t)A.U * H, share = (heads + blocks - 1) / blocks;
-    w.per = (all + blocks - 1) / blocks;
-    if (share * longest <= w.per + kJoinTiles) w.per = 0;
-    int find_u = 0, base = 0;                                         // a unit and the tiles of a head of each of those before it
-    if (w.per != 0) {
-        w.x = blockIdx.x * w.per;
-        w.end = min(all, w.x + w.per);
-        if (w.x >= w.end) return false;
-        const int owner = __ffs(__ballot_sync(0xFFFFFFFFu, w.x < upto * H)) - 1;
-        if (lane == owner) {
-            base = upto - mine;
-            for (find_u = u0; find_u < u1 - 1; ++find_u) {
-                const int t = tiles_of(unit_rows(A, find_u));
-                if (w.x < (uint32_t)(base + t) * H) break;
-                base += t;
-            }
-        }
-        w.u = __shfl_sync(0xFFFFFFFFu, find_u, owner);
-        base = __shfl_sync(0xFFFFFFFFu, base, owner);
-        w.rows = unit_rows(A, w.u);
-        w.tiles = tiles_of(w.rows);
-        const uint32_t in = w.x - (uint32_t)base * H;
-        w.h = in / w.tiles;
-        w.t0 = in - w.h * w.tiles;
-        w.head = w.x - w.t0;
+    c.blocks = blocks;
+    c.all = __shfl_sync(0xFFFFFFFFu, c.upto, 31) * A.Hkv;
+    const uint32_t heads = (uint32_t)A.U * A.Hkv, even = (c.all + blocks - 1) / blocks;
+    c.heads = heads <= blocks ? 1 : (heads + blocks - 1) / blocks;
+    if (c.heads * longest <= even + kJoinTiles) {
+        c.share = 0;
+        c.piece = 1;
     } else {
-        const uint32_t from = blockIdx.x * share, to = min(heads, from + share);
-        if (from >= to) return false;
-        // numbers of the first tiles of the heads `from` and `to`
-        uint32_t number[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const uint32_t head = i ? to : from;
-            const int v = head / H, g = head - v * H, owner = v < A.U ? v / each : 31;
-            uint32_t before = upto;
-            int t = 0;
-            if (lane == owner && v < A.U) {
-                before = upto - mine;
-                for (int u = u0; u < v; ++u) before += tiles_of(unit_rows(A, u));
-                t = tiles_of(unit_rows(A, v));
-            }
-            number[i] = __shfl_sync(0xFFFFFFFFu, before * H + g * t, owner);
-            if (i == 0) { w.u = v; w.h = g; }
-        }
-        w.x = w.head = number[0];
-        w.end = number[1];
-        if (w.x >= w.end) return false;
-        w.rows = unit_rows(A, w.u);
-        w.tiles = tiles_of(w.rows);
-        while (w.tiles == 0 && w.u < A.U - 1) { w.h = 0; ++w.u; w.rows = unit_rows(A, w.u); w.tiles = tiles_of(w.rows); }
-        w.t0 = 0;
+        c.share = (even * 3 + 3) / 4;
+        const uint32_t left = c.all > c.share * blocks ? c.all - c.share * blocks : 0;
+        c.piece = max((uint32_t)kLeastPiece, (left + kMostPieces - 1) / kMostPieces);
     }
-    w.t1 = min(w.tiles, w.t0 + (int)(w.end - w.x));
+    return c;
+}
+// The first tile of a piece (or, for a number past the last piece, something not below c.all) and the piece that a tile is in; share > 0.
+__device__ __forceinline__ uint32_t piece_begin(const Cut &c, uint32_t i) {
+    return i <= c.blocks ? i * c.share : c.blocks * c.share + (i - c.blocks) * c.piece;
+}
+__device__ __forceinline__ uint32_t piece_of(const Cut &c, uint32_t x) {
+    return x < c.blocks * c.share ? x / c.share : c.blocks + (x - c.blocks * c.share) / c.piece;
+}
+
+// Tiles [t0, t1) of the head (u, h), whose first tile has the number `head`; t0 has the number x, the piece goes to `end`.
+struct Walk { int u, h, rows, tiles, t0, t1; uint32_t x, end, head; };
+
+// Where tile x is; x below c.all.  Called by a whole warp.
+__device__ __forceinline__ void walk_to(const AttnArgs &A, const Cut &c, uint32_t x, uint32_t end, Walk &w) {
+    const uint32_t H = A.Hkv;
+    const int owner = __ffs(__ballot_sync(0xFFFFFFFFu, x < c.upto * H)) - 1;
+    int u = 0;
+    uint32_t base = 0;                                                // tiles of a head of each of the units before
+    if (lane_id() == owner) {
+        base = c.upto - c.mine;
+        for (u = c.u0; u < c.u1 - 1; ++u) {
+            const int t = tiles_of(unit_rows(A, u));
+            if (x < (base + t) * H) break;
+            base += t;
+        }
+    }
+    w.u = __shfl_sync(0xFFFFFFFFu, u, owner);
+    base = __shfl_sync(0xFFFFFFFFu, base, owner) * H;
+    w.rows = unit_rows(A, w.u);
+    w.tiles = tiles_of(w.rows);
+    w.h = (x - base) / (uint32_t)w.tiles;
+    w.head = base + w.h * w.tiles;
+    w.t0 = x - w.head;
+    w.x = x;
+    w.end = end;
+    w.t1 = min(w.tiles, w.t0 + (int)(end - x));
+}
+// The first tile of the head number `head` (unit by unit), or of what comes after it; c.all behind the last.
+__device__ __forceinline__ uint32_t head_begin(const AttnArgs &A, const Cut &c, uint32_t head) {
+    const int v = head / A.Hkv, g = head - v * A.Hkv, owner = v < A.U ? v / c.each : 31;
+    uint32_t before = c.upto;
+    int t = 0;
+    if (lane_id() == owner && v < A.U) {
+        before = c.upto - c.mine;
+        for (int u = c.u0; u < v; ++u) before += tiles_of(unit_rows(A, u));
+        t = tiles_of(unit_rows(A, v));
+    }
+    return __shfl_sync(0xFFFFFFFFu, before * A.Hkv + g * t, owner);
+}
+// A block's piece number i (its own, then those drawn); false where there is none.
+__device__ __forceinline__ bool walk_piece(const AttnArgs &A, const Cut &c, uint32_t i, Walk &w) {
+    uint32_t x, end;
+    if (c.share != 0) {
+        x = piece_begin(c, i);
+        end = min(c.all, piece_begin(c, i + 1));
+    } else {
+        if (i >= c.blocks) return false;
+        const uint32_t heads = (uint32_t)A.U * A.Hkv;
+        x = head_begin(A, c, min(heads, i * c.heads));
+        end = head_begin(A, c, min(heads, (i + 1) * c.heads));
+    }
+    if (x >= end) return false;
+    walk_to(A, c, x, end, w);
     return true;
 }
-// On to the next head; false at the end of the share.
+// On to the next head of the piece; false at its end.
 __device__ __forceinline__ bool walk_next(const AttnArgs &A, Walk &w) {
     w.x += w.t1 - w.t0;
     if (w.x >= w.end) return false;
@@ -186,12 +218,14 @@ __device__ __forceinline__ bool walk_next(const AttnArgs &A, Walk &w) {
     w.t1 = min(w.tiles, (int)(w.end - w.x));
     return true;
 }
-// The blocks that have part in the head: the first one, and how many.
-__device__ __forceinline__ int walk_split(const Walk &w, uint32_t &first) {
-    if (w.per == 0 || (w.t0 == 0 && w.t1 == w.tiles)) return 1;
-    first = w.head / w.per;
-    return (w.head + w.tiles - 1) / w.per - first + 1;
-}
+
+// What a group is, from the loader to the other warps.
+struct Task {
+    int n, t, rows, u, h;                // tiles (0: no more groups), the first one's place in the unit, the unit's rows, unit, head
+    int record;                          // where the part of the head goes: -1: it is all of it, else the record's number
+    int first, last;                     // of the head's groups in the piece
+};
+static_assert(sizeof(Task) == 32, "as much as kSmemTask leaves");
 
 // A query head's rows of the operand, by a warp: four elements a lane.  Rows by half, piece, head.  Returns the factor of its logits:
 // the queries' power of two and the softmax's scale; NaN for a query that is not finite.
@@ -234,7 +268,6 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(ptc_smem + kSmemBar + 8 * kNumBars);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
     int *cta_status = reinterpret_cast<int *>(tmem_slot + 2);
-    volatile int *last = reinterpret_cast<volatile int *>(tmem_slot + 3);
     float *info = reinterpret_cast<float *>(ptc_smem + kSmemInfo), *first_factors = reinterpret_cast<float *>(ptc_smem + kSmemFirst);
     if ((base & 1023u) != 0) {                       // the swizzled tiles need a 1024-byte aligned base
         predecessor_done();
@@ -244,7 +277,7 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
     auto bar = [&](int i) { return bars + 8u * i; };
     if (threadIdx.x == 0) {
         for (int i = 0; i < kNumBars; ++i)
-            tc::mbar_init(bar(i), i == kBarPFull || i == kBarPFull + 1 ? (kByTiles ? 128 : 256) : i >= kBarIEmpty ? 256 : 1);
+            tc::mbar_init(bar(i), i == kBarPFull || i == kBarPFull + 1 ? (kByTiles ? 128 : 256) : i >= kBarIEmpty ? 257 : 1);
         *abort_flag = 0;
         *cta_status = 0;
         tc::mbar_init_fence();
@@ -259,20 +292,24 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
     predecessor_done();
     successor_may_start();
 
-    Walk begin;
-    const bool work = walk_begin(A, begin);
     const int G = A.G, tile_pages = kTile >> A.page_shift, record = record_floats<128>(G);
-    auto query = [&](const Walk &w, int g) {
-        return g < G ? *reinterpret_cast<const uint2 *>(static_cast<const __nv_bfloat16 *>(A.q) + ((int64_t)w.u * A.Hq + w.h * G + g) * 128 + lane * 4)
+    auto query = [&](int u, int h, int g) {
+        return g < G ? *reinterpret_cast<const uint2 *>(static_cast<const __nv_bfloat16 *>(A.q) + ((int64_t)u * A.Hq + h * G + g) * 128 + lane * 4)
                      : make_uint2(0, 0);
     };
-    if (!work) {
-    } else if (warp == 0) {
+    Task *tasks = reinterpret_cast<Task *>(ptc_smem + kSmemTask);
+    // the next group's task, for the warps that do the loader's bidding
+    auto wait_task = [&](int group, Task &t) {
+        if (!tc::mbar_wait_warp(bar(kBarTask + group % kInfos), group / kInfos & 1, abort_flag, cta_status)) return false;
+        t = tasks[group % kInfos];
+        return t.n != 0;
+    };
+    if (warp == 0) {
         // A group's pages, two a lane: their numbers, and their scales.
         struct Pages { int a, b; float ka, kb, va, vb; };
-        auto numbers = [&](const Walk &w, int t, Pages &p) {
-            const int j = (t << (7 - A.page_shift)) + lane, end = min((w.rows + A.page - 1) >> A.page_shift, min(t + kGroup, w.t1) << (7 - A.page_shift));
-            const int *table = A.table + (int64_t)w.u * A.max_pages;
+        auto numbers = [&](const Task &g, Pages &p) {
+            const int j = (g.t << (7 - A.page_shift)) + lane, end = min((g.rows + A.page - 1) >> A.page_shift, (g.t + g.n) << (7 - A.page_shift));
+            const int *table = A.table + (int64_t)g.u * A.max_pages;
             p.a = j < end ? table[j] : 0;
             p.b = j + 32 < end ? table[j + 32] : 0;
             if ((unsigned)p.a >= (unsigned)A.n_pages) { report(A.status, kStatusIndex); p.a = 0; }
@@ -284,55 +321,74 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
             if (lane + 32 < kGroup * tile_pages) { p.kb = A.k_scale[b]; p.vb = A.v_scale[b]; }
         };
         int st = 0, phase = 0;
-        struct Group { Pages p; int h, t, n, pages; };               // n tiles from t on of a unit of so many pages
+        struct Group { Task is; Pages p; };
         auto load_tile = [&](const CUtensorMap *m, const Group &g, int i) {
             if (!tc::mbar_wait_warp(bar(kBarEmpty + st), phase ^ 1, abort_flag, cta_status)) return false;
             const int slot = i * tile_pages + lane;
             const int x = __shfl_sync(0xFFFFFFFFu, g.p.a, slot & 31), y = __shfl_sync(0xFFFFFFFFu, g.p.b, slot & 31), id = slot < 32 ? x : y;
-            const int here = min(tile_pages, g.pages - (g.t + i) * tile_pages);      // pages of the tile that there are
+            const int here = min(tile_pages, ((g.is.rows + A.page - 1) >> A.page_shift) - (g.is.t + i) * tile_pages);     // pages of the tile that there are
             if (tc::elect_one()) tc::mbar_expect_tx(bar(kBarFull + st), (uint32_t)here << (A.page_shift + 7));
             __syncwarp();
-            if (lane < here) tc::tma_load_4d(base + st * kStageBytes + ((uint32_t)lane << (A.page_shift + 7)), m, bar(kBarFull + st), 0, 0, g.h, id);
+            if (lane < here) tc::tma_load_4d(base + st * kStageBytes + ((uint32_t)lane << (A.page_shift + 7)), m, bar(kBarFull + st), 0, 0, g.is.h, id);
             __syncwarp();
             if (++st == kStages) { st = 0; phase ^= 1; }
             return true;
         };
         auto load_tiles = [&](const Group &k, const Group &v) {
             bool ok = true;
-            for (int i = 0; ok && i < max(k.n, v.n); ++i) {
-                if (i < k.n) ok = load_tile(&kmap, k, i);
-                if (ok && i < v.n) ok = load_tile(&vmap, v, i);
+            for (int i = 0; ok && i < max(k.is.n, v.is.n); ++i) {
+                if (i < k.is.n) ok = load_tile(&kmap, k, i);
+                if (ok && i < v.is.n) ok = load_tile(&vmap, v, i);
             }
             return ok;
         };
-        Walk ahead = begin;                                          // the head of the group after this one
-        int group = 0, head = 0, end = begin.t1;
-        bool ok = true, more = true;
+        const Cut cut = make_cut(A, gridDim.x);
+        Walk w = {};                                                 // the head of the group after `now`
+        int drawn = 0, group = 0, head = 0;
+        auto draw = [&]() { if (cut.share != 0 && lane == 0) drawn = atomicAdd(A.counter, 1); };     // (looked at when the piece before is at its end)
+        auto set = [&](Group &g, int t) {
+            g.is.n = min(kGroup, w.t1 - t); g.is.t = t; g.is.rows = w.rows; g.is.u = w.u; g.is.h = w.h;
+            g.is.first = t == w.t0; g.is.last = t + g.is.n == w.t1;
+            g.is.record = w.t0 == 0 && w.t1 == w.tiles ? -1 : 2 * (int)piece_of(cut, w.x) + (w.t0 == 0);
+            numbers(g.is, g.p);
+        };
+        bool ok = true, more = walk_piece(A, cut, blockIdx.x, w);
         float factor = 0.f;                                          // of query head `lane` (from the second head on)
         Group now, next, before;
         uint2 q[kHeads];                                             // the next head's query
-        before.n = 0; before.h = before.t = before.pages = before.p.a = before.p.b = 0;
-        auto set = [&](Group &g, const Walk &w, int t) {
-            g.h = w.h; g.t = t; g.n = min(kGroup, w.t1 - t); g.pages = (w.rows + A.page - 1) >> A.page_shift;
-            numbers(w, t, g.p);
-        };
-        set(now, begin, begin.t0);
-        scales(now.h, now.p);
+        now.is.n = before.is.n = 0;
+        if (more) {
+            draw();
+            set(now, w.t0);
+            scales(now.is.h, now.p);
+        }
         while (true) {
+            // the task, K's tiles with those of V of the group before, the scales
+            const int buffer = group % kInfos;
+            ok = tc::mbar_wait_warp(bar(kBarIEmpty + buffer), (group / kInfos & 1) ^ 1, abort_flag, cta_status);
+            if (!ok) break;
+            if (lane == 0) {
+                tasks[buffer] = now.is;
+                tc::mbar_arrive(bar(kBarTask + buffer));
+            }
+            if (now.is.n == 0) break;
             // the group after this one: its pages' numbers, and its head's query, on their way
-            const bool same = now.t + now.n < end;
-            if (!same) { more = walk_next(A, ahead); end = ahead.t1; }
-            if (more) {
-                set(next, ahead, same ? now.t + now.n : ahead.t0);
-                if (!same) {
+            next.is.n = 0;
+            if (!now.is.last) {
+                set(next, now.is.t + now.is.n);
+            } else {
+                more = walk_next(A, w);
+                if (!more && cut.share != 0) {
+                    more = walk_piece(A, cut, cut.blocks + __shfl_sync(0xFFFFFFFFu, drawn, 0), w);
+                    if (more) draw();
+                }
+                if (more) {
+                    set(next, w.t0);
 #pragma unroll
-                    for (int g = 0; g < kHeads; ++g) q[g] = query(ahead, g);
+                    for (int g = 0; g < kHeads; ++g) q[g] = query(w.u, w.h, g);
                 }
             }
             ok = load_tiles(now, before);
-            if (!ok) break;
-            const int buffer = group % kInfos;
-            ok = tc::mbar_wait_warp(bar(kBarIEmpty + buffer), (group / kInfos & 1) ^ 1, abort_flag, cta_status);
             if (!ok) break;
             float *to = info + buffer * kInfo;
             if (lane < kMaxHeads) to[2 * kMostPages + lane] = factor;
@@ -340,10 +396,8 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
             if (lane + 32 < kMostPages) { to[lane + 32] = now.p.kb; to[kMostPages + lane + 32] = log2_of(now.p.vb); }
             __syncwarp();
             if (lane == 0) tc::mbar_arrive(bar(kBarIFull + buffer));
-            before = now;
-            if (!more) break;
-            scales(next.h, next.p);
-            if (!same) {                                             // the next head's operand (the first one's is made below)
+            if (next.is.n != 0) scales(next.is.h, next.p);
+            if (next.is.n != 0 && next.is.first) {                   // the next head's operand (the first one's is made below)
                 ++head;
                 ok = tc::mbar_wait_warp(bar(kBarQEmpty + (head & 1)), (head >> 1 & 1) ^ 1, abort_flag, cta_status);
                 if (!ok) break;
@@ -356,12 +410,9 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
                 __syncwarp();
                 if (lane == 0) tc::mbar_arrive(bar(kBarQFull + (head & 1)));
             }
-            now = next; ++group;
+            before = now; now = next; ++group;
         }
-        if (ok) {
-            now.n = 0;
-            ok = load_tiles(now, before);
-        }
+        if (ok) ok = load_tiles(now, before);                        // (no tiles of K: the last group's V)
         if (!ok)         // winding down after a timeout: give copies already issued a moment to land
             for (int i = 0; i < kStages; ++i)
                 for (int s = 0; s < (1 << 16) && !tc::mbar_try_wait(bar(kBarFull + i), 0) && !tc::mbar_try_wait(bar(kBarFull + i), 1); ++s) {}
@@ -407,27 +458,31 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
             next();
             return true;
         };
-        Walk w = begin;
+        Task now;
         bool ok = true;
-        int group = 0, head = 0, before_n = 0, before_valid = 0;
-        do {
-            const uint32_t q_lo = tc::desc_lo(base + kSmemQ + (head & 1) * kQCols * 128);
-            ok = tc::mbar_wait_warp(bar(kBarQFull + (head & 1)), head >> 1 & 1, abort_flag, cta_status);
-            for (int t = w.t0; ok && t < w.t1; t += kGroup, ++group) {
-                const int n = min(kGroup, w.t1 - t);
-                for (int i = 0; ok && i < max(n, before_n); ++i) {   // (as the loader sends them)
-                    if (i < n) ok = logits(group, i, q_lo);
-                    if (ok && i < before_n) ok = output(i, before_n, before_valid);
-                }
-                if (ok && t + n == w.t1) {
-                    if (tc::elect_one()) tc::umma_commit(bar(kBarQEmpty + (head & 1)));
-                    __syncwarp();
-                }
-                before_n = n;
-                before_valid = min(kTile, w.rows - (t + n - 1) * kTile);
+        int group = 0, head = -1, before_n = 0, before_valid = 0;
+        uint32_t q_lo = 0;
+        while (wait_task(group, now)) {
+            if (tc::elect_one()) tc::mbar_arrive(bar(kBarIEmpty + group % kInfos));
+            __syncwarp();
+            if (now.first) {
+                ++head;
+                q_lo = tc::desc_lo(base + kSmemQ + (head & 1) * kQCols * 128);
+                ok = tc::mbar_wait_warp(bar(kBarQFull + (head & 1)), head >> 1 & 1, abort_flag, cta_status);
             }
-            ++head;
-        } while (ok && walk_next(A, w));
+            for (int i = 0; ok && i < max(now.n, before_n); ++i) {   // (as the loader sends them)
+                if (i < now.n) ok = logits(group, i, q_lo);
+                if (ok && i < before_n) ok = output(i, before_n, before_valid);
+            }
+            if (!ok) break;
+            if (now.last) {
+                if (tc::elect_one()) tc::umma_commit(bar(kBarQEmpty + (head & 1)));
+                __syncwarp();
+            }
+            before_n = now.n;
+            before_valid = min(kTile, now.rows - (now.t + now.n - 1) * kTile);
+            ++group;
+        }
         for (int i = 0; ok && i < before_n; ++i) ok = output(i, before_n, before_valid);
     } else {
         const int e = threadIdx.x - 64, half = e >> 7;               // 0 .. 255
@@ -437,16 +492,19 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
         constexpr int parts = kByTiles ? 2 : 1;                      // ... and tiles: all, or those with the number of the half
         const uint32_t tcols = trow + set * 8;                       // columns of their logits within a tile's
         float *red = reinterpret_cast<float *>(ptc_smem + kSmemRed);
-        if ((e >> 5) < kHeads) {                                     // the first head's operand, a warp per query head
-            const float f = put_query(base + kSmemQ, e >> 5, query(begin, e >> 5), A.scale_log2);
-            if (lane == 0) first_factors[e >> 5] = f;
+        Task now, done;
+        bool ok = true, more = wait_task(0, now);
+        if (more) {                                                  // the first head's operand, a warp per query head
+            if ((e >> 5) < kHeads) {
+                const float f = put_query(base + kSmemQ, e >> 5, query(now.u, now.h, e >> 5), A.scale_log2);
+                if (lane == 0) first_factors[e >> 5] = f;
+            }
+            fence_proxy_async();
         }
-        fence_proxy_async();
         epi_sync();
-        if (e == 0) tc::mbar_arrive(bar(kBarQFull));
+        if (more && e == 0) tc::mbar_arrive(bar(kBarQFull));
 
         float cq[kHalf], m[kHalf], mv[kHalf], l[kHalf], acc[kHalf];
-        bool ok = true;
         auto add_output = [&](int group) {                           // a group's product into acc
             if (kByTiles && half != 0) return;                       // (one thread a dim is enough)
             ok = ok && tc::mbar_wait_warp(bar(kBarO), group & 1, abort_flag, cta_status);
@@ -466,12 +524,9 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
                 if (lane == 0) all[(e >> 5) * 3 * kHalf + 2 * kHalf + g] = sum;
             }
         };
-        auto finish = [&](const Walk &w, const float *all) {
+        auto finish = [&](const Task &t, const float *all) {
             if ((kByTiles && half != 0) || !ok) return;
-            uint32_t first = 0;
-            const int n_split = walk_split(w, first);
-            float *out = A.out + ((int64_t)w.u * A.Hq + w.h * G) * 128 + row;
-            float *part = A.part + ((int64_t)2 * blockIdx.x + (w.t0 == 0)) * record;
+            float *out = A.out + ((int64_t)t.u * A.Hq + t.h * G) * 128 + row, *part = A.part + (int64_t)t.record * record;
 #pragma unroll
             for (int g = 0; g < kHalf; ++g) {
                 if (g0 + g < G) {
@@ -479,7 +534,7 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
 #pragma unroll
                     for (int i = 0; i < 4 * parts; ++i) sum += all[(4 * (kByTiles ? 0 : half) + i) * 3 * kHalf + 2 * kHalf + g];
                     const float o = acc[g] * tc::ex2(mv[g] - m[g] - 8.f);       // relative to the logits' maximum
-                    if (n_split == 1) {
+                    if (t.record < 0) {
                         out[(g0 + g) * 128] = o / sum;
                     } else {
                         part[(g0 + g) * 128 + row] = o;
@@ -488,117 +543,115 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
                 }
             }
         };
-        Walk w = begin, done = begin;
-        int group = 0, head = 0, tile = 0;
-        while (true) {
-            for (int t1 = w.t0; t1 < w.t1; t1 += kGroup, ++group) {
-                const int n = min(kGroup, w.t1 - t1), first_key = t1 * kTile, buffer = group % kInfos;
-                const int from = kByTiles ? (tile + half) & 1 : 0;   // this half's first tile of the group
-                const float *in = info + buffer * kInfo, *factors = (head == 0 ? first_factors : in + 2 * kMostPages) + g0;
-                ok = ok && tc::mbar_wait_warp(bar(kBarIFull + buffer), group / kInfos & 1, abort_flag, cta_status);
-                float top[kHalf], topv[kHalf];
+        int group = 0, head = -1, tile = 0;
+        for (; more; ++group, more = wait_task(group, now)) {
+            const int n = now.n, first_key = now.t * kTile, buffer = group % kInfos;
+            const int from = kByTiles ? (tile + half) & 1 : 0;       // this half's first tile of the group
+            head += now.first;
+            const float *in = info + buffer * kInfo, *factors = (head == 0 ? first_factors : in + 2 * kMostPages) + g0;
+            ok = ok && tc::mbar_wait_warp(bar(kBarIFull + buffer), group / kInfos & 1, abort_flag, cta_status);
+            float top[kHalf], topv[kHalf];
 #pragma unroll
-                for (int g = 0; g < kHalf; ++g) { top[g] = kLowest; topv[g] = kLowest; cq[g] = ok ? factors[g] : 0.f; }
-                for (int t = from; t < n; t += parts) {
-                    const int turn = (tile + t) / (2 * kGroup);
-                    ok = ok && tc::mbar_wait_warp(bar(kBarS + tile + t - turn * 2 * kGroup), turn & 1, abort_flag, cta_status);
-                    if (!ok) continue;
-                    tc::tc_fence_after();
-                    float s[8];
-                    tmem_ld8(tcols + kColS + ((group & 1) * kGroup + t) * kQCols, s);
-                    if (first_key + t * kTile + row < w.rows) {
-                        const int j = (t * kTile + row) >> A.page_shift;
-                        const float ks = in[j], lv = in[kMostPages + j];
-#pragma unroll
-                        for (int g = 0; g < kHalf; ++g) {
-                            const float z = fmaf(s[4 + g], 0.0625f, s[g]) * (ks * cq[g]);
-                            top[g] = fmaxf(top[g], z);
-                            topv[g] = fmaxf(topv[g], z + lv);
-                        }
-                    }
-                }
-                float *all = red + (group & 1) * 8 * 3 * kHalf;
-#pragma unroll
-                for (int g = 0; g < kHalf; ++g) {
-#pragma unroll
-                    for (int o = 16; o > 0; o >>= 1) {
-                        top[g] = fmaxf(top[g], __shfl_xor_sync(0xFFFFFFFFu, top[g], o));
-                        topv[g] = fmaxf(topv[g], __shfl_xor_sync(0xFFFFFFFFu, topv[g], o));
-                    }
-                    if (lane == 0) { all[(e >> 5) * 3 * kHalf + g] = top[g]; all[(e >> 5) * 3 * kHalf + kHalf + g] = topv[g]; }
-                }
-                const bool first = t1 == w.t0;
-                if (group > 0) {                                     // (before the barrier: behind it this group's product may begin)
-                    add_output(group - 1);
-                    tc::tc_fence_before();
-                    if (first) leave_sums(all);
-                }
-                epi_sync();
-                if (first) {
-                    if (group > 0) finish(done, all);
-#pragma unroll
-                    for (int g = 0; g < kHalf; ++g) { m[g] = kLowest; mv[g] = kLowest; l[g] = 0.f; acc[g] = 0.f; }
-                    done = w;
-                }
-#pragma unroll
-                for (int g = 0; g < kHalf; ++g) {
-                    float a = m[g], b = mv[g];
-#pragma unroll
-                    for (int i = 0; i < 4 * parts; ++i) {
-                        const float *of = all + (4 * (kByTiles ? 0 : half) + i) * 3 * kHalf;
-                        a = fmaxf(a, of[g]);
-                        b = fmaxf(b, of[kHalf + g]);
-                    }
-                    l[g] *= tc::ex2(m[g] - a);
-                    acc[g] *= tc::ex2(mv[g] - b);
-                    m[g] = a; mv[g] = b;
-                }
-                for (int t = from; t < n; t += parts) {
-                    const int i = tile + t, pb = i & 1;
-                    ok = ok && tc::mbar_wait_warp(bar(kBarPEmpty + pb), ((i >> 1) & 1) ^ 1, abort_flag, cta_status);
-                    if (!ok) continue;
-                    float s[8];
-                    tmem_ld8(tcols + kColS + ((group & 1) * kGroup + t) * kQCols, s);
-                    const bool valid = first_key + t * kTile + row < w.rows;
+            for (int g = 0; g < kHalf; ++g) { top[g] = kLowest; topv[g] = kLowest; cq[g] = ok ? factors[g] : 0.f; }
+            for (int t = from; t < n; t += parts) {
+                const int turn = (tile + t) / (2 * kGroup);
+                ok = ok && tc::mbar_wait_warp(bar(kBarS + tile + t - turn * 2 * kGroup), turn & 1, abort_flag, cta_status);
+                if (!ok) continue;
+                tc::tc_fence_after();
+                float s[8];
+                tmem_ld8(tcols + kColS + ((group & 1) * kGroup + t) * kQCols, s);
+                if (first_key + t * kTile + row < now.rows) {
                     const int j = (t * kTile + row) >> A.page_shift;
-                    const float ks = in[j], lv = in[kMostPages + j] + 8.f;                  // (weights times 256)
-                    // rows of the operand by half, piece, head: their number's last three bits, which the swizzle takes, are those of 4 piece + head
-                    const uint32_t at = base + kSmemP + pb * kPCols * 128 + set * 16 * 128 + (row & 15);
+                    const float ks = in[j], lv = in[kMostPages + j];
 #pragma unroll
-                    for (int g = 0; g < kHalf; g += 2) {
-                        if (g0 + g < G) {
-                            float x[2];
+                    for (int g = 0; g < kHalf; ++g) {
+                        const float z = fmaf(s[4 + g], 0.0625f, s[g]) * (ks * cq[g]);
+                        top[g] = fmaxf(top[g], z);
+                        topv[g] = fmaxf(topv[g], z + lv);
+                    }
+                }
+            }
+            float *all = red + (group & 1) * 8 * 3 * kHalf;
 #pragma unroll
-                            for (int k = 0; k < 2; ++k) {
-                                const float z = fmaf(s[4 + g + k], 0.0625f, s[g + k]) * (ks * cq[g + k]);
-                                l[g + k] += valid ? tc::ex2(z - m[g + k]) : 0.f;
-                                x[k] = valid ? tc::ex2(z + lv - mv[g + k]) : 0.f;
-                            }
-                            uint32_t piece[4];
-                            four_pieces(x[0], x[1], piece);
+            for (int g = 0; g < kHalf; ++g) {
 #pragma unroll
-                            for (int k = 0; k < 4; ++k) {
-                                const int n0 = 4 * k + g, n1 = n0 + 1;
-                                sts8(at + n0 * 128 + (((row >> 4) ^ (n0 & 7)) << 4), piece[k]);
-                                sts8(at + n1 * 128 + (((row >> 4) ^ (n1 & 7)) << 4), piece[k] >> 8);
-                            }
+                for (int o = 16; o > 0; o >>= 1) {
+                    top[g] = fmaxf(top[g], __shfl_xor_sync(0xFFFFFFFFu, top[g], o));
+                    topv[g] = fmaxf(topv[g], __shfl_xor_sync(0xFFFFFFFFu, topv[g], o));
+                }
+                if (lane == 0) { all[(e >> 5) * 3 * kHalf + g] = top[g]; all[(e >> 5) * 3 * kHalf + kHalf + g] = topv[g]; }
+            }
+            const bool first = now.first;
+            if (group > 0) {                                     // (before the barrier: behind it this group's product may begin)
+                add_output(group - 1);
+                tc::tc_fence_before();
+                if (first) leave_sums(all);
+            }
+            epi_sync();
+            if (first) {
+                if (group > 0) finish(done, all);
+#pragma unroll
+                for (int g = 0; g < kHalf; ++g) { m[g] = kLowest; mv[g] = kLowest; l[g] = 0.f; acc[g] = 0.f; }
+                done = now;
+            }
+#pragma unroll
+            for (int g = 0; g < kHalf; ++g) {
+                float a = m[g], b = mv[g];
+#pragma unroll
+                for (int i = 0; i < 4 * parts; ++i) {
+                    const float *of = all + (4 * (kByTiles ? 0 : half) + i) * 3 * kHalf;
+                    a = fmaxf(a, of[g]);
+                    b = fmaxf(b, of[kHalf + g]);
+                }
+                l[g] *= tc::ex2(m[g] - a);
+                acc[g] *= tc::ex2(mv[g] - b);
+                m[g] = a; mv[g] = b;
+            }
+            for (int t = from; t < n; t += parts) {
+                const int i = tile + t, pb = i & 1;
+                ok = ok && tc::mbar_wait_warp(bar(kBarPEmpty + pb), ((i >> 1) & 1) ^ 1, abort_flag, cta_status);
+                if (!ok) continue;
+                float s[8];
+                tmem_ld8(tcols + kColS + ((group & 1) * kGroup + t) * kQCols, s);
+                const bool valid = first_key + t * kTile + row < now.rows;
+                const int j = (t * kTile + row) >> A.page_shift;
+                const float ks = in[j], lv = in[kMostPages + j] + 8.f;                  // (weights times 256)
+                // rows of the operand by half, piece, head: their number's last three bits, which the swizzle takes, are those of 4 piece + head
+                const uint32_t at = base + kSmemP + pb * kPCols * 128 + set * 16 * 128 + (row & 15);
+#pragma unroll
+                for (int g = 0; g < kHalf; g += 2) {
+                    if (g0 + g < G) {
+                        float x[2];
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            const float z = fmaf(s[4 + g + k], 0.0625f, s[g + k]) * (ks * cq[g + k]);
+                            l[g + k] += valid ? tc::ex2(z - m[g + k]) : 0.f;
+                            x[k] = valid ? tc::ex2(z + lv - mv[g + k]) : 0.f;
+                        }
+                        uint32_t piece[4];
+                        four_pieces(x[0], x[1], piece);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const int n0 = 4 * k + g, n1 = n0 + 1;
+                            sts8(at + n0 * 128 + (((row >> 4) ^ (n0 & 7)) << 4), piece[k]);
+                            sts8(at + n1 * 128 + (((row >> 4) ^ (n1 & 7)) << 4), piece[k] >> 8);
                         }
                     }
-                    fence_proxy_async();
-                    tc::tc_fence_before();
-                    tc::mbar_arrive(bar(kBarPFull + pb));
                 }
-                tc::mbar_arrive(bar(kBarIEmpty + buffer));
-                tile += n;
+                fence_proxy_async();
+                tc::tc_fence_before();
+                tc::mbar_arrive(bar(kBarPFull + pb));
             }
-            ++head;
-            if (!walk_next(A, w)) break;
+            tc::mbar_arrive(bar(kBarIEmpty + buffer));
+            tile += n;
         }
-        add_output(group - 1);
-        float *all = red + (group & 1) * 8 * 3 * kHalf;
-        leave_sums(all);
-        epi_sync();
-        finish(done, all);
+        if (group > 0) {
+            add_output(group - 1);
+            float *all = red + (group & 1) * 8 * 3 * kHalf;
+            leave_sums(all);
+            epi_sync();
+            finish(done, all);
+        }
     }
     // units without rows, shared out over the blocks
     for (int u = blockIdx.x; u < A.U; u += gridDim.x) {
@@ -612,25 +665,26 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
     tc::tc_fence_after();
     if (warp == 1) tc::tmem_dealloc(tmem, kTmemCols);
     if (threadIdx.x == 0 && *abort_flag != 0) report(A.status, *cta_status);
-    if (!work || begin.per == 0) return;
-    // the first and the last head of the share may be others' too
-    Walk w = begin;
-    do {
-        uint32_t first = 0;
-        const int n = walk_split(w, first);
-        if (n > 1) {
-            if (threadIdx.x == 0) {
-                unsigned long long *ticket = A.ticket + (int64_t)w.u * A.Hkv + w.h;
-                *last = take_ticket(ticket, *reinterpret_cast<volatile unsigned long long *>(ticket), A.call, n);
-            }
-            __syncthreads();
-            if (*last) {
-                // (the first block's record is its last head's, in the second place, the others' their first head's)
-                join_ranges<kThreads, 128>(A.part + (int64_t)2 * first * record, record, (int64_t)2 * record, n, G, A.out + ((int64_t)w.u * A.Hq + w.h * G) * 128);
-            }
-            __syncthreads();
-        }
-    } while (walk_next(A, w));
+}
+
+// Joins the heads that were cut, a block for every place between two pieces: the first such place inside a head joins the head's records.
+// Also sets the counter that pieces are drawn from back.
+__global__ void __launch_bounds__(256) cache_join_kernel(const AttnArgs A, const uint32_t blocks) {
+    predecessor_done();
+    successor_may_start();
+    if (blockIdx.x == 0 && threadIdx.x == 0) *A.counter = 0;
+    const Cut cut = make_cut(A, blocks);
+    if (cut.share == 0) return;
+    const uint32_t x = piece_begin(cut, blockIdx.x + 1);
+    if (x >= cut.all) return;
+    Walk w;
+    walk_to(A, cut, x, cut.all, w);
+    if (w.t0 == 0) return;                                            // (between two heads)
+    const uint32_t first = piece_of(cut, w.head), last = piece_of(cut, w.head + w.tiles - 1);
+    if (first != blockIdx.x) return;                                  // (another place inside the head comes before)
+    const int record = record_floats<128>(A.G);
+    // the first piece's record is that of its last head, in the second place, unless it begins with the head, too; the others' are their first heads'
+    join_ranges<256, 128>(A.part + (int64_t)2 * first * record, record, (int64_t)2 * record, last - first + 1, A.G, A.out + ((int64_t)w.u * A.Hq + w.h * A.G) * 128);
 }
 
 }  // namespace ptc
