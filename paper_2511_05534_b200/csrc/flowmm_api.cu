@@ -1472,7 +1472,7 @@ flowmm_status validate_cache(const flowmm_cache_params *p) {
 
 int page_shift(int page) { return page == 16 ? 4 : page == 32 ? 5 : page == 64 ? 6 : 7; }
 
-// The attention's cut and scratch: [status word, 256 bytes][tickets][records].
+// The attention's cut and scratch: [status word, 256 bytes][tickets or cut heads][records].
 struct CachePlan {
     bool tc;                       // the tensor-core kernel (bf16 queries, heads of 128) or the SIMT one
     bool joins;                    // tensor cores: a head may be cut
@@ -1489,13 +1489,13 @@ CachePlan cache_plan(const flowmm_cache_params &p, int path) {
     c.groups = (G + c.gp - 1) / c.gp;
     c.target = (c.tc ? 2 : 4) * kScoreCtas;
     const int64_t heads = (int64_t)p.n_units * p.n_kv_heads * c.groups, keys = (int64_t)p.max_pages * p.page_size;
-    // tensor cores: two records for each piece; SIMT: a block and a record for each range
+    // tensor cores: two records and the note of a cut head for each block; SIMT: a block and a record for each range, a ticket for each head
     const int64_t tiles = (keys + paged::ptc::kTile - 1) / paged::ptc::kTile;
     c.joins = c.tc && !(heads <= c.target && tiles <= paged::kJoinTiles + 1);
     if (c.tc) c.blocks = std::min<int64_t>(heads * tiles, c.target);
     else c.blocks = std::min(heads * ((keys + paged::kSimtKeys - 1) / paged::kSimtKeys), c.target + heads);
-    c.part = 256 + align256((size_t)heads * sizeof(unsigned long long));
-    const int64_t records = !c.tc ? c.blocks : c.joins ? 2 * (c.blocks + paged::ptc::kMostPieces) : 0;
+    c.part = 256 + align256(c.tc ? (size_t)c.blocks * sizeof(int4) : (size_t)heads * sizeof(unsigned long long));
+    const int64_t records = !c.tc ? c.blocks : c.joins ? 2 * c.blocks : 0;
     c.total = c.part + align256((size_t)records * ((c.gp * (p.head_dim + 2) + 3) & ~3) * sizeof(float));
     return c;
 }
@@ -1549,13 +1549,14 @@ flowmm_status launch_cache_attention_tc(const flowmm_cache_params &p, const page
     const uint64_t strides[3] = {128, head, head * p.n_kv_heads};
     const uint32_t box[4] = {128, (uint32_t)p.page_size, 1, 1};
     if (!tc::make_byte_map(&kmap, a.k, 4, dims, strides, box) || !tc::make_byte_map(&vmap, a.v, 4, dims, strides, box)) return FLOWMM_ERR_CUDA;
-    auto kernel = a.G <= paged::ptc::kHalf ? paged::ptc::cache_attention_tc_kernel<true> : paged::ptc::cache_attention_tc_kernel<false>;
+    auto kernel = a.G <= 2 ? paged::ptc::cache_attention_tc_kernel<true, 1> :
+                  a.G <= paged::ptc::kHalf ? paged::ptc::cache_attention_tc_kernel<true, 2> : paged::ptc::cache_attention_tc_kernel<false, 2>;
     if (!allow_smem(kernel) || cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared) != cudaSuccess)
         return FLOWMM_ERR_CUDA;
     launch(kernel, (unsigned)c.blocks, paged::ptc::kThreads, paged::ptc::kSmemBytes, st, kmap, vmap, a);
     FLOWMM_LAUNCHED("cache_attention_tc");
     if (!c.joins) return FLOWMM_OK;
-    launch(paged::ptc::cache_join_kernel, (unsigned)(c.blocks + paged::ptc::kMostPieces), 256, 0, st, a, (uint32_t)c.blocks);
+    launch(paged::ptc::cache_join_kernel, (unsigned)c.blocks, 256, 0, st, a);
     FLOWMM_LAUNCHED("cache_join");
     return FLOWMM_OK;
 }
@@ -1684,7 +1685,7 @@ extern "C" flowmm_status flowmm_cache_attention(const flowmm_cache_params *p, co
     paged::AttnArgs a;
     a.q = q; a.k = static_cast<const uint8_t *>(k_pages); a.v = static_cast<const uint8_t *>(v_pages);
     a.k_scale = k_scale; a.v_scale = v_scale; a.table = block_table; a.rows = rows; a.out = out;
-    a.ticket = at<unsigned long long>(ws, 256); a.part = at<float>(ws, c.part); a.status = static_cast<int *>(ws); a.counter = at<int>(ws, 128);
+    a.ticket = at<unsigned long long>(ws, 256); a.part = at<float>(ws, c.part); a.status = static_cast<int *>(ws); a.cut_heads = c.joins ? at<int4>(ws, 256) : nullptr;
     a.call = status_call_number();
     a.U = p->n_units; a.Hq = p->n_q_heads; a.Hkv = p->n_kv_heads; a.G = p->n_q_heads / p->n_kv_heads; a.groups = c.groups;
     a.page = p->page_size; a.page_shift = page_shift(p->page_size); a.n_pages = p->n_pages; a.max_pages = p->max_pages;

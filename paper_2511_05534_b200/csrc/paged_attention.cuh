@@ -19,7 +19,7 @@ struct AttnArgs {
     float *part;                       // [blocks] records (record_floats)
     unsigned long long *ticket;        // [U * Hkv * groups]: (call, ranges done)
     int *status;
-    int *counter;                      // pieces drawn (tensor cores); zero between calls
+    int4 *cut_heads;                   // [blocks] heads to be joined (tensor cores); null: none can be
     uint32_t call;
     int U, Hq, Hkv, G, groups, page, page_shift, n_pages, max_pages, q_bf16;
     int target;                        // ranges in all that the call is cut into, about

@@ -9,12 +9,12 @@
 // The pages' scales join in fp32: K's on the logits; V's in the exponent of the weights, w_j = 2^(z_j + log2 sv_j - max), with a maximum of
 // its own, so that the largest weight is 1 whatever the scales are.  The sum of the softmax, sum_j 2^(z_j - max z), is apart.
 //
-// The tiles of 128 keys of all heads stand in a row, by unit, head and key, and are cut into pieces: a long one for every block of the launch
-// (two to an SM), three quarters of its even share, and short ones that the blocks draw from a counter when they are
-// done.  (Even shares alone left the SMs done between 85 and 125 us after the start, 16 sequences of up to 33 792 rows, 8 heads: they do not all get
-// the same of the memory.  Ranges of equal length of each head by itself, a block each, left a last round half empty: 174 us.)
-// A head that several pieces have part in leaves a record for each, and cache_join_kernel joins them in order, so that results do not
-// depend on who drew what.  A block goes through its tiles in groups of up to
+// How the work is shared out over the blocks of the launch, two to an SM, is found on the device, where alone the lengths are known.
+// The tiles of 128 keys of all heads stand in a row, by unit, head and key, and every block takes an equal piece of the row.  A head
+// that several blocks have part in leaves a record for each, and cache_join_kernel joins them in order.  (Ranges of equal
+// length of each head by itself, a block each, left a last round half empty, 16 sequences of up to 33 792 rows, 8 heads, 174 us; this way 120.  Three
+// quarters of a piece to each block and the rest drawn from a counter in pieces of three tiles and more: 132.)
+// A block goes through its tiles in groups of up to
 // seven of one head, the roles of its warps one or two groups apart, across the heads' borders too:
 //   warp 0     K tiles and V tiles by TMA, a box per page, into a ring of six stages of 16 KB: a tile of K of group c + 1 and one of V of
 //              group c in turn; the next head's query operand; the scales of a group's pages
@@ -64,12 +64,24 @@ __device__ __forceinline__ void umma_e4m3(uint32_t tmem_d, uint32_t a_lo, uint32
         ::"r"(tmem_d), "r"(a_lo), "r"(b_lo), "r"(tc::kDescSw128Hi), "r"(idesc), "r"(accumulate)
         : "memory");
 }
-// 8 consecutive fp32 columns of this thread's TMEM lane, waited for.
+// 8 consecutive fp32 columns of this thread's TMEM lane, and the wait tied to them (so that a load may stay on its way across other work).
 __device__ __forceinline__ void tmem_ld8(uint32_t taddr, float (&r)[8]) {
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];\n\ttcgen05.wait::ld.sync.aligned;"
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
                  : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7])
                  : "r"(taddr)
                  : "memory");
+}
+__device__ __forceinline__ void tmem_ld_wait(float (&r)[8]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+f"(r[0]), "+f"(r[1]), "+f"(r[2]), "+f"(r[3]), "+f"(r[4]), "+f"(r[5]), "+f"(r[6]), "+f"(r[7])
+                 :
+                 : "memory");
+}
+// The largest of a warp's values (NaN counts for nothing).
+__device__ __forceinline__ float warp_max(float x) {
+    float y;
+    asm("redux.sync.max.f32 %0, %1, 0xFFFFFFFF;" : "=f"(y) : "f"(x));
+    return y;
 }
 __device__ __forceinline__ void epi_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
 __device__ __forceinline__ void sts8(uint32_t addr, uint32_t v) { asm volatile("st.shared.b8 [%0], %1;" ::"r"(addr), "r"(v) : "memory"); }
@@ -94,19 +106,17 @@ __device__ __forceinline__ void four_pieces(float a, float b, uint32_t (&piece)[
 
 
 // ---- pieces --------------------------------------------------------------------------------------
-constexpr int kMostPieces = 1184, kLeastPiece = 3;      // short pieces of a call; tiles of one
-
 __device__ __forceinline__ int tiles_of(int rows) { return (rows + kTile - 1) / kTile; }
 
-// How a call is cut; every warp that asks finds it by itself, each lane from some consecutive units.
+// How a call is cut; a warp finds it, each lane from some consecutive units.
 struct Cut {
     int each, u0, u1;                    // this lane's units
     uint32_t mine, upto;                 // their tiles, of one head; with all units before
-    uint32_t all, blocks, share, piece;  // tiles of all heads; long pieces and their tiles; tiles of a short piece.  share 0: whole heads
-    uint32_t heads;                      // ... so many a block
+    uint32_t all, share;                 // tiles of all heads; of a block's piece, or 0: blocks have whole heads,
+    uint32_t heads;                      // ... so many
 };
 // Where whole heads make the longest piece no more than kJoinTiles longer than an even one, heads are not cut: joining costs that much.
-__device__ __forceinline__ Cut make_cut(const AttnArgs &A, uint32_t blocks) {
+__device__ __forceinline__ Cut make_cut(const AttnArgs &A) {
     Cut c;
     const int lane = lane_id();
     c.each = (A.U + 31) >> 5;
@@ -127,26 +137,12 @@ __device__ __forceinline__ Cut make_cut(const AttnArgs &A, uint32_t blocks) {
         if (lane >= o) c.upto += x;
         longest = max(longest, __shfl_xor_sync(0xFFFFFFFFu, longest, o));
     }
-    c.blocks = blocks;
+    const uint32_t blocks = gridDim.x, heads = (uint32_t)A.U * A.Hkv;
     c.all = __shfl_sync(0xFFFFFFFFu, c.upto, 31) * A.Hkv;
-    const uint32_t heads = (uint32_t)A.U * A.Hkv, even = (c.all + blocks - 1) / blocks;
     c.heads = heads <= blocks ? 1 : (heads + blocks - 1) / blocks;
-    if (c.heads * longest <= even + kJoinTiles) {
-        c.share = 0;
-        c.piece = 1;
-    } else {
-        c.share = (even * 3 + 3) / 4;
-        const uint32_t left = c.all > c.share * blocks ? c.all - c.share * blocks : 0;
-        c.piece = max((uint32_t)kLeastPiece, (left + kMostPieces - 1) / kMostPieces);
-    }
+    c.share = (c.all + blocks - 1) / blocks;
+    if (c.heads * longest <= c.share + kJoinTiles) c.share = 0;
     return c;
-}
-// The first tile of a piece (or, for a number past the last piece, something not below c.all) and the piece that a tile is in; share > 0.
-__device__ __forceinline__ uint32_t piece_begin(const Cut &c, uint32_t i) {
-    return i <= c.blocks ? i * c.share : c.blocks * c.share + (i - c.blocks) * c.piece;
-}
-__device__ __forceinline__ uint32_t piece_of(const Cut &c, uint32_t x) {
-    return x < c.blocks * c.share ? x / c.share : c.blocks + (x - c.blocks * c.share) / c.piece;
 }
 
 // Tiles [t0, t1) of the head (u, h), whose first tile has the number `head`; t0 has the number x, the piece goes to `end`.
@@ -189,14 +185,14 @@ __device__ __forceinline__ uint32_t head_begin(const AttnArgs &A, const Cut &c, 
     }
     return __shfl_sync(0xFFFFFFFFu, before * A.Hkv + g * t, owner);
 }
-// A block's piece number i (its own, then those drawn); false where there is none.
-__device__ __forceinline__ bool walk_piece(const AttnArgs &A, const Cut &c, uint32_t i, Walk &w) {
+// The block's piece; false where there is none.
+__device__ __forceinline__ bool walk_piece(const AttnArgs &A, const Cut &c, Walk &w) {
+    const uint32_t i = blockIdx.x;
     uint32_t x, end;
     if (c.share != 0) {
-        x = piece_begin(c, i);
-        end = min(c.all, piece_begin(c, i + 1));
+        x = i * c.share;
+        end = min(c.all, x + c.share);
     } else {
-        if (i >= c.blocks) return false;
         const uint32_t heads = (uint32_t)A.U * A.Hkv;
         x = head_begin(A, c, min(heads, i * c.heads));
         end = head_begin(A, c, min(heads, (i + 1) * c.heads));
@@ -256,8 +252,8 @@ __device__ __forceinline__ float put_query(uint32_t operand, int g, uint2 v, flo
     return is_finite(size) ? power_of_two(ex) * scale_log2 : __uint_as_float(0x7FC00000u);
 }
 
-// kByTiles: at most four query heads, the halves take every other tile; else the halves have four heads each.
-template <bool kByTiles>
+// kByTiles: at most four query heads, or two (kPairs: of one half), the halves take every other tile; else the halves have four heads each.
+template <bool kByTiles, int kPairs>
 __global__ void __launch_bounds__(kThreads, 2)
 cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap, const AttnArgs A) {
     constexpr int kCols = kByTiles ? kPCols / 2 : kPCols, kHeads = kByTiles ? kHalf : kMaxHeads;    // N of the second product; heads served
@@ -342,23 +338,23 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
             }
             return ok;
         };
-        const Cut cut = make_cut(A, gridDim.x);
+        const Cut cut = make_cut(A);
         Walk w = {};                                                 // the head of the group after `now`
-        int drawn = 0, group = 0, head = 0;
-        auto draw = [&]() { if (cut.share != 0 && lane == 0) drawn = atomicAdd(A.counter, 1); };     // (looked at when the piece before is at its end)
+        int group = 0, head = 0;
+        int4 cut_head = make_int4(0, 0, 0, 0);                       // unit, head and number of pieces of a head that begins here and goes on in other blocks
         auto set = [&](Group &g, int t) {
             g.is.n = min(kGroup, w.t1 - t); g.is.t = t; g.is.rows = w.rows; g.is.u = w.u; g.is.h = w.h;
             g.is.first = t == w.t0; g.is.last = t + g.is.n == w.t1;
-            g.is.record = w.t0 == 0 && w.t1 == w.tiles ? -1 : 2 * (int)piece_of(cut, w.x) + (w.t0 == 0);
+            g.is.record = w.t0 == 0 && w.t1 == w.tiles ? -1 : 2 * (int)blockIdx.x + (w.t0 == 0);
+            if (w.t0 == 0 && w.t1 < w.tiles) cut_head = make_int4(w.u, w.h, (int)((w.head + w.tiles - 1) / cut.share - blockIdx.x + 1), 0);
             numbers(g.is, g.p);
         };
-        bool ok = true, more = walk_piece(A, cut, blockIdx.x, w);
+        bool ok = true, more = walk_piece(A, cut, w);
         float factor = 0.f;                                          // of query head `lane` (from the second head on)
         Group now, next, before;
         uint2 q[kHeads];                                             // the next head's query
         now.is.n = before.is.n = 0;
         if (more) {
-            draw();
             set(now, w.t0);
             scales(now.is.h, now.p);
         }
@@ -378,10 +374,6 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
                 set(next, now.is.t + now.is.n);
             } else {
                 more = walk_next(A, w);
-                if (!more && cut.share != 0) {
-                    more = walk_piece(A, cut, cut.blocks + __shfl_sync(0xFFFFFFFFu, drawn, 0), w);
-                    if (more) draw();
-                }
                 if (more) {
                     set(next, w.t0);
 #pragma unroll
@@ -412,6 +404,7 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
             }
             before = now; now = next; ++group;
         }
+        if (A.cut_heads && lane == 0) A.cut_heads[blockIdx.x] = cut_head;
         if (ok) ok = load_tiles(now, before);                        // (no tiles of K: the last group's V)
         if (!ok)         // winding down after a timeout: give copies already issued a moment to land
             for (int i = 0; i < kStages; ++i)
@@ -513,6 +506,8 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
             float o[8], o2[8];
             tmem_ld8(trow + set * 16, o);
             tmem_ld8(trow + set * 16 + 8, o2);
+            tmem_ld_wait(o);
+            tmem_ld_wait(o2);
 #pragma unroll
             for (int g = 0; g < kHalf; ++g) acc[g] += fmaf(fmaf(fmaf(o2[4 + g], 0.0625f, o2[g]), 0.0625f, o[4 + g]), 0.0625f, o[g]);
         };
@@ -553,32 +548,44 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
             float top[kHalf], topv[kHalf];
 #pragma unroll
             for (int g = 0; g < kHalf; ++g) { top[g] = kLowest; topv[g] = kLowest; cq[g] = ok ? factors[g] : 0.f; }
-            for (int t = from; t < n; t += parts) {
+            const uint32_t scol = tcols + kColS + (group & 1) * kGroup * kQCols;
+            float s[8];
+            // The logits are there one after the other: of the first group each is waited for, of the others, which have been
+            // made beside the group before, the last one.
+            auto wait_logits = [&](int t) {
                 const int turn = (tile + t) / (2 * kGroup);
                 ok = ok && tc::mbar_wait_warp(bar(kBarS + tile + t - turn * 2 * kGroup), turn & 1, abort_flag, cta_status);
-                if (!ok) continue;
                 tc::tc_fence_after();
-                float s[8];
-                tmem_ld8(tcols + kColS + ((group & 1) * kGroup + t) * kQCols, s);
+            };
+            if (group > 0 && from < n) wait_logits(n - 1);
+            if (ok && group > 0 && from < n) tmem_ld8(scol + from * kQCols, s);
+            for (int t = from; t < n; t += parts) {
+                if (group == 0) {
+                    wait_logits(t);
+                    if (ok) tmem_ld8(scol + t * kQCols, s);
+                }
+                if (!ok) continue;
+                tmem_ld_wait(s);
+                float z[kHalf];
+#pragma unroll
+                for (int g = 0; g < kHalf; ++g) z[g] = fmaf(s[4 + g], 0.0625f, s[g]);
+                if (group > 0 && t + parts < n) tmem_ld8(scol + (t + parts) * kQCols, s);
                 if (first_key + t * kTile + row < now.rows) {
                     const int j = (t * kTile + row) >> A.page_shift;
                     const float ks = in[j], lv = in[kMostPages + j];
 #pragma unroll
                     for (int g = 0; g < kHalf; ++g) {
-                        const float z = fmaf(s[4 + g], 0.0625f, s[g]) * (ks * cq[g]);
-                        top[g] = fmaxf(top[g], z);
-                        topv[g] = fmaxf(topv[g], z + lv);
+                        const float x = z[g] * (ks * cq[g]);
+                        top[g] = fmaxf(top[g], x);
+                        topv[g] = fmaxf(topv[g], x + lv);
                     }
                 }
             }
             float *all = red + (group & 1) * 8 * 3 * kHalf;
 #pragma unroll
             for (int g = 0; g < kHalf; ++g) {
-#pragma unroll
-                for (int o = 16; o > 0; o >>= 1) {
-                    top[g] = fmaxf(top[g], __shfl_xor_sync(0xFFFFFFFFu, top[g], o));
-                    topv[g] = fmaxf(topv[g], __shfl_xor_sync(0xFFFFFFFFu, topv[g], o));
-                }
+                top[g] = warp_max(top[g]);
+                topv[g] = warp_max(topv[g]);
                 if (lane == 0) { all[(e >> 5) * 3 * kHalf + g] = top[g]; all[(e >> 5) * 3 * kHalf + kHalf + g] = topv[g]; }
             }
             const bool first = now.first;
@@ -607,35 +614,36 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
                 acc[g] *= tc::ex2(mv[g] - b);
                 m[g] = a; mv[g] = b;
             }
+            if (ok && from < n) tmem_ld8(scol + from * kQCols, s);
             for (int t = from; t < n; t += parts) {
                 const int i = tile + t, pb = i & 1;
-                ok = ok && tc::mbar_wait_warp(bar(kBarPEmpty + pb), ((i >> 1) & 1) ^ 1, abort_flag, cta_status);
                 if (!ok) continue;
-                float s[8];
-                tmem_ld8(tcols + kColS + ((group & 1) * kGroup + t) * kQCols, s);
+                tmem_ld_wait(s);
                 const bool valid = first_key + t * kTile + row < now.rows;
                 const int j = (t * kTile + row) >> A.page_shift;
                 const float ks = in[j], lv = in[kMostPages + j] + 8.f;                  // (weights times 256)
+                float x[2 * kPairs];
+#pragma unroll
+                for (int g = 0; g < 2 * kPairs; ++g) {
+                    const float z = fmaf(s[4 + g], 0.0625f, s[g]) * (ks * cq[g]);
+                    l[g] += valid ? tc::ex2(z - m[g]) : 0.f;
+                    x[g] = valid ? tc::ex2(z + lv - mv[g]) : 0.f;
+                }
+                if (t + parts < n) tmem_ld8(scol + (t + parts) * kQCols, s);
+                uint32_t piece[kPairs][4];
+#pragma unroll
+                for (int g = 0; g < kPairs; ++g) four_pieces(x[2 * g], x[2 * g + 1], piece[g]);
+                ok = tc::mbar_wait_warp(bar(kBarPEmpty + pb), ((i >> 1) & 1) ^ 1, abort_flag, cta_status);
+                if (!ok) continue;
                 // rows of the operand by half, piece, head: their number's last three bits, which the swizzle takes, are those of 4 piece + head
                 const uint32_t at = base + kSmemP + pb * kPCols * 128 + set * 16 * 128 + (row & 15);
 #pragma unroll
-                for (int g = 0; g < kHalf; g += 2) {
-                    if (g0 + g < G) {
-                        float x[2];
+                for (int g = 0; g < kPairs; ++g) {
 #pragma unroll
-                        for (int k = 0; k < 2; ++k) {
-                            const float z = fmaf(s[4 + g + k], 0.0625f, s[g + k]) * (ks * cq[g + k]);
-                            l[g + k] += valid ? tc::ex2(z - m[g + k]) : 0.f;
-                            x[k] = valid ? tc::ex2(z + lv - mv[g + k]) : 0.f;
-                        }
-                        uint32_t piece[4];
-                        four_pieces(x[0], x[1], piece);
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            const int n0 = 4 * k + g, n1 = n0 + 1;
-                            sts8(at + n0 * 128 + (((row >> 4) ^ (n0 & 7)) << 4), piece[k]);
-                            sts8(at + n1 * 128 + (((row >> 4) ^ (n1 & 7)) << 4), piece[k] >> 8);
-                        }
+                    for (int k = 0; k < 4; ++k) {
+                        const int n0 = 4 * k + 2 * g, n1 = n0 + 1;
+                        sts8(at + n0 * 128 + (((row >> 4) ^ (n0 & 7)) << 4), piece[g][k]);
+                        sts8(at + n1 * 128 + (((row >> 4) ^ (n1 & 7)) << 4), piece[g][k] >> 8);
                     }
                 }
                 fence_proxy_async();
@@ -667,24 +675,16 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
     if (threadIdx.x == 0 && *abort_flag != 0) report(A.status, *cta_status);
 }
 
-// Joins the heads that were cut, a block for every place between two pieces: the first such place inside a head joins the head's records.
-// Also sets the counter that pieces are drawn from back.
-__global__ void __launch_bounds__(256) cache_join_kernel(const AttnArgs A, const uint32_t blocks) {
+// Joins the heads that were cut: a block for every block that a cut head begins in, a warp for each of its query heads.
+__global__ void __launch_bounds__(256) cache_join_kernel(const AttnArgs A) {
     predecessor_done();
     successor_may_start();
-    if (blockIdx.x == 0 && threadIdx.x == 0) *A.counter = 0;
-    const Cut cut = make_cut(A, blocks);
-    if (cut.share == 0) return;
-    const uint32_t x = piece_begin(cut, blockIdx.x + 1);
-    if (x >= cut.all) return;
-    Walk w;
-    walk_to(A, cut, x, cut.all, w);
-    if (w.t0 == 0) return;                                            // (between two heads)
-    const uint32_t first = piece_of(cut, w.head), last = piece_of(cut, w.head + w.tiles - 1);
-    if (first != blockIdx.x) return;                                  // (another place inside the head comes before)
+    const int4 head = A.cut_heads[blockIdx.x];
+    if (head.z == 0) return;
     const int record = record_floats<128>(A.G);
-    // the first piece's record is that of its last head, in the second place, unless it begins with the head, too; the others' are their first heads'
-    join_ranges<256, 128>(A.part + (int64_t)2 * first * record, record, (int64_t)2 * record, last - first + 1, A.G, A.out + ((int64_t)w.u * A.Hq + w.h * A.G) * 128);
+    // (the first block's record is that of its last head, in the second place; the others' are those of their first heads)
+    join_ranges<256, 128>(A.part + (int64_t)2 * blockIdx.x * record, record, (int64_t)2 * record, head.z, A.G,
+                          A.out + ((int64_t)head.x * A.Hq + head.y * A.G) * 128);
 }
 
 }  // namespace ptc
