@@ -112,10 +112,18 @@ __device__ __forceinline__ int tiles_of(int rows) { return (rows + kTile - 1) / 
 struct Cut {
     int each, u0, u1;                    // this lane's units
     uint32_t mine, upto;                 // their tiles, of one head; with all units before
-    uint32_t all, share;                 // tiles of all heads; of a block's piece, or 0: blocks have whole heads,
-    uint32_t heads;                      // ... so many
+    uint32_t all, share;                 // tiles of all heads; of a block's piece, or 0: blocks have whole heads
+    uint32_t sorted0, sorted1;           // whole heads, more than blocks: the units by falling length, those in places `lane` and 32 + lane: tiles * 64 + unit
 };
+constexpr int kMostSorted = 64;
+// The tiles of the unit in place r, with its number, for a lane's own r.
+__device__ __forceinline__ uint32_t sorted_unit(const Cut &c, uint32_t r) {
+    const uint32_t a = __shfl_sync(0xFFFFFFFFu, c.sorted0, r & 31), b = __shfl_sync(0xFFFFFFFFu, c.sorted1, r & 31);
+    return r < 32 ? a : b;
+}
 // Where whole heads make the longest piece no more than kJoinTiles longer than an even one, heads are not cut: joining costs that much.
+// With at most as many heads as blocks each has one; up to twice as many, of at most 64 units, a block has the i-th longest and the i-th last
+// (64 units of up to 1690 rows, 512 heads: 41 us cut, 36 so).
 __device__ __forceinline__ Cut make_cut(const AttnArgs &A) {
     Cut c;
     const int lane = lane_id();
@@ -139,9 +147,46 @@ __device__ __forceinline__ Cut make_cut(const AttnArgs &A) {
     }
     const uint32_t blocks = gridDim.x, heads = (uint32_t)A.U * A.Hkv;
     c.all = __shfl_sync(0xFFFFFFFFu, c.upto, 31) * A.Hkv;
-    c.heads = heads <= blocks ? 1 : (heads + blocks - 1) / blocks;
     c.share = (c.all + blocks - 1) / blocks;
-    if (c.heads * longest <= c.share + kJoinTiles) c.share = 0;
+    c.sorted0 = c.sorted1 = 0;
+    const uint32_t most = c.share + kJoinTiles;
+    if (heads > 2 * blocks || (heads > blocks && A.U > kMostSorted) || longest > most) return c;
+    if (heads > blocks) {
+        // units by length: a unit's place is the number of longer ones, or as long ones before it
+        uint32_t mine[2], place[2] = {0, 0};
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int u = lane + 32 * i;
+            mine[i] = u < A.U ? (uint32_t)tiles_of(unit_rows(A, u)) * 64 + 63 - u : 0;       // (all different, and 0 for none)
+        }
+        for (int k = 0; k < 32; ++k) {
+            const uint32_t a = __shfl_sync(0xFFFFFFFFu, mine[0], k), b = __shfl_sync(0xFFFFFFFFu, mine[1], k);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) place[i] += (a > mine[i]) + (b > mine[i]);
+        }
+        for (int k = 0; k < 32; ++k) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const uint32_t at = __shfl_sync(0xFFFFFFFFu, place[i], k), is = __shfl_sync(0xFFFFFFFFu, mine[i], k) ^ 63;      // (63 - u back to u)
+                if (k + 32 * i < A.U) {
+                    if (at == (uint32_t)lane) c.sorted0 = is;
+                    if (at == (uint32_t)lane + 32) c.sorted1 = is;
+                }
+            }
+        }
+        // the longest pair: of each unit's heads the last one that comes first in a block, since it has the longest partner
+        uint32_t pair = 0;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t r = lane + 32 * i, item = min(r * A.Hkv + A.Hkv - 1, blocks - 1), partner = 2 * blocks - 1 - item;
+            const uint32_t with = sorted_unit(c, partner < heads ? partner / A.Hkv : 0) >> 6;
+            if (r < (uint32_t)A.U && r * A.Hkv < blocks) pair = max(pair, ((i ? c.sorted1 : c.sorted0) >> 6) + (partner < heads ? with : 0));
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) pair = max(pair, __shfl_xor_sync(0xFFFFFFFFu, pair, o));
+        if (pair > most) return c;
+    }
+    c.share = 0;
     return c;
 }
 
@@ -173,32 +218,26 @@ __device__ __forceinline__ void walk_to(const AttnArgs &A, const Cut &c, uint32_
     w.end = end;
     w.t1 = min(w.tiles, w.t0 + (int)(end - x));
 }
-// The first tile of the head number `head` (unit by unit), or of what comes after it; c.all behind the last.
-__device__ __forceinline__ uint32_t head_begin(const AttnArgs &A, const Cut &c, uint32_t head) {
-    const int v = head / A.Hkv, g = head - v * A.Hkv, owner = v < A.U ? v / c.each : 31;
-    uint32_t before = c.upto;
-    int t = 0;
-    if (lane_id() == owner && v < A.U) {
-        before = c.upto - c.mine;
-        for (int u = c.u0; u < v; ++u) before += tiles_of(unit_rows(A, u));
-        t = tiles_of(unit_rows(A, v));
-    }
-    return __shfl_sync(0xFFFFFFFFu, before * A.Hkv + g * t, owner);
+// Whole heads: the block's first or second one.
+__device__ __forceinline__ bool walk_head(const AttnArgs &A, const Cut &c, int second, Walk &w) {
+    const uint32_t blocks = gridDim.x, heads = (uint32_t)A.U * A.Hkv, i = second ? 2 * blocks - 1 - blockIdx.x : blockIdx.x;
+    if (i >= heads) return false;
+    const uint32_t r = i / A.Hkv;
+    w.u = heads <= blocks ? r : sorted_unit(c, r) & 63;
+    w.h = i - r * A.Hkv;
+    w.rows = unit_rows(A, w.u);
+    w.tiles = w.t1 = tiles_of(w.rows);
+    w.t0 = 0;
+    w.x = w.head = 0;
+    w.end = w.tiles;
+    return w.tiles > 0;
 }
 // The block's piece; false where there is none.
 __device__ __forceinline__ bool walk_piece(const AttnArgs &A, const Cut &c, Walk &w) {
-    const uint32_t i = blockIdx.x;
-    uint32_t x, end;
-    if (c.share != 0) {
-        x = i * c.share;
-        end = min(c.all, x + c.share);
-    } else {
-        const uint32_t heads = (uint32_t)A.U * A.Hkv;
-        x = head_begin(A, c, min(heads, i * c.heads));
-        end = head_begin(A, c, min(heads, (i + 1) * c.heads));
-    }
-    if (x >= end) return false;
-    walk_to(A, c, x, end, w);
+    if (c.share == 0) return walk_head(A, c, 0, w);
+    const uint32_t x = blockIdx.x * c.share;
+    if (x >= c.all) return false;
+    walk_to(A, c, x, min(c.all, x + c.share), w);
     return true;
 }
 // On to the next head of the piece; false at its end.
@@ -340,7 +379,7 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
         };
         const Cut cut = make_cut(A);
         Walk w = {};                                                 // the head of the group after `now`
-        int group = 0, head = 0;
+        int group = 0, head = 0, second = 0;
         int4 cut_head = make_int4(0, 0, 0, 0);                       // unit, head and number of pieces of a head that begins here and goes on in other blocks
         auto set = [&](Group &g, int t) {
             g.is.n = min(kGroup, w.t1 - t); g.is.t = t; g.is.rows = w.rows; g.is.u = w.u; g.is.h = w.h;
@@ -374,6 +413,7 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
                 set(next, now.is.t + now.is.n);
             } else {
                 more = walk_next(A, w);
+                if (!more && cut.share == 0 && !second) more = walk_head(A, cut, second = 1, w);
                 if (more) {
                     set(next, w.t0);
 #pragma unroll
