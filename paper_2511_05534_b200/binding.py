@@ -384,6 +384,10 @@ class CacheParams:
     softmax_scale: float = 0.0
     path: int = PATH_AUTO
 
+    def __setattr__(self, name, value):
+        object.__setattr__(self, name, value)
+        object.__setattr__(self, "calls", {})     # what _cache_struct has seen of calls with these values
+
     def c(self, k=None, v=None) -> _CCacheParams:
         dense = (self.n_kv_heads * self.n_rows * self.head_dim, self.n_rows * self.head_dim, self.head_dim)
         cp = _CCacheParams(*_CACHE_FIELDS(self))
@@ -401,7 +405,6 @@ _CODE_TYPES = (torch.uint8, torch.float8_e4m3fn)
 # numel together fix what memory a tensor covers.
 _strides, _numel, _device, _address = torch.Tensor.stride, torch.Tensor.numel, torch.Tensor.get_device, torch.Tensor.data_ptr
 _type = operator.attrgetter("dtype")
-_seen = {}
 
 
 def _cache_struct(p: CacheParams, what: str, tensors, expected, n_dense=0):
@@ -410,7 +413,7 @@ def _cache_struct(p: CacheParams, what: str, tensors, expected, n_dense=0):
     if not tensors[0].is_cuda:
         raise ValueError("flowmm takes CUDA tensors")
     look = (*map(_strides, tensors), *map(_numel, tensors), *map(_type, tensors), *map(_device, tensors), torch._C._cuda_getDevice())
-    calls = _seen.get((what, _CACHE_FIELDS(p)))
+    calls = p.calls.get(what)
     if calls is not None:
         for known, ref in calls:
             if known == look:
@@ -423,9 +426,7 @@ def _cache_struct(p: CacheParams, what: str, tensors, expected, n_dense=0):
         if t.stride(3) != 1 if i < n_dense else not t.is_contiguous():
             raise ValueError("%s: %s must %s" % (what, name, "have contiguous head_dim" if i < n_dense else "be contiguous"))
     ref = ctypes.byref(p.c(*tensors[:n_dense]))                     # (holds on to the struct)
-    if len(_seen) >= _MAX_STRUCTS:
-        _seen.clear()
-    calls = _seen.setdefault((what, _CACHE_FIELDS(p)), [])
+    calls = p.calls.setdefault(what, [])
     if len(calls) >= 8:
         calls.clear()
     calls.append((look, ref))

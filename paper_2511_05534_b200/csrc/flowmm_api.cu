@@ -1522,17 +1522,18 @@ flowmm_status launch_store(const paged::StoreArgs &a, cudaStream_t st) {
 // A team holds its page's rows in registers, 64 elements a thread; pages of 16 rows and calls of at most 16 rows take a warp.
 template <typename T>
 flowmm_status run_store(const flowmm_cache_params &p, const paged::StoreArgs &a, cudaStream_t st) {
+    constexpr int vecs = 64 / Elem<T>::kVec;
     const int rows = std::min(p.page_size, p.n_rows);
     if (p.head_dim == 128) {
-        if (rows <= 16) return launch_store<T, 128, 32, 4>(a, st);
-        if (p.page_size == 32) return launch_store<T, 128, 64, 4>(a, st);
-        if (p.page_size == 64) return launch_store<T, 128, 128, 4>(a, st);
-        return launch_store<T, 128, 256, 4>(a, st);
+        if (rows <= 16) return launch_store<T, 128, 32, vecs>(a, st);
+        if (p.page_size == 32) return launch_store<T, 128, 64, vecs>(a, st);
+        if (p.page_size == 64) return launch_store<T, 128, 128, vecs>(a, st);
+        return launch_store<T, 128, 256, vecs>(a, st);
     }
-    if (rows <= 16) return launch_store<T, 64, 32, 2>(a, st);
-    if (p.page_size == 32) return launch_store<T, 64, 32, 4>(a, st);
-    if (p.page_size == 64) return launch_store<T, 64, 64, 4>(a, st);
-    return launch_store<T, 64, 128, 4>(a, st);
+    if (rows <= 16) return launch_store<T, 64, 32, vecs / 2>(a, st);
+    if (p.page_size == 32) return launch_store<T, 64, 32, vecs>(a, st);
+    if (p.page_size == 64) return launch_store<T, 64, 64, vecs>(a, st);
+    return launch_store<T, 64, 128, vecs>(a, st);
 }
 
 template <typename T>
@@ -1648,10 +1649,7 @@ extern "C" flowmm_status flowmm_cache_load(const flowmm_cache_params *p, const v
         !strides_ok(p->v_stride, p->head_dim) || !aligned4(k_scale) || !aligned4(v_scale) || !aligned4(block_table) || !aligned4(rows))
         return FLOWMM_ERR_ALIGN;
     FLOWMM_TRY(check_cache_ws(p, ws, ws_bytes));
-    const int64_t pages = ((int64_t)p->n_rows + p->page_size - 1) / p->page_size, items = 2 * (int64_t)p->n_units * p->n_kv_heads * pages;
-    if (items >= (int64_t)1 << 31) return FLOWMM_ERR_SHAPE;
-    constexpr int block = paged::kLoadThreads * paged::kLoadVecs;
-    const int64_t blocks = (items * p->page_size * (p->head_dim / 16) + block - 1) / block;
+    const int64_t chunks = ((int64_t)p->n_rows + paged::kLoadRows - 1) / paged::kLoadRows, blocks = 2 * (int64_t)p->n_units * p->n_kv_heads * chunks;
     if (blocks >= (int64_t)1 << 31) return FLOWMM_ERR_SHAPE;
     FLOWMM_TRY(check_device());
     paged::LoadArgs a;
@@ -1661,7 +1659,7 @@ extern "C" flowmm_status flowmm_cache_load(const flowmm_cache_params *p, const v
     a.Hkv = p->n_kv_heads; a.n_rows = p->n_rows; a.page = p->page_size; a.page_shift = page_shift(p->page_size);
     a.n_pages = p->n_pages; a.max_pages = p->max_pages;
     for (int i = 0; i < 3; ++i) { a.stride[0][i] = p->k_stride[i]; a.stride[1][i] = p->v_stride[i]; }
-    a.items = (uint32_t)items; a.by_heads = make_fastdiv(p->n_kv_heads); a.by_pages = make_fastdiv((uint32_t)pages);
+    a.by_heads = make_fastdiv(p->n_kv_heads); a.by_chunks = make_fastdiv((uint32_t)chunks);
     return p->dtype == FLOWMM_BF16 ? run_load<__nv_bfloat16>(*p, a, blocks, st) : run_load<float>(*p, a, blocks, st);
 }
 

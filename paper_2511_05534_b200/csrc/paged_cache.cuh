@@ -38,12 +38,6 @@ __device__ __forceinline__ void from_e4m3x16(const uint4 &c, float (&x)[16]) {
         x[4 * i] = a.x; x[4 * i + 1] = a.y; x[4 * i + 2] = b.x; x[4 * i + 3] = b.y;
     }
 }
-__device__ __forceinline__ uint4 to_e4m3x16(const float (&x)[16]) {
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = to_e4m3x2(x[4 * i], x[4 * i + 1]) | to_e4m3x2(x[4 * i + 2], x[4 * i + 3]) << 16;
-    return make_uint4(w[0], w[1], w[2], w[3]);
-}
 __device__ __forceinline__ bool is_finite(float x) { return (__float_as_uint(x) & 0x7F800000u) != 0x7F800000u; }
 
 // Exponent of the smallest power of two s with size <= 448 s (448 = 1.75 * 2^8), size finite and not negative.
@@ -196,15 +190,51 @@ struct StoreArgs {
     FastDiv by_heads, by_runs;
 };
 
+// kN codes (4 or 8) in memory as a word of that many bytes
+template <int kN> struct Codes;
+template <> struct Codes<4> { typedef uint32_t Word; };
+template <> struct Codes<8> { typedef uint2 Word; };
+__device__ __forceinline__ void unpack_codes(uint32_t c, float (&x)[4]) {
+    const float2 a = from_e4m3x2(c), b = from_e4m3x2(c >> 16);
+    x[0] = a.x; x[1] = a.y; x[2] = b.x; x[3] = b.y;
+}
+__device__ __forceinline__ void unpack_codes(const uint2 &c, float (&x)[8]) {
+    const uint32_t w[2] = {c.x, c.y};
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const float2 a = from_e4m3x2(w[i]), b = from_e4m3x2(w[i] >> 16);
+        x[4 * i] = a.x; x[4 * i + 1] = a.y; x[4 * i + 2] = b.x; x[4 * i + 3] = b.y;
+    }
+}
+__device__ __forceinline__ uint32_t pack_codes(const float (&x)[4]) { return to_e4m3x2(x[0], x[1]) | to_e4m3x2(x[2], x[3]) << 16; }
+__device__ __forceinline__ uint2 pack_codes(const float (&x)[8]) {
+    return make_uint2(to_e4m3x2(x[0], x[1]) | to_e4m3x2(x[2], x[3]) << 16, to_e4m3x2(x[4], x[5]) | to_e4m3x2(x[6], x[7]) << 16);
+}
+
+// The largest size among 16 bytes of elements, as the bits of an fp32 (bits without the sign order like the numbers; infinities and NaN are above all)
+template <typename T> __device__ __forceinline__ uint32_t largest_bits(const uint4 &v);
+template <> __device__ __forceinline__ uint32_t largest_bits<float>(const uint4 &v) {
+    return max(max(v.x & 0x7FFFFFFFu, v.y & 0x7FFFFFFFu), max(v.z & 0x7FFFFFFFu, v.w & 0x7FFFFFFFu));
+}
+template <> __device__ __forceinline__ uint32_t largest_bits<__nv_bfloat16>(const uint4 &v) {
+    const uint32_t m = __vmaxu2(__vmaxu2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu), __vmaxu2(v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu));
+    return max(m << 16, m & 0xFFFF0000u);
+}
+constexpr uint32_t kInfinityBits = 0x7F800000u;
+__device__ __forceinline__ uint32_t warp_max_bits(uint32_t x) { return __reduce_max_sync(0xFFFFFFFFu, x); }
+
 // One team of threads per (unit, page that its rows reach, KV head, K or V): the rows of the page are read once, into
-// registers, their largest size found, and written as codes.  Reading bounds it: 16 elements a thread and load step, kVecs steps
-// on their way at once.
-// Rows of a unit fill consecutive places, so the team knows from the first row's slot which rows are its page's; every row's own
+// registers, their largest size found, and written as codes.  Memory bounds it: 16 bytes a thread and load, neighbours side by side, kVecs loads
+// on their way at once, and nothing before them but the unit's first slot.  Next to it come the instructions for each element, so sizes are
+// compared as integers, two bf16 at a time, and whether a number is finite is only asked where a thread has met one that is not
+// (80 units of 1690 rows, 8 heads: 178 us with both for each element).
+// Rows of a unit fill consecutive places, so the team knows from that slot which rows are its page's; every row's own
 // slot is still looked at, and one that is not where it should be is left out and reported.
 template <typename T, int D, int kTeam, int kVecs>
 __global__ void __launch_bounds__(kTeam < 128 ? 128 : kTeam) cache_store_kernel(const StoreArgs A) {
-    constexpr int kBlock = kTeam < 128 ? 128 : kTeam, kLanes = D / 16, kRows = kTeam / kLanes, kLoads = 16 / Elem<T>::kVec;
-    __shared__ float wide[kBlock / 32];
+    constexpr int kBlock = kTeam < 128 ? 128 : kTeam, kN = Elem<T>::kVec, kLanes = D / kN, kRows = kTeam / kLanes;
+    typedef typename Codes<kN>::Word Word;
+    __shared__ uint32_t wide[kBlock / 32];
     predecessor_done();
     successor_may_start();
     const int team = threadIdx.x / kTeam, me = threadIdx.x % kTeam, lane = me % kLanes, row0 = me / kLanes;
@@ -216,87 +246,92 @@ __global__ void __launch_bounds__(kTeam < 128 ? 128 : kTeam) cache_store_kernel(
     const int first = on ? slots[0] : -1;
     if (first < -1 && me == 0) report(A.status, kStatusIndex);
     const int held0 = first & (A.page - 1);
-    const int t0 = run == 0 ? 0 : (int)run * A.page - held0;
+    const int t0 = run == 0 ? 0 : (int)run * A.page - held0, held = run == 0 ? held0 : 0;      // the page's first new row; rows that it has already
     on = on && first >= 0 && t0 < A.T;
-    const int slot = !on ? -1 : run == 0 ? first : slots[t0];
-    const int held = run == 0 ? held0 : 0;                            // rows that the page has already
-    const bool sound = slot < A.n_pages << A.page_shift && slot >= 0 && (slot & (A.page - 1)) == held;
-    if (on && !sound && slot != -1 && me == 0) report(A.status, kStatusIndex);
-    on = on && sound;
     const int n = on ? min(A.T - t0, A.page - held) : 0;              // rows of this page
-    const T *x = static_cast<const T *>(A.x[which]) + u * A.stride[which][0] + h * A.stride[which][1] + (int64_t)t0 * A.stride[which][2] + lane * 16;
-    uint4 raw[kVecs][kLoads];
-    bool mine[kVecs];
+    const T *x = static_cast<const T *>(A.x[which]) + u * A.stride[which][0] + h * A.stride[which][1] + (int64_t)t0 * A.stride[which][2] + lane * kN;
+    uint4 raw[kVecs];
+    int at[kVecs];
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
         const int r = row0 + i * kRows;
-        mine[i] = r < n;
-        if (mine[i]) {
-#pragma unroll
-            for (int j = 0; j < kLoads; ++j) raw[i][j] = load_raw16(x + (int64_t)r * A.stride[which][2] + j * Elem<T>::kVec);
+        at[i] = -1;
+        if (r < n) {
+            raw[i] = load_raw16(x + (int64_t)r * A.stride[which][2]);
+            at[i] = slots[t0 + r];
         }
     }
+    const int slot = on ? slots[t0] : -1;
+    const bool sound = slot < A.n_pages << A.page_shift && slot >= 0 && (slot & (A.page - 1)) == held;
+    if (on && !sound && slot != -1 && me == 0) report(A.status, kStatusIndex);
+    on = on && sound;
     const uint32_t page = on ? (uint32_t)slot >> A.page_shift : 0u;
     const uint32_t ph = page * A.by_heads.d + h;
     const float had = on && held > 0 ? A.scale[which][ph] : 0.f;
-    float size = 0.f;
+    uint32_t size = 0;
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
-        if (!mine[i]) continue;
-        const int want = slot + row0 + i * kRows, is = slots[t0 + row0 + i * kRows];
-        if (is != want) {
-            mine[i] = false;
-            if (is != -1 && lane == 0) report(A.status, kStatusIndex);
-            continue;
-        }
-#pragma unroll
-        for (int j = 0; j < kLoads; ++j) {
-            float f[Elem<T>::kVec];
-            Elem<T>::unpack(raw[i][j], f);
-#pragma unroll
-            for (int e = 0; e < Elem<T>::kVec; ++e) size = fmaxf(size, is_finite(f[e]) ? fabsf(f[e]) : 0.f);
+        const int r = row0 + i * kRows;
+        if (at[i] < 0 || !on) {
+            if (at[i] < -1) report(A.status, kStatusIndex);
+            at[i] = -1;
+        } else if (at[i] != slot + r) {
+            at[i] = -1;
+            if (lane == 0) report(A.status, kStatusIndex);
+        } else {
+            size = max(size, largest_bits<T>(raw[i]));
         }
     }
+    const bool odd = size >= kInfinityBits;                           // something that is not finite among this thread's
+    if (odd) {
+        size = 0;
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) size = fmaxf(size, __shfl_xor_sync(0xFFFFFFFFu, size, o));
+        for (int i = 0; i < kVecs; ++i) {
+            if (at[i] < 0) continue;
+            float f[kN];
+            Elem<T>::unpack(raw[i], f);
+#pragma unroll
+            for (int e = 0; e < kN; ++e) size = max(size, is_finite(f[e]) ? __float_as_uint(f[e]) & 0x7FFFFFFFu : 0u);
+        }
+    }
+    size = warp_max_bits(size);
     if (kTeam > 32) {
         if (lane_id() == 0) wide[threadIdx.x >> 5] = size;
         __syncthreads();                                              // (also: the whole team has read the page's old scale)
 #pragma unroll
-        for (int w = 0; w < kTeam / 32; ++w) size = fmaxf(size, wide[team * (kTeam / 32) + w]);
+        for (int w = 0; w < kTeam / 32; ++w) size = max(size, wide[team * (kTeam / 32) + w]);
     } else {
         __syncwarp();
     }
     if (!on) return;
-    const int e = max(held > 0 ? held_exponent(had) : kLowestExponent, scale_exponent(size));
+    const int e = max(held > 0 ? held_exponent(had) : kLowestExponent, scale_exponent(__uint_as_float(size)));
     const float inverse = power_of_two(-e);
-    uint8_t *out = A.pages[which] + ((int64_t)ph << A.page_shift) * D + lane * 16;
+    uint8_t *out = A.pages[which] + ((int64_t)ph << A.page_shift) * D + lane * kN;
     if (held > 0) {
         const float ratio = had * inverse;                            // (exact: both are powers of two)
         if (ratio != 1.f) {
             for (int r = row0; r < held; r += kRows) {
-                uint4 *at = reinterpret_cast<uint4 *>(out + r * D);
-                float f[16];
-                from_e4m3x16(*at, f);
+                Word *old = reinterpret_cast<Word *>(out + r * D);
+                float f[kN];
+                unpack_codes(*old, f);
 #pragma unroll
-                for (int k = 0; k < 16; ++k) f[k] *= ratio;
-                *at = to_e4m3x16(f);
+                for (int k = 0; k < kN; ++k) f[k] *= ratio;
+                *old = pack_codes(f);
             }
         }
     }
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
-        if (!mine[i]) continue;
-        float f[16];
+        if (at[i] < 0) continue;
+        float f[kN];
+        Elem<T>::unpack(raw[i], f);
+        if (odd) {
 #pragma unroll
-        for (int j = 0; j < kLoads; ++j) {
-            float g[Elem<T>::kVec];
-            Elem<T>::unpack(raw[i][j], g);
-#pragma unroll
-            for (int k = 0; k < Elem<T>::kVec; ++k)
-                f[j * Elem<T>::kVec + k] = is_finite(g[k]) ? g[k] * inverse : __uint_as_float(0x7FC00000u);
+            for (int k = 0; k < kN; ++k) f[k] = is_finite(f[k]) ? f[k] : __uint_as_float(0x7FC00000u);
         }
-        *reinterpret_cast<uint4 *>(out + (held + row0 + i * kRows) * D) = to_e4m3x16(f);
+#pragma unroll
+        for (int k = 0; k < kN; ++k) f[k] *= inverse;
+        *reinterpret_cast<Word *>(out + (held + row0 + i * kRows) * D) = pack_codes(f);
     }
     if (me == 0) A.scale[which][ph] = power_of_two(e);
 }
@@ -310,54 +345,52 @@ struct LoadArgs {
     int *status;
     int Hkv, n_rows, page, page_shift, n_pages, max_pages;
     int64_t stride[2][3];
-    uint32_t items;                    // U * pages of n_rows * Hkv * 2
-    FastDiv by_heads, by_pages;
+    FastDiv by_heads, by_chunks;
 };
-constexpr int kLoadThreads = 128, kLoadVecs = 4;
+constexpr int kLoadThreads = 128, kLoadRows = 64;
 
-// A block takes 128 * 4 groups of 16 codes of consecutive pages' heads: a thread's four loads are on their way at once.
+// A block takes 64 rows of one (unit, KV head, K or V); 16 bytes of output a thread and store, neighbours side by side, all its codes on their
+// way at once.  Writing bounds it.
 template <typename T, int D>
 __global__ void __launch_bounds__(kLoadThreads) cache_load_kernel(const LoadArgs A) {
-    constexpr int kLanes = D / 16;
+    constexpr int kN = Elem<T>::kVec, kLanes = D / kN, kRows = kLoadThreads / kLanes, kVecs = kLoadRows / kRows;
+    typedef typename Codes<kN>::Word Word;
     predecessor_done();
     successor_may_start();
-    const int shift = A.page_shift + (D == 128 ? 3 : 2);              // groups of a page's head, as a shift
-    uint4 codes[kLoadVecs];
-    float scale[kLoadVecs];
-    T *to[kLoadVecs];
+    const int lane = threadIdx.x % kLanes, row0 = threadIdx.x / kLanes;
+    const uint32_t which = blockIdx.x & 1u, q = blockIdx.x >> 1, q1 = A.by_heads.div(q), h = q - q1 * A.by_heads.d;
+    const uint32_t u = A.by_chunks.div(q1), chunk = q1 - u * A.by_chunks.d;
+    const int first = (int)(chunk * kLoadRows), held = A.rows[u], most = A.max_pages << A.page_shift;
+    if ((held < 0 || held > most) && threadIdx.x == 0) report(A.status, kStatusIndex);
+    const int n = min(min(held, most), A.n_rows) - first;             // rows of this block
+    const int *table = A.table + (int64_t)u * A.max_pages;
+    int id[kVecs];
+    Word codes[kVecs];
+    float scale[kVecs];
 #pragma unroll
-    for (int i = 0; i < kLoadVecs; ++i) {
-        const uint64_t g = ((uint64_t)blockIdx.x * kLoadVecs + i) * kLoadThreads + threadIdx.x;
-        const uint64_t item64 = g >> shift;
-        to[i] = nullptr;
-        if (item64 >= A.items) continue;
-        const uint32_t item = (uint32_t)item64;
-        const int at = (int)(g & ((1u << shift) - 1u)), r = at / kLanes, lane = at % kLanes;
-        const uint32_t which = item & 1u, q = item >> 1, q1 = A.by_heads.div(q), h = q - q1 * A.by_heads.d;
-        const uint32_t u = A.by_pages.div(q1), j = q1 - u * A.by_pages.d;
-        const int row = (int)(j << A.page_shift) + r;
-        const int n = A.rows[u];
-        if (n < 0 || n > A.max_pages << A.page_shift) { if (at == 0 && j == 0) report(A.status, kStatusIndex); }
-        if (row >= min(n, A.n_rows) || (int)j >= A.max_pages) continue;
-        const int id = A.table[(int64_t)u * A.max_pages + j];
-        if (id < 0 || id >= A.n_pages) { report(A.status, kStatusIndex); continue; }
-        const int64_t ph = (int64_t)id * A.Hkv + h;
-        codes[i] = *reinterpret_cast<const uint4 *>(A.pages[which] + ((ph << A.page_shift) + r) * D + lane * 16);
-        scale[i] = A.scale[which][ph];
-        to[i] = static_cast<T *>(A.x[which]) + u * A.stride[which][0] + h * A.stride[which][1] + (int64_t)row * A.stride[which][2] + lane * 16;
+    for (int i = 0; i < kVecs; ++i) {
+        const int r = row0 + i * kRows;
+        id[i] = r < n ? table[(first + r) >> A.page_shift] : 0;
+        if ((unsigned)id[i] >= (unsigned)A.n_pages) { report(A.status, kStatusIndex); id[i] = -1; }
+        if (r >= n) id[i] = -1;
     }
 #pragma unroll
-    for (int i = 0; i < kLoadVecs; ++i) {
-        if (to[i] == nullptr) continue;
-        float f[16];
-        from_e4m3x16(codes[i], f);
+    for (int i = 0; i < kVecs; ++i) {
+        if (id[i] < 0) continue;
+        const int64_t ph = (int64_t)id[i] * A.Hkv + h;
+        const int at = (first + row0 + i * kRows) & (A.page - 1);
+        codes[i] = *reinterpret_cast<const Word *>(A.pages[which] + ((ph << A.page_shift) + at) * D + lane * kN);
+        scale[i] = A.scale[which][ph];
+    }
+    T *x = static_cast<T *>(A.x[which]) + u * A.stride[which][0] + h * A.stride[which][1] + (int64_t)first * A.stride[which][2] + lane * kN;
 #pragma unroll
-        for (int k = 0; k < 16 / Elem<T>::kVec; ++k) {
-            float part[Elem<T>::kVec];
+    for (int i = 0; i < kVecs; ++i) {
+        if (id[i] < 0) continue;
+        float f[kN];
+        unpack_codes(codes[i], f);
 #pragma unroll
-            for (int e = 0; e < Elem<T>::kVec; ++e) part[e] = f[k * Elem<T>::kVec + e] * scale[i];
-            Elem<T>::store16(to[i] + k * Elem<T>::kVec, part);
-        }
+        for (int k = 0; k < kN; ++k) f[k] *= scale[i];
+        Elem<T>::store16(x + (int64_t)(row0 + i * kRows) * A.stride[which][2], f);
     }
 }
 
