@@ -1538,8 +1538,10 @@ flowmm_status run_store(const flowmm_cache_params &p, const paged::StoreArgs &a,
 
 template <typename T>
 flowmm_status run_load(const flowmm_cache_params &p, const paged::LoadArgs &a, int64_t blocks, cudaStream_t st) {
-    if (p.head_dim == 128) launch(paged::cache_load_kernel<T, 128>, (unsigned)blocks, paged::kLoadThreads, 0, st, a);
-    else launch(paged::cache_load_kernel<T, 64>, (unsigned)blocks, paged::kLoadThreads, 0, st, a);
+    const bool one = p.page_size >= paged::kLoadRows;
+    auto kernel = p.head_dim == 128 ? (one ? paged::cache_load_kernel<T, 128, true> : paged::cache_load_kernel<T, 128, false>)
+                                    : (one ? paged::cache_load_kernel<T, 64, true> : paged::cache_load_kernel<T, 64, false>);
+    launch(kernel, (unsigned)blocks, paged::kLoadThreads, 0, st, a);
     FLOWMM_LAUNCHED("cache_load");
     return FLOWMM_OK;
 }

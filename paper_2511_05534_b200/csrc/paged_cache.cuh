@@ -350,8 +350,8 @@ struct LoadArgs {
 constexpr int kLoadThreads = 128, kLoadRows = 64;
 
 // A block takes 64 rows of one (unit, KV head, K or V); 16 bytes of output a thread and store, neighbours side by side, all its codes on their
-// way at once.  Writing bounds it.
-template <typename T, int D>
+// way at once.  Writing bounds it.  kOnePage: pages of 64 rows and more, so that the block has one page's number and scale.
+template <typename T, int D, bool kOnePage>
 __global__ void __launch_bounds__(kLoadThreads) cache_load_kernel(const LoadArgs A) {
     constexpr int kN = Elem<T>::kVec, kLanes = D / kN, kRows = kLoadThreads / kLanes, kVecs = kLoadRows / kRows;
     typedef typename Codes<kN>::Word Word;
@@ -364,33 +364,36 @@ __global__ void __launch_bounds__(kLoadThreads) cache_load_kernel(const LoadArgs
     if ((held < 0 || held > most) && threadIdx.x == 0) report(A.status, kStatusIndex);
     const int n = min(min(held, most), A.n_rows) - first;             // rows of this block
     const int *table = A.table + (int64_t)u * A.max_pages;
-    int id[kVecs];
+    if (n <= 0) return;
+    constexpr int kPages = kOnePage ? 1 : kVecs;
+    int id[kPages];
     Word codes[kVecs];
-    float scale[kVecs];
+    float scale[kPages];
 #pragma unroll
-    for (int i = 0; i < kVecs; ++i) {
-        const int r = row0 + i * kRows;
-        id[i] = r < n ? table[(first + r) >> A.page_shift] : 0;
-        if ((unsigned)id[i] >= (unsigned)A.n_pages) { report(A.status, kStatusIndex); id[i] = -1; }
-        if (r >= n) id[i] = -1;
+    for (int i = 0; i < kPages; ++i) {
+        const int r = kOnePage ? 0 : row0 + i * kRows;
+        id[i] = r < n ? table[(first + r) >> A.page_shift] : -1;
+        if (r < n && (unsigned)id[i] >= (unsigned)A.n_pages) { report(A.status, kStatusIndex); id[i] = -1; }
     }
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
-        if (id[i] < 0) continue;
-        const int64_t ph = (int64_t)id[i] * A.Hkv + h;
-        const int at = (first + row0 + i * kRows) & (A.page - 1);
+        const int r = row0 + i * kRows, page = id[kOnePage ? 0 : i];
+        if (page < 0 || r >= n) continue;
+        const int64_t ph = (int64_t)page * A.Hkv + h;
+        const int at = (first + r) & (A.page - 1);
         codes[i] = *reinterpret_cast<const Word *>(A.pages[which] + ((ph << A.page_shift) + at) * D + lane * kN);
-        scale[i] = A.scale[which][ph];
+        if (!kOnePage || i == 0) scale[kOnePage ? 0 : i] = A.scale[which][ph];
     }
     T *x = static_cast<T *>(A.x[which]) + u * A.stride[which][0] + h * A.stride[which][1] + (int64_t)first * A.stride[which][2] + lane * kN;
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
-        if (id[i] < 0) continue;
+        const int r = row0 + i * kRows;
+        if (id[kOnePage ? 0 : i] < 0 || r >= n) continue;
         float f[kN];
         unpack_codes(codes[i], f);
 #pragma unroll
-        for (int k = 0; k < kN; ++k) f[k] *= scale[i];
-        Elem<T>::store16(x + (int64_t)(row0 + i * kRows) * A.stride[which][2], f);
+        for (int k = 0; k < kN; ++k) f[k] *= scale[kOnePage ? 0 : i];
+        Elem<T>::store16(x + (int64_t)r * A.stride[which][2], f);
     }
 }
 
