@@ -8,6 +8,8 @@ libflowmm.so is missing or a call fails, an exception is raised.
 from __future__ import annotations
 
 import ctypes
+import importlib.machinery
+import importlib.util
 import math
 import operator
 import os
@@ -18,6 +20,7 @@ import torch
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libflowmm.so")
+MARSHAL_PATH = os.path.join(_PKG, "_marshal.so")
 
 F32, BF16 = 0, 1
 INTRA, CROSS = 0, 1
@@ -371,7 +374,8 @@ class _CCacheParams(ctypes.Structure):
 
 @dataclass
 class CacheParams:
-    """Mirror of flowmm_cache_params; the strides of the dense rows are taken from the tensors each call receives."""
+    """Mirror of flowmm_cache_params; the strides of the dense rows are taken from the tensors each call receives.  Keeps the handles
+    of the calls made with it (_cache_call) until a field changes."""
     n_units: int
     n_q_heads: int
     n_kv_heads: int
@@ -386,68 +390,64 @@ class CacheParams:
 
     def __setattr__(self, name, value):
         object.__setattr__(self, name, value)
-        object.__setattr__(self, "calls", {})     # what _cache_struct has seen of calls with these values
+        object.__setattr__(self, "calls", {})
 
-    def c(self, k=None, v=None) -> _CCacheParams:
+    def c(self) -> _CCacheParams:
         dense = (self.n_kv_heads * self.n_rows * self.head_dim, self.n_rows * self.head_dim, self.head_dim)
         cp = _CCacheParams(*_CACHE_FIELDS(self))
-        cp.k_stride = (ctypes.c_int64 * 3)(*(dense if k is None else k.stride()[:3]))
-        cp.v_stride = (ctypes.c_int64 * 3)(*(dense if v is None else v.stride()[:3]))
+        cp.k_stride = cp.v_stride = (ctypes.c_int64 * 3)(*dense)
         return cp
 
 
 _CACHE_FIELDS = operator.attrgetter("n_units", "n_q_heads", "n_kv_heads", "head_dim", "page_size", "n_pages", "max_pages",
                                     "n_rows", "dtype", "softmax_scale", "path")
-_CODE_TYPES = (torch.uint8, torch.float8_e4m3fn)
+_CODE_TYPES, _INT32, _BYTES, _FLOAT = (torch.uint8, torch.float8_e4m3fn), (torch.int32,), (torch.uint8,), (torch.float32,)
+_marshal = None
 
 
-# What a call's tensors look like, in C loops: ten tensors' shapes and strides by hand cost twice what the rest of a call does.  Strides and
-# numel together fix what memory a tensor covers.
-_strides, _numel, _device, _address = torch.Tensor.stride, torch.Tensor.numel, torch.Tensor.get_device, torch.Tensor.data_ptr
-_type = operator.attrgetter("dtype")
+def _load_marshal():
+    """The module that looks at the tensors of the paged cache's calls and passes their addresses on (csrc/marshal.cpp)."""
+    global _marshal
+    if _marshal is None:
+        if not os.path.exists(MARSHAL_PATH):
+            raise FileNotFoundError("%s is missing: build it with `python -m paper_2511_05534_b200.build`" % MARSHAL_PATH)
+        spec = importlib.util.spec_from_loader("_marshal", importlib.machinery.ExtensionFileLoader("_marshal", MARSHAL_PATH))
+        _marshal = importlib.util.module_from_spec(spec)
+    return _marshal
 
 
-def _cache_struct(p: CacheParams, what: str, tensors, expected, n_dense=0):
-    """The call's struct, after a look at what the C side cannot see: the tensors' shapes, types and devices.  expected(): (name, shape,
-    types) of each; the first n_dense, the rows of K and V, may have strides.  Calls alike in all of that are looked at once."""
-    if not tensors[0].is_cuda:
-        raise ValueError("flowmm takes CUDA tensors")
-    look = (*map(_strides, tensors), *map(_numel, tensors), *map(_type, tensors), *map(_device, tensors), torch._C._cuda_getDevice())
-    calls = p.calls.get(what)
-    if calls is not None:
-        for known, ref in calls:
-            if known == look:
-                return ref
-    for i, (t, (name, shape, types)) in enumerate(zip(tensors, expected())):
-        if tuple(t.shape) != shape or t.dtype not in types:
-            raise ValueError("%s: %s must be a %s tensor of shape %s" % (what, name, " or ".join(str(x) for x in types), list(shape)))
-        if t.get_device() != look[-1]:
-            raise ValueError("%s: %s is not on the current device" % (what, name))
-        if t.stride(3) != 1 if i < n_dense else not t.is_contiguous():
-            raise ValueError("%s: %s must %s" % (what, name, "have contiguous head_dim" if i < n_dense else "be contiguous"))
-    ref = ctypes.byref(p.c(*tensors[:n_dense]))                     # (holds on to the struct)
-    calls = p.calls.setdefault(what, [])
-    if len(calls) >= 8:
-        calls.clear()
-    calls.append((look, ref))
-    return ref
+def _cache_call(p: CacheParams, what: str):
+    """The handle of the entry point with these params: what its tensors have to look like, in the order of its pointers."""
+    U, rows = p.n_units, (p.n_units, p.n_kv_heads, p.n_rows, p.head_dim)
+    codes, scales, table, own = (p.n_pages, p.n_kv_heads, p.page_size, p.head_dim), (p.n_pages, p.n_kv_heads), (U, p.max_pages), (torch_dtype(p.dtype),)
+    pool = (("k_pages", codes, _CODE_TYPES, 0, False), ("v_pages", codes, _CODE_TYPES, 0, False),
+            ("k_scale", scales, _FLOAT, 0, False), ("v_scale", scales, _FLOAT, 0, False))
+    dense = (("k", rows, own, 1, False), ("v", rows, own, 2, False))
+    held = (("block_table", table, _INT32, 0, False), ("rows", (U,), _INT32, 0, False))
+    heads = (U, p.n_q_heads, p.head_dim)
+    arguments = {
+        "flowmm_cache_plan": (("grow", (U,), _INT32, 0, False), ("rows", (U,), _INT32, 0, False), ("rows_out", (U,), _INT32, 0, False),
+                              ("free_pages", (p.n_pages,), _INT32, 0, False), ("free_state", (2,), _INT32, 0, False),
+                              ("free_state_out", (2,), _INT32, 0, False), ("block_table", table, _INT32, 0, False),
+                              ("slots", (U, p.n_rows), _INT32, 0, True)),
+        "flowmm_cache_store": dense + (("slots", (U, p.n_rows), _INT32, 0, False),) + pool,
+        "flowmm_cache_load": pool + held + dense,
+        "flowmm_cache_attention": (("q", heads, own, 0, False),) + pool + held + (("out", heads, _FLOAT, 0, False),),
+    }[what] + (("ws", (-1,), _BYTES, 0, False),)
+    function = ctypes.cast(getattr(load(), what), ctypes.c_void_p).value
+    cp = p.c()
+    handle = _load_marshal().make(what, function, ctypes.addressof(cp), arguments)
+    p.calls[what] = handle = (_lib, _marshal.run, handle)
+    return handle
 
 
-def _expect_pool(p: CacheParams):
-    codes, scales = (p.n_pages, p.n_kv_heads, p.page_size, p.head_dim), (p.n_pages, p.n_kv_heads)
-    return (("k_pages", codes, _CODE_TYPES), ("v_pages", codes, _CODE_TYPES), ("k_scale", scales, _FLOAT), ("v_scale", scales, _FLOAT))
-
-
-def _expect_rows(p: CacheParams):
-    shape, types = (p.n_units, p.n_kv_heads, p.n_rows, p.head_dim), (torch_dtype(p.dtype),)
-    return (("k", shape, types), ("v", shape, types))
-
-
-_INT32, _BYTES, _FLOAT = (torch.int32,), (torch.uint8,), (torch.float32,)
-
-
-def _cache_ws(ws):
-    return ("ws", (ws.numel(),), _BYTES)
+def _cache_run(p: CacheParams, what: str, *tensors):
+    call = p.calls.get(what)
+    if call is None or call[0] is not _lib:
+        call = _cache_call(p, what)
+    code = call[1](call[2], *tensors)
+    if code != 0:
+        raise FlowmmError(code, what)
 
 
 def flowmm_cache_workspace_bytes(p: CacheParams) -> int:
@@ -466,40 +466,22 @@ def alloc_cache_workspace(p: CacheParams, device="cuda") -> torch.Tensor:
 
 def flowmm_cache_plan(p: CacheParams, grow, rows, rows_out, free_pages, free_state, free_state_out, block_table, slots, ws):
     """Pages and slots for units that go from rows to rows + grow rows; slots may be None."""
-    tensors = (grow, rows, rows_out, free_pages, free_state, free_state_out, block_table, ws) + (() if slots is None else (slots,))
-    U = (p.n_units,)
-    ref = _cache_struct(p, "flowmm_cache_plan", tensors, lambda: (
-        ("grow", U, _INT32), ("rows", U, _INT32), ("rows_out", U, _INT32), ("free_pages", (p.n_pages,), _INT32), ("free_state", (2,), _INT32),
-        ("free_state_out", (2,), _INT32), ("block_table", (p.n_units, p.max_pages), _INT32), _cache_ws(ws), ("slots", (p.n_units, p.n_rows), _INT32)))
-    *at, ws_at = map(_address, tensors[:8])
-    _check((_lib or load()).flowmm_cache_plan(ref, *at, None if slots is None else slots.data_ptr(), ws_at, ws.numel(), torch._C._cuda_getCurrentRawStream(ws.get_device())), "flowmm_cache_plan")
+    _cache_run(p, "flowmm_cache_plan", grow, rows, rows_out, free_pages, free_state, free_state_out, block_table, slots, ws)
 
 
 def flowmm_cache_store(p: CacheParams, k, v, slots, k_pages, v_pages, k_scale, v_scale, ws):
     """Rows k, v [units, kv_heads, n_rows, head_dim] into pages (uint8 or float8_e4m3fn tensors), as slots says."""
-    tensors = (k, v, slots, k_pages, v_pages, k_scale, v_scale, ws)
-    ref = _cache_struct(p, "flowmm_cache_store", tensors, lambda: (
-        *_expect_rows(p), ("slots", (p.n_units, p.n_rows), _INT32), *_expect_pool(p), _cache_ws(ws)), 2)
-    _check((_lib or load()).flowmm_cache_store(ref, *map(_address, tensors), ws.numel(), torch._C._cuda_getCurrentRawStream(ws.get_device())), "flowmm_cache_store")
+    _cache_run(p, "flowmm_cache_store", k, v, slots, k_pages, v_pages, k_scale, v_scale, ws)
 
 
 def flowmm_cache_load(p: CacheParams, k_pages, v_pages, k_scale, v_scale, block_table, rows, k, v, ws):
     """The first min(rows[u], n_rows) rows of every unit into k, v [units, kv_heads, n_rows, head_dim]."""
-    tensors = (k, v, k_pages, v_pages, k_scale, v_scale, block_table, rows, ws)
-    ref = _cache_struct(p, "flowmm_cache_load", tensors, lambda: (
-        *_expect_rows(p), *_expect_pool(p), ("block_table", (p.n_units, p.max_pages), _INT32), ("rows", (p.n_units,), _INT32), _cache_ws(ws)), 2)
-    k_at, v_at, *at, ws_at = map(_address, tensors)
-    _check((_lib or load()).flowmm_cache_load(ref, *at, k_at, v_at, ws_at, ws.numel(), torch._C._cuda_getCurrentRawStream(ws.get_device())), "flowmm_cache_load")
+    _cache_run(p, "flowmm_cache_load", k_pages, v_pages, k_scale, v_scale, block_table, rows, k, v, ws)
 
 
 def flowmm_cache_attention(p: CacheParams, q, k_pages, v_pages, k_scale, v_scale, block_table, rows, out, ws):
     """Decode attention over the paged cache; q [units, q_heads, head_dim], out the same in float32."""
-    tensors = (q, k_pages, v_pages, k_scale, v_scale, block_table, rows, out, ws)
-    heads = (p.n_units, p.n_q_heads, p.head_dim)
-    ref = _cache_struct(p, "flowmm_cache_attention", tensors, lambda: (
-        ("q", heads, (torch_dtype(p.dtype),)), *_expect_pool(p), ("block_table", (p.n_units, p.max_pages), _INT32), ("rows", (p.n_units,), _INT32),
-        ("out", heads, _FLOAT), _cache_ws(ws)))
-    _check((_lib or load()).flowmm_cache_attention(ref, *map(_address, tensors), ws.numel(), torch._C._cuda_getCurrentRawStream(ws.get_device())), "flowmm_cache_attention")
+    _cache_run(p, "flowmm_cache_attention", q, k_pages, v_pages, k_scale, v_scale, block_table, rows, out, ws)
 
 
 def flowmm_selftest_wait_timeout(ws):

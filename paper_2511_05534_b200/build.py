@@ -1,7 +1,8 @@
-"""Builds the CUDA library (libflowmm.so) in-tree with nvcc for sm_100a."""
+"""Builds the CUDA library (libflowmm.so, nvcc for sm_100a) and the Python marshalling module beside it (_marshal.so, g++) in-tree."""
 from __future__ import annotations
 
 import os
+import shutil
 import subprocess
 import sys
 
@@ -11,10 +12,12 @@ CSRC = os.path.join(_PKG, "csrc")
 LIB_PATH = os.path.join(_PKG, "libflowmm.so")
 DEBUG_LIB_PATH = os.path.join(_PKG, "libflowmm_debug.so")     # the same sources with -DFLOWMM_DEBUG (index checks)
 SOURCES = ["flowmm_api.cu"]
+MARSHAL_PATH = os.path.join(_PKG, "_marshal.so")
+MARSHAL_SOURCE = "marshal.cpp"
 
 
 def _newest_source_mtime() -> float:
-    paths = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(_ROOT, "include", "flowmm.h")]
+    paths = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f != MARSHAL_SOURCE] + [os.path.join(_ROOT, "include", "flowmm.h")]
     return max(os.path.getmtime(p) for p in paths)
 
 
@@ -29,9 +32,29 @@ def nvcc_command(out: str, verbose_ptxas: bool = False, debug: bool = False):
     return cmd + [os.path.join(CSRC, s) for s in SOURCES]
 
 
+def _build_marshal(force: bool) -> None:
+    source = os.path.join(CSRC, MARSHAL_SOURCE)
+    newest = max(os.path.getmtime(source), os.path.getmtime(os.path.join(_ROOT, "include", "flowmm.h")))
+    if not force and os.path.exists(MARSHAL_PATH) and os.path.getmtime(MARSHAL_PATH) >= newest:
+        return
+    import sysconfig
+
+    import torch
+    from torch.utils import cpp_extension
+    tmp = MARSHAL_PATH + ".%d.tmp" % os.getpid()
+    cuda = os.path.join(os.path.dirname(os.path.dirname(os.path.realpath(shutil.which("nvcc") or "/usr/local/cuda/bin/nvcc"))), "include")
+    include = cpp_extension.include_paths() + [cuda, sysconfig.get_paths()["include"], os.path.join(_ROOT, "include")]
+    subprocess.check_call(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch.compiled_with_cxx11_abi(),
+                           *("-I" + d for d in include), source, "-o", tmp,
+                           *("-L" + d for d in cpp_extension.library_paths()), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"])
+    os.replace(tmp, MARSHAL_PATH)
+
+
 def build(force: bool = False, verbose_ptxas: bool = False, debug: bool = False) -> str:
     """Compile if the library is missing or older than any source; returns its path.  debug: the build with
     index checks (libflowmm_debug.so) instead of the release library."""
+    if not debug:
+        _build_marshal(force)
     path = DEBUG_LIB_PATH if debug else LIB_PATH
     if force or not os.path.exists(path) or os.path.getmtime(path) < _newest_source_mtime():
         tmp = path + ".%d.tmp" % os.getpid()
