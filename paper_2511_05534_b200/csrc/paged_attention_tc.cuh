@@ -377,7 +377,9 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
             }
             return ok;
         };
-        const Cut cut = make_cut(A);
+        // (a call whose heads cannot be cut has one for each block at most: nothing to find)
+        Cut cut = {};
+        if (A.cut_heads) cut = make_cut(A);
         Walk w = {};                                                 // the head of the group after `now`
         int group = 0, head = 0, second = 0;
         int4 cut_head = make_int4(0, 0, 0, 0);                       // unit, head and number of pieces of a head that begins here and goes on in other blocks
@@ -526,10 +528,14 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
         const uint32_t tcols = trow + set * 8;                       // columns of their logits within a tile's
         float *red = reinterpret_cast<float *>(ptc_smem + kSmemRed);
         Task now, done;
+        uint2 q = make_uint2(0, 0);
+        const uint32_t own_u = blockIdx.x / A.Hkv;
+        if (!A.cut_heads && own_u < (uint32_t)A.U) q = query(own_u, blockIdx.x - own_u * A.Hkv, e >> 5);       // (known before the lengths are)
         bool ok = true, more = wait_task(0, now);
         if (more) {                                                  // the first head's operand, a warp per query head
             if ((e >> 5) < kHeads) {
-                const float f = put_query(base + kSmemQ, e >> 5, query(now.u, now.h, e >> 5), A.scale_log2);
+                if (A.cut_heads) q = query(now.u, now.h, e >> 5);
+                const float f = put_query(base + kSmemQ, e >> 5, q, A.scale_log2);
                 if (lane == 0) first_factors[e >> 5] = f;
             }
             fence_proxy_async();

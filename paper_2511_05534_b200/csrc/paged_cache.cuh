@@ -132,8 +132,11 @@ __global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(const PlanArgs
             if (need > 0 && upto > count) ok = false;
             if (!ok) { me.want = me.held; me.grow = 0; }
             if (ok && need > 0) atomicMax(&taken_max, (unsigned)upto);
-            me.at = (unsigned)(((long long)head + upto - need) % n);
-            me.to = (unsigned)(((long long)head + count + given - back) % n);
+            if (ok && need > 0) me.at = ring_place(head + (unsigned)(upto - need), n);
+            if (back > 0) {                                        // (a remainder only where more comes back than the ring can hold)
+                const unsigned long long to = (unsigned long long)head + count + given - back;
+                me.to = to < 2ull * n ? ring_place((unsigned)to, n) : (unsigned)(to % n);
+            }
             if (first) {
                 A.rows_out[u] = ok ? max(0, me.rows + me.grow) : me.rows;
                 if (!ok) report(A.status, kStatusPool);
@@ -149,8 +152,24 @@ __global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(const PlanArgs
             const PlanUnit p = unit[i];
             int *row = A.table + (int64_t)(u0 + i) * A.max_pages;
             if (c == 0) {
-                for (int j = p.held + lane; j < p.want; j += 32) row[j] = A.ring[ring_place(p.at + (j - p.held), n)];
-                for (int j = p.want + lane; j < p.held; j += 32) A.ring[(p.to + (j - p.want)) % n] = row[j];
+                // (four reads on their way before the first write: an ended request gives hundreds of pages back)
+                for (int j0 = p.held + lane; j0 < p.want; j0 += 128) {
+                    int x[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) x[k] = j0 + 32 * k < p.want ? A.ring[ring_place(p.at + (j0 + 32 * k - p.held), n)] : 0;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) if (j0 + 32 * k < p.want) row[j0 + 32 * k] = x[k];
+                }
+                for (int j0 = p.want + lane; j0 < p.held; j0 += 128) {
+                    int x[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) x[k] = j0 + 32 * k < p.held ? row[j0 + 32 * k] : 0;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const unsigned to = ring_place(p.to + (j0 + 32 * k - p.want), n);
+                        if (j0 + 32 * k < p.held) A.ring[to < n ? to : to % n] = x[k];      // (the remainder: more than the ring can hold)
+                    }
+                }
             }
             if (A.slots == nullptr) continue;
             int *out = A.slots + (int64_t)(u0 + i) * A.T;
