@@ -1559,7 +1559,10 @@ flowmm_status launch_cache_attention_tc(const flowmm_cache_params &p, const page
     launch(kernel, (unsigned)c.blocks, paged::ptc::kThreads, paged::ptc::kSmemBytes, st, kmap, vmap, a);
     FLOWMM_LAUNCHED("cache_attention_tc");
     if (!c.joins) return FLOWMM_OK;
-    launch(paged::ptc::cache_join_kernel, (unsigned)c.blocks, 256, 0, st, a);
+    if ((int64_t)p.n_units * p.n_kv_heads <= paged::ptc::kFewHeads)
+        launch(paged::ptc::cache_join_kernel<4>, dim3((unsigned)c.blocks, (a.G + 1) / 2), paged::ptc::kJoinThreads, 0, st, a);
+    else
+        launch(paged::ptc::cache_join_kernel<1>, (unsigned)c.blocks, paged::ptc::kJoinThreads, 0, st, a);
     FLOWMM_LAUNCHED("cache_join");
     return FLOWMM_OK;
 }

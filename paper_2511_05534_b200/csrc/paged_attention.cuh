@@ -131,42 +131,61 @@ __device__ __forceinline__ bool take_ticket(unsigned long long *ticket, unsigned
 // A range's record: its G heads' outputs, relative to the maximum, then the maxima (log2) and the sums of weights.
 template <int D> __device__ __forceinline__ int record_floats(int G) { return (G * (D + 2) + 3) & ~3; }
 
-// Joins the records of one head group's ranges, `step` floats apart (the first one `ahead` floats behind its place), in the ranges' order: a warp per query head, four or two dims a
-// lane.  The ranges' maxima and sums are read by the lanes, all of 32 ranges at once, the outputs sixteen ranges at a time.
-template <int kThreads, int D>
-__device__ __forceinline__ void join_ranges(const float *rec, int64_t ahead, int64_t step, int n, int G, float *out) {
+// A warp's part of joining one query head: records first, first + stride, ... below n of its ranges, `step` floats apart (the first range's
+// `ahead` floats behind its place), relative to the largest of their maxima.  The maxima and sums are read 32 at once, the outputs eight.
+template <int D> struct Joined { float top, sum, o[D / 32]; };
+template <int D>
+__device__ __forceinline__ Joined<D> join_part(const float *rec, int64_t ahead, int64_t step, int first, int stride, int n, int G, int g) {
     constexpr int V = D / 32;
-    const int lane = lane_id();
-    for (int g = threadIdx.x >> 5; g < G; g += kThreads / 32) {
-        const float *top = rec + G * D + g;
-        float mx = kLowest, l = 0.f, o[V];
+    const int lane = lane_id(), count = first < n ? (n - first + stride - 1) / stride : 0;
+    auto record = [&](int i) { const int s = first + i * stride; return rec + s * step + (s == 0 ? ahead : 0); };
+    Joined<D> j;
+    j.top = kLowest;
+    j.sum = 0.f;
 #pragma unroll
-        for (int i = 0; i < V; ++i) o[i] = 0.f;
-        for (int s = lane; s < n; s += 32) mx = fmaxf(mx, __ldcg(top + s * step + (s == 0 ? ahead : 0)));
+    for (int i = 0; i < V; ++i) j.o[i] = 0.f;
+    for (int i = lane; i < count; i += 32) j.top = fmaxf(j.top, __ldcg(record(i) + G * D + g));
 #pragma unroll
-        for (int i = 16; i > 0; i >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, i));
-        for (int s0 = 0; s0 < n; s0 += 32) {
-            const bool on = s0 + lane < n;
-            const float *mine = top + (s0 + lane) * step + (s0 + lane == 0 ? ahead : 0);
-            const float w = on ? tc::ex2(__ldcg(mine) - mx) : 0.f;
-            if (on) l = fmaf(__ldcg(mine + G), w, l);
-            const int end = min(32, n - s0);
-            const float *at = rec + s0 * step + g * D + lane * V;
-#pragma unroll 16
-            for (int s = 0; s < end; ++s) {
-                const float c = __shfl_sync(0xFFFFFFFFu, w, s);
+    for (int i = 16; i > 0; i >>= 1) j.top = fmaxf(j.top, __shfl_xor_sync(0xFFFFFFFFu, j.top, i));
+    for (int i0 = 0; i0 < count; i0 += 32) {
+        const bool on = i0 + lane < count;
+        const float w = on ? tc::ex2(__ldcg(record(i0 + lane) + G * D + g) - j.top) : 0.f;
+        if (on) j.sum = fmaf(__ldcg(record(i0 + lane) + G * D + G + g), w, j.sum);
+        for (int i1 = i0; i1 < min(count, i0 + 32); i1 += 8) {
+            float x[8][V];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {                             // (places past the last range: the last one again, with a weight of zero)
+                const float *at = record(min(i1 + i, count - 1)) + g * D + lane * V;
                 if (V == 4) {
-                    const float4 x = __ldcg(reinterpret_cast<const float4 *>(at + s * step + (s0 + s == 0 ? ahead : 0)));
-                    o[0] = fmaf(x.x, c, o[0]); o[1] = fmaf(x.y, c, o[1]); o[2] = fmaf(x.z, c, o[2]); o[3] = fmaf(x.w, c, o[3]);
+                    const float4 v = __ldcg(reinterpret_cast<const float4 *>(at));
+                    x[i][0] = v.x; x[i][1] = v.y; x[i][V - 2] = v.z; x[i][V - 1] = v.w;
                 } else {
-                    const float2 x = __ldcg(reinterpret_cast<const float2 *>(at + s * step + (s0 + s == 0 ? ahead : 0)));
-                    o[0] = fmaf(x.x, c, o[0]); o[1] = fmaf(x.y, c, o[1]);
+                    const float2 v = __ldcg(reinterpret_cast<const float2 *>(at));
+                    x[i][0] = v.x; x[i][1] = v.y;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float c = __shfl_sync(0xFFFFFFFFu, w, (i1 - i0 + i) & 31);
+                if (i1 + i < count) {
+#pragma unroll
+                    for (int k = 0; k < V; ++k) j.o[k] = fmaf(x[i][k], c, j.o[k]);
                 }
             }
         }
-        l = warp_sum(l);
+    }
+    j.sum = warp_sum(j.sum);
+    return j;
+}
+
+// Joins the records of one head group's ranges in an order that goes by their number alone: a warp per query head.
+template <int kThreads, int D>
+__device__ __forceinline__ void join_ranges(const float *rec, int64_t step, int n, int G, float *out) {
+    constexpr int V = D / 32;
+    for (int g = threadIdx.x >> 5; g < G; g += kThreads / 32) {
+        const Joined<D> j = join_part<D>(rec, 0, step, 0, 1, n, G, g);
 #pragma unroll
-        for (int i = 0; i < V; ++i) out[g * D + lane * V + i] = o[i] / l;
+        for (int i = 0; i < V; ++i) out[g * D + lane_id() * V + i] = j.o[i] / j.sum;
     }
 }
 
@@ -316,7 +335,7 @@ __global__ void __launch_bounds__(kSimtThreads) cache_attention_kernel(const Att
     }
     __syncthreads();
     if (!last) return;
-    join_ranges<kSimtThreads, D>(A.part + ((int64_t)blockIdx.x - (int64_t)r.split * heads) * record, 0, (int64_t)heads * record, r.n_split, G, out);
+    join_ranges<kSimtThreads, D>(A.part + ((int64_t)blockIdx.x - (int64_t)r.split * heads) * record, (int64_t)heads * record, r.n_split, G, out);
 }
 
 }  // namespace paged

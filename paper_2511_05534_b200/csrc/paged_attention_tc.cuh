@@ -9,10 +9,12 @@
 // The pages' scales join in fp32: K's on the logits; V's in the exponent of the weights, w_j = 2^(z_j + log2 sv_j - max), with a maximum of
 // its own, so that the largest weight is 1 whatever the scales are.  The sum of the softmax, sum_j 2^(z_j - max z), is apart.
 //
-// How the work is shared out over the blocks of the launch, two to an SM, is found on the device, where alone the lengths are known.
-// The tiles of 128 keys of all heads stand in a row, by unit, head and key, and every block takes an equal piece of the row.  A head
+// How the work is shared out over the blocks of the launch, two to an SM, is found on the device, where alone the lengths are known (Cut).
+// With few tiles to a block each has one range of one head, all of the same length but for a head's last one.  With many, the tiles of 128
+// keys of all heads stand in a row, by unit, head and key, and every block takes an equal piece of the row, parts of heads or several, one
+// after the other.  A head
 // that several blocks have part in leaves a record for each, and cache_join_kernel joins them in order.  (Ranges of equal
-// length of each head by itself, a block each, left a last round half empty, 16 sequences of up to 33 792 rows, 8 heads, 174 us; this way 120.  Three
+// length of each head by itself, a block each, left a last round half empty, 16 sequences of up to 33 792 rows, 8 heads, 174 us; as pieces 118.  Three
 // quarters of a piece to each block and the rest drawn from a counter in pieces of three tiles and more: 132.)
 // A block goes through its tiles in groups of up to
 // seven of one head, the roles of its warps one or two groups apart, across the heads' borders too:
@@ -112,7 +114,9 @@ __device__ __forceinline__ int tiles_of(int rows) { return (rows + kTile - 1) / 
 struct Cut {
     int each, u0, u1;                    // this lane's units
     uint32_t mine, upto;                 // their tiles, of one head; with all units before
-    uint32_t all, share;                 // tiles of all heads; of a block's piece, or 0: blocks have whole heads
+    uint32_t all, share;                 // tiles of all heads; of a block's piece, or 0:
+    uint32_t per;                        // tiles of a range, or 0: blocks have one whole head or two
+    uint32_t ranges, ranges_upto;        // ranges of a head of each of this lane's units; with all units before
     uint32_t sorted0, sorted1;           // whole heads, more than blocks: the units by falling length, those in places `lane` and 32 + lane: tiles * 64 + unit
 };
 constexpr int kMostSorted = 64;
@@ -121,9 +125,13 @@ __device__ __forceinline__ uint32_t sorted_unit(const Cut &c, uint32_t r) {
     const uint32_t a = __shfl_sync(0xFFFFFFFFu, c.sorted0, r & 31), b = __shfl_sync(0xFFFFFFFFu, c.sorted1, r & 31);
     return r < 32 ? a : b;
 }
-// Where whole heads make the longest piece no more than kJoinTiles longer than an even one, heads are not cut: joining costs that much.
-// With at most as many heads as blocks each has one; up to twice as many, of at most 64 units, a block has the i-th longest and the i-th last
+// Heads are not cut for a range kJoinTiles longer: joining costs that much.  With at most as many heads as blocks, ranges of a head each,
+// unless they become kSwitchTiles longer than an even piece: the way from one head to the next costs 3 us where a block has few tiles (one
+// sequence of 1100 rows, 4 heads: 10.4 us by ranges, 13.9 by pieces of two tiles of one head or of two).  At most 32 ranges of a head, which one round of the joining
+// kernel's lanes takes (8448 rows, 4 heads: 66 ranges 15.5 us, 22 13.1).
+// With up to twice as many heads as blocks, of at most 64 units, a block has the i-th longest and the i-th last
 // (64 units of up to 1690 rows, 512 heads: 41 us cut, 36 so).
+constexpr int kSwitchTiles = 4;
 __device__ __forceinline__ Cut make_cut(const AttnArgs &A) {
     Cut c;
     const int lane = lane_id();
@@ -149,9 +157,33 @@ __device__ __forceinline__ Cut make_cut(const AttnArgs &A) {
     c.all = __shfl_sync(0xFFFFFFFFu, c.upto, 31) * A.Hkv;
     c.share = (c.all + blocks - 1) / blocks;
     c.sorted0 = c.sorted1 = 0;
+    c.per = c.ranges = c.ranges_upto = 0;
     const uint32_t most = c.share + kJoinTiles;
-    if (heads > 2 * blocks || (heads > blocks && A.U > kMostSorted) || longest > most) return c;
-    if (heads > blocks) {
+    if (heads <= blocks) {
+        auto count = [&](uint32_t per) {                              // ranges of a head of each unit, by lane
+            uint32_t n = 0;
+#pragma unroll 2
+            for (int u = c.u0; u < c.u1; ++u) n += ((uint32_t)tiles_of(unit_rows(A, u)) + per - 1) / per;
+            return n;
+        };
+        for (uint32_t per = max(max(1u, c.share), (uint32_t)(longest + 31) / 32); per <= c.share + kSwitchTiles || per + kJoinTiles >= (uint32_t)longest; ++per) {
+            if (per + kJoinTiles >= (uint32_t)longest) per = max(1, longest);
+            c.ranges = count(per);
+            if (__reduce_add_sync(0xFFFFFFFFu, c.ranges) * A.Hkv > blocks) continue;
+            c.ranges_upto = c.ranges;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const uint32_t x = __shfl_up_sync(0xFFFFFFFFu, c.ranges_upto, o);
+                if (lane >= o) c.ranges_upto += x;
+            }
+            c.per = per;
+            c.share = 0;
+            break;
+        }
+        return c;
+    }
+    if (heads > 2 * blocks || A.U > kMostSorted || longest > most) return c;
+    {
         // units by length: a unit's place is the number of longer ones, or as long ones before it
         uint32_t mine[2], place[2] = {0, 0};
 #pragma unroll
@@ -218,6 +250,33 @@ __device__ __forceinline__ void walk_to(const AttnArgs &A, const Cut &c, uint32_
     w.end = end;
     w.t1 = min(w.tiles, w.t0 + (int)(end - x));
 }
+// The block's range; false where there is none.  Ranges are numbered by unit, head and key.
+__device__ __forceinline__ bool walk_range(const AttnArgs &A, const Cut &c, Walk &w) {
+    const uint32_t H = A.Hkv, i = blockIdx.x, hit = __ballot_sync(0xFFFFFFFFu, i < c.ranges_upto * H);
+    if (hit == 0) return false;
+    const int owner = __ffs(hit) - 1;
+    int u = 0;
+    uint32_t base = 0, n = 0;                                         // ranges of all heads of the units before; of one of this unit's
+    if (lane_id() == owner) {
+        base = (c.ranges_upto - c.ranges) * H;
+        for (u = c.u0; u < c.u1; ++u) {
+            n = ((uint32_t)tiles_of(unit_rows(A, u)) + c.per - 1) / c.per;
+            if (i < base + n * H) break;
+            base += n * H;
+        }
+    }
+    w.u = __shfl_sync(0xFFFFFFFFu, u, owner);
+    n = __shfl_sync(0xFFFFFFFFu, n, owner);
+    const uint32_t in = i - __shfl_sync(0xFFFFFFFFu, base, owner);
+    w.h = in / n;
+    w.rows = unit_rows(A, w.u);
+    w.tiles = tiles_of(w.rows);
+    w.t0 = (in - w.h * n) * c.per;
+    w.t1 = min(w.tiles, w.t0 + (int)c.per);
+    w.x = w.head = 0;
+    w.end = w.t1 - w.t0;
+    return true;
+}
 // Whole heads: the block's first or second one.
 __device__ __forceinline__ bool walk_head(const AttnArgs &A, const Cut &c, int second, Walk &w) {
     const uint32_t blocks = gridDim.x, heads = (uint32_t)A.U * A.Hkv, i = second ? 2 * blocks - 1 - blockIdx.x : blockIdx.x;
@@ -234,7 +293,7 @@ __device__ __forceinline__ bool walk_head(const AttnArgs &A, const Cut &c, int s
 }
 // The block's piece; false where there is none.
 __device__ __forceinline__ bool walk_piece(const AttnArgs &A, const Cut &c, Walk &w) {
-    if (c.share == 0) return walk_head(A, c, 0, w);
+    if (c.share == 0) return c.per != 0 ? walk_range(A, c, w) : walk_head(A, c, 0, w);
     const uint32_t x = blockIdx.x * c.share;
     if (x >= c.all) return false;
     walk_to(A, c, x, min(c.all, x + c.share), w);
@@ -387,7 +446,8 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
             g.is.n = min(kGroup, w.t1 - t); g.is.t = t; g.is.rows = w.rows; g.is.u = w.u; g.is.h = w.h;
             g.is.first = t == w.t0; g.is.last = t + g.is.n == w.t1;
             g.is.record = w.t0 == 0 && w.t1 == w.tiles ? -1 : 2 * (int)blockIdx.x + (w.t0 == 0);
-            if (w.t0 == 0 && w.t1 < w.tiles) cut_head = make_int4(w.u, w.h, (int)((w.head + w.tiles - 1) / cut.share - blockIdx.x + 1), 0);
+            if (w.t0 == 0 && w.t1 < w.tiles) cut_head = make_int4(w.u, w.h, 
+                cut.share == 0 ? (w.tiles + (int)cut.per - 1) / (int)cut.per : (int)((w.head + w.tiles - 1) / cut.share - blockIdx.x + 1), 0);
             numbers(g.is, g.p);
         };
         bool ok = true, more = walk_piece(A, cut, w);
@@ -415,7 +475,7 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
                 set(next, now.is.t + now.is.n);
             } else {
                 more = walk_next(A, w);
-                if (!more && cut.share == 0 && !second) more = walk_head(A, cut, second = 1, w);
+                if (!more && cut.share == 0 && cut.per == 0 && !second) more = walk_head(A, cut, second = 1, w);
                 if (more) {
                     set(next, w.t0);
 #pragma unroll
@@ -721,16 +781,43 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
     if (threadIdx.x == 0 && *abort_flag != 0) report(A.status, *cta_status);
 }
 
-// Joins the heads that were cut: a block for every block that a cut head begins in, a warp for each of its query heads.
-__global__ void __launch_bounds__(256) cache_join_kernel(const AttnArgs A) {
+// Joins the heads that were cut: a block for every block that such a head can begin in, kWarps warps for each of its query heads, with every
+// kWarps-th record each.  Four where heads are few, and so cut into many ranges (a sequence of 8448 rows, 4 heads, 66 records of each: 28 us for the
+// call with one, 15 so), else one, which makes the blocks that find nothing to do fewer (16 of up to 33 792, 8 heads: 122 us with four, 118 so).
+constexpr int kJoinThreads = 256, kFewHeads = 74;
+template <int kWarps>
+__global__ void __launch_bounds__(kJoinThreads) cache_join_kernel(const AttnArgs A) {
+    constexpr int kTeams = kJoinThreads / 32 / kWarps;
     predecessor_done();
     successor_may_start();
     const int4 head = A.cut_heads[blockIdx.x];
-    if (head.z == 0) return;
-    const int record = record_floats<128>(A.G);
+    const int lane = lane_id(), team = (threadIdx.x >> 5) / kWarps, p = (threadIdx.x >> 5) % kWarps, record = record_floats<128>(A.G);
+    const int g = blockIdx.y * kTeams + team;
+    if (head.z == 0 || g >= A.G) return;                              // (whole teams)
     // (the first block's record is that of its last head, in the second place; the others' are those of their first heads)
-    join_ranges<256, 128>(A.part + (int64_t)2 * blockIdx.x * record, record, (int64_t)2 * record, head.z, A.G,
-                          A.out + ((int64_t)head.x * A.Hq + head.y * A.G) * 128);
+    const Joined<128> j = join_part<128>(A.part + (int64_t)2 * blockIdx.x * record, record, (int64_t)2 * record, p, kWarps, head.z, A.G, g);
+    float *out = A.out + ((int64_t)head.x * A.Hq + head.y * A.G + g) * 128;
+    if constexpr (kWarps == 1) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) out[lane * 4 + i] = j.o[i] / j.sum;
+    } else {
+        __shared__ float parts[kTeams][kWarps][128], tops[kTeams][kWarps], sums[kTeams][kWarps];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) parts[team][p][lane * 4 + i] = j.o[i];
+        if (lane == 0) { tops[team][p] = j.top; sums[team][p] = j.sum; }
+        asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "n"(kWarps * 32) : "memory");
+        float top = kLowest, sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < kWarps; ++i) top = fmaxf(top, tops[team][i]);
+#pragma unroll
+        for (int i = 0; i < kWarps; ++i) sum = fmaf(sums[team][i], tc::ex2(tops[team][i] - top), sum);
+        for (int d = p * 32 + lane; d < 128; d += kWarps * 32) {
+            float o = 0.f;
+#pragma unroll
+            for (int i = 0; i < kWarps; ++i) o = fmaf(parts[team][i][d], tc::ex2(tops[team][i] - top), o);
+            out[d] = o / sum;
+        }
+    }
 }
 
 }  // namespace ptc

@@ -286,6 +286,88 @@ def test_attention_of_long_and_many_units(path, D):
     _check(T.params(40, 14, 2, D, 128, 1, 1, path=path), rng, rng.integers(0, 2000, 40), 128, wide=64)
 
 
+@pytest.mark.parametrize("U,Hq,Hkv,lengths", [
+    (1, 8, 2, [1700]),                                  # few heads: ranges, a few a head
+    (1, 7, 1, [40000]),                                 # ... thirty and more
+    (3, 64, 8, [129, 4000, 1]), (30, 28, 4, None), (7, 5, 5, None),
+    (37, 32, 8, None), (38, 8, 8, None), (64, 64, 8, None), (64, 9, 9, None), (60, 16, 8, [0, 1700, 0, 900]),   # about and above 296 heads, up to 592: pairs
+    (64, 8, 8, [1700]), (48, 8, 8, [5000] + [100] * 47),                                    # ... which would be uneven: pieces
+    (70, 16, 8, None), (75, 64, 8, [1, 0, 300]), (300, 1, 1, [30000] + [20] * 299)])        # many: pieces, some of a hundred to a head
+def test_every_way_to_share_the_work_out(U, Hq, Hkv, lengths):
+    rng = np.random.default_rng(U + Hq)
+    rows = rng.integers(0, 1800, U) if lengths is None else np.array([lengths[u % len(lengths)] for u in range(U)])
+    _check(T.params(U, Hq, Hkv, 128, 64, 1, 1), rng, rows, 64)
+
+
+def test_queries_of_one_sequence_share_its_pages():
+    """Several new tokens of a sequence: units with the same row of the block table, each one row longer than the one before."""
+    rng = np.random.default_rng(2)
+    n, rows = 5, np.array([700])
+    table, n_pages = T.random_table(rng, rows, 64)
+    codes_k, ks = T.random_pool(rng, n_pages, 2, 64, 128, rows, table, (-9, -6))
+    codes_v, vs = T.random_pool(rng, n_pages, 2, 64, 128, rows, table)
+    tables, lens = np.repeat(table, n, 0), rows[0] - n + 1 + np.arange(n)
+    q = inputs.round_to_bf16(rng.standard_normal((n, 8, 128)).astype(np.float32))
+    for path in (F.PATH_AUTO, F.PATH_SIMT):
+        got, status = T.attend(T.params(n, 8, 2, 128, 64, n_pages, table.shape[1], path=path), q, codes_k, codes_v, ks, vs, tables, lens)
+        want, size, logits = P.attention(q, P.E4M3[codes_k], P.E4M3[codes_v], ks, vs, tables, lens)
+        assert status == 0
+        for u in range(n):
+            assert (np.abs(got[u] - want[u]) <= T.attention_bound(size[u], logits[u], int(lens[u]), 128)).all()
+
+
+class Guarded:
+    """A tensor between two margins that must keep their bytes."""
+
+    def __init__(self, t):
+        n = t.numel() * t.element_size()
+        self.raw = torch.full((4096 + n + 4096,), 0xA5, dtype=torch.uint8, device="cuda")
+        self.t = self.raw[4096:4096 + n].view(t.dtype).view(t.shape)
+        self.t.copy_(t)
+
+    def intact(self):
+        return bool((self.raw[:4096] == 0xA5).all() and (self.raw[4096 + self.t.numel() * self.t.element_size():] == 0xA5).all())
+
+
+@pytest.mark.parametrize("D,dtype,path", [(128, F.BF16, F.PATH_AUTO), (128, F.BF16, F.PATH_SIMT), (64, F.F32, F.PATH_AUTO)])
+def test_nothing_is_written_beside_the_outputs(D, dtype, path):
+    """Every array of the four calls, and a workspace of exactly the size that is asked for, between guards; inputs keep their bytes."""
+    rng = np.random.default_rng(D + path)
+    U, Hq, H, page, n = 9, 21, 3, 32, 77
+    rows = np.array([0, 5, 1000, 31, 32, 33, 400, 77, 2000])
+    table, n_pages = T.random_table(rng, rows + n, page, spare=50)
+    p = T.params(U, Hq, H, D, page, n_pages, table.shape[1], n, dtype, path=path)
+    guards = {}
+
+    def guard(name, t):
+        guards[name] = Guarded(t)
+        return guards[name].t
+    ws = guard("ws", F.alloc_cache_workspace(p))
+    pool = [guard("pool%d" % i, T.dev(x)) for i, x in enumerate((*(T.random_pool(rng, n_pages, H, page, D, rows, table)[0] for _ in "kv"),
+                                                                 *(np.ones((n_pages, H), np.float32) for _ in "kv")))]
+    i32 = lambda x: T.dev(np.asarray(x, np.int32))
+    ring = guard("ring", i32(np.full(n_pages, 3)))
+    fresh = {"rows": guard("rows", i32(rows)), "grow": guard("grow", i32(np.full(U, n))), "state": guard("state", i32([0, 40]))}
+    table_d, slots = guard("table", i32(np.where(table < n_pages, table, 0))), guard("slots", i32(np.zeros((U, n))))
+    keep = {k: t.clone() for k, t in fresh.items()}
+    rows_out, state_out = guard("rows_out", i32(np.zeros(U))), guard("state_out", i32([0, 0]))
+    F.flowmm_cache_plan(p, fresh["grow"], fresh["rows"], rows_out, ring, fresh["state"], state_out, table_d, slots, ws)
+    assert F.flowmm_last_device_status(ws) in (0, 11)
+    pos = rows[:, None] + np.arange(n)
+    slots.copy_(i32(np.take_along_axis(table, pos // page, 1) * page + pos % page))
+    table_d.copy_(i32(np.where(table < n_pages, table, 0)))
+    tdt = F.torch_dtype(dtype)
+    k, v = guard("k", torch.randn(U, H, n, D, device="cuda", dtype=tdt)), guard("v", torch.randn(U, H, n, D, device="cuda", dtype=tdt))
+    q, out = guard("q", torch.randn(U, Hq, D, device="cuda", dtype=tdt)), guard("out", torch.zeros(U, Hq, D, device="cuda"))
+    F.flowmm_cache_store(p, k, v, slots, *pool, ws)
+    held = i32(rows + n)
+    F.flowmm_cache_attention(p, q, *pool, table_d, held, out, ws)
+    F.flowmm_cache_load(p, *pool, table_d, held, k, v, ws)
+    assert F.flowmm_last_device_status(ws) == 0 and torch.isfinite(out).all()
+    assert all(g.intact() for g in guards.values()), [name for name, g in guards.items() if not g.intact()]
+    assert all(torch.equal(t, fresh[k]) for k, t in keep.items())
+
+
 @pytest.mark.parametrize("path", [F.PATH_AUTO, F.PATH_SIMT])
 def test_sharp_and_flat_softmax_and_scales_far_apart(path):
     rng = np.random.default_rng(17 + path)
