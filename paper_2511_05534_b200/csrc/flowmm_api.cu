@@ -1472,10 +1472,10 @@ flowmm_status validate_cache(const flowmm_cache_params *p) {
 
 int page_shift(int page) { return page == 16 ? 4 : page == 32 ? 5 : page == 64 ? 6 : 7; }
 
-// The attention's cut and scratch: [status word, 256 bytes][tickets or cut heads][records].
+// The attention's cut and scratch: [status word, 256 bytes][cut heads][records].
 struct CachePlan {
     bool tc;                       // the tensor-core kernel (bf16 queries, heads of 128) or the SIMT one
-    bool joins;                    // tensor cores: a head may be cut
+    bool joins;                    // a head may be cut
     int groups, gp, target;        // groups of query heads that are ranges of their own, heads of one, ranges aimed at
     int64_t blocks;                // of the launch: no fewer than ranges can come out (paged_attention.cuh)
     size_t part, total;            // where the records start; bytes
@@ -1485,18 +1485,17 @@ CachePlan cache_plan(const flowmm_cache_params &p, int path) {
     CachePlan c;
     const int G = p.n_q_heads / p.n_kv_heads;
     c.tc = p.dtype == FLOWMM_BF16 && p.head_dim == 128 && path != FLOWMM_PATH_SIMT;
-    c.gp = c.tc ? G : G <= 1 ? 1 : G <= 2 ? 2 : 4;
+    c.gp = c.tc ? G : std::min(G, 2);
     c.groups = (G + c.gp - 1) / c.gp;
     c.target = (c.tc ? 2 : 4) * kScoreCtas;
     const int64_t heads = (int64_t)p.n_units * p.n_kv_heads * c.groups, keys = (int64_t)p.max_pages * p.page_size;
-    // tensor cores: two records and the note of a cut head for each block; SIMT: a block and a record for each range, a ticket for each head
-    const int64_t tiles = (keys + paged::ptc::kTile - 1) / paged::ptc::kTile;
-    c.joins = c.tc && !(heads <= c.target && tiles <= paged::kJoinTiles + 1);
-    if (c.tc) c.blocks = std::min<int64_t>(heads * tiles, c.target);
-    else c.blocks = std::min(heads * ((keys + paged::kSimtKeys - 1) / paged::kSimtKeys), c.target + heads);
-    c.part = 256 + align256(c.tc ? (size_t)c.blocks * sizeof(int4) : (size_t)heads * sizeof(unsigned long long));
-    const int64_t records = !c.tc ? c.blocks : c.joins ? 2 * c.blocks : 0;
-    c.total = c.part + align256((size_t)records * ((c.gp * (p.head_dim + 2) + 3) & ~3) * sizeof(float));
+    // tensor cores: two records for each block; SIMT: a block and a record for each range.  A note of what is cut for each block.
+    const int tile = c.tc ? paged::ptc::kTile : paged::kSimtKeys;
+    const int64_t tiles = (keys + tile - 1) / tile;
+    c.joins = !((!c.tc || heads <= c.target) && tiles <= paged::kJoinTiles + 1);
+    c.blocks = std::min(heads * tiles, c.tc ? (int64_t)c.target : c.target + heads);
+    c.part = 256 + (c.joins ? align256((size_t)c.blocks * sizeof(int4)) : 0);
+    c.total = c.part + (c.joins ? align256((size_t)c.blocks * (c.tc ? 2 : 1) * paged::record_floats(c.gp, p.head_dim) * sizeof(float)) : 0);
     return c;
 }
 
@@ -1546,6 +1545,18 @@ flowmm_status run_load(const flowmm_cache_params &p, const paged::LoadArgs &a, i
     return FLOWMM_OK;
 }
 
+template <int D>
+flowmm_status launch_cache_join(const paged::AttnArgs &a, const CachePlan &c, int heads, int own, int first, int step, cudaStream_t st) {
+    if (!c.joins) return FLOWMM_OK;
+    const int record = paged::record_floats(c.gp, D);
+    if (heads <= paged::kFewHeads)
+        launch(paged::cache_join_kernel<D, 4>, dim3((unsigned)c.blocks, (c.gp + 1) / 2), paged::kJoinThreads, 0, st, a, record, own, first, step);
+    else
+        launch(paged::cache_join_kernel<D, 1>, (unsigned)c.blocks, paged::kJoinThreads, 0, st, a, record, own, first, step);
+    FLOWMM_LAUNCHED("cache_join");
+    return FLOWMM_OK;
+}
+
 flowmm_status launch_cache_attention_tc(const flowmm_cache_params &p, const paged::AttnArgs &a, const CachePlan &c, cudaStream_t st) {
     CUtensorMap kmap, vmap;
     const uint64_t head = (uint64_t)p.page_size * 128, dims[4] = {128, (uint64_t)p.page_size, (uint64_t)p.n_kv_heads, (uint64_t)p.n_pages};
@@ -1558,25 +1569,17 @@ flowmm_status launch_cache_attention_tc(const flowmm_cache_params &p, const page
         return FLOWMM_ERR_CUDA;
     launch(kernel, (unsigned)c.blocks, paged::ptc::kThreads, paged::ptc::kSmemBytes, st, kmap, vmap, a);
     FLOWMM_LAUNCHED("cache_attention_tc");
-    if (!c.joins) return FLOWMM_OK;
-    if ((int64_t)p.n_units * p.n_kv_heads <= paged::ptc::kFewHeads)
-        launch(paged::ptc::cache_join_kernel<4>, dim3((unsigned)c.blocks, (a.G + 1) / 2), paged::ptc::kJoinThreads, 0, st, a);
-    else
-        launch(paged::ptc::cache_join_kernel<1>, (unsigned)c.blocks, paged::ptc::kJoinThreads, 0, st, a);
-    FLOWMM_LAUNCHED("cache_join");
-    return FLOWMM_OK;
+    // (the first part of a head is its block's last one, in the second of the block's records; the others are their blocks' first)
+    return launch_cache_join<128>(a, c, p.n_units * p.n_kv_heads, 2, 1, 2, st);
 }
 
 template <int D>
 flowmm_status launch_cache_attention(const paged::AttnArgs &a, const CachePlan &c, cudaStream_t st) {
     const unsigned blocks = (unsigned)c.blocks;
-    switch (c.gp) {
-        case 1: launch(paged::cache_attention_kernel<D, 1>, blocks, paged::kSimtThreads, 0, st, a); break;
-        case 2: launch(paged::cache_attention_kernel<D, 2>, blocks, paged::kSimtThreads, 0, st, a); break;
-        default: launch(paged::cache_attention_kernel<D, 4>, blocks, paged::kSimtThreads, 0, st, a); break;
-    }
+    launch(c.gp == 1 ? paged::cache_attention_kernel<D, 1> : paged::cache_attention_kernel<D, 2>, blocks, paged::kSimtThreads, 0, st, a);
     FLOWMM_LAUNCHED("cache_attention");
-    return FLOWMM_OK;
+    const int heads = a.Hkv * a.groups;                              // (ranges of a head are so many blocks apart)
+    return launch_cache_join<D>(a, c, a.U * heads, 1, 0, heads, st);
 }
 
 }  // namespace
@@ -1688,8 +1691,7 @@ extern "C" flowmm_status flowmm_cache_attention(const flowmm_cache_params *p, co
     paged::AttnArgs a;
     a.q = q; a.k = static_cast<const uint8_t *>(k_pages); a.v = static_cast<const uint8_t *>(v_pages);
     a.k_scale = k_scale; a.v_scale = v_scale; a.table = block_table; a.rows = rows; a.out = out;
-    a.ticket = at<unsigned long long>(ws, 256); a.part = at<float>(ws, c.part); a.status = static_cast<int *>(ws); a.cut_heads = c.joins ? at<int4>(ws, 256) : nullptr;
-    a.call = status_call_number();
+    a.part = at<float>(ws, c.part); a.status = static_cast<int *>(ws); a.cut_heads = c.joins ? at<int4>(ws, 256) : nullptr;
     a.U = p->n_units; a.Hq = p->n_q_heads; a.Hkv = p->n_kv_heads; a.G = p->n_q_heads / p->n_kv_heads; a.groups = c.groups;
     a.page = p->page_size; a.page_shift = page_shift(p->page_size); a.n_pages = p->n_pages; a.max_pages = p->max_pages;
     a.q_bf16 = p->dtype == FLOWMM_BF16; a.target = c.target; a.by_heads = make_fastdiv(p->n_kv_heads * c.groups);

@@ -1,7 +1,7 @@
 // Decode attention over the paged 8-bit cache: one new query per query head, lengths of their own for every unit.
 //   o = sum_j softmax_j(scale * q . (sk_j k_j)) (sv_j v_j),   k_j, v_j: e4m3 codes, sk_j, sv_j: their page's scales
-// This file: how a call is cut into ranges of keys on the device, where alone the lengths are known, how the ranges of a head are
-// joined, and the SIMT kernel (fp32 queries, heads of 64).
+// This file: how the SIMT kernel's work is cut into ranges of keys on the device, where alone the lengths are known, the kernel that joins
+// ranges, and the SIMT kernel (fp32 queries, heads of 64).
 #pragma once
 #include "common.cuh"
 #include "paged_cache.cuh"
@@ -17,10 +17,9 @@ struct AttnArgs {
     const int *table, *rows;           // [U, max_pages], [U]
     float *out;                        // [U, Hq, D]
     float *part;                       // [blocks] records (record_floats)
-    unsigned long long *ticket;        // [U * Hkv * groups]: (call, ranges done)
     int *status;
-    int4 *cut_heads;                   // [blocks] heads to be joined (tensor cores); null: none can be
-    uint32_t call;
+    int4 *cut_heads;                   // [blocks]: unit, first query head, number of records (0: nothing) and query heads of what begins in the
+                                       // block and is to be joined; null: nothing can be
     int U, Hq, Hkv, G, groups, page, page_shift, n_pages, max_pages, q_bf16;
     int target;                        // ranges in all that the call is cut into, about
     FastDiv by_heads;                  // by Hkv * groups
@@ -110,26 +109,8 @@ __device__ __forceinline__ void check_lengths(const AttnArgs &A) {
 }
 
 // ---- joining -------------------------------------------------------------------------------------
-// A block that has written its range's record takes a ticket of its head; the one that takes the last joins the records.  The
-// ticket carries the call's number, so the memory may hold anything before, and is back at zero after the last one.
-// `seen`: what the ticket was read as earlier on, to spare a read here.  One thread calls this, behind a barrier of the block.
-__device__ __forceinline__ bool take_ticket(unsigned long long *ticket, unsigned long long seen, uint32_t call, int n) {
-    __threadfence();                                                  // (the block's record, ordered before by the barrier)
-    bool last = false;
-    for (int tries = 0; tries <= n; ++tries) {                        // (a lost exchange is a read too early or another block's ticket: n at most)
-        const uint32_t done = (uint32_t)(seen >> 32) == call ? (uint32_t)seen + 1u : 1u;
-        last = done >= (uint32_t)n;
-        const unsigned long long prev = atomicCAS(ticket, seen, (unsigned long long)call << 32 | (last ? 0u : done));
-        if (prev == seen) break;
-        seen = prev;
-        last = false;
-    }
-    __threadfence();
-    return last;
-}
-
 // A range's record: its G heads' outputs, relative to the maximum, then the maxima (log2) and the sums of weights.
-template <int D> __device__ __forceinline__ int record_floats(int G) { return (G * (D + 2) + 3) & ~3; }
+__host__ __device__ __forceinline__ int record_floats(int G, int D) { return (G * (D + 2) + 3) & ~3; }
 
 // A warp's part of joining one query head: records first, first + stride, ... below n of its ranges, `step` floats apart (the first range's
 // `ahead` floats behind its place), relative to the largest of their maxima.  The maxima and sums are read 32 at once, the outputs eight.
@@ -178,14 +159,43 @@ __device__ __forceinline__ Joined<D> join_part(const float *rec, int64_t ahead, 
     return j;
 }
 
-// Joins the records of one head group's ranges in an order that goes by their number alone: a warp per query head.
-template <int kThreads, int D>
-__device__ __forceinline__ void join_ranges(const float *rec, int64_t step, int n, int G, float *out) {
-    constexpr int V = D / 32;
-    for (int g = threadIdx.x >> 5; g < G; g += kThreads / 32) {
-        const Joined<D> j = join_part<D>(rec, 0, step, 0, 1, n, G, g);
+// Joins what was cut (AttnArgs::cut_heads), in an order that goes by the ranges' number alone: a block for every block that it can begin in,
+// kWarps warps for each query head, with every kWarps-th record each.  A block of the kernel before has `own` records; the first one of a
+// join is the `first`-th of its block, the next ones are `step` records apart, counted from its block's first.
+// (By the range that ended last, which it learnt from a ticket: 35 ranges that end together drew theirs one after the other, 4 sequences of 2200 rows, 4 heads of 64,
+// 22.6 us, so 10.)  Four warps where heads are few, and so cut into many ranges (a sequence of 8448 rows, 4 heads, 66 records of each: 28 us for the
+// call with one, 15 so), else one, which makes the blocks that find nothing to do fewer (16 of up to 33 792, 8 heads: 122 us with four, 118 so).
+constexpr int kJoinThreads = 256, kFewHeads = 74;
+template <int D, int kWarps>
+__global__ void __launch_bounds__(kJoinThreads) cache_join_kernel(const AttnArgs A, const int record, const int own, const int first, const int step) {
+    constexpr int kTeams = kJoinThreads / 32 / kWarps, V = D / 32;
+    predecessor_done();
+    successor_may_start();
+    const int4 cut = A.cut_heads[blockIdx.x];
+    const int lane = lane_id(), team = (threadIdx.x >> 5) / kWarps, p = (threadIdx.x >> 5) % kWarps, g = blockIdx.y * kTeams + team, G = cut.w;
+    if (cut.z == 0 || g >= G) return;                                 // (whole teams)
+    const Joined<D> j = join_part<D>(A.part + (int64_t)blockIdx.x * own * record, (int64_t)first * record, (int64_t)step * record, p, kWarps, cut.z, G, g);
+    float *out = A.out + ((int64_t)cut.x * A.Hq + cut.y + g) * D;
+    if constexpr (kWarps == 1) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) out[g * D + lane_id() * V + i] = j.o[i] / j.sum;
+        for (int i = 0; i < V; ++i) out[lane * V + i] = j.o[i] / j.sum;
+    } else {
+        __shared__ float parts[kTeams][kWarps][D], tops[kTeams][kWarps], sums[kTeams][kWarps];
+#pragma unroll
+        for (int i = 0; i < V; ++i) parts[team][p][lane * V + i] = j.o[i];
+        if (lane == 0) { tops[team][p] = j.top; sums[team][p] = j.sum; }
+        asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "n"(kWarps * 32) : "memory");
+        float top = kLowest, sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < kWarps; ++i) top = fmaxf(top, tops[team][i]);
+#pragma unroll
+        for (int i = 0; i < kWarps; ++i) sum = fmaf(sums[team][i], tc::ex2(tops[team][i] - top), sum);
+        for (int d = p * 32 + lane; d < D; d += kWarps * 32) {
+            float o = 0.f;
+#pragma unroll
+            for (int i = 0; i < kWarps; ++i) o = fmaf(parts[team][i][d], tc::ex2(tops[team][i] - top), o);
+            out[d] = o / sum;
+        }
     }
 }
 
@@ -193,20 +203,25 @@ __device__ __forceinline__ void join_ranges(const float *rec, int64_t step, int 
 constexpr int kSimtThreads = 128, kSimtKeys = 64, kSimtPages = 256;
 
 // A group of D / 16 lanes shares a row (16 codes a lane); the groups of a block take the range's keys in turn, kStep rows each with
-// K and V on their way at once.  GP: query heads of a range, 1, 2 or 4 (more of a KV head are ranges of their own).
+// K and V on their way at once.  GP: query heads of a range, 1 or 2; more of a KV head are ranges of their own, which find its rows in L2 (four to a
+// range took 212 registers: 8 units of up to 2200 rows, 8 heads of 4 query heads 17.2 us, by two 14.2; 200 units 178 and 171).
 template <int D, int GP>
 __global__ void __launch_bounds__(kSimtThreads) cache_attention_kernel(const AttnArgs A) {
-    constexpr int kLanes = D / 16, kGroups = kSimtThreads / kLanes, kStep = 2;
+    constexpr int kLanes = D / 16, kGroups = kSimtThreads / kLanes, kStep = GP == 1 ? 4 : 2;
     __shared__ float rec[kGroups][GP][D + 2];
     __shared__ int ids[kSimtPages];
     __shared__ float ks[kSimtPages], vs[kSimtPages];
-    __shared__ int last;
     predecessor_done();
     successor_may_start();
-    Range r;
-    const int heads = A.Hkv * A.groups;
+    Range r = {};
     check_lengths(A);
-    if (!find_range<kSimtKeys>(A, blockIdx.x, r)) return;
+    const bool work = find_range<kSimtKeys>(A, blockIdx.x, r);
+    if (A.cut_heads && threadIdx.x == 0) {
+        const int g0 = (r.h % A.groups) * GP;
+        A.cut_heads[blockIdx.x] = work && r.split == 0 && r.n_split > 1 ? make_int4(r.u, r.h / A.groups * A.G + g0, r.n_split, min(GP, A.G - g0))
+                                                                         : make_int4(0, 0, 0, 0);
+    }
+    if (!work) return;
     const int tid = threadIdx.x, sub = tid % kLanes, grp = tid / kLanes;
     const int h = r.h / A.groups, g0 = (r.h % A.groups) * GP, G = min(GP, A.G - g0);
     float *out = A.out + ((int64_t)r.u * A.Hq + h * A.G + g0) * D;
@@ -309,7 +324,7 @@ __global__ void __launch_bounds__(kSimtThreads) cache_attention_kernel(const Att
         if (sub == 0) { rec[grp][g][D] = m[g]; rec[grp][g][D + 1] = l[g]; }
     }
     __syncthreads();
-    const int record = record_floats<D>(GP);
+    const int record = record_floats(GP, D);
     float *part = A.part + (int64_t)blockIdx.x * record;
     for (int i = tid; i < G * D; i += kSimtThreads) {
         const int g = i / D, d = i % D;
@@ -327,15 +342,6 @@ __global__ void __launch_bounds__(kSimtThreads) cache_attention_kernel(const Att
             if (d == 0) { part[G * D + g] = mx; part[G * D + G + g] = ls; }
         }
     }
-    if (r.n_split == 1) return;
-    __syncthreads();
-    if (tid == 0) {
-        unsigned long long *ticket = A.ticket + (int64_t)r.u * heads + r.h;
-        last = take_ticket(ticket, *reinterpret_cast<volatile unsigned long long *>(ticket), A.call, r.n_split);
-    }
-    __syncthreads();
-    if (!last) return;
-    join_ranges<kSimtThreads, D>(A.part + ((int64_t)blockIdx.x - (int64_t)r.split * heads) * record, (int64_t)heads * record, r.n_split, G, out);
 }
 
 }  // namespace paged

@@ -386,7 +386,7 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
     predecessor_done();
     successor_may_start();
 
-    const int G = A.G, tile_pages = kTile >> A.page_shift, record = record_floats<128>(G);
+    const int G = A.G, tile_pages = kTile >> A.page_shift, record = record_floats(G, 128);
     auto query = [&](int u, int h, int g) {
         return g < G ? *reinterpret_cast<const uint2 *>(static_cast<const __nv_bfloat16 *>(A.q) + ((int64_t)u * A.Hq + h * G + g) * 128 + lane * 4)
                      : make_uint2(0, 0);
@@ -441,13 +441,13 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
         if (A.cut_heads) cut = make_cut(A);
         Walk w = {};                                                 // the head of the group after `now`
         int group = 0, head = 0, second = 0;
-        int4 cut_head = make_int4(0, 0, 0, 0);                       // unit, head and number of pieces of a head that begins here and goes on in other blocks
+        int4 cut_head = make_int4(0, 0, 0, 0);                       // a head that begins here and goes on in other blocks
         auto set = [&](Group &g, int t) {
             g.is.n = min(kGroup, w.t1 - t); g.is.t = t; g.is.rows = w.rows; g.is.u = w.u; g.is.h = w.h;
             g.is.first = t == w.t0; g.is.last = t + g.is.n == w.t1;
             g.is.record = w.t0 == 0 && w.t1 == w.tiles ? -1 : 2 * (int)blockIdx.x + (w.t0 == 0);
-            if (w.t0 == 0 && w.t1 < w.tiles) cut_head = make_int4(w.u, w.h, 
-                cut.share == 0 ? (w.tiles + (int)cut.per - 1) / (int)cut.per : (int)((w.head + w.tiles - 1) / cut.share - blockIdx.x + 1), 0);
+            if (w.t0 == 0 && w.t1 < w.tiles) cut_head = make_int4(w.u, w.h * G,
+                cut.share == 0 ? (w.tiles + (int)cut.per - 1) / (int)cut.per : (int)((w.head + w.tiles - 1) / cut.share - blockIdx.x + 1), G);
             numbers(g.is, g.p);
         };
         bool ok = true, more = walk_piece(A, cut, w);
@@ -779,45 +779,6 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
     tc::tc_fence_after();
     if (warp == 1) tc::tmem_dealloc(tmem, kTmemCols);
     if (threadIdx.x == 0 && *abort_flag != 0) report(A.status, *cta_status);
-}
-
-// Joins the heads that were cut: a block for every block that such a head can begin in, kWarps warps for each of its query heads, with every
-// kWarps-th record each.  Four where heads are few, and so cut into many ranges (a sequence of 8448 rows, 4 heads, 66 records of each: 28 us for the
-// call with one, 15 so), else one, which makes the blocks that find nothing to do fewer (16 of up to 33 792, 8 heads: 122 us with four, 118 so).
-constexpr int kJoinThreads = 256, kFewHeads = 74;
-template <int kWarps>
-__global__ void __launch_bounds__(kJoinThreads) cache_join_kernel(const AttnArgs A) {
-    constexpr int kTeams = kJoinThreads / 32 / kWarps;
-    predecessor_done();
-    successor_may_start();
-    const int4 head = A.cut_heads[blockIdx.x];
-    const int lane = lane_id(), team = (threadIdx.x >> 5) / kWarps, p = (threadIdx.x >> 5) % kWarps, record = record_floats<128>(A.G);
-    const int g = blockIdx.y * kTeams + team;
-    if (head.z == 0 || g >= A.G) return;                              // (whole teams)
-    // (the first block's record is that of its last head, in the second place; the others' are those of their first heads)
-    const Joined<128> j = join_part<128>(A.part + (int64_t)2 * blockIdx.x * record, record, (int64_t)2 * record, p, kWarps, head.z, A.G, g);
-    float *out = A.out + ((int64_t)head.x * A.Hq + head.y * A.G + g) * 128;
-    if constexpr (kWarps == 1) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) out[lane * 4 + i] = j.o[i] / j.sum;
-    } else {
-        __shared__ float parts[kTeams][kWarps][128], tops[kTeams][kWarps], sums[kTeams][kWarps];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) parts[team][p][lane * 4 + i] = j.o[i];
-        if (lane == 0) { tops[team][p] = j.top; sums[team][p] = j.sum; }
-        asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "n"(kWarps * 32) : "memory");
-        float top = kLowest, sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < kWarps; ++i) top = fmaxf(top, tops[team][i]);
-#pragma unroll
-        for (int i = 0; i < kWarps; ++i) sum = fmaf(sums[team][i], tc::ex2(tops[team][i] - top), sum);
-        for (int d = p * 32 + lane; d < 128; d += kWarps * 32) {
-            float o = 0.f;
-#pragma unroll
-            for (int i = 0; i < kWarps; ++i) o = fmaf(parts[team][i][d], tc::ex2(tops[team][i] - top), o);
-            out[d] = o / sum;
-        }
-    }
 }
 
 }  // namespace ptc

@@ -624,7 +624,7 @@ def test_binding_refuses_wrong_tensors():
     with pytest.raises(ValueError):
         F.flowmm_cache_store(p, k, k[:, :, :7], i32(2, 8), *pool, ws)
     with pytest.raises(F.FlowmmError):
-        F.flowmm_cache_store(p, k, k, i32(2, 8), *pool, ws[:256])
+        F.flowmm_cache_store(p, k, k, i32(2, 8), *pool, ws[:255])
     fp8 = [t.view(torch.float8_e4m3fn) for t in pool[:2]] + pool[2:]
     F.flowmm_cache_store(p, k, k, torch.full((2, 8), -1, dtype=torch.int32, device="cuda"), *fp8, ws)
     assert F.flowmm_last_device_status(ws) == 0
