@@ -37,7 +37,7 @@ constexpr int kQCols = 2 * kMaxHeads, kPCols = 4 * kMaxHeads;            // N of
 constexpr int kMostPages = kGroup * kTile / 16;                          // pages of a group
 constexpr uint32_t kStageBytes = kTile * 128;
 constexpr int kInfos = 4;                                                // groups whose scales are kept
-constexpr uint32_t kSmemQ = kStages * kStageBytes, kSmemP = kSmemQ + 2 * kQCols * 128, kSmemRed = kSmemP + 2 * kPCols * 128;
+constexpr uint32_t kSmemQ = kStages * kStageBytes, kPBytes = kTile * kPCols, kSmemP = kSmemQ + 2 * kQCols * 128, kSmemRed = kSmemP + 2 * kPBytes;
 constexpr uint32_t kSmemInfo = kSmemRed + 2 * 8 * 3 * kHalf * 4;          // red: [group parity][warp][maxima, with V's scales, sums][head]
 constexpr int kInfo = 2 * kMostPages + kMaxHeads;                         // [K's scale, log2 of V's][page], the queries' factors
 constexpr uint32_t kSmemFirst = kSmemInfo + kInfos * kInfo * 4;           // the factors of the first head's queries
@@ -53,17 +53,21 @@ static_assert(2 * (kSmemBytes + 1024) <= 227 * 1024, "two blocks to an SM");
 
 __host__ __device__ constexpr uint32_t idesc_e4m3(uint32_t M, uint32_t N) { return (1u << 4) | ((N >> 3) << 17) | ((M >> 4) << 24); }
 constexpr uint32_t kIdescQK = idesc_e4m3(kTile, kQCols);
-constexpr uint32_t kIdescPV = 1u << 15;                                   // V with the dims (M) contiguous: a row is one key
+// The second product's operands have the contraction's index, the key, as rows: V a row of dims (M) in the 128-byte swizzle, the weights a row of 32
+// (N) in the 32-byte one, groups of eight rows 256 bytes apart; so a thread writes its key's weights of four heads with one store.
+constexpr uint32_t kIdescPV = idesc_e4m3(128, kPCols) | 1u << 15 | 1u << 16;
+constexpr uint32_t kDescPHi = (256u >> 4) | (1u << 14) | (6u << 29);
 
 // D[tmem] (+)= A[smem] B[smem]^T, e4m3 inputs, fp32 accumulate; one thread issues.
-__device__ __forceinline__ void umma_e4m3(uint32_t tmem_d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
+// A in the 128-byte swizzle.
+__device__ __forceinline__ void umma_e4m3(uint32_t tmem_d, uint32_t a_lo, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
         "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\t"
-        "setp.ne.b32 p, %5, 0;\n\t"
-        "mov.b64 a, {%1, %3};\n\t"
-        "mov.b64 b, {%2, %3};\n\t"
-        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a, b, %4, p;\n\t}"
-        ::"r"(tmem_d), "r"(a_lo), "r"(b_lo), "r"(tc::kDescSw128Hi), "r"(idesc), "r"(accumulate)
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "mov.b64 a, {%1, %2};\n\t"
+        "mov.b64 b, {%3, %4};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a, b, %5, p;\n\t}"
+        ::"r"(tmem_d), "r"(a_lo), "r"(tc::kDescSw128Hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate)
         : "memory");
 }
 // 8 consecutive fp32 columns of this thread's TMEM lane, and the wait tied to them (so that a load may stay on its way across other work).
@@ -86,7 +90,9 @@ __device__ __forceinline__ float warp_max(float x) {
     return y;
 }
 __device__ __forceinline__ void epi_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
-__device__ __forceinline__ void sts8(uint32_t addr, uint32_t v) { asm volatile("st.shared.b8 [%0], %1;" ::"r"(addr), "r"(v) : "memory"); }
+__device__ __forceinline__ void sts128(uint32_t addr, const uint32_t (&v)[4]) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
+}
 __device__ __forceinline__ void sts32(uint32_t addr, uint32_t v) { asm volatile("st.shared.b32 [%0], %1;" ::"r"(addr), "r"(v) : "memory"); }
 __device__ __forceinline__ void fence_proxy_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ float log2_of(float x) {
@@ -95,17 +101,14 @@ __device__ __forceinline__ float log2_of(float x) {
     return y;
 }
 // x in [0, 256] as four e4m3 numbers, p0 + p1 / 16 + p2 / 256 + p3 / 4096, for two x at once; each piece two codes
-__device__ __forceinline__ void four_pieces(float a, float b, uint32_t (&piece)[4]) {
+__device__ __forceinline__ void four_pieces(float2 x, uint32_t (&piece)[4]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        piece[i] = to_e4m3x2(a, b);
+        piece[i] = to_e4m3x2(x.x, x.y);
         if (i == 3) break;
-        const float2 f = from_e4m3x2(piece[i]);
-        a = (a - f.x) * 16.f;
-        b = (b - f.y) * 16.f;
+        x = tc::ffma2(from_e4m3x2(piece[i]), make_float2(-16.f, -16.f), tc::fmul2(x, make_float2(16.f, 16.f)));    // 16 (x - piece), exact
     }
 }
-
 
 // ---- pieces --------------------------------------------------------------------------------------
 __device__ __forceinline__ int tiles_of(int rows) { return (rows + kTile - 1) / kTile; }
@@ -354,8 +357,7 @@ __device__ __forceinline__ float put_query(uint32_t operand, int g, uint2 v, flo
 template <bool kByTiles, int kPairs>
 __global__ void __launch_bounds__(kThreads, 2)
 cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap, const AttnArgs A) {
-    constexpr int kCols = kByTiles ? kPCols / 2 : kPCols, kHeads = kByTiles ? kHalf : kMaxHeads;    // N of the second product; heads served
-    constexpr uint32_t kPv = kIdescPV | idesc_e4m3(128, kCols);
+    constexpr int kHeads = kByTiles ? kHalf : kMaxHeads;             // heads served
     extern __shared__ __align__(1024) uint8_t ptc_smem[];
     const uint32_t base = tc::smem_u32(ptc_smem), bars = base + kSmemBar;
     const int warp = tc::warp_number(), lane = threadIdx.x & 31;
@@ -520,7 +522,7 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
             const uint32_t a_lo = tc::desc_lo(base + st * kStageBytes), at = tmem + kColS + ((group & 1) * kGroup + t) * kQCols;
             if (tc::elect_one()) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) umma_e4m3(at, a_lo + 2 * j, q_lo + 2 * j, kIdescQK, j > 0);
+                for (int j = 0; j < 4; ++j) umma_e4m3(at, a_lo + 2 * j, q_lo + 2 * j, tc::kDescSw128Hi, kIdescQK, j > 0);
                 tc::umma_commit(bar(kBarEmpty + st));
                 tc::umma_commit(bar(kBarS + made));
             }
@@ -540,10 +542,10 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
             }
             if (!tc::mbar_wait_warp(bar(kBarPFull + pb), (tile >> 1) & 1, abort_flag, cta_status)) return false;
             tc::tc_fence_after();
-            const uint32_t a_lo = tc::desc_lo(base + st * kStageBytes), p_lo = tc::desc_lo(base + kSmemP + pb * kPCols * 128);
+            const uint32_t a_lo = tc::desc_lo(base + st * kStageBytes), p_lo = tc::desc_lo(base + kSmemP + pb * kPBytes);
             if (tc::elect_one()) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) umma_e4m3(tmem, a_lo + 256 * j, p_lo + 2 * j, kPv, (t | j) != 0);
+                for (int j = 0; j < 4; ++j) umma_e4m3(tmem, a_lo + 256 * j, p_lo + 64 * j, kDescPHi, kIdescPV, (t | j) != 0);
                 tc::umma_commit(bar(kBarEmpty + st));
                 tc::umma_commit(bar(kBarPEmpty + pb));
                 if (t == n - 1) tc::umma_commit(bar(kBarO));
@@ -731,27 +733,27 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
                 float x[2 * kPairs];
 #pragma unroll
                 for (int g = 0; g < 2 * kPairs; ++g) {
-                    const float z = fmaf(s[4 + g], 0.0625f, s[g]) * (ks * cq[g]);
-                    l[g] += valid ? tc::ex2(z - m[g]) : 0.f;
-                    x[g] = valid ? tc::ex2(z + lv - mv[g]) : 0.f;
+                    const float z = fmaf(s[4 + g], 0.0625f, s[g]);
+                    const float c = ks * cq[g];
+                    const float p = tc::ex2(fmaf(z, c, -m[g]));
+                    l[g] += valid ? p : 0.f;
+                    x[g] = valid ? tc::ex2(fmaf(z, c, lv - mv[g])) : 0.f;
                 }
                 if (t + parts < n) tmem_ld8(scol + (t + parts) * kQCols, s);
-                uint32_t piece[kPairs][4];
+                uint32_t lower[4], word[4];
+                four_pieces(make_float2(x[0], x[1]), lower);
+                if constexpr (kPairs == 2) {
+                    four_pieces(make_float2(x[2], x[3]), word);
 #pragma unroll
-                for (int g = 0; g < kPairs; ++g) four_pieces(x[2 * g], x[2 * g + 1], piece[g]);
+                    for (int k = 0; k < 4; ++k) word[k] = lower[k] | word[k] << 16;
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) word[k] = lower[k];
+                }
                 ok = tc::mbar_wait_warp(bar(kBarPEmpty + pb), ((i >> 1) & 1) ^ 1, abort_flag, cta_status);
                 if (!ok) continue;
-                // rows of the operand by half, piece, head: their number's last three bits, which the swizzle takes, are those of 4 piece + head
-                const uint32_t at = base + kSmemP + pb * kPCols * 128 + set * 16 * 128 + (row & 15);
-#pragma unroll
-                for (int g = 0; g < kPairs; ++g) {
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const int n0 = 4 * k + 2 * g, n1 = n0 + 1;
-                        sts8(at + n0 * 128 + (((row >> 4) ^ (n0 & 7)) << 4), piece[g][k]);
-                        sts8(at + n1 * 128 + (((row >> 4) ^ (n1 & 7)) << 4), piece[g][k] >> 8);
-                    }
-                }
+                // the key's row of the operand: 32 weights by half, piece, head; the swizzle exchanges the halves of every other four rows
+                sts128(base + kSmemP + pb * kPBytes + row * 32 + ((set ^ ((row >> 2) & 1)) << 4), word);
                 fence_proxy_async();
                 tc::tc_fence_before();
                 tc::mbar_arrive(bar(kBarPFull + pb));
