@@ -1599,7 +1599,7 @@ extern "C" flowmm_status flowmm_cache_plan(const flowmm_cache_params *p, const i
     profile_begin(st);
     FLOWMM_TRY(validate_cache(p));
     if (!grow || !rows || !rows_out || !free_pages || !free_state || !free_state_out || !block_table) return FLOWMM_ERR_NULL;
-    if (rows_out == rows || free_state_out == free_state || (slots && p->n_rows < 1)) return FLOWMM_ERR_SHAPE;
+    if (rows_out == rows || rows_out == grow || free_state_out == free_state || (slots && p->n_rows < 1)) return FLOWMM_ERR_SHAPE;
     if (!aligned4(grow) || !aligned4(rows) || !aligned4(rows_out) || !aligned4(free_pages) || !aligned4(free_state) ||
         !aligned4(free_state_out) || !aligned4(block_table) || !aligned4(slots))
         return FLOWMM_ERR_ALIGN;

@@ -5,25 +5,27 @@
 //   S[key, head]: a bf16 query, scaled by a power of two, is the sum of two e4m3 numbers, 8 bits of significand as 4 + 4 (exact but
 //                 for elements 2^13 times smaller than the largest): N = 8 heads x 2
 //   O[dim, head]: a weight is kept as four e4m3 numbers, each the rounded rest of the one before times 16, within 2^-16 of
-//                 itself: N = 8 heads x 4.  (Two, the error of a bf16 weight, would not shorten anything that bounds: see below.)
+//                 itself: N = 8 heads x 4.  (Two would do for a bf16 result; the time without any splitting is 1 % less where memory bounds.)
 // The pages' scales join in fp32: K's on the logits; V's in the exponent of the weights, w_j = 2^(z_j + log2 sv_j - max), with a maximum of
 // its own, so that the largest weight is 1 whatever the scales are.  The sum of the softmax, sum_j 2^(z_j - max z), is apart.
 //
 // How the work is shared out over the blocks of the launch, two to an SM, is found on the device, where alone the lengths are known (Cut).
-// With few tiles to a block each has one range of one head, all of the same length but for a head's last one.  With many, the tiles of 128
-// keys of all heads stand in a row, by unit, head and key, and every block takes an equal piece of the row, parts of heads or several, one
-// after the other.  A head
-// that several blocks have part in leaves a record for each, and cache_join_kernel joins them in order.  (Ranges of equal
-// length of each head by itself, a block each, left a last round half empty, 16 sequences of up to 33 792 rows, 8 heads, 174 us; as pieces 118.  Three
+// Few heads: a block has one range of one head, all of the same length but for a head's last one.  Many: a block has two whole heads, or the
+// tiles of 128 keys of all heads stand in a row, by unit, head and key, and every block takes an equal piece of the row, parts of heads or
+// several, one after the other.  A head that several blocks have part in leaves a record for each, and cache_join_kernel joins
+// them in order.  (Ranges alone left a last round half empty, 16 sequences of up to 33 792 rows, 8 heads, 174 us; pieces 118.  Three
 // quarters of a piece to each block and the rest drawn from a counter in pieces of three tiles and more: 132.)
-// A block goes through its tiles in groups of up to
-// seven of one head, the roles of its warps one or two groups apart, across the heads' borders too:
+// A block goes through its tiles in groups of up to seven of one head, the roles of its warps one or two groups apart, across the
+// heads' borders too:
 //   warp 0     K tiles and V tiles by TMA, a box per page, into a ring of six stages of 16 KB: a tile of K of group c + 1 and one of V of
 //              group c in turn; the next head's query operand; the scales of a group's pages
 //   warp 1     the products, in the same order; the logits of two groups stay in tensor memory
 //   warps 2-9  a thread per key of a tile: maxima of a group, then its weights; a thread per dim: the output, rescaled once a group.
 //              Two halves of four warps: for more than four query heads each has four of them, for fewer every other tile.  (One half
 //              alone took 1800 clocks for a tile of eight heads, longer than its share of the memory's time.)
+// Memory bounds long calls: 16 sequences of up to 33 792 rows, 686 MB of pages, 118 us, 5.8 TB/s.  Short ones are bound by the way of one group through the
+// block, about 6 us from the lengths to the output (one sequence of 218 rows), and by the ends of the blocks, which fall together: 64
+// sequences of up to 1690 rows, 131 MB, 35.7 us.  (Groups of two to five tiles, and smaller groups at a block's end, were no faster.)
 // Every wait is bounded.
 #pragma once
 #include "paged_attention.cuh"
@@ -86,7 +88,7 @@ __device__ __forceinline__ void tmem_ld_wait(float (&r)[8]) {
 // The largest of a warp's values (NaN counts for nothing).
 __device__ __forceinline__ float warp_max(float x) {
     float y;
-    asm("redux.sync.max.f32 %0, %1, 0xFFFFFFFF;" : "=f"(y) : "f"(x));
+    asm volatile("redux.sync.max.f32 %0, %1, 0xFFFFFFFF;" : "=f"(y) : "f"(x));      // (volatile: not to be moved to where one lane alone needs it)
     return y;
 }
 __device__ __forceinline__ void epi_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
@@ -130,11 +132,12 @@ __device__ __forceinline__ uint32_t sorted_unit(const Cut &c, uint32_t r) {
 }
 // Heads are not cut for a range kJoinTiles longer: joining costs that much.  With at most as many heads as blocks, ranges of a head each,
 // unless they become kSwitchTiles longer than an even piece: the way from one head to the next costs 3 us where a block has few tiles (one
-// sequence of 1100 rows, 4 heads: 10.4 us by ranges, 13.9 by pieces of two tiles of one head or of two).  At most 32 ranges of a head, which one round of the joining
-// kernel's lanes takes (8448 rows, 4 heads: 66 ranges 15.5 us, 22 13.1).
+// sequence of 1100 rows, 4 heads: 10.4 us by ranges, 13.9 by pieces of two tiles of one head or of two).  At most 64 ranges of a head, whose joining
+// is the longer the more there are (one head of 33 792 rows by at most 16, 32 and 64 ranges, and by 132 pieces: 22.7, 17.2, 14.7 and 17.6 us; two heads 23.2, 17.8,
+// 15.2, 15.2; eight 25.0, 25.2, 23.0, 23.3).
 // With up to twice as many heads as blocks, of at most 64 units, a block has the i-th longest and the i-th last
 // (64 units of up to 1690 rows, 512 heads: 41 us cut, 36 so).
-constexpr int kSwitchTiles = 4;
+constexpr int kSwitchTiles = 4, kMostRanges = 64;
 __device__ __forceinline__ Cut make_cut(const AttnArgs &A) {
     Cut c;
     const int lane = lane_id();
@@ -169,7 +172,8 @@ __device__ __forceinline__ Cut make_cut(const AttnArgs &A) {
             for (int u = c.u0; u < c.u1; ++u) n += ((uint32_t)tiles_of(unit_rows(A, u)) + per - 1) / per;
             return n;
         };
-        for (uint32_t per = max(max(1u, c.share), (uint32_t)(longest + 31) / 32); per <= c.share + kSwitchTiles || per + kJoinTiles >= (uint32_t)longest; ++per) {
+        const uint32_t least = max(max(1u, c.share), (uint32_t)(longest + kMostRanges - 1) / kMostRanges);
+        for (uint32_t per = least; per <= least + kSwitchTiles || per + kJoinTiles >= (uint32_t)longest; ++per) {
             if (per + kJoinTiles >= (uint32_t)longest) per = max(1, longest);
             c.ranges = count(per);
             if (__reduce_add_sync(0xFFFFFFFFu, c.ranges) * A.Hkv > blocks) continue;

@@ -288,7 +288,7 @@ def test_attention_of_long_and_many_units(path, D):
 
 @pytest.mark.parametrize("U,Hq,Hkv,lengths", [
     (1, 8, 2, [1700]),                                  # few heads: ranges, a few a head
-    (1, 7, 1, [40000]),                                 # ... thirty and more
+    (1, 7, 1, [40000]), (1, 1, 1, [9000]),              # ... and up to 64
     (3, 64, 8, [129, 4000, 1]), (30, 28, 4, None), (7, 5, 5, None),
     (37, 32, 8, None), (38, 8, 8, None), (64, 64, 8, None), (64, 9, 9, None), (60, 16, 8, [0, 1700, 0, 900]),   # about and above 296 heads, up to 592: pairs
     (64, 8, 8, [1700]), (48, 8, 8, [5000] + [100] * 47),                                    # ... which would be uneven: pieces
@@ -581,6 +581,42 @@ def test_captured_step_with_changing_lengths(path):
         for u in range(U):
             assert (np.abs(out[u].cpu().numpy() - ref[u]) <= T.attention_bound(size[u], logits[u], int(r[u]), D)).all(), (i, u)
     assert F.flowmm_last_device_status(s.ws) == 0
+
+
+def test_graphs_of_cut_heads_share_a_workspace():
+    """Two captured calls whose heads are cut, of different shapes, on one workspace, replayed in turn with eager calls and other lengths between."""
+    rng = np.random.default_rng(33)
+    for path in (F.PATH_AUTO, F.PATH_SIMT):
+        cases = []
+        for U, Hq, H, most in ((2, 16, 2, 9000), (40, 14, 14, 3000)):
+            rows = rng.integers(1, most, U)
+            p = T.params(U, Hq, H, 128, 64, 1, 1, path=path)
+            _, q, arrays = _check(p, rng, rows, 64)
+            cases.append((p, q, arrays, T.dev(rows.astype(np.int32)), [T.dev(x) for x in arrays[:4]] + [T.dev(np.where(arrays[4] < 1 << 29, arrays[4], 0))], T.dev(q, F.BF16),
+                          torch.empty((U, Hq, 128), device="cuda"), rows))
+        ws = torch.full((max(F.flowmm_cache_workspace_bytes(c[0]) for c in cases),), 255, dtype=torch.uint8, device="cuda")
+        ws[:256] = 0
+        side, graphs = torch.cuda.Stream(), []
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            for p, _, _, rows_d, d, qd, out, _ in cases:
+                g = torch.cuda.CUDAGraph()
+                with torch.cuda.graph(g, stream=side):
+                    F.flowmm_cache_attention(p, qd, *d, rows_d, out, ws)
+                graphs.append(g)
+        torch.cuda.current_stream().wait_stream(side)
+        for step in range(6):
+            i = step % 2
+            p, q, (ck, cv, ks, vs, table), rows_d, d, qd, out, most = cases[i]
+            rows = most if step < 2 else rng.integers(0, most + 1)
+            rows_d.copy_(T.dev(rows.astype(np.int32)))
+            graphs[i].replay()
+            if step % 3 == 0:
+                F.flowmm_cache_attention(p, qd, *d, rows_d, torch.empty_like(out), ws)
+            assert F.flowmm_last_device_status(ws) == 0
+            want, size, logits = P.attention(q, P.E4M3[ck], P.E4M3[cv], ks, vs, table, rows)
+            for u, n in enumerate(rows):
+                assert (np.abs(out[u].cpu().numpy() - want[u]) <= T.attention_bound(size[u], logits[u], int(n), 128)).all(), (step, u)
 
 
 def test_two_streams_with_workspaces_of_their_own():

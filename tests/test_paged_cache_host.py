@@ -101,7 +101,7 @@ def test_refusals_of_alignment_and_aliases(lib):
                 getattr(c, field)[i] = bad
                 assert _call(lib, name, c, _args(name)) == 6, (name, field, i)
         assert _call(lib, name, F.CacheParams(**{**GOOD, "n_rows": 0}).c(), _args(name)) == 2
-    for same in ((1, 2), (4, 5)):                       # rows_out on rows, free_state_out on free_state
+    for same in ((1, 2), (0, 2), (4, 5)):               # rows_out on rows and on grow, free_state_out on free_state
         args = _args("flowmm_cache_plan")
         args[same[1]] = args[same[0]]
         assert _call(lib, "flowmm_cache_plan", p.c(), args) == 2
