@@ -371,7 +371,10 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
     float *info = reinterpret_cast<float *>(ptc_smem + kSmemInfo), *first_factors = reinterpret_cast<float *>(ptc_smem + kSmemFirst);
     if ((base & 1023u) != 0) {                       // the swizzled tiles need a 1024-byte aligned base
         predecessor_done();
-        if (threadIdx.x == 0) report(A.status, 6);
+        if (threadIdx.x == 0) {
+            report(A.status, 6);
+            if (A.cut_heads) A.cut_heads[blockIdx.x] = make_int4(0, 0, 0, 0);
+        }
         return;
     }
     auto bar = [&](int i) { return bars + 8u * i; };

@@ -70,6 +70,33 @@ def test_plan_equals_oracle(U, page, wide, n_rows, spare, slots):
         assert status == (11 if want[5] else 0), (kind, status)
 
 
+def test_plan_without_slots_takes_any_growth_and_none():
+    """n_rows = 0, slots NULL: pages are given out and taken back, whatever the growth."""
+    rng = np.random.default_rng(5)
+    rows, g, ring, state, table = _plan_case(rng, 6, 16, 50, 1, 120, lambda r: np.array([300, -5, 0, 90, -10000, 1], np.int32))
+    got, status = _plan(T.params(6, 1, 1, 128, 16, len(ring), 50, 0), rows, g, ring, state, table, slots=False)
+    want = P.plan(g, rows, ring, state, table, 16, 0, False)
+    assert status == (11 if want[5] else 0) and all(np.array_equal(a, b) for a, b in zip(got[:4], want[:4]))
+
+
+def test_a_plan_thrown_away_is_made_again():
+    """The same step planned twice gives the same, and so does another one planned between."""
+    rng = np.random.default_rng(6)
+    rows, g, ring, state, table = _plan_case(rng, 40, 32, 30, 5, 90, lambda r: rng.integers(-400, 6, 40).astype(np.int32))
+    p = T.params(40, 1, 1, 128, 32, len(ring), 30, 5)
+    i32 = lambda *s: torch.zeros(s, dtype=torch.int32, device="cuda")
+    d = [T.dev(x) for x in (g, rows, ring, state, table)]
+    ws, results = F.alloc_cache_workspace(p), []
+    for grow in (d[0], torch.ones_like(d[0]), d[0]):
+        out, left, slots = i32(40), i32(2), i32(40, 5)
+        F.flowmm_cache_plan(p, grow, d[1], out, d[2], d[3], left, d[4], slots, ws)
+        held = (out.cpu().numpy() + 31) // 32
+        results.append([out.cpu(), left.cpu(), slots.cpu(), [d[4].cpu()[u, :held[u]] for u in range(40)]])
+    for a, b in zip(results[0][:3], results[2][:3]):
+        assert torch.equal(a, b)
+    assert all(torch.equal(a, b) for a, b in zip(results[0][3], results[2][3]))
+
+
 def test_plan_of_unsound_state_changes_nothing():
     """Numbers out of range where the call reads lengths or the ring's state: reported, and nothing is taken."""
     rng = np.random.default_rng(3)
@@ -292,7 +319,9 @@ def test_attention_of_long_and_many_units(path, D):
     (3, 64, 8, [129, 4000, 1]), (30, 28, 4, None), (7, 5, 5, None),
     (37, 32, 8, None), (38, 8, 8, None), (64, 64, 8, None), (64, 9, 9, None), (60, 16, 8, [0, 1700, 0, 900]),   # about and above 296 heads, up to 592: pairs
     (64, 8, 8, [1700]), (48, 8, 8, [5000] + [100] * 47),                                    # ... which would be uneven: pieces
-    (70, 16, 8, None), (75, 64, 8, [1, 0, 300]), (300, 1, 1, [30000] + [20] * 299)])        # many: pieces, some of a hundred to a head
+    (70, 16, 8, None), (75, 64, 8, [1, 0, 300]), (300, 1, 1, [30000] + [20] * 299),         # many: pieces, some of a hundred to a head
+    (1, 1000, 1000, [40]), (2, 1400, 700, [0, 130]),    # ... and many heads to a piece
+    (3, 8, 2, [0]), (40, 8, 8, [0]), (80, 16, 8, [0])]) # nothing at all
 def test_every_way_to_share_the_work_out(U, Hq, Hkv, lengths):
     rng = np.random.default_rng(U + Hq)
     rows = rng.integers(0, 1800, U) if lengths is None else np.array([lengths[u % len(lengths)] for u in range(U)])
@@ -617,6 +646,18 @@ def test_graphs_of_cut_heads_share_a_workspace():
             want, size, logits = P.attention(q, P.E4M3[ck], P.E4M3[cv], ks, vs, table, rows)
             for u, n in enumerate(rows):
                 assert (np.abs(out[u].cpu().numpy() - want[u]) <= T.attention_bound(size[u], logits[u], int(n), 128)).all(), (step, u)
+
+
+def test_profile_names_the_kernels():
+    rng = np.random.default_rng(1)
+    p = T.params(2, 8, 2, 128, 64, 1, 1)
+    F.flowmm_profile_enable(True)
+    try:
+        _check(p, rng, np.array([5000, 70]), 64)
+        assert F.flowmm_last_launch_count() == 2
+        assert [name for name, ms in F.flowmm_profile_read()] == ["cache_attention_tc", "cache_join"]
+    finally:
+        F.flowmm_profile_enable(False)
 
 
 def test_two_streams_with_workspaces_of_their_own():
