@@ -364,6 +364,8 @@ flowmm_status flowmm_cache_load(const flowmm_cache_params *p, const void *k_page
  * unit, zero for a unit without rows.  What stands behind a unit's last row (codes of NaN too) has no influence.  Several new
  * queries of a sequence are units that share a row of the block table and differ in rows.
  *   q [U, Hq, D] dense, element type `dtype`;  out [U, Hq, D] f32
+ * `path`: AUTO runs both contractions on the tensor cores (tcgen05, the codes as operands) when dtype is bf16, and SIMT fp32 kernels
+ * otherwise; SIMT forces the latter.  The workspace serves both.
  */
 flowmm_status flowmm_cache_attention(const flowmm_cache_params *p, const void *q, const void *k_pages, const void *v_pages,
                                      const float *k_scale, const float *v_scale, const int32_t *block_table, const int32_t *rows,

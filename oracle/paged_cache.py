@@ -98,9 +98,10 @@ def load(values, scale, table, n):
     return np.moveaxis(x, 1, 0).reshape(x.shape[1], -1, x.shape[3])[:, :n]
 
 
-def attention(q, k_values, v_values, k_scale, v_scale, table, rows, softmax_scale=0.0):
-    """(out, size, logits): q [U, Hq, D]; size[u, hq, d] = sum_j p_j |v_jd|, logits[u, hq] = the largest scale * sum_d |q_d k_jd|,
-    by both of which an implementation's rounding errors go."""
+def attention(q, k_values, v_values, k_scale, v_scale, table, rows, softmax_scale=0.0, least=2.0 ** -14):
+    """(out, size, logits): q [U, Hq, D]; size[u, hq, d] = sum_j max(w_j, least * max_i w_i) |code_jd| with w_j = p_j sv_j, a key's weight and V's
+    scale, logits[u, hq] = the largest scale * sum_d |q_d k_jd|: by both of these the rounding errors go of an implementation that holds weights w with
+    a relative error down to `least` of the largest, and with the absolute error that belongs to that below."""
     U, Hq, D = q.shape
     H = k_values.shape[1]
     c = softmax_scale or 1 / math.sqrt(D)
@@ -113,6 +114,8 @@ def attention(q, k_values, v_values, k_scale, v_scale, table, rows, softmax_scal
             h = g // (Hq // H)
             z = c * (k[h] @ q[u, g])
             w = np.exp(z - np.max(z))
-            out[u, g], size[u, g] = w @ v[h] / w.sum(), w @ np.abs(v[h]) / w.sum()
+            sv = np.repeat(v_scale[table[u, :pages(int(rows[u]), v_values.shape[2])], h], v_values.shape[2])[:rows[u]].astype(np.float64)
+            weight = np.maximum(w * sv, least * np.max(w * sv)) / sv
+            out[u, g], size[u, g] = w @ v[h] / w.sum(), weight @ np.abs(v[h]) / w.sum()
             logits[u, g] = c * np.max(np.abs(k[h]) @ np.abs(q[u, g]))
     return out, size, logits

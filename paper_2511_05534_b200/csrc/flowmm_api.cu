@@ -1474,7 +1474,7 @@ int page_shift(int page) { return page == 16 ? 4 : page == 32 ? 5 : page == 64 ?
 
 // The attention's cut and scratch: [status word, 256 bytes][cut heads][records].
 struct CachePlan {
-    bool tc;                       // the tensor-core kernel (bf16 queries, heads of 128) or the SIMT one
+    bool tc;                       // the tensor-core kernel (bf16 queries) or the SIMT one
     bool joins;                    // a head may be cut
     int groups, gp, target;        // groups of query heads that are ranges of their own, heads of one, ranges aimed at
     int64_t blocks;                // of the launch: no fewer than ranges can come out (paged_attention.cuh)
@@ -1484,7 +1484,7 @@ struct CachePlan {
 CachePlan cache_plan(const flowmm_cache_params &p, int path) {
     CachePlan c;
     const int G = p.n_q_heads / p.n_kv_heads;
-    c.tc = p.dtype == FLOWMM_BF16 && p.head_dim == 128 && path != FLOWMM_PATH_SIMT;
+    c.tc = p.dtype == FLOWMM_BF16 && path != FLOWMM_PATH_SIMT;
     c.gp = c.tc ? G : std::min(G, 2);
     c.groups = (G + c.gp - 1) / c.gp;
     c.target = (c.tc ? 2 : 4) * kScoreCtas;
@@ -1557,20 +1557,22 @@ flowmm_status launch_cache_join(const paged::AttnArgs &a, const CachePlan &c, in
     return FLOWMM_OK;
 }
 
+template <int D>
 flowmm_status launch_cache_attention_tc(const flowmm_cache_params &p, const paged::AttnArgs &a, const CachePlan &c, cudaStream_t st) {
+    namespace ptc = paged::ptc;
     CUtensorMap kmap, vmap;
-    const uint64_t head = (uint64_t)p.page_size * 128, dims[4] = {128, (uint64_t)p.page_size, (uint64_t)p.n_kv_heads, (uint64_t)p.n_pages};
-    const uint64_t strides[3] = {128, head, head * p.n_kv_heads};
-    const uint32_t box[4] = {128, (uint32_t)p.page_size, 1, 1};
+    const uint64_t head = (uint64_t)p.page_size * D, dims[4] = {D, (uint64_t)p.page_size, (uint64_t)p.n_kv_heads, (uint64_t)p.n_pages};
+    const uint64_t strides[3] = {D, head, head * p.n_kv_heads};
+    const uint32_t box[4] = {D, (uint32_t)p.page_size, 1, 1};
     if (!tc::make_byte_map(&kmap, a.k, 4, dims, strides, box) || !tc::make_byte_map(&vmap, a.v, 4, dims, strides, box)) return FLOWMM_ERR_CUDA;
-    auto kernel = a.G <= 2 ? paged::ptc::cache_attention_tc_kernel<true, 1> :
-                  a.G <= paged::ptc::kHalf ? paged::ptc::cache_attention_tc_kernel<true, 2> : paged::ptc::cache_attention_tc_kernel<false, 2>;
+    auto kernel = a.G <= 2 ? ptc::cache_attention_tc_kernel<D, true, 1> :
+                  a.G <= ptc::kHalf ? ptc::cache_attention_tc_kernel<D, true, 2> : ptc::cache_attention_tc_kernel<D, false, 2>;
     if (!allow_smem(kernel) || cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared) != cudaSuccess)
         return FLOWMM_ERR_CUDA;
-    launch(kernel, (unsigned)c.blocks, paged::ptc::kThreads, paged::ptc::kSmemBytes, st, kmap, vmap, a);
+    launch(kernel, (unsigned)c.blocks, ptc::kThreads, ptc::Lay<D>::kSmemBytes, st, kmap, vmap, a);
     FLOWMM_LAUNCHED("cache_attention_tc");
     // (the first part of a head is its block's last one, in the second of the block's records; the others are their blocks' first)
-    return launch_cache_join<128>(a, c, p.n_units * p.n_kv_heads, 2, 1, 2, st);
+    return launch_cache_join<D>(a, c, p.n_units * p.n_kv_heads, 2, 1, 2, st);
 }
 
 template <int D>
@@ -1697,7 +1699,7 @@ extern "C" flowmm_status flowmm_cache_attention(const flowmm_cache_params *p, co
     a.q_bf16 = p->dtype == FLOWMM_BF16; a.target = c.target; a.by_heads = make_fastdiv(p->n_kv_heads * c.groups);
     const float scale = p->softmax_scale != 0.f ? p->softmax_scale : 1.f / sqrtf((float)p->head_dim);
     a.scale_log2 = scale * kLog2e;
-    if (c.tc) return launch_cache_attention_tc(*p, a, c, st);
+    if (c.tc) return p->head_dim == 128 ? launch_cache_attention_tc<128>(*p, a, c, st) : launch_cache_attention_tc<64>(*p, a, c, st);
     return p->head_dim == 128 ? launch_cache_attention<128>(a, c, st) : launch_cache_attention<64>(a, c, st);
 }
 

@@ -1,7 +1,7 @@
 // Decode attention over the paged 8-bit cache: one new query per query head, lengths of their own for every unit.
 //   o = sum_j softmax_j(scale * q . (sk_j k_j)) (sv_j v_j),   k_j, v_j: e4m3 codes, sk_j, sv_j: their page's scales
 // This file: how the SIMT kernel's work is cut into ranges of keys on the device, where alone the lengths are known, the kernel that joins
-// ranges, and the SIMT kernel (fp32 queries, heads of 64).
+// ranges, and the SIMT kernel (fp32 queries).
 #pragma once
 #include "common.cuh"
 #include "paged_cache.cuh"

@@ -1,11 +1,11 @@
-// Decode attention over the paged 8-bit cache on the tensor cores: bf16 queries, heads of 128.
+// Decode attention over the paged 8-bit cache on the tensor cores: bf16 queries.
 //
 // The codes go into the matrix instructions as they are (kind::f8f6f4), with the keys on the wide side, so no code is ever
 // converted and every row of K and V is read once.  The narrow side is split into e4m3 numbers that stand side by side as columns:
 //   S[key, head]: a bf16 query, scaled by a power of two, is the sum of two e4m3 numbers, 8 bits of significand as 4 + 4 (exact but
 //                 for elements 2^13 times smaller than the largest): N = 8 heads x 2
 //   O[dim, head]: a weight is kept as four e4m3 numbers, each the rounded rest of the one before times 16, within 2^-16 of
-//                 itself: N = 8 heads x 4.  (Two would do for a bf16 result; the time without any splitting is 1 % less where memory bounds.)
+//                 itself or 2^-30 of the largest: N = 8 heads x 4.  (Two would do for a bf16 result; the time without any splitting is 1 % less where memory bounds.)
 // The pages' scales join in fp32: K's on the logits; V's in the exponent of the weights, w_j = 2^(z_j + log2 sv_j - max), with a maximum of
 // its own, so that the largest weight is 1 whatever the scales are.  The sum of the softmax, sum_j 2^(z_j - max z), is apart.
 //
@@ -17,7 +17,7 @@
 // quarters of a piece to each block and the rest drawn from a counter in pieces of three tiles and more: 132.)
 // A block goes through its tiles in groups of up to seven of one head, the roles of its warps one or two groups apart, across the
 // heads' borders too:
-//   warp 0     K tiles and V tiles by TMA, a box per page, into a ring of six stages of 16 KB: a tile of K of group c + 1 and one of V of
+//   warp 0     K tiles and V tiles by TMA, a box per page, into a ring of six stages of 16 KB (ten of 8): a tile of K of group c + 1 and one of V of
 //              group c in turn; the next head's query operand; the scales of a group's pages
 //   warp 1     the products, in the same order; the logits of two groups stay in tensor memory
 //   warps 2-9  a thread per key of a tile: maxima of a group, then its weights; a thread per dim: the output, rescaled once a group.
@@ -34,42 +34,53 @@ namespace flowmm {
 namespace paged {
 namespace ptc {
 
-constexpr int kTile = 128, kStages = 6, kMaxHeads = 8, kHalf = 4, kGroup = 7, kThreads = 320, kTmemCols = 256;
+constexpr int kTile = 128, kMaxHeads = 8, kHalf = 4, kGroup = 7, kThreads = 320, kTmemCols = 256;
 constexpr int kQCols = 2 * kMaxHeads, kPCols = 4 * kMaxHeads;            // N of the two products; by half, piece, head
 constexpr int kMostPages = kGroup * kTile / 16;                          // pages of a group
-constexpr uint32_t kStageBytes = kTile * 128;
 constexpr int kInfos = 4;                                                // groups whose scales are kept
-constexpr uint32_t kSmemQ = kStages * kStageBytes, kPBytes = kTile * kPCols, kSmemP = kSmemQ + 2 * kQCols * 128, kSmemRed = kSmemP + 2 * kPBytes;
-constexpr uint32_t kSmemInfo = kSmemRed + 2 * 8 * 3 * kHalf * 4;          // red: [group parity][warp][maxima, with V's scales, sums][head]
 constexpr int kInfo = 2 * kMostPages + kMaxHeads;                         // [K's scale, log2 of V's][page], the queries' factors
-constexpr uint32_t kSmemFirst = kSmemInfo + kInfos * kInfo * 4;           // the factors of the first head's queries
-constexpr uint32_t kSmemTask = kSmemFirst + kMaxHeads * 4;                // tasks: [group mod 4]
-constexpr uint32_t kSmemBar = kSmemTask + kInfos * 32;
-constexpr int kBarFull = 0, kBarEmpty = kStages, kBarQFull = 2 * kStages, kBarQEmpty = kBarQFull + 2, kBarS = kBarQEmpty + 2,
-              kBarPFull = kBarS + 2 * kGroup /* a tile's logits, by its number in the block */, kBarPEmpty = kBarPFull + 2, kBarO = kBarPEmpty + 2, kBarTask = kBarO + 1,
-              kBarIFull = kBarTask + kInfos, kBarIEmpty = kBarIFull + kInfos, kNumBars = kBarIEmpty + kInfos;
-constexpr uint32_t kSmemBytes = kSmemBar + 8 * kNumBars + 16;             // (+ TMEM address, abort flag, status)
+constexpr uint32_t kPBytes = kTile * kPCols;                              // the weights of a tile
 constexpr uint32_t kColS = kPCols;                                        // O in the first columns, then the two groups' logits
 static_assert(kColS + 2 * kGroup * kQCols <= kTmemCols, "tensor memory");
-static_assert(2 * (kSmemBytes + 1024) <= 227 * 1024, "two blocks to an SM");
+
+// What goes by the heads' dims: the ring (of 96 or 80 KB), the rows of tiles and query operands, in the swizzle of their length, and the
+// places of it all in shared memory.
+template <int D> struct Lay {
+    static constexpr int kStages = D == 128 ? 6 : 10;
+    static constexpr uint32_t kStageBytes = kTile * D, kQBytes = kQCols * D;
+    static constexpr uint32_t kSmemQ = kStages * kStageBytes, kSmemP = kSmemQ + 2 * kQBytes, kSmemRed = kSmemP + 2 * kPBytes;
+    static constexpr uint32_t kSmemInfo = kSmemRed + 2 * 8 * 3 * kHalf * 4;   // red: [group parity][warp][maxima, with V's scales, sums][head]
+    static constexpr uint32_t kSmemFirst = kSmemInfo + kInfos * kInfo * 4;    // the factors of the first head's queries
+    static constexpr uint32_t kSmemTask = kSmemFirst + kMaxHeads * 4;         // tasks: [group mod 4]
+    static constexpr uint32_t kSmemBar = kSmemTask + kInfos * 32;
+    static constexpr int kBarFull = 0, kBarEmpty = kStages, kBarQFull = 2 * kStages, kBarQEmpty = kBarQFull + 2,
+        kBarS = kBarQEmpty + 2 /* a tile's logits, by its number in the block */, kBarPFull = kBarS + 2 * kGroup, kBarPEmpty = kBarPFull + 2,
+        kBarO = kBarPEmpty + 2, kBarTask = kBarO + 1, kBarIFull = kBarTask + kInfos, kBarIEmpty = kBarIFull + kInfos, kNumBars = kBarIEmpty + kInfos;
+    static constexpr uint32_t kSmemBytes = kSmemBar + 8 * kNumBars + 16;      // (+ TMEM address, abort flag, status)
+    static_assert(2 * (kSmemBytes + 1024) <= 227 * 1024, "two blocks to an SM");
+    // rows of 128 bytes in the 128-byte swizzle, of 64 in the 64-byte one, groups of eight rows one after the other
+    static constexpr uint32_t kDescHi = D == 128 ? tc::kDescSw128Hi : (512u >> 4) | (1u << 14) | (4u << 29);
+    // where 16 bytes of a row go
+    static __device__ __forceinline__ uint32_t chunk(int row, int c) { return (uint32_t)(row * D + ((D == 128 ? c ^ (row & 7) : c ^ (row >> 1 & 3)) << 4)); }
+};
 
 __host__ __device__ constexpr uint32_t idesc_e4m3(uint32_t M, uint32_t N) { return (1u << 4) | ((N >> 3) << 17) | ((M >> 4) << 24); }
 constexpr uint32_t kIdescQK = idesc_e4m3(kTile, kQCols);
-// The second product's operands have the contraction's index, the key, as rows: V a row of dims (M) in the 128-byte swizzle, the weights a row of 32
-// (N) in the 32-byte one, groups of eight rows 256 bytes apart; so a thread writes its key's weights of four heads with one store.
+// The second product's operands have the contraction's index, the key, as rows: V a row of dims (M) as it came, the weights a row of 32
+// (N) in the 32-byte swizzle, groups of eight rows 256 bytes apart; so a thread writes its key's weights of four heads with one store.
+// M is 128 for heads of 64 as well: the next 64 dims are said to be 0 bytes further on, are the first ones again, and are not looked at.
 constexpr uint32_t kIdescPV = idesc_e4m3(128, kPCols) | 1u << 15 | 1u << 16;
 constexpr uint32_t kDescPHi = (256u >> 4) | (1u << 14) | (6u << 29);
 
 // D[tmem] (+)= A[smem] B[smem]^T, e4m3 inputs, fp32 accumulate; one thread issues.
-// A in the 128-byte swizzle.
-__device__ __forceinline__ void umma_e4m3(uint32_t tmem_d, uint32_t a_lo, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, uint32_t accumulate) {
+__device__ __forceinline__ void umma_e4m3(uint32_t tmem_d, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
         "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\t"
         "setp.ne.b32 p, %6, 0;\n\t"
         "mov.b64 a, {%1, %2};\n\t"
         "mov.b64 b, {%3, %4};\n\t"
         "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a, b, %5, p;\n\t}"
-        ::"r"(tmem_d), "r"(a_lo), "r"(tc::kDescSw128Hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate)
+        ::"r"(tmem_d), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate)
         : "memory");
 }
 // 8 consecutive fp32 columns of this thread's TMEM lane, and the wait tied to them (so that a load may stay on its way across other work).
@@ -95,6 +106,7 @@ __device__ __forceinline__ void epi_sync() { asm volatile("bar.sync 1, 256;" :::
 __device__ __forceinline__ void sts128(uint32_t addr, const uint32_t (&v)[4]) {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
 }
+__device__ __forceinline__ void sts16(uint32_t addr, uint32_t v) { asm volatile("st.shared.b16 [%0], %1;" ::"r"(addr), "h"((unsigned short)v) : "memory"); }
 __device__ __forceinline__ void sts32(uint32_t addr, uint32_t v) { asm volatile("st.shared.b32 [%0], %1;" ::"r"(addr), "r"(v) : "memory"); }
 __device__ __forceinline__ void fence_proxy_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ float log2_of(float x) {
@@ -326,49 +338,62 @@ struct Task {
     int record;                          // where the part of the head goes: -1: it is all of it, else the record's number
     int first, last;                     // of the head's groups in the piece
 };
-static_assert(sizeof(Task) == 32, "as much as kSmemTask leaves");
+static_assert(sizeof(Task) == 32, "as much as Lay::kSmemTask leaves");
 
-// A query head's rows of the operand, by a warp: four elements a lane.  Rows by half, piece, head.  Returns the factor of its logits:
+// A lane's part of a query, two or four elements.
+template <int D> struct alignas(D / 16) Query { uint32_t w[D / 64]; };
+// A query head's rows of the operand, by a warp.  Rows by half, piece, head.  Returns the factor of its logits:
 // the queries' power of two and the softmax's scale; NaN for a query that is not finite.
-__device__ __forceinline__ float put_query(uint32_t operand, int g, uint2 v, float scale_log2) {
+template <int D>
+__device__ __forceinline__ float put_query(uint32_t operand, int g, const Query<D> &v, float scale_log2) {
+    constexpr int V = D / 32;
     const int lane = lane_id();
-    const float x[4] = {__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xFFFF0000u), __uint_as_float(v.y << 16), __uint_as_float(v.y & 0xFFFF0000u)};
+    float x[V];
+#pragma unroll
+    for (int i = 0; i < V / 2; ++i) { x[2 * i] = __uint_as_float(v.w[i] << 16); x[2 * i + 1] = __uint_as_float(v.w[i] & 0xFFFF0000u); }
     float size = 0.f;
     bool fine = true;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) { size = fmaxf(size, fabsf(x[i])); fine = fine && is_finite(x[i]); }
+    for (int i = 0; i < V; ++i) { size = fmaxf(size, fabsf(x[i])); fine = fine && is_finite(x[i]); }
     if (!fine) size = __uint_as_float(0x7F800000u);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) size = fmaxf(size, __shfl_xor_sync(0xFFFFFFFFu, size, o));
     const int ex = is_finite(size) ? max(-100, (int)(__float_as_uint(size) >> 23) - 127) - 7 : 0;   // the largest element to [128, 256)
     const float f = power_of_two(-ex);
-    uint32_t lo[2], hi[2];
+    uint32_t lo[V / 2], hi[V / 2];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < V / 2; ++i) {
         const float a = x[2 * i] * f, b = x[2 * i + 1] * f;
         hi[i] = to_e4m3x2(a, b);
         const float2 h = from_e4m3x2(hi[i]);
         lo[i] = to_e4m3x2((a - h.x) * 16.f, (b - h.y) * 16.f);
     }
-    const int n = (g >> 2) * 8 + (g & 3);
-    const uint32_t at = operand + (lane & 3) * 4;
-    sts32(at + n * 128 + (((lane >> 2) ^ (n & 7)) << 4), hi[0] | hi[1] << 16);
-    sts32(at + (n + 4) * 128 + (((lane >> 2) ^ ((n + 4) & 7)) << 4), lo[0] | lo[1] << 16);
+    const int n = (g >> 2) * 8 + (g & 3), c = lane * V >> 4;
+    const uint32_t at = operand + (lane * V & 15), first = at + Lay<D>::chunk(n, c), second = at + Lay<D>::chunk(n + 4, c);
+    if constexpr (V == 4) {
+        sts32(first, hi[0] | hi[V / 2 - 1] << 16);
+        sts32(second, lo[0] | lo[V / 2 - 1] << 16);
+    } else {
+        sts16(first, hi[0]);
+        sts16(second, lo[0]);
+    }
     return is_finite(size) ? power_of_two(ex) * scale_log2 : __uint_as_float(0x7FC00000u);
 }
 
 // kByTiles: at most four query heads, or two (kPairs: of one half), the halves take every other tile; else the halves have four heads each.
-template <bool kByTiles, int kPairs>
+template <int D, bool kByTiles, int kPairs>
 __global__ void __launch_bounds__(kThreads, 2)
 cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap, const AttnArgs A) {
-    constexpr int kHeads = kByTiles ? kHalf : kMaxHeads;             // heads served
+    typedef Lay<D> L;
+    constexpr int kStages = L::kStages, kHeads = kByTiles ? kHalf : kMaxHeads;       // heads served
+    constexpr int kShift = D == 128 ? 7 : 6;                         // bytes of a row, as a shift
     extern __shared__ __align__(1024) uint8_t ptc_smem[];
-    const uint32_t base = tc::smem_u32(ptc_smem), bars = base + kSmemBar;
+    const uint32_t base = tc::smem_u32(ptc_smem), bars = base + L::kSmemBar;
     const int warp = tc::warp_number(), lane = threadIdx.x & 31;
-    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(ptc_smem + kSmemBar + 8 * kNumBars);
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(ptc_smem + L::kSmemBar + 8 * L::kNumBars);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
     int *cta_status = reinterpret_cast<int *>(tmem_slot + 2);
-    float *info = reinterpret_cast<float *>(ptc_smem + kSmemInfo), *first_factors = reinterpret_cast<float *>(ptc_smem + kSmemFirst);
+    float *info = reinterpret_cast<float *>(ptc_smem + L::kSmemInfo), *first_factors = reinterpret_cast<float *>(ptc_smem + L::kSmemFirst);
     if ((base & 1023u) != 0) {                       // the swizzled tiles need a 1024-byte aligned base
         predecessor_done();
         if (threadIdx.x == 0) {
@@ -379,8 +404,8 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
     }
     auto bar = [&](int i) { return bars + 8u * i; };
     if (threadIdx.x == 0) {
-        for (int i = 0; i < kNumBars; ++i)
-            tc::mbar_init(bar(i), i == kBarPFull || i == kBarPFull + 1 ? (kByTiles ? 128 : 256) : i >= kBarIEmpty ? 257 : 1);
+        for (int i = 0; i < L::kNumBars; ++i)
+            tc::mbar_init(bar(i), i == L::kBarPFull || i == L::kBarPFull + 1 ? (kByTiles ? 128 : 256) : i >= L::kBarIEmpty ? 257 : 1);
         *abort_flag = 0;
         *cta_status = 0;
         tc::mbar_init_fence();
@@ -395,15 +420,15 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
     predecessor_done();
     successor_may_start();
 
-    const int G = A.G, tile_pages = kTile >> A.page_shift, record = record_floats(G, 128);
+    const int G = A.G, tile_pages = kTile >> A.page_shift, record = record_floats(G, D);
     auto query = [&](int u, int h, int g) {
-        return g < G ? *reinterpret_cast<const uint2 *>(static_cast<const __nv_bfloat16 *>(A.q) + ((int64_t)u * A.Hq + h * G + g) * 128 + lane * 4)
-                     : make_uint2(0, 0);
+        return g < G ? *reinterpret_cast<const Query<D> *>(static_cast<const __nv_bfloat16 *>(A.q) + ((int64_t)u * A.Hq + h * G + g) * D + lane * (D / 32))
+                     : Query<D>{};
     };
-    Task *tasks = reinterpret_cast<Task *>(ptc_smem + kSmemTask);
+    Task *tasks = reinterpret_cast<Task *>(ptc_smem + L::kSmemTask);
     // the next group's task, for the warps that do the loader's bidding
     auto wait_task = [&](int group, Task &t) {
-        if (!tc::mbar_wait_warp(bar(kBarTask + group % kInfos), group / kInfos & 1, abort_flag, cta_status)) return false;
+        if (!tc::mbar_wait_warp(bar(L::kBarTask + group % kInfos), group / kInfos & 1, abort_flag, cta_status)) return false;
         t = tasks[group % kInfos];
         return t.n != 0;
     };
@@ -426,13 +451,13 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
         int st = 0, phase = 0;
         struct Group { Task is; Pages p; };
         auto load_tile = [&](const CUtensorMap *m, const Group &g, int i) {
-            if (!tc::mbar_wait_warp(bar(kBarEmpty + st), phase ^ 1, abort_flag, cta_status)) return false;
+            if (!tc::mbar_wait_warp(bar(L::kBarEmpty + st), phase ^ 1, abort_flag, cta_status)) return false;
             const int slot = i * tile_pages + lane;
             const int x = __shfl_sync(0xFFFFFFFFu, g.p.a, slot & 31), y = __shfl_sync(0xFFFFFFFFu, g.p.b, slot & 31), id = slot < 32 ? x : y;
             const int here = min(tile_pages, ((g.is.rows + A.page - 1) >> A.page_shift) - (g.is.t + i) * tile_pages);     // pages of the tile that there are
-            if (tc::elect_one()) tc::mbar_expect_tx(bar(kBarFull + st), (uint32_t)here << (A.page_shift + 7));
+            if (tc::elect_one()) tc::mbar_expect_tx(bar(L::kBarFull + st), (uint32_t)here << (A.page_shift + kShift));
             __syncwarp();
-            if (lane < here) tc::tma_load_4d(base + st * kStageBytes + ((uint32_t)lane << (A.page_shift + 7)), m, bar(kBarFull + st), 0, 0, g.is.h, id);
+            if (lane < here) tc::tma_load_4d(base + st * L::kStageBytes + ((uint32_t)lane << (A.page_shift + kShift)), m, bar(L::kBarFull + st), 0, 0, g.is.h, id);
             __syncwarp();
             if (++st == kStages) { st = 0; phase ^= 1; }
             return true;
@@ -462,7 +487,7 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
         bool ok = true, more = walk_piece(A, cut, w);
         float factor = 0.f;                                          // of query head `lane` (from the second head on)
         Group now, next, before;
-        uint2 q[kHeads];                                             // the next head's query
+        Query<D> q[kHeads];                                          // the next head's query
         now.is.n = before.is.n = 0;
         if (more) {
             set(now, w.t0);
@@ -471,11 +496,11 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
         while (true) {
             // the task, K's tiles with those of V of the group before, the scales
             const int buffer = group % kInfos;
-            ok = tc::mbar_wait_warp(bar(kBarIEmpty + buffer), (group / kInfos & 1) ^ 1, abort_flag, cta_status);
+            ok = tc::mbar_wait_warp(bar(L::kBarIEmpty + buffer), (group / kInfos & 1) ^ 1, abort_flag, cta_status);
             if (!ok) break;
             if (lane == 0) {
                 tasks[buffer] = now.is;
-                tc::mbar_arrive(bar(kBarTask + buffer));
+                tc::mbar_arrive(bar(L::kBarTask + buffer));
             }
             if (now.is.n == 0) break;
             // the group after this one: its pages' numbers, and its head's query, on their way
@@ -498,20 +523,20 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
             to[lane] = now.p.ka; to[kMostPages + lane] = log2_of(now.p.va);
             if (lane + 32 < kMostPages) { to[lane + 32] = now.p.kb; to[kMostPages + lane + 32] = log2_of(now.p.vb); }
             __syncwarp();
-            if (lane == 0) tc::mbar_arrive(bar(kBarIFull + buffer));
+            if (lane == 0) tc::mbar_arrive(bar(L::kBarIFull + buffer));
             if (next.is.n != 0) scales(next.is.h, next.p);
             if (next.is.n != 0 && next.is.first) {                   // the next head's operand (the first one's is made below)
                 ++head;
-                ok = tc::mbar_wait_warp(bar(kBarQEmpty + (head & 1)), (head >> 1 & 1) ^ 1, abort_flag, cta_status);
+                ok = tc::mbar_wait_warp(bar(L::kBarQEmpty + (head & 1)), (head >> 1 & 1) ^ 1, abort_flag, cta_status);
                 if (!ok) break;
 #pragma unroll
                 for (int g = 0; g < kHeads; ++g) {
-                    const float f = put_query(base + kSmemQ + (head & 1) * kQCols * 128, g, q[g], A.scale_log2);
+                    const float f = put_query<D>(base + L::kSmemQ + (head & 1) * L::kQBytes, g, q[g], A.scale_log2);
                     factor = lane == g ? f : factor;
                 }
                 fence_proxy_async();
                 __syncwarp();
-                if (lane == 0) tc::mbar_arrive(bar(kBarQFull + (head & 1)));
+                if (lane == 0) tc::mbar_arrive(bar(L::kBarQFull + (head & 1)));
             }
             before = now; now = next; ++group;
         }
@@ -519,19 +544,19 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
         if (ok) ok = load_tiles(now, before);                        // (no tiles of K: the last group's V)
         if (!ok)         // winding down after a timeout: give copies already issued a moment to land
             for (int i = 0; i < kStages; ++i)
-                for (int s = 0; s < (1 << 16) && !tc::mbar_try_wait(bar(kBarFull + i), 0) && !tc::mbar_try_wait(bar(kBarFull + i), 1); ++s) {}
+                for (int s = 0; s < (1 << 16) && !tc::mbar_try_wait(bar(L::kBarFull + i), 0) && !tc::mbar_try_wait(bar(L::kBarFull + i), 1); ++s) {}
     } else if (warp == 1) {
         int st = 0, phase = 0, tile = 0, made = 0;                   // made: the logits' bars, in turn
         auto next = [&]() { if (++st == kStages) { st = 0; phase ^= 1; } };
         auto logits = [&](int group, int t, uint32_t q_lo) {
-            if (!tc::mbar_wait_warp(bar(kBarFull + st), phase, abort_flag, cta_status)) return false;
+            if (!tc::mbar_wait_warp(bar(L::kBarFull + st), phase, abort_flag, cta_status)) return false;
             tc::tc_fence_after();
-            const uint32_t a_lo = tc::desc_lo(base + st * kStageBytes), at = tmem + kColS + ((group & 1) * kGroup + t) * kQCols;
+            const uint32_t a_lo = tc::desc_lo(base + st * L::kStageBytes), at = tmem + kColS + ((group & 1) * kGroup + t) * kQCols;
             if (tc::elect_one()) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) umma_e4m3(at, a_lo + 2 * j, q_lo + 2 * j, tc::kDescSw128Hi, kIdescQK, j > 0);
-                tc::umma_commit(bar(kBarEmpty + st));
-                tc::umma_commit(bar(kBarS + made));
+                for (int j = 0; j < D / 32; ++j) umma_e4m3(at, a_lo + 2 * j, L::kDescHi, q_lo + 2 * j, L::kDescHi, kIdescQK, j > 0);
+                tc::umma_commit(bar(L::kBarEmpty + st));
+                tc::umma_commit(bar(L::kBarS + made));
             }
             __syncwarp();
             if (++made == 2 * kGroup) made = 0;
@@ -540,22 +565,22 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
         };
         auto output = [&](int t, int n, int valid) {                 // valid: rows of the last tile that the unit has
             const int pb = tile & 1;
-            if (!tc::mbar_wait_warp(bar(kBarFull + st), phase, abort_flag, cta_status)) return false;
+            if (!tc::mbar_wait_warp(bar(L::kBarFull + st), phase, abort_flag, cta_status)) return false;
             if (t == n - 1 && valid < kTile) {
                 // rows of V behind the unit's last one: zeros, since a weight of zero times a NaN would not be nothing
-                for (int i = valid * 8 + lane; i < kTile * 8; i += 32) tc::sts128(base + st * kStageBytes + i * 16, 0.f, 0.f, 0.f, 0.f);
+                for (int i = valid * (D / 16) + lane; i < kTile * (D / 16); i += 32) tc::sts128(base + st * L::kStageBytes + i * 16, 0.f, 0.f, 0.f, 0.f);
                 fence_proxy_async();
                 __syncwarp();
             }
-            if (!tc::mbar_wait_warp(bar(kBarPFull + pb), (tile >> 1) & 1, abort_flag, cta_status)) return false;
+            if (!tc::mbar_wait_warp(bar(L::kBarPFull + pb), (tile >> 1) & 1, abort_flag, cta_status)) return false;
             tc::tc_fence_after();
-            const uint32_t a_lo = tc::desc_lo(base + st * kStageBytes), p_lo = tc::desc_lo(base + kSmemP + pb * kPBytes);
+            const uint32_t a_lo = tc::desc_lo(base + st * L::kStageBytes), p_lo = tc::desc_lo(base + L::kSmemP + pb * kPBytes);
             if (tc::elect_one()) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) umma_e4m3(tmem, a_lo + 256 * j, p_lo + 64 * j, kDescPHi, kIdescPV, (t | j) != 0);
-                tc::umma_commit(bar(kBarEmpty + st));
-                tc::umma_commit(bar(kBarPEmpty + pb));
-                if (t == n - 1) tc::umma_commit(bar(kBarO));
+                for (int j = 0; j < 4; ++j) umma_e4m3(tmem, a_lo + 2 * D * j, L::kDescHi, p_lo + 64 * j, kDescPHi, kIdescPV, (t | j) != 0);
+                tc::umma_commit(bar(L::kBarEmpty + st));
+                tc::umma_commit(bar(L::kBarPEmpty + pb));
+                if (t == n - 1) tc::umma_commit(bar(L::kBarO));
             }
             __syncwarp();
             ++tile;
@@ -567,12 +592,12 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
         int group = 0, head = -1, before_n = 0, before_valid = 0;
         uint32_t q_lo = 0;
         while (wait_task(group, now)) {
-            if (tc::elect_one()) tc::mbar_arrive(bar(kBarIEmpty + group % kInfos));
+            if (tc::elect_one()) tc::mbar_arrive(bar(L::kBarIEmpty + group % kInfos));
             __syncwarp();
             if (now.first) {
                 ++head;
-                q_lo = tc::desc_lo(base + kSmemQ + (head & 1) * kQCols * 128);
-                ok = tc::mbar_wait_warp(bar(kBarQFull + (head & 1)), head >> 1 & 1, abort_flag, cta_status);
+                q_lo = tc::desc_lo(base + L::kSmemQ + (head & 1) * L::kQBytes);
+                ok = tc::mbar_wait_warp(bar(L::kBarQFull + (head & 1)), head >> 1 & 1, abort_flag, cta_status);
             }
             for (int i = 0; ok && i < max(now.n, before_n); ++i) {   // (as the loader sends them)
                 if (i < now.n) ok = logits(group, i, q_lo);
@@ -580,7 +605,7 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
             }
             if (!ok) break;
             if (now.last) {
-                if (tc::elect_one()) tc::umma_commit(bar(kBarQEmpty + (head & 1)));
+                if (tc::elect_one()) tc::umma_commit(bar(L::kBarQEmpty + (head & 1)));
                 __syncwarp();
             }
             before_n = now.n;
@@ -595,27 +620,27 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
         const int set = kByTiles ? 0 : half, g0 = kHalf * set;       // this half's heads
         constexpr int parts = kByTiles ? 2 : 1;                      // ... and tiles: all, or those with the number of the half
         const uint32_t tcols = trow + set * 8;                       // columns of their logits within a tile's
-        float *red = reinterpret_cast<float *>(ptc_smem + kSmemRed);
+        float *red = reinterpret_cast<float *>(ptc_smem + L::kSmemRed);
         Task now, done;
-        uint2 q = make_uint2(0, 0);
+        Query<D> q = {};
         const uint32_t own_u = blockIdx.x / A.Hkv;
         if (!A.cut_heads && own_u < (uint32_t)A.U) q = query(own_u, blockIdx.x - own_u * A.Hkv, e >> 5);       // (known before the lengths are)
         bool ok = true, more = wait_task(0, now);
         if (more) {                                                  // the first head's operand, a warp per query head
             if ((e >> 5) < kHeads) {
                 if (A.cut_heads) q = query(now.u, now.h, e >> 5);
-                const float f = put_query(base + kSmemQ, e >> 5, q, A.scale_log2);
+                const float f = put_query<D>(base + L::kSmemQ, e >> 5, q, A.scale_log2);
                 if (lane == 0) first_factors[e >> 5] = f;
             }
             fence_proxy_async();
         }
         epi_sync();
-        if (more && e == 0) tc::mbar_arrive(bar(kBarQFull));
+        if (more && e == 0) tc::mbar_arrive(bar(L::kBarQFull));
 
         float cq[kHalf], m[kHalf], mv[kHalf], l[kHalf], acc[kHalf];
         auto add_output = [&](int group) {                           // a group's product into acc
             if (kByTiles && half != 0) return;                       // (one thread a dim is enough)
-            ok = ok && tc::mbar_wait_warp(bar(kBarO), group & 1, abort_flag, cta_status);
+            ok = ok && tc::mbar_wait_warp(bar(L::kBarO), group & 1, abort_flag, cta_status);
             if (!ok) return;
             tc::tc_fence_after();
             float o[8], o2[8];
@@ -635,8 +660,8 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
             }
         };
         auto finish = [&](const Task &t, const float *all) {
-            if ((kByTiles && half != 0) || !ok) return;
-            float *out = A.out + ((int64_t)t.u * A.Hq + t.h * G) * 128 + row, *part = A.part + (int64_t)t.record * record;
+            if ((kByTiles && half != 0) || row >= D || !ok) return;
+            float *out = A.out + ((int64_t)t.u * A.Hq + t.h * G) * D + row, *part = A.part + (int64_t)t.record * record;
 #pragma unroll
             for (int g = 0; g < kHalf; ++g) {
                 if (g0 + g < G) {
@@ -645,10 +670,10 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
                     for (int i = 0; i < 4 * parts; ++i) sum += all[(4 * (kByTiles ? 0 : half) + i) * 3 * kHalf + 2 * kHalf + g];
                     const float o = acc[g] * tc::ex2(mv[g] - m[g] - 8.f);       // relative to the logits' maximum
                     if (t.record < 0) {
-                        out[(g0 + g) * 128] = o / sum;
+                        out[(g0 + g) * D] = o / sum;
                     } else {
-                        part[(g0 + g) * 128 + row] = o;
-                        if (row == 0) { part[G * 128 + g0 + g] = m[g]; part[G * 128 + G + g0 + g] = sum; }
+                        part[(g0 + g) * D + row] = o;
+                        if (row == 0) { part[G * D + g0 + g] = m[g]; part[G * D + G + g0 + g] = sum; }
                     }
                 }
             }
@@ -659,7 +684,7 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
             const int from = kByTiles ? (tile + half) & 1 : 0;       // this half's first tile of the group
             head += now.first;
             const float *in = info + buffer * kInfo, *factors = (head == 0 ? first_factors : in + 2 * kMostPages) + g0;
-            ok = ok && tc::mbar_wait_warp(bar(kBarIFull + buffer), group / kInfos & 1, abort_flag, cta_status);
+            ok = ok && tc::mbar_wait_warp(bar(L::kBarIFull + buffer), group / kInfos & 1, abort_flag, cta_status);
             float top[kHalf], topv[kHalf];
 #pragma unroll
             for (int g = 0; g < kHalf; ++g) { top[g] = kLowest; topv[g] = kLowest; cq[g] = ok ? factors[g] : 0.f; }
@@ -669,7 +694,7 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
             // made beside the group before, the last one.
             auto wait_logits = [&](int t) {
                 const int turn = (tile + t) / (2 * kGroup);
-                ok = ok && tc::mbar_wait_warp(bar(kBarS + tile + t - turn * 2 * kGroup), turn & 1, abort_flag, cta_status);
+                ok = ok && tc::mbar_wait_warp(bar(L::kBarS + tile + t - turn * 2 * kGroup), turn & 1, abort_flag, cta_status);
                 tc::tc_fence_after();
             };
             if (group > 0 && from < n) wait_logits(n - 1);
@@ -757,15 +782,15 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
 #pragma unroll
                     for (int k = 0; k < 4; ++k) word[k] = lower[k];
                 }
-                ok = tc::mbar_wait_warp(bar(kBarPEmpty + pb), ((i >> 1) & 1) ^ 1, abort_flag, cta_status);
+                ok = tc::mbar_wait_warp(bar(L::kBarPEmpty + pb), ((i >> 1) & 1) ^ 1, abort_flag, cta_status);
                 if (!ok) continue;
                 // the key's row of the operand: 32 weights by half, piece, head; the swizzle exchanges the halves of every other four rows
-                sts128(base + kSmemP + pb * kPBytes + row * 32 + ((set ^ ((row >> 2) & 1)) << 4), word);
+                sts128(base + L::kSmemP + pb * kPBytes + row * 32 + ((set ^ ((row >> 2) & 1)) << 4), word);
                 fence_proxy_async();
                 tc::tc_fence_before();
-                tc::mbar_arrive(bar(kBarPFull + pb));
+                tc::mbar_arrive(bar(L::kBarPFull + pb));
             }
-            tc::mbar_arrive(bar(kBarIEmpty + buffer));
+            tc::mbar_arrive(bar(L::kBarIEmpty + buffer));
             tile += n;
         }
         if (group > 0) {
@@ -781,7 +806,7 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
         const int n = A.rows[u];
         if (n < 0 || n > A.max_pages << A.page_shift) { if (threadIdx.x == 0) report(A.status, kStatusIndex); }
         if (n <= 0)
-            for (int i = threadIdx.x; i < A.Hq * 128; i += kThreads) A.out[(int64_t)u * A.Hq * 128 + i] = 0.f;
+            for (int i = threadIdx.x; i < A.Hq * D; i += kThreads) A.out[(int64_t)u * A.Hq * D + i] = 0.f;
     }
     tc::tc_fence_before();
     __syncthreads();

@@ -25,10 +25,10 @@ inline EncodeTiledFn encode_fn() {
 }
 
 // Tensor of `rank` dims (innermost first, contiguous innermost), box as given (box[0] = one 128-byte swizzle span, 64 elements of
-// bf16 or 128 bytes), 128-byte swizzle, zero fill outside the tensor.
+// bf16 or 128 bytes), in that swizzle, zero fill outside the tensor.
 // strides_bytes[i] is the stride of dim i+1.  Returns false if the driver rejects the description.
 inline bool make_map(CUtensorMapDataType type, CUtensorMap *map, const void *base, int rank, const uint64_t *dims,
-                     const uint64_t *strides_bytes, const uint32_t *box_dims) {
+                     const uint64_t *strides_bytes, const uint32_t *box_dims, CUtensorMapSwizzle swizzle = CU_TENSOR_MAP_SWIZZLE_128B) {
     EncodeTiledFn fn = encode_fn();
     if (!fn) return false;
     cuuint64_t gdim[5], gstride[4];
@@ -37,7 +37,7 @@ inline bool make_map(CUtensorMapDataType type, CUtensorMap *map, const void *bas
     for (int i = 0; i + 1 < rank; ++i) gstride[i] = strides_bytes[i];
     auto encode = [&]() {
         return fn(map, type, (cuuint32_t)rank, const_cast<void *>(base), gdim, gstride, box,
-                  estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     };
     CUresult r = encode();
@@ -49,8 +49,10 @@ inline bool make_map(CUtensorMapDataType type, CUtensorMap *map, const void *bas
 inline bool make_bf16_map(CUtensorMap *map, const void *base, int rank, const uint64_t *dims, const uint64_t *strides_bytes, const uint32_t *box_dims) {
     return make_map(CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, map, base, rank, dims, strides_bytes, box_dims);
 }
+// (bytes, rows of 128 or of 64)
 inline bool make_byte_map(CUtensorMap *map, const void *base, int rank, const uint64_t *dims, const uint64_t *strides_bytes, const uint32_t *box_dims) {
-    return make_map(CU_TENSOR_MAP_DATA_TYPE_UINT8, map, base, rank, dims, strides_bytes, box_dims);
+    return make_map(CU_TENSOR_MAP_DATA_TYPE_UINT8, map, base, rank, dims, strides_bytes, box_dims,
+                    box_dims[0] == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
 // SM count of the current device (a benign race: every thread would store the same value).

@@ -51,6 +51,9 @@ def attention_bound(size, logits, n, D):
     """How far an fp32 implementation may be from the 64-bit one, per output.  Logits: D products and their sum in fp32, the scale
     and the scale of the page, each within 2^-23 (a tensor core that truncates), plus a bf16 query as two e4m3 numbers, exact but for
     elements 2^13 times smaller than the largest, 2^-18 covers it; weights: exp2 within 2^-21 and a split into four e4m3 numbers, 2^-16;
-    sums of n weights and products, each within 2^-23.  Numerator and denominator both carry the weights' error."""
+    sums of n weights and products, each within 2^-23.  Numerator and denominator both carry the weights' error.  The split: a weight x, 256 for the
+    largest, is rounded to e4m3 four times, its rest times 16 each time; a rest is at most 2^-4 of what was rounded, so four leave 2^-16 of x,
+    unless a rest falls below e4m3's least normal number: then half a step of the last piece, 2^-10 * 16^-3 = 2^-22, is left, 2^-30 of the
+    largest weight: 2^-16 of one 2^-14 times the largest, which `size` counts weights as at least (oracle.paged_cache.attention)."""
     rel = (D + 16) * 2.0 ** -23 * logits + 2.0 ** -18 * logits + 2.0 ** -16 + 2.0 ** -20 + (n + 16) * 2.0 ** -23
     return 2 * rel[:, None] * size + 1e-30

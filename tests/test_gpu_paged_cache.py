@@ -325,7 +325,7 @@ def test_attention_of_long_and_many_units(path, D):
 def test_every_way_to_share_the_work_out(U, Hq, Hkv, lengths):
     rng = np.random.default_rng(U + Hq)
     rows = rng.integers(0, 1800, U) if lengths is None else np.array([lengths[u % len(lengths)] for u in range(U)])
-    _check(T.params(U, Hq, Hkv, 128, 64, 1, 1), rng, rows, 64)
+    _check(T.params(U, Hq, Hkv, 128 if U % 2 else 64, 64, 1, 1), rng, rows, 64)
 
 
 def test_queries_of_one_sequence_share_its_pages():
@@ -358,7 +358,7 @@ class Guarded:
         return bool((self.raw[:4096] == 0xA5).all() and (self.raw[4096 + self.t.numel() * self.t.element_size():] == 0xA5).all())
 
 
-@pytest.mark.parametrize("D,dtype,path", [(128, F.BF16, F.PATH_AUTO), (128, F.BF16, F.PATH_SIMT), (64, F.F32, F.PATH_AUTO)])
+@pytest.mark.parametrize("D,dtype,path", [(64, F.BF16, F.PATH_AUTO), (128, F.BF16, F.PATH_AUTO), (128, F.BF16, F.PATH_SIMT), (64, F.F32, F.PATH_AUTO)])
 def test_nothing_is_written_beside_the_outputs(D, dtype, path):
     """Every array of the four calls, and a workspace of exactly the size that is asked for, between guards; inputs keep their bytes."""
     rng = np.random.default_rng(D + path)
@@ -397,21 +397,23 @@ def test_nothing_is_written_beside_the_outputs(D, dtype, path):
     assert all(torch.equal(t, fresh[k]) for k, t in keep.items())
 
 
+@pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("path", [F.PATH_AUTO, F.PATH_SIMT])
-def test_sharp_and_flat_softmax_and_scales_far_apart(path):
+def test_sharp_and_flat_softmax_and_scales_far_apart(path, D):
     rng = np.random.default_rng(17 + path)
     for scale, soft in ((6.0, 0.0), (1.0, 0.7), (1e-3, 0.0), (0.0, 0.0)):
-        _check(T.params(3, 8, 2, 128, 64, 1, 1, path=path), rng, np.array([700, 65, 1500]), 64, scale=scale, softmax_scale=soft)
+        _check(T.params(3, 8, 2, D, 64, 1, 1, path=path), rng, np.array([700, 65, 1500]), 64, scale=scale, softmax_scale=soft)
     for exponents in ((-90, -60), (-30, 30), (60, 100)):
-        _check(T.params(3, 8, 2, 128, 16, 1, 1, path=path), rng, np.array([700, 65, 1500]), 16, exponents=exponents)
+        _check(T.params(3, 8, 2, D, 16, 1, 1, path=path), rng, np.array([700, 65, 1500]), 16, exponents=exponents)
 
 
+@pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("dtype,path", [(F.F32, F.PATH_AUTO), (F.BF16, F.PATH_AUTO), (F.BF16, F.PATH_SIMT)])
-def test_nan_reaches_what_it_belongs_to_and_nothing_else(dtype, path):
+def test_nan_reaches_what_it_belongs_to_and_nothing_else(dtype, path, D):
     """A NaN in a row that a unit holds, or in a query: in that unit's outputs, in those heads and (from V) in that place.  (Rows
     behind the last one hold NaN in every test here.)"""
     rng = np.random.default_rng(5)
-    rows, page, D = np.array([200, 130]), 64, 128
+    rows, page = np.array([200, 130]), 64
     p = T.params(2, 4, 2, D, page, 1, 1, dtype=dtype, path=path)
     clean, q, (ck, cv, ks, vs, table) = _check(p, rng, rows, page)
     ck2 = ck.copy()
@@ -424,7 +426,7 @@ def test_nan_reaches_what_it_belongs_to_and_nothing_else(dtype, path):
     assert np.isnan(got[1, 2:, 9]).all() and np.isnan(got).sum() == 2 and np.array_equal(got[0], clean[0])
     for bad in (np.nan, np.inf):
         q2 = q.copy()
-        q2[0, 3, 100] = bad
+        q2[0, 3, 60] = bad
         got, _ = T.attend(p, q2, ck, cv, ks, vs, table, rows)
         assert np.isnan(got[0, 3]).all() and np.isnan(got).sum() == D and np.array_equal(got[0, :3], clean[0, :3])
 
