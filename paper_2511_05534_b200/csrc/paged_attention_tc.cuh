@@ -18,9 +18,10 @@
 // A block goes through its tiles in groups of up to seven of one head, the roles of its warps one or two groups apart, across the
 // heads' borders too:
 //   warp 0     K tiles and V tiles by TMA, a box per page, into a ring of six stages of 16 KB (ten of 8): a tile of K of group c + 1 and one of V of
-//              group c in turn; the next head's query operand; the scales of a group's pages
+//              group c in turn; the scales of a group's pages
 //   warp 1     the products, in the same order; the logits of two groups stay in tensor memory
-//   warps 2-9  a thread per key of a tile: maxima of a group, then its weights; a thread per dim: the output, rescaled once a group.
+//   warps 2-9  a thread per key of a tile: maxima of a group, then its weights; a thread per dim: the output, rescaled once a group; a warp per query
+//              head: the next head's query operand.
 //              Two halves of four warps: for more than four query heads each has four of them, for fewer every other tile.  (One half
 //              alone took 1800 clocks for a tile of eight heads, longer than its share of the memory's time.)
 // Memory bounds long calls: 16 sequences of up to 33 792 rows, 686 MB of pages, 118 us, 5.8 TB/s.  Short ones are bound by the way of one group through the
@@ -38,7 +39,7 @@ constexpr int kTile = 128, kMaxHeads = 8, kHalf = 4, kGroup = 7, kThreads = 320,
 constexpr int kQCols = 2 * kMaxHeads, kPCols = 4 * kMaxHeads;            // N of the two products; by half, piece, head
 constexpr int kMostPages = kGroup * kTile / 16;                          // pages of a group
 constexpr int kInfos = 4;                                                // groups whose scales are kept
-constexpr int kInfo = 2 * kMostPages + kMaxHeads;                         // [K's scale, log2 of V's][page], the queries' factors
+constexpr int kInfo = 2 * kMostPages;                                     // [K's scale, log2 of V's][page]
 constexpr uint32_t kPBytes = kTile * kPCols;                              // the weights of a tile
 constexpr uint32_t kColS = kPCols;                                        // O in the first columns, then the two groups' logits
 static_assert(kColS + 2 * kGroup * kQCols <= kTmemCols, "tensor memory");
@@ -50,11 +51,11 @@ template <int D> struct Lay {
     static constexpr uint32_t kStageBytes = kTile * D, kQBytes = kQCols * D;
     static constexpr uint32_t kSmemQ = kStages * kStageBytes, kSmemP = kSmemQ + 2 * kQBytes, kSmemRed = kSmemP + 2 * kPBytes;
     static constexpr uint32_t kSmemInfo = kSmemRed + 2 * 8 * 3 * kHalf * 4;   // red: [group parity][warp][maxima, with V's scales, sums][head]
-    static constexpr uint32_t kSmemFirst = kSmemInfo + kInfos * kInfo * 4;    // the factors of the first head's queries
-    static constexpr uint32_t kSmemTask = kSmemFirst + kMaxHeads * 4;         // tasks: [group mod 4]
+    static constexpr uint32_t kSmemFactor = kSmemInfo + kInfos * kInfo * 4;   // the factors of the queries: [head mod 2]
+    static constexpr uint32_t kSmemTask = kSmemFactor + 2 * kMaxHeads * 4;    // tasks: [group mod 4]
     static constexpr uint32_t kSmemBar = kSmemTask + kInfos * 32;
-    static constexpr int kBarFull = 0, kBarEmpty = kStages, kBarQFull = 2 * kStages, kBarQEmpty = kBarQFull + 2,
-        kBarS = kBarQEmpty + 2 /* a tile's logits, by its number in the block */, kBarPFull = kBarS + 2 * kGroup, kBarPEmpty = kBarPFull + 2,
+    static constexpr int kBarFull = 0, kBarEmpty = kStages, kBarQFull = 2 * kStages,
+        kBarS = kBarQFull + 2 /* a tile's logits, by its number in the block */, kBarPFull = kBarS + 2 * kGroup, kBarPEmpty = kBarPFull + 2,
         kBarO = kBarPEmpty + 2, kBarTask = kBarO + 1, kBarIFull = kBarTask + kInfos, kBarIEmpty = kBarIFull + kInfos, kNumBars = kBarIEmpty + kInfos;
     static constexpr uint32_t kSmemBytes = kSmemBar + 8 * kNumBars + 16;      // (+ TMEM address, abort flag, status)
     static_assert(2 * (kSmemBytes + 1024) <= 227 * 1024, "two blocks to an SM");
@@ -336,7 +337,8 @@ __device__ __forceinline__ bool walk_next(const AttnArgs &A, Walk &w) {
 struct Task {
     int n, t, rows, u, h;                // tiles (0: no more groups), the first one's place in the unit, the unit's rows, unit, head
     int record;                          // where the part of the head goes: -1: it is all of it, else the record's number
-    int first, last;                     // of the head's groups in the piece
+    int place;                           // 1: first, 2: last of the head's groups in the piece
+    int next;                            // the first query row of the next head in the block, or -1
 };
 static_assert(sizeof(Task) == 32, "as much as Lay::kSmemTask leaves");
 
@@ -393,7 +395,7 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(ptc_smem + L::kSmemBar + 8 * L::kNumBars);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
     int *cta_status = reinterpret_cast<int *>(tmem_slot + 2);
-    float *info = reinterpret_cast<float *>(ptc_smem + L::kSmemInfo), *first_factors = reinterpret_cast<float *>(ptc_smem + L::kSmemFirst);
+    float *info = reinterpret_cast<float *>(ptc_smem + L::kSmemInfo), *factors = reinterpret_cast<float *>(ptc_smem + L::kSmemFactor);
     if ((base & 1023u) != 0) {                       // the swizzled tiles need a 1024-byte aligned base
         predecessor_done();
         if (threadIdx.x == 0) {
@@ -405,7 +407,8 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
     auto bar = [&](int i) { return bars + 8u * i; };
     if (threadIdx.x == 0) {
         for (int i = 0; i < L::kNumBars; ++i)
-            tc::mbar_init(bar(i), i == L::kBarPFull || i == L::kBarPFull + 1 ? (kByTiles ? 128 : 256) : i >= L::kBarIEmpty ? 257 : 1);
+            tc::mbar_init(bar(i), i == L::kBarPFull || i == L::kBarPFull + 1 ? (kByTiles ? 128 : 256) : i >= L::kBarIEmpty ? 257
+                                  : i == L::kBarQFull || i == L::kBarQFull + 1 ? kHeads : 1);
         *abort_flag = 0;
         *cta_status = 0;
         tc::mbar_init_fence();
@@ -421,9 +424,8 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
     successor_may_start();
 
     const int G = A.G, tile_pages = kTile >> A.page_shift, record = record_floats(G, D);
-    auto query = [&](int u, int h, int g) {
-        return g < G ? *reinterpret_cast<const Query<D> *>(static_cast<const __nv_bfloat16 *>(A.q) + ((int64_t)u * A.Hq + h * G + g) * D + lane * (D / 32))
-                     : Query<D>{};
+    auto query = [&](int first, int g) {                             // of a head's first query row and a number
+        return g < G ? *reinterpret_cast<const Query<D> *>(static_cast<const __nv_bfloat16 *>(A.q) + ((int64_t)first + g) * D + lane * (D / 32)) : Query<D>{};
     };
     Task *tasks = reinterpret_cast<Task *>(ptc_smem + L::kSmemTask);
     // the next group's task, for the warps that do the loader's bidding
@@ -473,23 +475,29 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
         // (a call whose heads cannot be cut has one for each block at most: nothing to find)
         Cut cut = {};
         if (A.cut_heads) cut = make_cut(A);
-        Walk w = {};                                                 // the head of the group after `now`
-        int group = 0, head = 0, second = 0;
+        Walk w = {}, ahead = {};                                     // the head of the group after `now`, and the one after it
+        int group = 0, second = 0;
         int4 cut_head = make_int4(0, 0, 0, 0);                       // a head that begins here and goes on in other blocks
+        bool more = walk_piece(A, cut, w), more_ahead = false;
+        auto look_ahead = [&]() {
+            ahead = w;
+            more_ahead = walk_next(A, ahead);
+            if (!more_ahead && cut.share == 0 && !second) more_ahead = walk_head(A, cut, second = 1, ahead);
+        };
         auto set = [&](Group &g, int t) {
             g.is.n = min(kGroup, w.t1 - t); g.is.t = t; g.is.rows = w.rows; g.is.u = w.u; g.is.h = w.h;
-            g.is.first = t == w.t0; g.is.last = t + g.is.n == w.t1;
+            g.is.place = (t == w.t0 ? 1 : 0) | (t + g.is.n == w.t1 ? 2 : 0);
+            g.is.next = more_ahead ? ahead.u * A.Hq + ahead.h * G : -1;
             g.is.record = w.t0 == 0 && w.t1 == w.tiles ? -1 : 2 * (int)blockIdx.x + (w.t0 == 0);
             if (w.t0 == 0 && w.t1 < w.tiles) cut_head = make_int4(w.u, w.h * G,
                 cut.share == 0 ? (w.tiles + (int)cut.per - 1) / (int)cut.per : (int)((w.head + w.tiles - 1) / cut.share - blockIdx.x + 1), G);
             numbers(g.is, g.p);
         };
-        bool ok = true, more = walk_piece(A, cut, w);
-        float factor = 0.f;                                          // of query head `lane` (from the second head on)
+        bool ok = true;
         Group now, next, before;
-        Query<D> q[kHeads];                                          // the next head's query
         now.is.n = before.is.n = 0;
         if (more) {
+            if (A.cut_heads && cut.per == 0) look_ahead();           // (a range is the block's only one)
             set(now, w.t0);
             scales(now.is.h, now.p);
         }
@@ -503,41 +511,23 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
                 tc::mbar_arrive(bar(L::kBarTask + buffer));
             }
             if (now.is.n == 0) break;
-            // the group after this one: its pages' numbers, and its head's query, on their way
+            // the group after this one: its pages' numbers on their way
             next.is.n = 0;
-            if (!now.is.last) {
+            if (!(now.is.place & 2)) {
                 set(next, now.is.t + now.is.n);
-            } else {
-                more = walk_next(A, w);
-                if (!more && cut.share == 0 && cut.per == 0 && !second) more = walk_head(A, cut, second = 1, w);
-                if (more) {
-                    set(next, w.t0);
-#pragma unroll
-                    for (int g = 0; g < kHeads; ++g) q[g] = query(w.u, w.h, g);
-                }
+            } else if (more_ahead) {
+                w = ahead;
+                look_ahead();
+                set(next, w.t0);
             }
             ok = load_tiles(now, before);
             if (!ok) break;
             float *to = info + buffer * kInfo;
-            if (lane < kMaxHeads) to[2 * kMostPages + lane] = factor;
             to[lane] = now.p.ka; to[kMostPages + lane] = log2_of(now.p.va);
             if (lane + 32 < kMostPages) { to[lane + 32] = now.p.kb; to[kMostPages + lane + 32] = log2_of(now.p.vb); }
             __syncwarp();
             if (lane == 0) tc::mbar_arrive(bar(L::kBarIFull + buffer));
             if (next.is.n != 0) scales(next.is.h, next.p);
-            if (next.is.n != 0 && next.is.first) {                   // the next head's operand (the first one's is made below)
-                ++head;
-                ok = tc::mbar_wait_warp(bar(L::kBarQEmpty + (head & 1)), (head >> 1 & 1) ^ 1, abort_flag, cta_status);
-                if (!ok) break;
-#pragma unroll
-                for (int g = 0; g < kHeads; ++g) {
-                    const float f = put_query<D>(base + L::kSmemQ + (head & 1) * L::kQBytes, g, q[g], A.scale_log2);
-                    factor = lane == g ? f : factor;
-                }
-                fence_proxy_async();
-                __syncwarp();
-                if (lane == 0) tc::mbar_arrive(bar(L::kBarQFull + (head & 1)));
-            }
             before = now; now = next; ++group;
         }
         if (A.cut_heads && lane == 0) A.cut_heads[blockIdx.x] = cut_head;
@@ -594,7 +584,7 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
         while (wait_task(group, now)) {
             if (tc::elect_one()) tc::mbar_arrive(bar(L::kBarIEmpty + group % kInfos));
             __syncwarp();
-            if (now.first) {
+            if (now.place & 1) {
                 ++head;
                 q_lo = tc::desc_lo(base + L::kSmemQ + (head & 1) * L::kQBytes);
                 ok = tc::mbar_wait_warp(bar(L::kBarQFull + (head & 1)), head >> 1 & 1, abort_flag, cta_status);
@@ -604,10 +594,6 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
                 if (ok && i < before_n) ok = output(i, before_n, before_valid);
             }
             if (!ok) break;
-            if (now.last) {
-                if (tc::elect_one()) tc::umma_commit(bar(L::kBarQEmpty + (head & 1)));
-                __syncwarp();
-            }
             before_n = now.n;
             before_valid = min(kTile, now.rows - (now.t + now.n - 1) * kTile);
             ++group;
@@ -623,19 +609,23 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
         float *red = reinterpret_cast<float *>(ptc_smem + L::kSmemRed);
         Task now, done;
         Query<D> q = {};
-        const uint32_t own_u = blockIdx.x / A.Hkv;
-        if (!A.cut_heads && own_u < (uint32_t)A.U) q = query(own_u, blockIdx.x - own_u * A.Hkv, e >> 5);       // (known before the lengths are)
-        bool ok = true, more = wait_task(0, now);
-        if (more) {                                                  // the first head's operand, a warp per query head
-            if ((e >> 5) < kHeads) {
-                if (A.cut_heads) q = query(now.u, now.h, e >> 5);
-                const float f = put_query<D>(base + L::kSmemQ, e >> 5, q, A.scale_log2);
-                if (lane == 0) first_factors[e >> 5] = f;
-            }
+        const int own = (int)blockIdx.x * G;                         // a call whose heads cannot be cut: the block's head is known before the lengths are
+        if (!A.cut_heads && own < A.U * A.Hq) q = query(own, e >> 5);
+        // a head's operand, a warp per query head; with the number of the head in the block
+        auto put = [&](int head) {
+            if ((e >> 5) >= kHeads) return;
+            const float f = put_query<D>(base + L::kSmemQ + (head & 1) * L::kQBytes, e >> 5, q, A.scale_log2);
+            if (lane == 0) factors[(head & 1) * kMaxHeads + (e >> 5)] = f;
             fence_proxy_async();
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(bar(L::kBarQFull + (head & 1)));
+        };
+        bool ok = true, more = wait_task(0, now);
+        if (more) {
+            if (A.cut_heads) q = query(now.u * A.Hq + now.h * G, e >> 5);
+            put(0);
         }
         epi_sync();
-        if (more && e == 0) tc::mbar_arrive(bar(L::kBarQFull));
 
         float cq[kHalf], m[kHalf], mv[kHalf], l[kHalf], acc[kHalf];
         auto add_output = [&](int group) {                           // a group's product into acc
@@ -682,12 +672,14 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
         for (; more; ++group, more = wait_task(group, now)) {
             const int n = now.n, first_key = now.t * kTile, buffer = group % kInfos;
             const int from = kByTiles ? (tile + half) & 1 : 0;       // this half's first tile of the group
-            head += now.first;
-            const float *in = info + buffer * kInfo, *factors = (head == 0 ? first_factors : in + 2 * kMostPages) + g0;
+            const bool first = now.place & 1;
+            head += first;
+            const float *in = info + buffer * kInfo;
+            if (first && now.next >= 0) q = query(now.next, e >> 5); // (on its way)
             ok = ok && tc::mbar_wait_warp(bar(L::kBarIFull + buffer), group / kInfos & 1, abort_flag, cta_status);
             float top[kHalf], topv[kHalf];
 #pragma unroll
-            for (int g = 0; g < kHalf; ++g) { top[g] = kLowest; topv[g] = kLowest; cq[g] = ok ? factors[g] : 0.f; }
+            for (int g = 0; g < kHalf; ++g) { top[g] = kLowest; topv[g] = kLowest; }
             const uint32_t scol = tcols + kColS + (group & 1) * kGroup * kQCols;
             float s[8];
             // The logits are there one after the other: of the first group each is waited for, of the others, which have been
@@ -698,6 +690,9 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
                 tc::tc_fence_after();
             };
             if (group > 0 && from < n) wait_logits(n - 1);
+            // (a head's factors are there when its logits are, the first one's from the beginning)
+#pragma unroll
+            for (int g = 0; g < kHalf; ++g) cq[g] = factors[(head & 1) * kMaxHeads + g0 + g];
             if (ok && group > 0 && from < n) tmem_ld8(scol + from * kQCols, s);
             for (int t = from; t < n; t += parts) {
                 if (group == 0) {
@@ -728,7 +723,6 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
                 topv[g] = warp_max(topv[g]);
                 if (lane == 0) { all[(e >> 5) * 3 * kHalf + g] = top[g]; all[(e >> 5) * 3 * kHalf + kHalf + g] = topv[g]; }
             }
-            const bool first = now.first;
             if (group > 0) {                                     // (before the barrier: behind it this group's product may begin)
                 add_output(group - 1);
                 tc::tc_fence_before();
@@ -737,6 +731,8 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
             epi_sync();
             if (first) {
                 if (group > 0) finish(done, all);
+                // (the logits of the head before this one are made, and every thread has done with its factors)
+                if (now.next >= 0) put(head + 1);
 #pragma unroll
                 for (int g = 0; g < kHalf; ++g) { m[g] = kLowest; mv[g] = kLowest; l[g] = 0.f; acc[g] = 0.f; }
                 done = now;
