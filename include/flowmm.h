@@ -303,8 +303,8 @@ flowmm_status flowmm_decode_attention(const flowmm_decode_params *p, const void 
  * `ws` as everywhere (flowmm_cache_workspace_bytes, first 256 bytes zeroed once); calls that share one are kept in order.  Page
  * numbers, slots and rows are checked before use in every build: a bad one sets the device status to FLOWMM_ERR_INDEX, nothing is
  * read or written out of bounds for it, and the outputs of its unit are not valid.  Heads (at most
- * 8 query heads a KV head), head_dim and dtype as in flowmm_decode_params.  n_pages * page_size, max_pages * page_size and
- * n_units * n_rows are below 2^31.
+ * 8 query heads a KV head), head_dim and dtype as in flowmm_decode_params.  n_pages * page_size and n_units * n_rows are
+ * below 2^31, max_pages * page_size at most 2^30.
  */
 typedef struct {
     int32_t n_units, n_q_heads, n_kv_heads, head_dim;

@@ -26,7 +26,7 @@
 //              alone took 1800 clocks for a tile of eight heads, longer than its share of the memory's time.)
 // Memory bounds long calls: 16 sequences of up to 33 792 rows, 686 MB of pages, 118 us, 5.8 TB/s.  Short ones are bound by the way of one group through the
 // block, about 6 us from the lengths to the output (one sequence of 218 rows), and by the ends of the blocks, which fall together: 64
-// sequences of up to 1690 rows, 131 MB, 35.7 us.  (Groups of two to five tiles, and smaller groups at a block's end, were no faster.)
+// sequences of up to 1690 rows, 131 MB, 36 us.  (Groups of two to five tiles, and smaller groups at a block's end, were no faster.)
 // Every wait is bounded.
 #pragma once
 #include "paged_attention.cuh"
