@@ -304,7 +304,7 @@ flowmm_status flowmm_decode_attention(const flowmm_decode_params *p, const void 
  * numbers, slots and rows are checked before use in every build: a bad one sets the device status to FLOWMM_ERR_INDEX, nothing is
  * read or written out of bounds for it, and the outputs of its unit are not valid.  Heads (at most
  * 8 query heads a KV head), head_dim and dtype as in flowmm_decode_params.  n_pages * page_size and n_units * n_rows are
- * below 2^31, max_pages * page_size at most 2^30.
+ * below 2^31, max_pages * page_size and n_rows at most 2^30.
  */
 typedef struct {
     int32_t n_units, n_q_heads, n_kv_heads, head_dim;
@@ -342,8 +342,8 @@ flowmm_status flowmm_cache_plan(const flowmm_cache_params *p, const int32_t *gro
 
 /*
  * Rows into pages.  Row t of unit u goes to slots[u][t].  The rows of a unit go to consecutive places (the rest of a page, then
- * whole pages from their first place on), as flowmm_cache_plan lays them out; -1 only behind the last row.  No page is written for
- * two units.  Per page, KV head and tensor:
+ * whole pages from their first place on), as flowmm_cache_plan lays them out; -1 only behind the last row (rows of a page whose first
+ * one has no place are not stored, and reported).  No page is written for two units.  Per page, KV head and tensor:
  *   s = the smallest power of two, 2^-96 at least, with |x| <= 448 s for all finite new rows x of the page; where the page holds
  *       rows already (the first new row is not at its first place), not below its scale s_old
  *   new codes = e4m3(x / s), old codes = e4m3(code * s_old / s), round to nearest even; NaN and infinities become NaN

@@ -1459,7 +1459,7 @@ flowmm_status validate_cache(const flowmm_cache_params *p) {
     if (p->n_q_heads % p->n_kv_heads != 0 || p->n_q_heads / p->n_kv_heads > 8) return FLOWMM_ERR_SHAPE;
     if (p->head_dim != 64 && p->head_dim != 128) return FLOWMM_ERR_SHAPE;
     if (p->page_size != 16 && p->page_size != 32 && p->page_size != 64 && p->page_size != 128) return FLOWMM_ERR_SHAPE;
-    if (p->n_pages < 1 || p->max_pages < 1 || p->n_rows < 0) return FLOWMM_ERR_SHAPE;
+    if (p->n_pages < 1 || p->max_pages < 1 || p->n_rows < 0 || p->n_rows > 1 << 30) return FLOWMM_ERR_SHAPE;
     constexpr int64_t limit = (int64_t)1 << 31;
     if ((int64_t)p->n_pages * p->page_size >= limit || (int64_t)p->max_pages * p->page_size > limit / 2 || (int64_t)p->n_units * p->n_rows >= limit)
         return FLOWMM_ERR_SHAPE;

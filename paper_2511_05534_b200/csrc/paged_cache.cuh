@@ -94,6 +94,7 @@ __global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(const PlanArgs
     const long long most = (long long)A.max_pages << A.page_shift;
     const unsigned n = A.n_pages;
     long long need_before = 0, back_before = 0;                    // of the units of earlier tiles
+    unsigned largest = 0;                                          // page number that this thread has met
     for (int u0 = 0; u0 < A.U; u0 += kPlanThreads) {
         const int u = u0 + tid;
         PlanUnit me = {0, 0, 0, 0, 0u, 0u};
@@ -158,7 +159,10 @@ __global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(const PlanArgs
 #pragma unroll
                     for (int k = 0; k < 4; ++k) x[k] = j0 + 32 * k < p.want ? A.ring[ring_place(p.at + (j0 + 32 * k - p.held), n)] : 0;
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) if (j0 + 32 * k < p.want) row[j0 + 32 * k] = x[k];
+                    for (int k = 0; k < 4; ++k) {
+                        if (j0 + 32 * k < p.want) row[j0 + 32 * k] = x[k];
+                        largest = max(largest, (unsigned)x[k]);
+                    }
                 }
                 for (int j0 = p.want + lane; j0 < p.held; j0 += 128) {
                     int x[4];
@@ -166,6 +170,7 @@ __global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(const PlanArgs
                     for (int k = 0; k < 4; ++k) x[k] = j0 + 32 * k < p.held ? row[j0 + 32 * k] : 0;
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
+                        largest = max(largest, (unsigned)x[k]);
                         const unsigned to = ring_place(p.to + (j0 + 32 * k - p.want), n);
                         if (j0 + 32 * k < p.held) A.ring[to < n ? to : to % n] = x[k];      // (the remainder: more than the ring can hold)
                     }
@@ -179,12 +184,14 @@ __global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(const PlanArgs
                 if (t < p.grow) {
                     const int pos = p.rows + t, j = pos >> A.page_shift;
                     const int id = j < p.held ? row[j] : A.ring[ring_place(p.at + (j - p.held), n)];
-                    slot = (int)(((unsigned)id << A.page_shift) | (unsigned)(pos & (A.page - 1)));
+                    largest = max(largest, (unsigned)id);              // (the slot of a number out of range would be another page's)
+                    if ((unsigned)id < n) slot = (int)(((unsigned)id << A.page_shift) | (unsigned)(pos & (A.page - 1)));
                 }
                 out[t] = slot;
             }
         }
     }
+    if (largest >= n) report(A.status, kStatusIndex);
     if (first) {
         __syncthreads();
         if (tid == 0) {
@@ -266,6 +273,9 @@ __global__ void __launch_bounds__(kTeam < 128 ? 128 : kTeam) cache_store_kernel(
     if (first < -1 && me == 0) report(A.status, kStatusIndex);
     const int held0 = first & (A.page - 1);
     const int t0 = run == 0 ? 0 : (int)run * A.page - held0, held = run == 0 ? held0 : 0;      // the page's first new row; rows that it has already
+    if (on && first == -1 && which == 0 && h == 0)                    // a unit without new rows has no slots further on either
+        for (int t = run * A.page + me; t < min(A.T, ((int)run + 1) * A.page); t += kTeam)
+            if (slots[t] != -1) report(A.status, kStatusIndex);
     on = on && first >= 0 && t0 < A.T;
     const int n = on ? min(A.T - t0, A.page - held) : 0;              // rows of this page
     const T *x = static_cast<const T *>(A.x[which]) + u * A.stride[which][0] + h * A.stride[which][1] + (int64_t)t0 * A.stride[which][2] + lane * kN;
@@ -292,7 +302,7 @@ __global__ void __launch_bounds__(kTeam < 128 ? 128 : kTeam) cache_store_kernel(
     for (int i = 0; i < kVecs; ++i) {
         const int r = row0 + i * kRows;
         if (at[i] < 0 || !on) {
-            if (at[i] < -1) report(A.status, kStatusIndex);
+            if (at[i] != -1) report(A.status, kStatusIndex);          // (a row behind one without a place, too)
             at[i] = -1;
         } else if (at[i] != slot + r) {
             at[i] = -1;

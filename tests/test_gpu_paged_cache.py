@@ -118,6 +118,28 @@ def test_plan_of_unsound_state_changes_nothing():
     assert status == 11 and all(np.array_equal(a, b) for a, b in zip(got, want))
 
 
+def test_plan_reports_bad_page_numbers_and_makes_no_slots_of_them():
+    """Numbers out of range in the table (of a page that is held, of one given back) and in the ring."""
+    page, n_pages = 16, 6
+    rows, grow = np.array([20, 20, 20], np.int32), np.array([2, 2, -20], np.int32)
+    table, ring, state = np.array([[0, 1], [2, 3], [4, 5]], np.int32), np.zeros(n_pages, np.int32), np.array([0, 0], np.int32)
+    p = T.params(3, 1, 1, 128, page, n_pages, 2, 2)
+    got, status = _plan(p, rows, grow, ring, state, table)
+    assert status == 0 and got[4].tolist() == [[20, 21], [52, 53], [-1, -1]]
+    for bad in (-1, n_pages, 1 << 28, (1 << 28) + 1, 2 ** 31 - 1, -2 ** 31):      # (2^28 pages of 16: slots that would wrap to pages 0 and 1)
+        wrong = table.copy()
+        wrong[0, 1] = bad
+        got, status = _plan(p, rows, grow, ring, state, wrong)
+        assert status == 10 and got[4].tolist() == [[-1, -1], [52, 53], [-1, -1]] and got[0].tolist() == [22, 22, 0]
+        wrong = table.copy()
+        wrong[2, 0] = bad
+        got, status = _plan(p, rows, grow, ring, state, wrong)
+        assert status == 10 and got[4].tolist() == [[20, 21], [52, 53], [-1, -1]]
+        got, status = _plan(p, np.array([16, 16, 0], np.int32), np.array([1, 1, 0], np.int32), np.array([bad, 5, 0, 0, 0, 0], np.int32),
+                            np.array([0, 2], np.int32), table)
+        assert status == 10 and got[4].tolist() == [[-1, -1], [80, -1], [-1, -1]]
+
+
 # ---- store and load ------------------------------------------------------------------------------
 
 def _store(p, k, v, slots, codes_k, codes_v, ks, vs):
@@ -217,6 +239,28 @@ def test_bad_slots_are_reported_and_write_nothing_else():
     slots = np.full_like(good, -1)
     got, status = _store(p, x, x, slots, codes, codes, scale, scale)
     assert status == 0 and np.array_equal(got[0], codes) and np.array_equal(got[2], scale)
+
+
+@pytest.mark.parametrize("n", [20, 300])
+@pytest.mark.parametrize("D,page", [(64, 16), (128, 32), (128, 128)])
+def test_rows_behind_one_without_a_place_are_reported(D, page, n):
+    """Slots of -1 in front of a unit's rows, or where a page begins: the rows of those pages are not stored, and the call says so."""
+    rng = np.random.default_rng(page + n)
+    pages = n // page + 2
+    x = T.dev(rng.standard_normal((2, 2, n, D)).astype(np.float32))
+    p = T.params(2, 2, 2, D, page, 2 * pages, pages, n, F.F32)
+    codes, scale = rng.integers(0, 256, (2 * pages, 2, page, D)).astype(np.uint8), np.ones((2 * pages, 2), np.float32)
+    good = np.stack([np.arange(n), pages * page + np.arange(n)]).astype(np.int32)
+    want, status = _store(p, x, x, good, codes, codes, scale, scale)
+    assert status == 0
+    for t0, t1 in ((0, 1), (0, 3), (0, n - 1), (n // page * page, n // page * page + 1)):
+        if t1 >= n:
+            continue                                                # (nothing behind it)
+        slots = good.copy()
+        slots[0, t0:t1] = -1
+        got, status = _store(p, x, x, slots, codes, codes, scale, scale)
+        assert status == 10 and np.array_equal(got[0][pages:], want[0][pages:]) and np.array_equal(got[2][pages:], want[2][pages:]), (t0, t1)
+        assert np.array_equal(got[0][t0 // page], codes[t0 // page])
 
 
 @pytest.mark.parametrize("dtype", [F.F32, F.BF16])

@@ -67,7 +67,7 @@ def test_refusals(lib, name):
     """Every call here is refused by a check on the host, before the library looks for a device."""
     for change, code in [(dict(n_units=0), 2), (dict(n_q_heads=7), 2), (dict(n_q_heads=18), 2), (dict(n_kv_heads=0), 2), (dict(head_dim=96), 2),
                          (dict(page_size=48), 2), (dict(page_size=0), 2), (dict(n_pages=0), 2), (dict(max_pages=0), 2), (dict(n_rows=-1), 2),
-                         (dict(n_pages=1 << 26), 2), (dict(max_pages=1 << 25), 2), (dict(max_pages=(1 << 24) + 1), 2), (dict(n_units=1 << 12, n_rows=1 << 19), 2),
+                         (dict(n_pages=1 << 26), 2), (dict(max_pages=1 << 25), 2), (dict(max_pages=(1 << 24) + 1), 2), (dict(n_units=1, n_rows=(1 << 30) + 1), 2), (dict(n_units=1 << 12, n_rows=1 << 19), 2),
                          (dict(n_units=1 << 22), 2), (dict(dtype=2), 4), (dict(softmax_scale=-1.0), 2), (dict(softmax_scale=float("nan")), 2), (dict(path=3), 2)]:
         p = F.CacheParams(**{**GOOD, **change}).c()
         assert _call(lib, name, p, _args(name)) == code, change
