@@ -342,8 +342,8 @@ flowmm_status flowmm_cache_plan(const flowmm_cache_params *p, const int32_t *gro
 
 /*
  * Rows into pages.  Row t of unit u goes to slots[u][t].  The rows of a unit go to consecutive places (the rest of a page, then
- * whole pages from their first place on), as flowmm_cache_plan lays them out; -1 only behind the last row (rows of a page whose first
- * one has no place are not stored, and reported).  No page is written for two units.  Per page, KV head and tensor:
+ * whole pages from their first place on), as flowmm_cache_plan lays them out; -1 only behind the last row (a row with a place behind one without
+ * is reported; where it is in a page whose first new row has none it is not stored).  No page is written for two units.  Per page, KV head and tensor:
  *   s = the smallest power of two, 2^-96 at least, with |x| <= 448 s for all finite new rows x of the page; where the page holds
  *       rows already (the first new row is not at its first place), not below its scale s_old
  *   new codes = e4m3(x / s), old codes = e4m3(code * s_old / s), round to nearest even; NaN and infinities become NaN

@@ -255,7 +255,9 @@ __device__ __forceinline__ uint32_t warp_max_bits(uint32_t x) { return __reduce_
 // compared as integers, two bf16 at a time, and whether a number is finite is only asked where a thread has met one that is not
 // (80 units of 1690 rows, 8 heads: 178 us with both for each element).
 // Rows of a unit fill consecutive places, so the team knows from that slot which rows are its page's; every row's own
-// slot is still looked at, and one that is not where it should be is left out and reported.
+// slot is still looked at, and one that is not where it should be is left out and reported.  Rows without a place are a unit's last ones: one
+// with a row behind it that has a place is found by the teams of K's first head.  (Found by every team, so that the pages could be left as they were: 72
+// registers for 64, 80 units of 1690 rows 132 us for 127.)
 template <typename T, int D, int kTeam, int kVecs>
 __global__ void __launch_bounds__(kTeam < 128 ? 128 : kTeam) cache_store_kernel(const StoreArgs A) {
     constexpr int kBlock = kTeam < 128 ? 128 : kTeam, kN = Elem<T>::kVec, kLanes = D / kN, kRows = kTeam / kLanes;
@@ -273,9 +275,9 @@ __global__ void __launch_bounds__(kTeam < 128 ? 128 : kTeam) cache_store_kernel(
     if (first < -1 && me == 0) report(A.status, kStatusIndex);
     const int held0 = first & (A.page - 1);
     const int t0 = run == 0 ? 0 : (int)run * A.page - held0, held = run == 0 ? held0 : 0;      // the page's first new row; rows that it has already
-    if (on && first == -1 && which == 0 && h == 0)                    // a unit without new rows has no slots further on either
-        for (int t = run * A.page + me; t < min(A.T, ((int)run + 1) * A.page); t += kTeam)
-            if (slots[t] != -1) report(A.status, kStatusIndex);
+    if (on && which == 0 && h == 0)
+        for (int t = max(1, (int)run * A.page) + me; t < min(A.T, ((int)run + 1) * A.page); t += kTeam)
+            if (slots[t - 1] == -1 && slots[t] != -1) report(A.status, kStatusIndex);
     on = on && first >= 0 && t0 < A.T;
     const int n = on ? min(A.T - t0, A.page - held) : 0;              // rows of this page
     const T *x = static_cast<const T *>(A.x[which]) + u * A.stride[which][0] + h * A.stride[which][1] + (int64_t)t0 * A.stride[which][2] + lane * kN;

@@ -751,3 +751,34 @@ def test_binding_refuses_wrong_tensors():
     fp8 = [t.view(torch.float8_e4m3fn) for t in pool[:2]] + pool[2:]
     F.flowmm_cache_store(p, k, k, torch.full((2, 8), -1, dtype=torch.int32, device="cuda"), *fp8, ws)
     assert F.flowmm_last_device_status(ws) == 0
+
+
+@pytest.mark.parametrize("dtype", [F.F32, F.BF16])
+@pytest.mark.parametrize("D,page,n", [(64, 16, 40), (64, 128, 300), (128, 32, 9), (128, 32, 70), (128, 64, 130), (128, 128, 129)])
+def test_a_row_without_a_place_between_rows_is_reported(D, page, n, dtype):
+    """A slot of -1 with a good one behind it, wherever in its page: reported; other units' pages are stored, the unit's other rows are where they were to go."""
+    rng = np.random.default_rng(page + n + D)
+    for held in (0, 5):
+        pages = P.pages(held + n, page)
+        x = T.dev(rng.standard_normal((2, 2, n, D)).astype(np.float32), dtype)
+        p = T.params(2, 2, 2, D, page, 2 * pages, pages, n, dtype)
+        codes, scale = rng.integers(0, 256, (2 * pages, 2, page, D)).astype(np.uint8), np.ones((2 * pages, 2), np.float32)
+        good = held + np.stack([np.arange(n), pages * page + np.arange(n)]).astype(np.int32)
+        want, status = _store(p, x, x, good, codes, codes, scale, scale)
+        assert status == 0
+        # an inner place, several, the last place of a page, the last but one row, a whole page and more
+        for t0, t1 in ((1, 2), (2, 5), (page - held - 1, page - held), (n - 2, n - 1), (page - held, min(n - 1, 2 * page - held)), (1, n - 1)):
+            if not 0 < t0 < t1 < n:
+                continue
+            slots = good.copy()
+            slots[0, t0:t1] = -1
+            got, status = _store(p, x, x, slots, codes, codes, scale, scale)
+            assert status == 10, (held, t0, t1)
+            assert all(np.array_equal(a[pages:], b[pages:]) for a, b in zip(got, want)), (held, t0, t1)
+            left = np.zeros((pages, page), bool)                    # places in the unit's pages that no row goes to: (page, place)
+            left.reshape(-1)[np.setdiff1d(np.arange(pages * page), slots[0])] = True
+            left[:, :held] &= np.arange(pages)[:, None] > 0         # (rows held before may be rescaled)
+            assert np.array_equal(np.moveaxis(got[0][:pages], 2, 1)[left], np.moveaxis(codes[:pages], 2, 1)[left]), (held, t0, t1)
+        slots = good.copy()
+        slots[0, n - 1:] = -1                                       # (nothing behind it: no fault)
+        assert _store(p, x, x, slots, codes, codes, scale, scale)[1] == 0
