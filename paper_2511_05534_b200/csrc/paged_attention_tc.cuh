@@ -103,7 +103,19 @@ __device__ __forceinline__ float warp_max(float x) {
     asm volatile("redux.sync.max.f32 %0, %1, 0xFFFFFFFF;" : "=f"(y) : "f"(x));      // (volatile: not to be moved to where one lane alone needs it)
     return y;
 }
-__device__ __forceinline__ void epi_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+// The epilogue's warps meet; whether all of them go on.  (A wait may run out for one warp and not for another: then all leave here.)
+__device__ __forceinline__ bool epi_all(bool ok) {
+    uint32_t all;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "setp.ne.u32 p, %1, 0;\n\t"
+        "bar.red.and.pred q, 1, 256, p;\n\t"
+        "selp.u32 %0, 1, 0, q;\n\t}"
+        : "=r"(all)
+        : "r"((uint32_t)ok)
+        : "memory");
+    return all != 0;
+}
 __device__ __forceinline__ void sts128(uint32_t addr, const uint32_t (&v)[4]) {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
 }
@@ -607,7 +619,7 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
         constexpr int parts = kByTiles ? 2 : 1;                      // ... and tiles: all, or those with the number of the half
         const uint32_t tcols = trow + set * 8;                       // columns of their logits within a tile's
         float *red = reinterpret_cast<float *>(ptc_smem + L::kSmemRed);
-        Task now, done;
+        Task now = {}, done = {};
         Query<D> q = {};
         const int own = (int)blockIdx.x * G;                         // a call whose heads cannot be cut: the block's head is known before the lengths are
         if (!A.cut_heads && own < A.U * A.Hq) q = query(own, e >> 5);
@@ -620,12 +632,20 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
             __syncwarp();
             if (lane == 0) tc::mbar_arrive(bar(L::kBarQFull + (head & 1)));
         };
-        bool ok = true, more = wait_task(0, now);
-        if (more) {
+        // The group's task; false behind the last one.  A warp whose wait has run out goes on, without work, to the next meeting: they are
+        // as many for every warp.
+        bool ok = true;
+        auto take_task = [&](int group) {
+            ok = ok && tc::mbar_wait_warp(bar(L::kBarTask + group % kInfos), group / kInfos & 1, abort_flag, cta_status);
+            if (ok) now = tasks[group % kInfos];
+            return !ok || now.n != 0;
+        };
+        bool more = take_task(0);
+        if (ok && more) {
             if (A.cut_heads) q = query(now.u * A.Hq + now.h * G, e >> 5);
             put(0);
         }
-        epi_sync();
+        bool together = epi_all(ok);
 
         float cq[kHalf], m[kHalf], mv[kHalf], l[kHalf], acc[kHalf];
         auto add_output = [&](int group) {                           // a group's product into acc
@@ -669,7 +689,7 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
             }
         };
         int group = 0, head = -1, tile = 0;
-        for (; more; ++group, more = wait_task(group, now)) {
+        for (; together && more; ++group, more = take_task(group)) {
             const int n = now.n, first_key = now.t * kTile, buffer = group % kInfos;
             const int from = kByTiles ? (tile + half) & 1 : 0;       // this half's first tile of the group
             const bool first = now.place & 1;
@@ -728,7 +748,10 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
                 tc::tc_fence_before();
                 if (first) leave_sums(all);
             }
-            epi_sync();
+            if (!epi_all(ok)) {
+                together = false;
+                break;
+            }
             if (first) {
                 if (group > 0) finish(done, all);
                 // (the logits of the head before this one are made, and every thread has done with its factors)
@@ -789,12 +812,11 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
             tc::mbar_arrive(bar(L::kBarIEmpty + buffer));
             tile += n;
         }
-        if (group > 0) {
+        if (together && group > 0) {
             add_output(group - 1);
             float *all = red + (group & 1) * 8 * 3 * kHalf;
             leave_sums(all);
-            epi_sync();
-            finish(done, all);
+            if (epi_all(ok)) finish(done, all);
         }
     }
     // units without rows, shared out over the blocks
