@@ -719,8 +719,8 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
                     wait_logits(t);
                     if (ok) tmem_ld8(scol + t * kQCols, s);
                 }
+                tmem_ld_wait(s);                                     // (also where a wait has run out with a read on its way)
                 if (!ok) continue;
-                tmem_ld_wait(s);
                 float z[kHalf];
 #pragma unroll
                 for (int g = 0; g < kHalf; ++g) z[g] = fmaf(s[4 + g], 0.0625f, s[g]);
@@ -776,8 +776,8 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
             if (ok && from < n) tmem_ld8(scol + from * kQCols, s);
             for (int t = from; t < n; t += parts) {
                 const int i = tile + t, pb = i & 1;
-                if (!ok) continue;
                 tmem_ld_wait(s);
+                if (!ok) continue;
                 const bool valid = first_key + t * kTile + row < now.rows;
                 const int j = (t * kTile + row) >> A.page_shift;
                 const float ks = in[j], lv = in[kMostPages + j] + 8.f;                  // (weights times 256)

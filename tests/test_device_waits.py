@@ -34,3 +34,10 @@ def test_warps_that_meet_in_a_loop_leave_it_together():
     # left at once, and with no other barrier behind
     assert re.search(r"if \(!epi_all\(ok\)\) \{\s*together = false;\s*break;", meeting[0])
     assert re.search(r"if \(together && group > 0\)", kernel)
+
+
+def test_a_tensor_memory_read_on_its_way_is_waited_for_also_after_a_give_up():
+    """Its registers would be written when they already hold something else."""
+    text = _text("paged_attention_tc.cuh")
+    kernel = _body(text, text.index("cache_attention_tc_kernel(const __grid_constant__"))
+    assert kernel.count("tmem_ld_wait(s);") == 2 and len(re.findall(r"tmem_ld_wait\(s\);\s*if \(!ok\) continue;", kernel)) == 2
