@@ -128,9 +128,7 @@ decode_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant
             __syncwarp();
             if (++st == kStages) { st = 0; phase ^= 1; }
         }
-        if (!ok)         // winding down after a timeout: give copies already issued a moment to land
-            for (int i = 0; i < kStages; ++i)
-                for (int s = 0; s < (1 << 16) && !tc::mbar_try_wait(bar(kBarFull + i), 0) && !tc::mbar_try_wait(bar(kBarFull + i), 1); ++s) {}
+        tc::copies_land(bar(kBarFull), 8, kStages, st, phase);
         // the call's status word starts at zero; here, because this warp has nothing left to do (other CTAs may have reported already)
         if (blockIdx.x == 0 && blockIdx.y == 0 && tc::elect_one()) status_write(A.status, A.call, 0);
     } else if (warp == 1) {

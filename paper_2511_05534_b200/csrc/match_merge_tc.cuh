@@ -126,22 +126,18 @@ match_merge_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_con
         }
         __syncwarp();
     };
-    // winding down after a timeout: copies already issued to n barriers get a moment to land
-    auto let_land = [&](int first, int n) {
-        for (int b = 0; b < n; ++b)
-            for (int s = 0; s < (1 << 16) && !tc::mbar_try_wait(bar(first + b), 0) && !tc::mbar_try_wait(bar(first + b), 1); ++s) {}
-    };
 
     if (warp == 0) {
         bool ok = true;
-        int i = 0, it = 0;
-        for (int uh = blockIdx.x; ok && uh < A.n_items; uh += gridDim.x, ++it) {
+        int i = 0, it = 0;                                           // tiles, candidates of heads so far
+        for (int uh = blockIdx.x; ok && uh < A.n_items; uh += gridDim.x) {
             const int u = uh / A.Hkv, h = uh - u * A.Hkv, hp = it & 1;
-            for (int c = 0; ok && c < nt; ++c, ++i) {
+            for (int c = 0; ok && c < nt; ++c) {
                 const int st = i % kStagesK;
                 ok = tc::mbar_wait_warp(bar(kBarKEmpty + st), ((i / kStagesK) & 1) ^ 1, abort_flag, A.status);
                 if (!ok) break;
                 load_tile(base + st * kStageBytes, &kmap, bar(kBarKFull + st), c, h, u);
+                ++i;
                 if (c == 0) {                                        // the head's candidates, right behind its first tile
                     ok = tc::mbar_wait_warp(bar(kBarCandEmpty), (it & 1) ^ 1, abort_flag, A.status) &&
                          tc::mbar_wait_warp(bar(kBarMetaEmpty + hp), ((it >> 1) & 1) ^ 1, abort_flag, A.status);
@@ -155,22 +151,25 @@ match_merge_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_con
                         tc::bulk_load(md + 4u * (uint32_t)A.Ctot, A.cand_slot + (int64_t)uh * A.Ctot, 4u * (uint32_t)A.Ctot, full);
                     }
                     __syncwarp();
+                    ++it;
                 }
             }
         }
-        if (!ok) { let_land(kBarKFull, kStagesK); let_land(kBarCandFull, 2); }
+        tc::copies_land(bar(kBarKFull), 8, kStagesK, i);
+        tc::copies_land(bar(kBarCandFull), 8, 2, it);
     } else if (warp == kLoadWarp) {
         bool ok = true;
         int j = 0;                                                   // tiles so far: K's and V's of every step
         for (int uh = blockIdx.x; ok && uh < A.n_items; uh += gridDim.x) {
             const int u = uh / A.Hkv, h = uh - u * A.Hkv;
-            for (int t = 0; ok && t < 2 * nt; ++t, ++j) {
+            for (int t = 0; t < 2 * nt; ++t, ++j) {
                 const int st = j % kStagesX;
                 ok = tc::mbar_wait_warp(bar(kBarXEmpty + st), ((j / kStagesX) & 1) ^ 1, abort_flag, A.status);
-                if (ok) load_tile(base + kSmemX + st * kStageBytes, t & 1 ? &vmap : &kmap, bar(kBarXFull + st), t >> 1, h, u);
+                if (!ok) break;
+                load_tile(base + kSmemX + st * kStageBytes, t & 1 ? &vmap : &kmap, bar(kBarXFull + st), t >> 1, h, u);
             }
         }
-        if (!ok) let_land(kBarXFull, kStagesX);
+        tc::copies_land(bar(kBarXFull), 8, kStagesX, j);
     } else if (warp == 1) {
         const uint32_t idesc_out = tc::idesc_bf16(128, (uint32_t)N) | (1u << 15);        // A operand MN-major
         const uint32_t lead = (kPanel >> 4) << 16;                                       // (and the stride between its panels)

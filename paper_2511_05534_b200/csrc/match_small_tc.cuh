@@ -181,8 +181,8 @@ match_small_tc_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_co
     // every role walks the heads of the run: tiles [t_lo, t_hi) of head uh, hc heads before it, tile number i of the run
     if (warp == 0) {
         bool ok = true;
-        int hc = 0;
-        for (int g = g_lo; ok && g < g_hi; ++hc) {
+        int hc = 0, g = g_lo;
+        for (; ok && g < g_hi; ++hc) {
             const int uh = (int)A.by_nt.div(g), u = (int)A.by_hkv.div(uh), h = uh - u * A.Hkv, hp = hc % n_bbuf;
             ok = tc::mbar_wait_warp(bar(kBarBEmpty + hp), ((hc / n_bbuf) & 1) ^ 1, abort_flag, A.status);
             if (!ok) break;
@@ -208,12 +208,8 @@ match_small_tc_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_co
                 __syncwarp();
             }
         }
-        if (!ok) {       // winding down after a timeout: give copies already issued a moment to land
-            for (int b = 0; b < kStages; ++b)
-                for (int s = 0; s < (1 << 16) && !tc::mbar_try_wait(bar(kBarFull + b), 0) && !tc::mbar_try_wait(bar(kBarFull + b), 1); ++s) {}
-            for (int b = 0; b < 2; ++b)
-                for (int s = 0; s < (1 << 16) && !tc::mbar_try_wait(bar(kBarBFull + b), 0) && !tc::mbar_try_wait(bar(kBarBFull + b), 1); ++s) {}
-        }
+        tc::copies_land(bar(kBarFull), 8, kStages, g - g_lo);
+        tc::copies_land(bar(kBarBFull), 8, n_bbuf, hc);
     } else if (warp == 1) {
         bool ok = true;
         int hc = 0;

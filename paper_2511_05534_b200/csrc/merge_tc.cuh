@@ -180,9 +180,7 @@ merge_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
                     if (++st == A.n_stages) { st = 0; phase ^= 1; }
                 }
         }
-        if (!ok)         // winding down after a timeout: give copies already issued a moment to land
-            for (int i = 0; i < A.n_stages; ++i)
-                for (int n = 0; n < (1 << 16) && !tc::mbar_try_wait(bar(kBarFull + i), 0) && !tc::mbar_try_wait(bar(kBarFull + i), 1); ++n) {}
+        tc::copies_land(bar(kBarFull), 8, A.n_stages, st, phase);
     } else if (warp == 1) {
         const uint32_t idesc = tc::idesc_bf16(128, (uint32_t)N) | (1u << 15);           // A operand MN-major
         const uint32_t a_hi = tc::kDescSw128Hi, a_lead = (kPanel >> 4) << 16;            // (and the stride between its panels)

@@ -544,9 +544,7 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
         }
         if (A.cut_heads && lane == 0) A.cut_heads[blockIdx.x] = cut_head;
         if (ok) ok = load_tiles(now, before);                        // (no tiles of K: the last group's V)
-        if (!ok)         // winding down after a timeout: give copies already issued a moment to land
-            for (int i = 0; i < kStages; ++i)
-                for (int s = 0; s < (1 << 16) && !tc::mbar_try_wait(bar(L::kBarFull + i), 0) && !tc::mbar_try_wait(bar(L::kBarFull + i), 1); ++s) {}
+        tc::copies_land(bar(L::kBarFull), 8, kStages, st, phase);
     } else if (warp == 1) {
         int st = 0, phase = 0, tile = 0, made = 0;                   // made: the logits' bars, in turn
         auto next = [&]() { if (++st == kStages) { st = 0; phase ^= 1; } };

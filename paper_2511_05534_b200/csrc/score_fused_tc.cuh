@@ -127,12 +127,8 @@ score_fused_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
                 __syncwarp();
             }
         }
-        if (!ok) {       // winding down after a timeout: give copies already issued a moment to land
-            for (int b = 0; b < kStages; ++b)
-                for (int s = 0; s < (1 << 16) && !tc::mbar_try_wait(bar(kBarFull + b), 0) && !tc::mbar_try_wait(bar(kBarFull + b), 1); ++s) {}
-            for (int b = 0; b < 2; ++b)
-                for (int s = 0; s < (1 << 16) && !tc::mbar_try_wait(bar(kBarQFull + b), 0) && !tc::mbar_try_wait(bar(kBarQFull + b), 1); ++s) {}
-        }
+        tc::copies_land(bar(kBarFull), 8, kStages, i);
+        tc::copies_land(bar(kBarQFull), 8, 2, it);
     } else if (warp == 1) {
         constexpr uint32_t idesc = tc::idesc_bf16(kTile, GW);
         bool ok = true;

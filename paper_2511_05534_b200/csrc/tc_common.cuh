@@ -7,6 +7,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include "ring.cuh"
+
 namespace flowmm {
 namespace tc {
 
@@ -113,6 +115,16 @@ __device__ __forceinline__ bool mbar_wait_both_warp(uint32_t bar0, uint32_t pari
     if (__all_sync(0xFFFFFFFFu, there && too)) return true;
     return mbar_wait_warp(bar0, parity0, abort_flag, status_word) && mbar_wait_warp(bar1, parity1, abort_flag, status_word);
 }
+
+// The wait, by the warp that issues a ring's copies, until they have all landed: a block that ended before would leave its shared memory to
+// copies still on their way.  Where all went well their readers wait for them anyway.  Bounded, and whatever the abort flag says.  n stages, whose barriers
+// are `step` bytes apart from `full` on; `copies` have been issued, or the next one goes to stage `st` in round `phase`.
+constexpr int kLandSpins = 1 << 14;
+__device__ __forceinline__ void copies_land(uint32_t full, uint32_t step, int n, int st, int phase) {
+    for (int i = 0; i < n; ++i)
+        for (int s = 0; s < kLandSpins && !mbar_try_wait_for(full + i * step, last_copy_parity(i, st, phase), kWaitSuspendNs); ++s) {}
+}
+__device__ __forceinline__ void copies_land(uint32_t full, uint32_t step, int n, int copies) { copies_land(full, step, n, copies % n, copies / n & 1); }
 
 // ---- TMA ---------------------------------------------------------------------------------------
 __device__ __forceinline__ void tma_prefetch_desc(const CUtensorMap *m) {

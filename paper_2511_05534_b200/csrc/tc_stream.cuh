@@ -172,10 +172,11 @@ struct Skel {
     static __device__ __forceinline__ void producer(const Ctx &c, const CUtensorMap *ma, const CUtensorMap *mb, int n_items,
                                                     uint32_t a_bytes, uint32_t b_bytes, PlanFn plan, int *status) {
         int ia[2] = {0, 0}, bt = 0;
-        bool ok = true;
+        bool ok = true, extra = false;
         for (int item = blockIdx.x; ok && item < n_items; item += gridDim.x) {
             const TilePlan p = plan(item);
             if (p.empty()) continue;
+            extra = p.extra != nullptr;                      // (of every item or of none)
             for (int t = 0; ok && t < p.n_tiles; ++t) {
                 const int sb = bt % BST;
                 if (!p.reuse_b) ok = tc::mbar_wait_warp(c.bar(kBarBEmpty + sb), ((bt / BST) & 1) ^ 1, c.abort_flag, status);
@@ -218,12 +219,10 @@ struct Skel {
                 }
             }
         }
-        if (!ok) {          // winding down after a timeout: give copies already issued a moment to land
-            for (int i = 0; kLoadsA && i < 2 * AST; ++i)
-                for (int s = 0; s < (1 << 16) && !tc::mbar_try_wait(c.bar(kBarAFull + i), 0) && !tc::mbar_try_wait(c.bar(kBarAFull + i), 1); ++s) {}
-            for (int i = 0; i < BST; ++i)
-                for (int s = 0; s < (1 << 16) && !tc::mbar_try_wait(c.bar(kBarBFull + i), 0) && !tc::mbar_try_wait(c.bar(kBarBFull + i), 1); ++s) {}
-        }
+        tc::copies_land(c.bar(kBarBFull), 8, BST, bt);
+        if (extra) tc::copies_land(c.bar(kBarXFull), 8, kExtraSlots, bt);
+        if (kLoadsA)
+            for (int h = 0; h < 2; ++h) tc::copies_land(c.bar(kBarAFull + h), 16, AST, ia[h]);
     }
 
     // Call from a whole warp.  kQuads: accumulators are handed around by quad, else by half.
