@@ -18,9 +18,10 @@ from typing import Optional
 
 import torch
 
+from .build import marshal_path
+
 _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libflowmm.so")
-MARSHAL_PATH = os.path.join(_PKG, "_marshal.so")
 
 F32, BF16 = 0, 1
 INTRA, CROSS = 0, 1
@@ -409,9 +410,10 @@ def _load_marshal():
     """The module that looks at the tensors of the paged cache's calls and passes their addresses on (csrc/marshal.cpp)."""
     global _marshal
     if _marshal is None:
-        if not os.path.exists(MARSHAL_PATH):
-            raise FileNotFoundError("%s is missing: build it with `python -m paper_2511_05534_b200.build`" % MARSHAL_PATH)
-        spec = importlib.util.spec_from_loader("_marshal", importlib.machinery.ExtensionFileLoader("_marshal", MARSHAL_PATH))
+        path = marshal_path()
+        if not os.path.exists(path):
+            raise FileNotFoundError("%s is missing: build it with `python -m paper_2511_05534_b200.build`" % path)
+        spec = importlib.util.spec_from_loader("_marshal", importlib.machinery.ExtensionFileLoader("_marshal", path))
         _marshal = importlib.util.module_from_spec(spec)
     return _marshal
 

@@ -1,10 +1,12 @@
-"""Builds the CUDA library (libflowmm.so, nvcc for sm_100a) and the Python marshalling module beside it (_marshal.so, g++) in-tree."""
+"""Builds the CUDA library (libflowmm.so, nvcc for sm_100a) and the Python marshalling module beside it (_marshal.<tag>.so, g++) in-tree."""
 from __future__ import annotations
 
 import os
+import re
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_PKG)
@@ -12,7 +14,6 @@ CSRC = os.path.join(_PKG, "csrc")
 LIB_PATH = os.path.join(_PKG, "libflowmm.so")
 DEBUG_LIB_PATH = os.path.join(_PKG, "libflowmm_debug.so")     # the same sources with -DFLOWMM_DEBUG (index checks)
 SOURCES = ["flowmm_api.cu"]
-MARSHAL_PATH = os.path.join(_PKG, "_marshal.so")
 MARSHAL_SOURCE = "marshal.cpp"
 
 
@@ -32,22 +33,27 @@ def nvcc_command(out: str, verbose_ptxas: bool = False, debug: bool = False):
     return cmd + [os.path.join(CSRC, s) for s in SOURCES]
 
 
-def _build_marshal(force: bool) -> None:
-    source = os.path.join(CSRC, MARSHAL_SOURCE)
-    newest = max(os.path.getmtime(source), os.path.getmtime(os.path.join(_ROOT, "include", "flowmm.h")))
-    if not force and os.path.exists(MARSHAL_PATH) and os.path.getmtime(MARSHAL_PATH) >= newest:
-        return
-    import sysconfig
+def marshal_path() -> str:
+    """Where the marshalling module is that was built for this interpreter and this torch, whose objects' layouts it holds."""
+    import torch
+    tag = "%s.torch-%s" % (sysconfig.get_config_var("SOABI"), torch.__version__)
+    return os.path.join(_PKG, "_marshal.%s.so" % re.sub(r"[^0-9A-Za-z.]+", "-", tag))
 
+
+def _build_marshal(force: bool) -> None:
+    path, source = marshal_path(), os.path.join(CSRC, MARSHAL_SOURCE)
+    newest = max(os.path.getmtime(source), os.path.getmtime(os.path.join(_ROOT, "include", "flowmm.h")))
+    if not force and os.path.exists(path) and os.path.getmtime(path) >= newest:
+        return
     import torch
     from torch.utils import cpp_extension
-    tmp = MARSHAL_PATH + ".%d.tmp" % os.getpid()
+    tmp = path + ".%d.tmp" % os.getpid()
     cuda = os.path.join(os.path.dirname(os.path.dirname(os.path.realpath(shutil.which("nvcc") or "/usr/local/cuda/bin/nvcc"))), "include")
     include = cpp_extension.include_paths() + [cuda, sysconfig.get_paths()["include"], os.path.join(_ROOT, "include")]
     subprocess.check_call(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch.compiled_with_cxx11_abi(),
                            *("-I" + d for d in include), source, "-o", tmp,
                            *("-L" + d for d in cpp_extension.library_paths()), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"])
-    os.replace(tmp, MARSHAL_PATH)
+    os.replace(tmp, path)
 
 
 def build(force: bool = False, verbose_ptxas: bool = False, debug: bool = False) -> str:

@@ -1,0 +1,23 @@
+"""The marshalling module and the library are built, found and copied as a program's tree changes: no GPU."""
+import os
+
+import pytest
+import torch
+
+from paper_2511_05534_b200 import binding as F
+from paper_2511_05534_b200 import build
+
+
+def test_a_module_of_another_torch_or_interpreter_is_not_loaded(monkeypatch):
+    """It knows where torch's and Python's objects have their fields: one that was built for others would read addresses from elsewhere."""
+    build.build()
+    F._load_marshal()
+    here = build.marshal_path()
+    assert os.path.exists(here)
+    for change in (lambda m: m.setattr(torch, "__version__", "0.0.0+other"), lambda m: m.setattr("sysconfig.get_config_var", lambda name: "cpython-39-other")):
+        with monkeypatch.context() as m:
+            change(m)
+            m.setattr(F, "_marshal", None)
+            assert build.marshal_path() != here and not os.path.exists(build.marshal_path())
+            with pytest.raises(FileNotFoundError, match="build"):
+                F._load_marshal()
