@@ -59,13 +59,13 @@ def _build_marshal(force: bool) -> None:
 def build(force: bool = False, verbose_ptxas: bool = False, debug: bool = False) -> str:
     """Compile if the library is missing or older than any source; returns its path.  debug: the build with
     index checks (libflowmm_debug.so) instead of the release library."""
-    if not debug:
-        _build_marshal(force)
     path = DEBUG_LIB_PATH if debug else LIB_PATH
     if force or not os.path.exists(path) or os.path.getmtime(path) < _newest_source_mtime():
         tmp = path + ".%d.tmp" % os.getpid()
         subprocess.check_call(nvcc_command(tmp, verbose_ptxas, debug))
         os.replace(tmp, path)
+    if not debug:
+        _build_marshal(force)                # (last: the library needs neither g++ nor the headers of Python and torch)
     return path
 
 

@@ -21,3 +21,20 @@ def test_a_module_of_another_torch_or_interpreter_is_not_loaded(monkeypatch):
             assert build.marshal_path() != here and not os.path.exists(build.marshal_path())
             with pytest.raises(FileNotFoundError, match="build"):
                 F._load_marshal()
+
+
+def test_the_library_is_built_without_what_the_module_needs(monkeypatch, tmp_path):
+    """No g++, no headers of Python or torch: the C library is there all the same, and the build says what is missing."""
+    commands = []
+
+    def run(command, *args, **kwargs):
+        commands.append(command[0])
+        if command[0] != "nvcc":
+            raise FileNotFoundError(command[0])
+        open(command[command.index("-o") + 1], "w").close()
+    monkeypatch.setattr(build.subprocess, "check_call", run)
+    monkeypatch.setattr(build, "LIB_PATH", str(tmp_path / "libflowmm.so"))
+    monkeypatch.setattr(build, "marshal_path", lambda: str(tmp_path / "_marshal.so"))
+    with pytest.raises(FileNotFoundError, match="g\\+\\+"):
+        build.build(force=True)
+    assert commands == ["nvcc", "g++"] and os.path.exists(build.LIB_PATH) and not os.path.exists(build.marshal_path())
