@@ -393,6 +393,9 @@ class CacheParams:
         object.__setattr__(self, name, value)
         object.__setattr__(self, "calls", {})
 
+    def __reduce__(self):                    # (copies and pickles: the fields alone, a handle is an address of this process)
+        return type(self), _CACHE_FIELDS(self)
+
     def c(self) -> _CCacheParams:
         dense = (self.n_kv_heads * self.n_rows * self.head_dim, self.n_rows * self.head_dim, self.head_dim)
         cp = _CCacheParams(*_CACHE_FIELDS(self))

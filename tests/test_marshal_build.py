@@ -1,5 +1,8 @@
 """The marshalling module and the library are built, found and copied as a program's tree changes: no GPU."""
+import copy
+import dataclasses
 import os
+import pickle
 
 import pytest
 import torch
@@ -38,3 +41,19 @@ def test_the_library_is_built_without_what_the_module_needs(monkeypatch, tmp_pat
     with pytest.raises(FileNotFoundError, match="g\\+\\+"):
         build.build(force=True)
     assert commands == ["nvcc", "g++"] and os.path.exists(build.LIB_PATH) and not os.path.exists(build.marshal_path())
+
+
+def test_params_are_copied_and_sent_on_after_a_call():
+    """What a call leaves in them is an address of this process and of these fields: copies begin without it."""
+    build.build()
+    p = F.CacheParams(2, 8, 2, 128, 64, 10, 4, 8, softmax_scale=0.5)
+    F._cache_call(p, "flowmm_cache_plan")
+    assert p.calls
+    for q in (copy.copy(p), copy.deepcopy(p), pickle.loads(pickle.dumps(p)), dataclasses.replace(p)):
+        assert q == p and not q.calls and p.calls
+        q.n_rows = 3
+        F._cache_call(q, "flowmm_cache_plan")
+        assert p.n_rows == 8 and q.calls != p.calls
+    assert p.calls
+    p.n_rows = 3
+    assert not p.calls
