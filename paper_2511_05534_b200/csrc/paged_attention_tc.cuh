@@ -7,7 +7,8 @@
 //   O[dim, head]: a weight is kept as four e4m3 numbers, each the rounded rest of the one before times 16, within 2^-16 of
 //                 itself or 2^-30 of the largest: N = 8 heads x 4.  (Two would do for a bf16 result; the time without any splitting is 1 % less where memory bounds.)
 // The pages' scales join in fp32: K's on the logits; V's in the exponent of the weights, w_j = 2^(z_j + log2 sv_j - max), with a maximum of
-// its own, so that the largest weight is 1 whatever the scales are.  The sum of the softmax, sum_j 2^(z_j - max z), is apart.
+// its own, so that the largest weight is 1 whatever the scales are.  The sum of the softmax, sum_j 2^(z_j - max z), is apart.  The second maximum is held as
+// what it is above the first, and weights are formed from z_j - max z, a number of its own size: log2 sv_j would be lost next to logits of 2^24.
 //
 // How the work is shared out over the blocks of the launch, two to an SM, is found on the device, where alone the lengths are known (Cut).
 // Few heads: a block has one range of one head, all of the same length but for a head's last one.  Many: a block has two whole heads, or the
@@ -40,6 +41,7 @@ constexpr int kQCols = 2 * kMaxHeads, kPCols = 4 * kMaxHeads;            // N of
 constexpr int kMostPages = kGroup * kTile / 16;                          // pages of a group
 constexpr int kInfos = 4;                                                // groups whose scales are kept
 constexpr int kInfo = 2 * kMostPages;                                     // [K's scale, log2 of V's][page]
+constexpr float kFar = 1048576.f;                                         // a logit (log2) beyond which V's scales are not added to it
 constexpr uint32_t kPBytes = kTile * kPCols;                              // the weights of a tile
 constexpr uint32_t kColS = kPCols;                                        // O in the first columns, then the two groups' logits
 static_assert(kColS + 2 * kGroup * kQCols <= kTmemCols, "tensor memory");
@@ -645,7 +647,7 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
         }
         bool together = epi_all(ok);
 
-        float cq[kHalf], m[kHalf], mv[kHalf], l[kHalf], acc[kHalf];
+        float cq[kHalf], m[kHalf], mr[kHalf], l[kHalf], acc[kHalf];  // m: the maximum; mr: of the weights with V's scales, above it
         auto add_output = [&](int group) {                           // a group's product into acc
             if (kByTiles && half != 0) return;                       // (one thread a dim is enough)
             ok = ok && tc::mbar_wait_warp(bar(L::kBarO), group & 1, abort_flag, cta_status);
@@ -676,7 +678,7 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
                     float sum = 0.f;
 #pragma unroll
                     for (int i = 0; i < 4 * parts; ++i) sum += all[(4 * (kByTiles ? 0 : half) + i) * 3 * kHalf + 2 * kHalf + g];
-                    const float o = acc[g] * tc::ex2(mv[g] - m[g] - 8.f);       // relative to the logits' maximum
+                    const float o = acc[g] * tc::ex2(mr[g] - 8.f);       // relative to the logits' maximum
                     if (t.record < 0) {
                         out[(g0 + g) * D] = o / sum;
                     } else {
@@ -728,7 +730,7 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
                     const float ks = in[j], lv = in[kMostPages + j];
 #pragma unroll
                     for (int g = 0; g < kHalf; ++g) {
-                        const float x = z[g] * (ks * cq[g]);
+                        const float x = __fmul_rn(z[g], ks * cq[g]);
                         top[g] = fmaxf(top[g], x);
                         topv[g] = fmaxf(topv[g], x + lv);
                     }
@@ -755,21 +757,32 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
                 // (the logits of the head before this one are made, and every thread has done with its factors)
                 if (now.next >= 0) put(head + 1);
 #pragma unroll
-                for (int g = 0; g < kHalf; ++g) { m[g] = kLowest; mv[g] = kLowest; l[g] = 0.f; acc[g] = 0.f; }
+                for (int g = 0; g < kHalf; ++g) { m[g] = kLowest; mr[g] = 0.f; l[g] = 0.f; acc[g] = 0.f; }
                 done = now;
             }
+            // Beyond kFar log2 of V's scale is lost next to a logit, and the difference of the two maxima is not what it should be: the second one is
+            // then said to be the largest of the group's scales above the first, which no weight passes either.  (Found in every group: under a branch for the
+            // far ones the code around it was slower, 72.8 us for 71.2, 200 units of up to 2200 rows, 8 heads of 4 query heads of 64.)
+            const int pages = (min(n * kTile, now.rows - first_key) + A.page - 1) >> A.page_shift;
+            const float most = warp_max(fmaxf(lane < pages ? in[kMostPages + lane] : kLowest, lane + 32 < pages ? in[kMostPages + lane + 32] : kLowest));
+            float a[kHalf], b[kHalf];
 #pragma unroll
             for (int g = 0; g < kHalf; ++g) {
-                float a = m[g], b = mv[g];
+                a[g] = m[g]; b[g] = kLowest;
 #pragma unroll
                 for (int i = 0; i < 4 * parts; ++i) {
                     const float *of = all + (4 * (kByTiles ? 0 : half) + i) * 3 * kHalf;
-                    a = fmaxf(a, of[g]);
-                    b = fmaxf(b, of[kHalf + g]);
+                    a[g] = fmaxf(a[g], of[g]);
+                    b[g] = fmaxf(b[g], of[kHalf + g]);
                 }
-                l[g] *= tc::ex2(m[g] - a);
-                acc[g] *= tc::ex2(mv[g] - b);
-                m[g] = a; mv[g] = b;
+                b[g] = fabsf(a[g]) > kFar ? most : b[g] - a[g];
+            }
+#pragma unroll
+            for (int g = 0; g < kHalf; ++g) {
+                const float up = m[g] - a[g], r = fmaxf(mr[g] + up, b[g]);
+                l[g] *= tc::ex2(up);
+                acc[g] *= tc::ex2(up + (mr[g] - r));
+                m[g] = a[g]; mr[g] = r;
             }
             if (ok && from < n) tmem_ld8(scol + from * kQCols, s);
             for (int t = from; t < n; t += parts) {
@@ -779,20 +792,26 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
                 const bool valid = first_key + t * kTile + row < now.rows;
                 const int j = (t * kTile + row) >> A.page_shift;
                 const float ks = in[j], lv = in[kMostPages + j] + 8.f;                  // (weights times 256)
-                float x[2 * kPairs];
+                float2 x[kPairs];
 #pragma unroll
-                for (int g = 0; g < 2 * kPairs; ++g) {
-                    const float z = fmaf(s[4 + g], 0.0625f, s[g]);
-                    const float c = ks * cq[g];
-                    const float p = tc::ex2(fmaf(z, c, -m[g]));
-                    l[g] += valid ? p : 0.f;
-                    x[g] = valid ? tc::ex2(fmaf(z, c, lv - mv[g])) : 0.f;
+                for (int i = 0; i < kPairs; ++i) {
+                    // two heads at once; but for the products, which are rounded as for the maximum, so that none is above it: two at once were
+                    // compiled into one step with the difference, without a rounding between
+                    const int g = 2 * i;
+                    const float2 z = tc::ffma2(make_float2(s[4 + g], s[5 + g]), make_float2(0.0625f, 0.0625f), make_float2(s[g], s[g + 1]));
+                    const float2 c = tc::fmul2(make_float2(ks, ks), make_float2(cq[g], cq[g + 1]));
+                    const float2 d = tc::fadd2(make_float2(__fmul_rn(z.x, c.x), __fmul_rn(z.y, c.y)), make_float2(-m[g], -m[g + 1]));
+                    const float2 dv = tc::fadd2(d, tc::fadd2(make_float2(lv, lv), make_float2(-mr[g], -mr[g + 1])));
+                    l[g] += valid ? tc::ex2(d.x) : 0.f;
+                    l[g + 1] += valid ? tc::ex2(d.y) : 0.f;
+                    x[i].x = valid ? tc::ex2(dv.x) : 0.f;
+                    x[i].y = valid ? tc::ex2(dv.y) : 0.f;
                 }
                 if (t + parts < n) tmem_ld8(scol + (t + parts) * kQCols, s);
                 uint32_t lower[4], word[4];
-                four_pieces(make_float2(x[0], x[1]), lower);
+                four_pieces(x[0], lower);
                 if constexpr (kPairs == 2) {
-                    four_pieces(make_float2(x[2], x[3]), word);
+                    four_pieces(x[kPairs - 1], word);
 #pragma unroll
                     for (int k = 0; k < 4; ++k) word[k] = lower[k] | word[k] << 16;
                 } else {

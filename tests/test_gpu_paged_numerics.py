@@ -81,6 +81,34 @@ def test_queries_with_elements_far_apart(D, Hq, H):
 
 @pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("path", [F.PATH_AUTO, F.PATH_SIMT])
+@pytest.mark.parametrize("Hq,H", [(2, 2), (8, 2), (7, 1)])
+def test_logits_of_any_size(path, D, Hq, H):
+    """Queries of one element, 2^6 to 2^70, either sign: the largest logit is a key's, or two keys' alike, and so far above the others that they have all the
+    weight; every logit is exact, so that of the bound the errors of weights and sums are left (paged_util.attention_bound without logits)."""
+    rng = np.random.default_rng(D + Hq)
+    rows, page = np.array([300, 40, 1500, 128]), 32
+    p, ck, cv, ks, vs, table = _case(rng, 4, Hq, H, D, page, rows, F.BF16, path, exponents=(-6, 6))
+    ks[:] = 2.0 ** -8
+    ck[..., 5] = rng.integers(0x08, 0x58, ck.shape[:3])               # 2^-6 .. 15
+    for u, n in enumerate(rows):
+        for h in range(H):
+            top = rng.choice(n, 2, replace=False)
+            for sign, at in ((0, top[:1 + h % 2]), (0x80, rng.choice(np.setdiff1d(np.arange(n), top), 2, replace=False))):
+                ck[table[u, at // page], h, at % page, 5] = sign | 0x7E    # 448, -448
+    for e in (6, 10, 16, 20, 22, 24, 25, 26, 28, 31, 40, 70):
+        for sign in (1, -1):
+            q = np.zeros((4, Hq, D), np.float32)
+            q[..., 5] = sign * 2.0 ** (e + 3)                          # (largest logit: 448 * 2^-8 * 2^(e + 3) / sqrt(D))
+            got, status = T.attend(p, q, ck, cv, ks, vs, table, rows)
+            want, size, _ = P.attention(q, P.E4M3[ck], P.E4M3[cv], ks, vs, table, rows)
+            assert status == 0
+            for u, n in enumerate(rows):
+                bound = T.attention_bound(size[u], np.zeros(Hq), int(n), D)
+                assert (np.abs(got[u] - want[u]) <= bound).all(), (e, sign, u, np.max(np.abs(got[u] - want[u]) / bound))
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("path", [F.PATH_AUTO, F.PATH_SIMT])
 @pytest.mark.parametrize("U,Hq,H", [(1, 8, 2), (3, 40, 40)])
 def test_nan_in_a_head_that_is_cut(path, D, U, Hq, H):
     """Records of a range with a NaN among others: the head's outputs that it belongs to, bit for bit nothing else."""
