@@ -763,8 +763,6 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
             // Beyond kFar log2 of V's scale is lost next to a logit, and the difference of the two maxima is not what it should be: the second one is
             // then said to be the largest of the group's scales above the first, which no weight passes either.  (Found in every group: under a branch for the
             // far ones the code around it was slower, 72.8 us for 71.2, 200 units of up to 2200 rows, 8 heads of 4 query heads of 64.)
-            const int pages = (min(n * kTile, now.rows - first_key) + A.page - 1) >> A.page_shift;
-            const float most = warp_max(fmaxf(lane < pages ? in[kMostPages + lane] : kLowest, lane + 32 < pages ? in[kMostPages + lane + 32] : kLowest));
             float a[kHalf], b[kHalf];
 #pragma unroll
             for (int g = 0; g < kHalf; ++g) {
@@ -775,11 +773,12 @@ cache_attention_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid
                     a[g] = fmaxf(a[g], of[g]);
                     b[g] = fmaxf(b[g], of[kHalf + g]);
                 }
-                b[g] = fabsf(a[g]) > kFar ? most : b[g] - a[g];
             }
+            const int pages = (min(n * kTile, now.rows - first_key) + A.page - 1) >> A.page_shift;
+            const float most = warp_max(fmaxf(lane < pages ? in[kMostPages + lane] : kLowest, lane + 32 < pages ? in[kMostPages + lane + 32] : kLowest));
 #pragma unroll
             for (int g = 0; g < kHalf; ++g) {
-                const float up = m[g] - a[g], r = fmaxf(mr[g] + up, b[g]);
+                const float up = m[g] - a[g], r = fmaxf(mr[g] + up, fabsf(a[g]) > kFar ? most : b[g] - a[g]);
                 l[g] *= tc::ex2(up);
                 acc[g] *= tc::ex2(up + (mr[g] - r));
                 m[g] = a[g]; mr[g] = r;
