@@ -782,3 +782,40 @@ def test_a_row_without_a_place_between_rows_is_reported(D, page, n, dtype):
         slots = good.copy()
         slots[0, n - 1:] = -1                                       # (nothing behind it: no fault)
         assert _store(p, x, x, slots, codes, codes, scale, scale)[1] == 0
+
+
+def test_units_of_two_lengths_are_recompressed_group_by_group():
+    """Compressed to two budgets, grown, read back by units of one length (rows of the block table and of the lengths), compressed again with the rows' modalities that
+    the program has kept: what the same rows give that never were in pages."""
+    rng = np.random.default_rng(22)
+    U, Hq, H, D, L, W, new = 4, 8, 2, 128, 512, 16, 9
+    budgets, groups = (60, 44), ([0, 2], [1, 3])
+    gen = lambda *shape: T.dev(rng.standard_normal(shape).astype(np.float32), F.BF16)
+    s = Server(U, Hq, H, D, 16, 40, 8, F.BF16, rng)
+    grow, k, v = np.zeros(U, np.int32), torch.zeros((U, H, max(budgets), D), dtype=torch.bfloat16, device="cuda"), None
+    v, kept = torch.zeros_like(k), {}
+    for B, units in zip(budgets, groups):
+        fp = F.Params(2, Hq, H, D, L, W, B, theta=0.25, tau=8.0, tau_mode=F.TAU_REL)
+        modality = T.dev(rng.integers(0, 2, (2, L)).astype(np.uint8))
+        c = F.compress_layer_alloc(fp, gen(2, Hq, W, D), gen(2, H, L, D), gen(2, H, L, D), modality)
+        k[units, :, :B], v[units, :, :B], grow[units] = c["k_out"], c["v_out"], B
+        kept[B] = torch.cat([modality[:, None].expand(2, H, L).gather(2, c["retained"].long()), torch.zeros((2, H, new), dtype=torch.uint8, device="cuda")], 2)
+    s.store(k, v, s.plan(grow, max(budgets)))
+    k, v = gen(U, H, new, D), gen(U, H, new, D)
+    s.store(k, v, s.plan(np.full(U, new, np.int32), new))
+    for B, units in zip(budgets, groups):
+        n = B + new
+        p = T.params(2, Hq, H, D, 16, 40, 8, n)
+        dense = [torch.zeros((2, H, n, D), dtype=torch.bfloat16, device="cuda") for _ in "kv"]
+        F.flowmm_cache_load(p, *s.pool, s.table[units].contiguous(), s.rows[units].contiguous(), *dense, s.ws)
+        want = [T.dev(np.stack([P.load(s.mirror[i], s.mirror[2 + i], s.book[3][u], n) for u in units]).astype(np.float32), F.BF16) for i in range(2)]
+        assert all(torch.equal(a, b) for a, b in zip(dense, want))
+        rp = F.Params(2, Hq, H, D, n, W, 40, theta=0.25, tau=8.0, tau_mode=F.TAU_REL)
+        ws = torch.zeros(F.flowmm_recompress_workspace_bytes(rp), dtype=torch.uint8, device="cuda")
+        q, outs = gen(2, Hq, W, D), []
+        for x in (dense, want):
+            o = [torch.empty((2, H, 40, D), dtype=torch.bfloat16, device="cuda") for _ in "kv"] + [torch.empty((2, H, 40), dtype=torch.uint8, device="cuda")]
+            F.flowmm_recompress(rp, q, *x, kept[B], *o, ws)
+            outs.append(o)
+        assert F.flowmm_last_device_status(ws) == 0 and all(torch.equal(a, b) for a, b in zip(*outs))
+        assert 0 < int(outs[0][2].sum()) < outs[0][2].numel()
