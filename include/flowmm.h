@@ -290,12 +290,14 @@ flowmm_status flowmm_decode_attention(const flowmm_decode_params *p, const void 
  * them.  After compression every sequence keeps its own number of rows, and a decode step is bound by reading K and V: a row is held
  * in 8 bits instead of 16 or 32, and memory is given out by pages.  A cache is stored (flowmm_cache_store) from what
  * flowmm_compress_layer wrote or from dense caches, grows by a row a step, is attended to (flowmm_cache_attention) and, when it has
- * grown, is read back (flowmm_cache_load) for flowmm_recompress.
+ * grown, is read back (flowmm_cache_load) for flowmm_recompress.  That takes units of one length and the modality of every row: it is called for
+ * units of equal length at a time (their rows of the block table and of `rows`), and the rows' modalities, which the cache does not hold, are
+ * the caller's to keep (flowmm_recompress gives back those of the rows it keeps).
  *
  *   k_pages, v_pages [n_pages, Hkv, page_size, D] e4m3 codes (4 exponent bits of bias 7, 3 mantissa bits, 127 and 255 NaN, no
  *                    infinity), dense
  *   k_scale, v_scale [n_pages, Hkv] f32: a code stands for code * scale.  flowmm_cache_store writes powers of two from 2^-96 on;
- *                    the readers take any positive scale.
+ *                    the readers take any positive scale up to 2^120.
  *   block_table      [U, max_pages] int32: the pages of a unit, in order; entries behind its last page are not read
  *   rows             [U] int32: rows that a unit holds, 0 to max_pages * page_size
  *   slots            [U, n_rows] int32: where each new row of a unit goes, page * page_size + place in the page; -1: nowhere
@@ -304,7 +306,9 @@ flowmm_status flowmm_decode_attention(const flowmm_decode_params *p, const void 
  * numbers, slots and rows are checked before use in every build: a bad one sets the device status to FLOWMM_ERR_INDEX, nothing is
  * read or written out of bounds for it, and the outputs of its unit are not valid.  Heads (at most
  * 8 query heads a KV head), head_dim and dtype as in flowmm_decode_params.  n_pages * page_size and n_units * n_rows are
- * below 2^31, max_pages * page_size and n_rows at most 2^30.
+ * below 2^31, max_pages * page_size and n_rows at most 2^30, n_units * n_kv_heads at most 4 194 304.  Work is counted in 32 bits (FLOWMM_ERR_SHAPE
+ * otherwise): the store takes fewer than 2^30 n_units * n_kv_heads * pages that n_rows rows can reach, the load fewer than 2^30 n_units * n_kv_heads *
+ * n_rows / 64, the attention fewer than 2^31 n_units * n_q_heads * max_pages * page_size / 64.
  */
 typedef struct {
     int32_t n_units, n_q_heads, n_kv_heads, head_dim;
@@ -353,8 +357,8 @@ flowmm_status flowmm_cache_plan(const flowmm_cache_params *p, const int32_t *gro
 flowmm_status flowmm_cache_store(const flowmm_cache_params *p, const void *k, const void *v, const int32_t *slots, void *k_pages,
                                  void *v_pages, float *k_scale, float *v_scale, void *ws, size_t ws_bytes, void *cuda_stream);
 
-/* Pages into rows: k, v [U, Hkv, n_rows, D] out, code * scale rounded once, for the first min(rows[u], n_rows) rows of each unit;
- * the others are left as they were. */
+/* Pages into rows: k, v [U, Hkv, n_rows, D] out, code * scale in fp32 (exact with scales that flowmm_cache_store writes), rounded to the type, for the
+ * first min(rows[u], n_rows) rows of each unit; the others are left as they were. */
 flowmm_status flowmm_cache_load(const flowmm_cache_params *p, const void *k_pages, const void *v_pages, const float *k_scale,
                                 const float *v_scale, const int32_t *block_table, const int32_t *rows, void *k, void *v, void *ws,
                                 size_t ws_bytes, void *cuda_stream);
@@ -366,6 +370,10 @@ flowmm_status flowmm_cache_load(const flowmm_cache_params *p, const void *k_page
  *   q [U, Hq, D] dense, element type `dtype`;  out [U, Hq, D] f32
  * `path`: AUTO runs both contractions on the tensor cores (tcgen05, the codes as operands) when dtype is bf16, and SIMT fp32 kernels
  * otherwise; SIMT forces the latter.  The workspace serves both.
+ * Both sum in fp32, results without the division by the softmax's sum included: rows[u] * max |v| stays below 2^128.  The SIMT kernels multiply in fp32.  On
+ * the tensor cores a query is two e4m3 numbers, exact for elements down to 2^-13 of its largest one, others within 2^-21 of that; a weight, the
+ * softmax's times V's scale, is four, within 2^-16 of itself down to 2^-14 of the row's largest one, others within 2^-30 of that, so a page whose
+ * V scale is 2^30 times smaller than another's of the head adds nothing.  The measured error on data like a cache's is 2e-7 of the result.
  */
 flowmm_status flowmm_cache_attention(const flowmm_cache_params *p, const void *q, const void *k_pages, const void *v_pages,
                                      const float *k_scale, const float *v_scale, const int32_t *block_table, const int32_t *rows,

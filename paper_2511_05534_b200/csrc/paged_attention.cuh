@@ -16,7 +16,7 @@ struct AttnArgs {
     const float *k_scale, *v_scale;    // [n_pages, Hkv]
     const int *table, *rows;           // [U, max_pages], [U]
     float *out;                        // [U, Hq, D]
-    float *part;                       // [blocks] records (record_floats)
+    float *part;                       // records (record_floats): one for each block, two on the tensor cores
     int *status;
     int4 *cut_heads;                   // [blocks]: unit, first query head, number of records (0: nothing) and query heads of what begins in the
                                        // block and is to be joined; null: nothing can be
@@ -163,8 +163,10 @@ __device__ __forceinline__ Joined<D> join_part(const float *rec, int64_t ahead, 
 // kWarps warps for each query head, with every kWarps-th record each.  A block of the kernel before has `own` records; the first one of a
 // join is the `first`-th of its block, the next ones are `step` records apart, counted from its block's first.
 // (By the range that ended last, which it learnt from a ticket: 35 ranges that end together drew theirs one after the other, 4 sequences of 2200 rows, 4 heads of 64,
-// 22.6 us, so 10.)  Four warps where heads are few, and so cut into many ranges (a sequence of 8448 rows, 4 heads, 66 records of each: 28 us for the
-// call with one, 15 so), else one, which makes the blocks that find nothing to do fewer (16 of up to 33 792, 8 heads: 122 us with four, 118 so).
+// 22.6 us, so 10.)  Four warps where heads are few, and so cut into many ranges, else one, which makes the blocks that find nothing to do fewer.  The call with
+// four and with one, sequences of up to 8448 rows: tensor cores, 4 heads (33 records of each) 12.4 and 14.5 us, 16 heads 14.8 and 15.3, 32 heads 18.4 and
+// 18.4, 72 heads 26.6 and 25.5; SIMT, 32 heads 13.2 and 14.3, 64 heads 19.6 and 20.1, 80 heads 24.0 and 23.9.  16 sequences of up to 33 792 rows,
+// 8 heads: 108.9 and 107.0.
 constexpr int kJoinThreads = 256, kFewHeads = 74;
 template <int D, int kWarps>
 __global__ void __launch_bounds__(kJoinThreads) cache_join_kernel(const AttnArgs A, const int record, const int own, const int first, const int step) {

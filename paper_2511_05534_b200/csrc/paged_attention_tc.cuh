@@ -14,8 +14,8 @@
 // Few heads: a block has one range of one head, all of the same length but for a head's last one.  Many: a block has two whole heads, or the
 // tiles of 128 keys of all heads stand in a row, by unit, head and key, and every block takes an equal piece of the row, parts of heads or
 // several, one after the other.  A head that several blocks have part in leaves a record for each, and cache_join_kernel joins
-// them in order.  (Ranges alone left a last round half empty, 16 sequences of up to 33 792 rows, 8 heads, 174 us; pieces 118.  Three
-// quarters of a piece to each block and the rest drawn from a counter in pieces of three tiles and more: 132.)
+// them in order.  (Ranges alone left a last round half empty, 16 sequences of up to 33 792 rows, 8 heads, 174 us when pieces took 118.  Three
+// quarters of a piece to each block and the rest drawn from a counter in pieces of three tiles and more: 132 then.)
 // A block goes through its tiles in groups of up to seven of one head, the roles of its warps one or two groups apart, across the
 // heads' borders too:
 //   warp 0     K tiles and V tiles by TMA, a box per page, into a ring of six stages of 16 KB (ten of 8): a tile of K of group c + 1 and one of V of
@@ -25,9 +25,9 @@
 //              head: the next head's query operand.
 //              Two halves of four warps: for more than four query heads each has four of them, for fewer every other tile.  (One half
 //              alone took 1800 clocks for a tile of eight heads, longer than its share of the memory's time.)
-// Memory bounds long calls: 16 sequences of up to 33 792 rows, 686 MB of pages, 118 us, 5.8 TB/s.  Short ones are bound by the way of one group through the
+// Memory bounds long calls: 16 sequences of up to 33 792 rows, 654 MB of pages, 107 us, 6.1 TB/s.  Short ones are bound by the way of one group through the
 // block, about 6 us from the lengths to the output (one sequence of 218 rows), and by the ends of the blocks, which fall together: 64
-// sequences of up to 1690 rows, 131 MB, 36 us.  (Groups of two to five tiles, and smaller groups at a block's end, were no faster.)
+// sequences of up to 1690 rows, 129 MB, 34.5 us.  (Groups of two to five tiles, and smaller groups at a block's end, were no faster.)
 // Every wait is bounded.
 #pragma once
 #include "paged_attention.cuh"
@@ -158,12 +158,12 @@ __device__ __forceinline__ uint32_t sorted_unit(const Cut &c, uint32_t r) {
     return r < 32 ? a : b;
 }
 // Heads are not cut for a range kJoinTiles longer: joining costs that much.  With at most as many heads as blocks, ranges of a head each,
-// unless they become kSwitchTiles longer than an even piece: the way from one head to the next costs 3 us where a block has few tiles (one
-// sequence of 1100 rows, 4 heads: 10.4 us by ranges, 13.9 by pieces of two tiles of one head or of two).  At most 64 ranges of a head, whose joining
-// is the longer the more there are (one head of 33 792 rows by at most 16, 32 and 64 ranges, and by 132 pieces: 22.7, 17.2, 14.7 and 17.6 us; two heads 23.2, 17.8,
-// 15.2, 15.2; eight 25.0, 25.2, 23.0, 23.3).
-// With up to twice as many heads as blocks, of at most 64 units, a block has the i-th longest and the i-th last
-// (64 units of up to 1690 rows, 512 heads: 41 us cut, 36 so).
+// unless they become kSwitchTiles longer than an even piece: the way from one head to the next costs where a block has few tiles (by ranges and by
+// pieces: 12 sequences of up to 3000 rows, 4 heads, 14.0 and 15.5 us; 36 of 1690, 8 heads, 25.2 and 26.8; 4 of 2000, 12.8 and 13.5).  At most 64 ranges of a
+// head, whose joining is the longer the more there are (one head of 33 792 rows by at most 16, 32 and 64 ranges, and by 132 pieces: 22.8, 17.4, 14.5 and
+// 17.9 us; two heads 23.1, 17.9, 14.8, 15.6; eight 25.2, 23.5, 24.2, 23.6).
+// With up to twice as many heads as blocks, of at most 64 units (two to a lane), a block has the i-th longest and the i-th last: 64 units of
+// up to 1690 rows, 8 heads, 34.7 us so, 35.5 by pieces.  More units take pieces: 65 of 8 heads 36.6 us, 128 of 4 heads 35.5.
 constexpr int kSwitchTiles = 4, kMostRanges = 64;
 __device__ __forceinline__ Cut make_cut(const AttnArgs &A) {
     Cut c;
