@@ -307,8 +307,8 @@ flowmm_status flowmm_decode_attention(const flowmm_decode_params *p, const void 
  * read or written out of bounds for it, and the outputs of its unit are not valid.  Heads (at most
  * 8 query heads a KV head), head_dim and dtype as in flowmm_decode_params.  n_pages * page_size and n_units * n_rows are
  * below 2^31, max_pages * page_size and n_rows at most 2^30, n_units * n_kv_heads at most 4 194 304.  Work is counted in 32 bits (FLOWMM_ERR_SHAPE
- * otherwise): the store takes fewer than 2^30 n_units * n_kv_heads * pages that n_rows rows can reach, the load fewer than 2^30 n_units * n_kv_heads *
- * n_rows / 64, the attention fewer than 2^31 n_units * n_q_heads * max_pages * page_size / 64.
+ * otherwise): the store takes fewer than 2^31 n_units * (2 n_kv_heads + 1) * pages that n_rows rows can reach, the load fewer than 2^30
+ * n_units * n_kv_heads * n_rows / 64, the attention fewer than 2^31 n_units * n_q_heads * max_pages * page_size / 64.
  */
 typedef struct {
     int32_t n_units, n_q_heads, n_kv_heads, head_dim;

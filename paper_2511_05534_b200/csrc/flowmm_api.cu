@@ -1513,7 +1513,7 @@ bool aligned4(const void *ptr) { return (reinterpret_cast<uintptr_t>(ptr) & 3) =
 template <typename T, int D, int kTeam, int kVecs>
 flowmm_status launch_store(const paged::StoreArgs &a, cudaStream_t st) {
     constexpr int block = kTeam < 128 ? 128 : kTeam, teams = block / kTeam;
-    launch(paged::cache_store_kernel<T, D, kTeam, kVecs>, (a.items + teams - 1) / teams, block, 0, st, a);
+    launch(paged::cache_store_kernel<T, D, kTeam, kVecs>, (a.items + a.looks + teams - 1) / teams, block, 0, st, a);
     FLOWMM_LAUNCHED("cache_store");
     return FLOWMM_OK;
 }
@@ -1635,7 +1635,8 @@ extern "C" flowmm_status flowmm_cache_store(const flowmm_cache_params *p, const 
     FLOWMM_TRY(check_cache_ws(p, ws, ws_bytes));
     // pages that n_rows rows can reach, wherever in its page the first one goes
     const int64_t runs = ((int64_t)p->n_rows + 2 * p->page_size - 2) / p->page_size, items = 2 * (int64_t)p->n_units * p->n_kv_heads * runs;
-    if (items >= (int64_t)1 << 31) return FLOWMM_ERR_SHAPE;
+    const int64_t parts = p->n_rows > 1 ? ((int64_t)p->n_rows + paged::kLookRows - 1) / paged::kLookRows : 0, looks = p->n_units * parts;
+    if (items + looks >= (int64_t)1 << 31) return FLOWMM_ERR_SHAPE;
     FLOWMM_TRY(check_device());
     paged::StoreArgs a;
     a.x[0] = k; a.x[1] = v; a.slots = slots;
@@ -1643,7 +1644,8 @@ extern "C" flowmm_status flowmm_cache_store(const flowmm_cache_params *p, const 
     a.scale[0] = k_scale; a.scale[1] = v_scale; a.status = static_cast<int *>(ws);
     a.Hkv = p->n_kv_heads; a.T = p->n_rows; a.page = p->page_size; a.page_shift = page_shift(p->page_size); a.n_pages = p->n_pages;
     for (int i = 0; i < 3; ++i) { a.stride[0][i] = p->k_stride[i]; a.stride[1][i] = p->v_stride[i]; }
-    a.items = (uint32_t)items; a.by_heads = make_fastdiv(p->n_kv_heads); a.by_runs = make_fastdiv((uint32_t)runs);
+    a.items = (uint32_t)items; a.looks = (uint32_t)looks; a.by_heads = make_fastdiv(p->n_kv_heads); a.by_runs = make_fastdiv((uint32_t)runs);
+    a.by_parts = make_fastdiv((uint32_t)std::max<int64_t>(1, parts));
     return p->dtype == FLOWMM_BF16 ? run_store<__nv_bfloat16>(*p, a, st) : run_store<float>(*p, a, st);
 }
 

@@ -819,3 +819,23 @@ def test_units_of_two_lengths_are_recompressed_group_by_group():
             outs.append(o)
         assert F.flowmm_last_device_status(ws) == 0 and all(torch.equal(a, b) for a, b in zip(*outs))
         assert 0 < int(outs[0][2].sum()) < outs[0][2].numel()
+
+
+@pytest.mark.parametrize("D,page,dtype", [(64, 16, F.F32), (128, 128, F.BF16)])
+def test_every_row_without_a_place_is_looked_at(D, page, dtype):
+    """Many rows of many units: one hole at any place is found, and none where there is none."""
+    rng = np.random.default_rng(page)
+    U, n = 3, 1100
+    pages = P.pages(n, page)
+    x = T.dev(rng.standard_normal((U, 1, n, D)).astype(np.float32), dtype)
+    p = T.params(U, 1, 1, D, page, U * pages, pages, n, dtype)
+    pool = [torch.zeros((U * pages, 1, page, D), dtype=torch.uint8, device="cuda") for _ in "kv"] + [torch.ones((U * pages, 1), device="cuda") for _ in "kv"]
+    good = (np.arange(U)[:, None] * pages * page + np.arange(n)).astype(np.int32)
+    ws = F.alloc_cache_workspace(p)
+    for u in range(U):
+        for t in (None, 0, 1, 510, 511, 512, 513, 1022, 1023, 1024, 1025, n - 2, n - 1):
+            slots = good.copy()
+            if t is not None:
+                slots[u, t] = -1
+            F.flowmm_cache_store(p, x, x, T.dev(slots), *pool, ws)
+            assert F.flowmm_last_device_status(ws) == (0 if t in (None, n - 1) else 10), (u, t)
