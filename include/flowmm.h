@@ -58,7 +58,7 @@ typedef enum {
     FLOWMM_ERR_CUDA = 7,               /* a CUDA runtime call or launch failed */
     FLOWMM_ERR_TIMEOUT = 8,            /* device status: a bounded wait inside a kernel ran out */
     FLOWMM_ERR_UNSUPPORTED_DEVICE = 9,
-    FLOWMM_ERR_INDEX = 10,             /* an index was out of range (index lists: debug build only; pages, slots and rows of the paged cache: always) */
+    FLOWMM_ERR_INDEX = 10,             /* an index was out of range (index lists: debug build only; pages, slots and rows of the paged caches: always) */
     FLOWMM_ERR_POOL = 11               /* device status: the page pool, the block table or the slot map had no room for a unit's rows */
 } flowmm_status;
 
@@ -378,6 +378,95 @@ flowmm_status flowmm_cache_load(const flowmm_cache_params *p, const void *k_page
 flowmm_status flowmm_cache_attention(const flowmm_cache_params *p, const void *q, const void *k_pages, const void *v_pages,
                                      const float *k_scale, const float *v_scale, const int32_t *block_table, const int32_t *rows,
                                      float *out, void *ws, size_t ws_bytes, void *cuda_stream);
+
+/*
+ * The paged 4-bit cache: the same pools, block tables, slots and plans (flowmm_cache_plan) with rows held in 4.5 bits an element, a little over half of
+ * the 8-bit cache's bytes, for decode steps that are bound by reading K and V and pools that are bound by memory.  Rows do not depend on one another: a
+ * row that is stored changes no other one's codes.
+ *
+ *   k_pages, v_pages [n_pages, Hkv, page_size, D / 2] bytes of two e2m1 codes, the even channel's in the low half (sign, two exponent bits of bias 1, one
+ *                    mantissa bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6), dense
+ *   k_scale, v_scale [n_pages, Hkv, page_size, D / 16] bytes, dense: a scale for 16 neighbouring channels of a row, five exponent bits of bias 15 and three
+ *                    mantissa bits (an fp16 without sign and its lowest seven bits; 31 in the exponent: infinity and NaN).  A code stands for code *
+ *                    scale.  flowmm_nibble_store writes 2^-14 to 10240 (bytes 8 to 226) and NaN (255); the readers take all bytes up to 226, and 255.
+ *
+ * Params, block_table, rows, slots, workspaces (of flowmm_nibble_workspace_bytes) and what is checked on the device as for the paged 8-bit cache;
+ * `path` is not used.  Pages and scales are 16-byte aligned.  Work is counted in 32 bits (FLOWMM_ERR_SHAPE otherwise): the store takes fewer than 2^31
+ * n_units * n_kv_heads * n_rows, the load fewer than 2^30 n_units * n_kv_heads * n_rows / 64, the attention fewer than 2^31
+ * n_units * n_q_heads * max_pages * page_size / 64.
+ */
+flowmm_status flowmm_nibble_workspace_bytes(const flowmm_cache_params *p, size_t *bytes);
+
+/*
+ * Rows into pages.  Row t of unit u goes to slots[u][t], anywhere in the pool; -1: nowhere.  No place is written for two rows.  Per row, KV head, tensor and group of
+ * 16 channels:
+ *   s = max|x| / 6 rounded to four significant bits (to the nearest, ties to even), at least 2^-14, at most 10240
+ *   codes = e2m1(x / s), to the nearest, ties to the even code, at most 6 in size (so elements beyond 61 440 become that), the sign of zeros kept
+ * A group with an infinity or a NaN has the scale NaN and codes of zero.  Quotients are rounded as real numbers are: results do not depend on how they are formed.
+ *   k, v [U, Hkv, n_rows, D] with the element strides k_stride, v_stride
+ */
+flowmm_status flowmm_nibble_store(const flowmm_cache_params *p, const void *k, const void *v, const int32_t *slots, void *k_pages,
+                                  void *v_pages, void *k_scale, void *v_scale, void *ws, size_t ws_bytes, void *cuda_stream);
+
+/* Pages into rows: k, v [U, Hkv, n_rows, D] out, code * scale, exactly (a product has six significant bits), for the first min(rows[u], n_rows) rows of each unit; the
+ * others are left as they were. */
+flowmm_status flowmm_nibble_load(const flowmm_cache_params *p, const void *k_pages, const void *v_pages, const void *k_scale,
+                                 const void *v_scale, const int32_t *block_table, const int32_t *rows, void *k, void *v, void *ws,
+                                 size_t ws_bytes, void *cuda_stream);
+
+/*
+ * flowmm_decode_attention over the paged 4-bit cache: o = softmax(scale * q . K^T) V over the rows[u] rows of each unit, zero for a unit without rows.  What
+ * stands behind a unit's last row (scales of NaN too) has no influence.  Several new queries of a sequence are units that share a row of the block table
+ * and differ in rows.
+ *   q, out [U, Hq, D] dense, element type `dtype`
+ */
+flowmm_status flowmm_nibble_attention(const flowmm_cache_params *p, const void *q, const void *k_pages, const void *v_pages,
+                                      const void *k_scale, const void *v_scale, const int32_t *block_table, const int32_t *rows,
+                                      void *out, void *ws, size_t ws_bytes, void *cuda_stream);
+
+/*
+ * Rotary positions: queries and keys turned by their tokens' positions, before the keys are cached or scored.  A row's place in a cache that was
+ * compressed is not its token's position any more, so positions are given for every row; image tokens may have three (time, height, width).
+ * The first R = rotary_dim channels of a head are R / 2 pairs (a, b), pair i at angle t = position * f_i:
+ *   (a, b) -> amplitude * (a cos t - b sin t, b cos t + a sin t);   the other D - R channels are copied
+ *   f_i = base^(-2 i / R), by `scaling`: PLAIN as it is; LINEAR f_i / factor; BY_PARTS g f_i + (1 - g) f_i / factor with
+ *         g = min(1, max(0, (trained * f_i / (2 pi) - low) / (high - low))): by how many turns the pair makes over the context that was trained on
+ * adjoint = 1 turns by -t: the gradient's way back, and for amplitude 1 the inverse (keys taken out of a cache and put to other positions).
+ *
+ * flowmm_rotary_table writes what the call needs of the frequencies, once for a model: table [R / 2] uint64, pair i's f_i / (2 pi) as a 64-bit fraction of a
+ * turn.  Positions are multiplied with it modulo whole turns, so any int32 position has its angle within 2^-31 turns; cos and sin and the products are fp32.
+ *
+ *   q, q_out [U, Hq, T, D], k, k_out [U, Hkv, T, D] with the element strides given, T = n_rows; q with q_out, or k with k_out, may be NULL (not both).
+ *   q_out may be q (the same strides), k_out may be k; otherwise outputs must not overlap inputs.
+ *   positions [U, n_axes, T] int32
+ * rotary_dim is a multiple of 16 up to head_dim (0: head_dim).  n_axes is 1, or 3: then section[a] pairs go by position a, in order, R / 2 in all.
+ * base at least 1, factor above 0, high above low, trained at least 0 are asked for where `scaling` uses them; amplitude 0 selects 1.
+ * U * T is below 2^31.  No workspace: nothing on the device can fail.
+ */
+typedef enum { FLOWMM_ROTARY_HALVES = 0,        /* channels i and i + R / 2 are pair i */
+               FLOWMM_ROTARY_PAIRS = 1          /* channels 2 i and 2 i + 1 are pair i */
+} flowmm_rotary_layout;
+typedef enum { FLOWMM_ROTARY_PLAIN = 0, FLOWMM_ROTARY_LINEAR = 1, FLOWMM_ROTARY_BY_PARTS = 2 } flowmm_rotary_scaling;
+
+typedef struct {
+    int32_t n_units, n_q_heads, n_kv_heads, head_dim;
+    int32_t n_rows;                     /* T */
+    int32_t dtype;                      /* flowmm_dtype of q, k and the outputs */
+    int32_t rotary_dim;                 /* R */
+    int32_t layout;                     /* flowmm_rotary_layout */
+    int32_t adjoint;
+    int32_t n_axes, section[3];
+    int32_t scaling;                    /* flowmm_rotary_scaling */
+    float amplitude;
+    int32_t trained;                    /* positions of the context that was trained on */
+    double base, factor, low, high;
+    int64_t q_stride[3], k_stride[3];   /* element strides (unit, head, row) */
+    int64_t q_out_stride[3], k_out_stride[3];
+} flowmm_rotary_params;
+
+flowmm_status flowmm_rotary_table(const flowmm_rotary_params *p, uint64_t *table, void *cuda_stream);
+flowmm_status flowmm_rotary(const flowmm_rotary_params *p, const void *q, const void *k, const int32_t *positions, const uint64_t *table,
+                            void *q_out, void *k_out, void *cuda_stream);
 
 /* Waits for `cuda_stream`, then returns the device status word at the start of `ws`
  * (FLOWMM_OK, or the first error a kernel recorded) and clears it. */

@@ -29,6 +29,8 @@ MERGE_EXPSIM, MERGE_MEAN = 0, 1
 TAU_ABS, TAU_REL = 0, 1
 FLOW_AUTO, FLOW_FORCE_INTRA, FLOW_FORCE_CROSS, FLOW_MISALIGNED = 0, 1, 2, 3
 PATH_AUTO, PATH_SIMT = 0, 1
+ROTARY_HALVES, ROTARY_PAIRS = 0, 1
+ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_BY_PARTS = 0, 1, 2
 
 EXPORTS = (
     "flowmm_workspace_bytes", "flowmm_score", "flowmm_layer_flow", "flowmm_select", "flowmm_match", "flowmm_merge",
@@ -39,6 +41,8 @@ EXPORTS = (
     "flowmm_merge_static_status", "flowmm_merge_static_poke_status",
     "flowmm_recompress_workspace_bytes", "flowmm_recompress", "flowmm_debug_build",
     "flowmm_cache_workspace_bytes", "flowmm_cache_plan", "flowmm_cache_store", "flowmm_cache_load", "flowmm_cache_attention",
+    "flowmm_nibble_workspace_bytes", "flowmm_nibble_store", "flowmm_nibble_load", "flowmm_nibble_attention",
+    "flowmm_rotary_table", "flowmm_rotary",
 )
 
 
@@ -172,6 +176,9 @@ def load() -> ctypes.CDLL:
                             ("flowmm_cache_workspace_bytes", [P] * 2), ("flowmm_cache_plan", [P] * 10 + [N, P]),
                             ("flowmm_cache_store", [P] * 9 + [N, P]), ("flowmm_cache_load", [P] * 10 + [N, P]),
                             ("flowmm_cache_attention", [P] * 10 + [N, P]),
+                            ("flowmm_nibble_workspace_bytes", [P] * 2), ("flowmm_nibble_store", [P] * 9 + [N, P]),
+                            ("flowmm_nibble_load", [P] * 10 + [N, P]), ("flowmm_nibble_attention", [P] * 10 + [N, P]),
+                            ("flowmm_rotary_table", [P] * 3), ("flowmm_rotary", [P] * 8),
                             ("flowmm_last_device_status", [P] * 2), ("flowmm_selftest_wait_timeout", [P] * 2),
                             ("flowmm_merge_static_status", [P]), ("flowmm_merge_static_poke_status", [ctypes.c_int32, P])):
             getattr(lib, name).argtypes = types
@@ -430,6 +437,9 @@ def _cache_call(p: CacheParams, what: str):
     dense = (("k", rows, own, 1, False), ("v", rows, own, 2, False))
     held = (("block_table", table, _INT32, 0, False), ("rows", (U,), _INT32, 0, False))
     heads = (U, p.n_q_heads, p.head_dim)
+    pairs, groups = codes[:3] + (p.head_dim // 2,), codes[:3] + (p.head_dim // 16,)       # of the 4-bit cache: bytes of two codes, scales
+    nibbles = (("k_pages", pairs, _BYTES, 0, False), ("v_pages", pairs, _BYTES, 0, False),
+               ("k_scale", groups, _BYTES, 0, False), ("v_scale", groups, _BYTES, 0, False))
     arguments = {
         "flowmm_cache_plan": (("grow", (U,), _INT32, 0, False), ("rows", (U,), _INT32, 0, False), ("rows_out", (U,), _INT32, 0, False),
                               ("free_pages", (p.n_pages,), _INT32, 0, False), ("free_state", (2,), _INT32, 0, False),
@@ -438,6 +448,9 @@ def _cache_call(p: CacheParams, what: str):
         "flowmm_cache_store": dense + (("slots", (U, p.n_rows), _INT32, 0, False),) + pool,
         "flowmm_cache_load": pool + held + dense,
         "flowmm_cache_attention": (("q", heads, own, 0, False),) + pool + held + (("out", heads, _FLOAT, 0, False),),
+        "flowmm_nibble_store": dense + (("slots", (U, p.n_rows), _INT32, 0, False),) + nibbles,
+        "flowmm_nibble_load": nibbles + held + dense,
+        "flowmm_nibble_attention": (("q", heads, own, 0, False),) + nibbles + held + (("out", heads, own, 0, False),),
     }[what] + (("ws", (-1,), _BYTES, 0, False),)
     function = ctypes.cast(getattr(load(), what), ctypes.c_void_p).value
     cp = p.c()
@@ -487,6 +500,121 @@ def flowmm_cache_load(p: CacheParams, k_pages, v_pages, k_scale, v_scale, block_
 def flowmm_cache_attention(p: CacheParams, q, k_pages, v_pages, k_scale, v_scale, block_table, rows, out, ws):
     """Decode attention over the paged cache; q [units, q_heads, head_dim], out the same in float32."""
     _cache_run(p, "flowmm_cache_attention", q, k_pages, v_pages, k_scale, v_scale, block_table, rows, out, ws)
+
+
+# ---- paged 4-bit cache (params, plans, block tables and slots of the 8-bit one) --------------------
+
+def flowmm_nibble_workspace_bytes(p: CacheParams) -> int:
+    n = ctypes.c_size_t(0)
+    cp = p.c()
+    _check(load().flowmm_nibble_workspace_bytes(ctypes.byref(cp), ctypes.byref(n)), "flowmm_nibble_workspace_bytes")
+    return int(n.value)
+
+
+def alloc_nibble_workspace(p: CacheParams, device="cuda") -> torch.Tensor:
+    """A workspace of the required size with its status word cleared."""
+    ws = torch.empty(flowmm_nibble_workspace_bytes(p), dtype=torch.uint8, device=device)
+    ws[:256].zero_()
+    return ws
+
+
+def flowmm_nibble_store(p: CacheParams, k, v, slots, k_pages, v_pages, k_scale, v_scale, ws):
+    """Rows k, v [units, kv_heads, n_rows, head_dim] into pages [n_pages, kv_heads, page_size, head_dim / 2] and their scales
+    [n_pages, kv_heads, page_size, head_dim / 16], all uint8, as slots says."""
+    _cache_run(p, "flowmm_nibble_store", k, v, slots, k_pages, v_pages, k_scale, v_scale, ws)
+
+
+def flowmm_nibble_load(p: CacheParams, k_pages, v_pages, k_scale, v_scale, block_table, rows, k, v, ws):
+    """The first min(rows[u], n_rows) rows of every unit into k, v [units, kv_heads, n_rows, head_dim]."""
+    _cache_run(p, "flowmm_nibble_load", k_pages, v_pages, k_scale, v_scale, block_table, rows, k, v, ws)
+
+
+def flowmm_nibble_attention(p: CacheParams, q, k_pages, v_pages, k_scale, v_scale, block_table, rows, out, ws):
+    """Decode attention over the paged 4-bit cache; q and out [units, q_heads, head_dim]."""
+    _cache_run(p, "flowmm_nibble_attention", q, k_pages, v_pages, k_scale, v_scale, block_table, rows, out, ws)
+
+
+# ---- rotary positions -----------------------------------------------------------------------------
+
+class _CRotaryParams(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_units", "n_q_heads", "n_kv_heads", "head_dim", "n_rows", "dtype", "rotary_dim", "layout", "adjoint",
+                                              "n_axes")] + [
+        ("section", ctypes.c_int32 * 3), ("scaling", ctypes.c_int32), ("amplitude", ctypes.c_float), ("trained", ctypes.c_int32)] + [
+        (n, ctypes.c_double) for n in ("base", "factor", "low", "high")] + [
+        (n, ctypes.c_int64 * 3) for n in ("q_stride", "k_stride", "q_out_stride", "k_out_stride")]
+
+
+@dataclass
+class RotaryParams:
+    """Mirror of flowmm_rotary_params; rotary_dim 0: the whole head; sections: pairs that go by each of three positions, None: one position a row.
+    The strides are taken from the tensors each call receives."""
+    n_units: int
+    n_q_heads: int
+    n_kv_heads: int
+    head_dim: int
+    n_rows: int
+    dtype: int = BF16
+    rotary_dim: int = 0
+    layout: int = ROTARY_HALVES
+    adjoint: bool = False
+    sections: Optional[tuple] = None
+    scaling: int = ROTARY_PLAIN
+    base: float = 10000.0
+    factor: float = 1.0
+    low: float = 1.0
+    high: float = 32.0
+    trained: int = 0
+    amplitude: float = 1.0
+
+    @property
+    def pairs(self) -> int:
+        return (self.rotary_dim or self.head_dim) // 2
+
+    def c(self, *tensors) -> _CRotaryParams:
+        """tensors: q, k, q_out, k_out, each may be None or missing."""
+        section = (0, 0, 0) if self.sections is None else tuple(self.sections)
+        if len(section) != 3:
+            raise ValueError("sections must be three numbers of pairs")
+        cp = _CRotaryParams(self.n_units, self.n_q_heads, self.n_kv_heads, self.head_dim, self.n_rows, self.dtype, self.rotary_dim, self.layout,
+                            int(self.adjoint), 1 if self.sections is None else 3, (ctypes.c_int32 * 3)(*section), self.scaling, self.amplitude, self.trained,
+                            self.base, self.factor, self.low, self.high)
+        for name, heads, t in zip(("q_stride", "k_stride", "q_out_stride", "k_out_stride"), (self.n_q_heads, self.n_kv_heads) * 2, tensors + (None,) * 4):
+            if t is None:
+                dense = (heads * self.n_rows * self.head_dim, self.n_rows * self.head_dim, self.head_dim)
+                setattr(cp, name, (ctypes.c_int64 * 3)(*dense))
+                continue
+            if t.shape != (self.n_units, heads, self.n_rows, self.head_dim) or t.stride(3) != 1 or t.dtype != torch_dtype(self.dtype):
+                raise ValueError("flowmm_rotary: expected a %s tensor of shape %s with contiguous head_dim"
+                                 % (torch_dtype(self.dtype), (self.n_units, heads, self.n_rows, self.head_dim)))
+            setattr(cp, name, (ctypes.c_int64 * 3)(*t.stride()[:3]))
+        return cp
+
+
+def alloc_rotary_table(p: RotaryParams, device="cuda") -> torch.Tensor:
+    """The phases of the pairs, written by flowmm_rotary_table; once for a model."""
+    table = torch.empty(p.pairs, dtype=torch.int64, device=device)
+    flowmm_rotary_table(p, table)
+    return table
+
+
+def flowmm_rotary_table(p: RotaryParams, table):
+    """table [pairs] int64: 64-bit fractions of a turn."""
+    if table.dtype != torch.int64 or table.shape != (p.pairs,) or not table.is_contiguous():
+        raise ValueError("flowmm_rotary_table: table must be a contiguous int64 tensor of %d elements" % p.pairs)
+    cp = p.c()
+    _check(load().flowmm_rotary_table(ctypes.byref(cp), _p(table), _stream()), "flowmm_rotary_table")
+
+
+def flowmm_rotary(p: RotaryParams, q, k, positions, table, q_out, k_out):
+    """Queries q [units, q_heads, n_rows, head_dim] and keys k turned by positions [units, n_rows] ([units, 3, n_rows] with sections);
+    q and q_out, or k and k_out, may be None, an output may be its input."""
+    cp = p.c(q, k, q_out, k_out)
+    want = (p.n_units, p.n_rows) if p.sections is None else (p.n_units, 3, p.n_rows)
+    if positions.dtype != torch.int32 or positions.numel() != math.prod(want) or positions.shape[-1] != p.n_rows or not positions.is_contiguous():
+        raise ValueError("flowmm_rotary: positions must be a contiguous int32 tensor of shape %s" % (want,))
+    if table.dtype != torch.int64 or table.shape != (p.pairs,) or not table.is_contiguous():
+        raise ValueError("flowmm_rotary: table must be a contiguous int64 tensor of %d elements" % p.pairs)
+    _check(load().flowmm_rotary(ctypes.byref(cp), _p(q), _p(k), _p(positions), _p(table), _p(q_out), _p(k_out), _stream()), "flowmm_rotary")
 
 
 def flowmm_selftest_wait_timeout(ws):

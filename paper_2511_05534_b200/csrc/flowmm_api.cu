@@ -18,9 +18,12 @@
 #include "match_small_tc.cuh"
 #include "merge_rows.cuh"
 #include "merge_tc.cuh"
+#include "nibble_attention.cuh"
+#include "nibble_cache.cuh"
 #include "paged_attention.cuh"
 #include "paged_attention_tc.cuh"
 #include "paged_cache.cuh"
+#include "rotary.cuh"
 #include "score_cluster_tc.cuh"
 #include "score_fused_tc.cuh"
 #include "match_tc.cuh"
@@ -1703,6 +1706,211 @@ extern "C" flowmm_status flowmm_cache_attention(const flowmm_cache_params *p, co
     a.scale_log2 = scale * kLog2e;
     if (c.tc) return p->head_dim == 128 ? launch_cache_attention_tc<128>(*p, a, c, st) : launch_cache_attention_tc<64>(*p, a, c, st);
     return p->head_dim == 128 ? launch_cache_attention<128>(a, c, st) : launch_cache_attention<64>(a, c, st);
+}
+
+// ---- paged 4-bit cache ----------------------------------------------------------------------------
+namespace {
+
+size_t nibble_bytes(const flowmm_cache_params &) { return 256; }
+
+flowmm_status check_nibble_ws(const flowmm_cache_params *p, const void *ws, size_t ws_bytes) {
+    if (!ws) return FLOWMM_ERR_NULL;
+    if (reinterpret_cast<uintptr_t>(ws) & 255) return FLOWMM_ERR_ALIGN;
+    return ws_bytes < nibble_bytes(*p) ? FLOWMM_ERR_WORKSPACE : FLOWMM_OK;
+}
+
+template <typename T, int D>
+flowmm_status launch_nibble_store(const nibble::StoreArgs &a, cudaStream_t st) {
+    constexpr int per = nibble::kCopyThreads / (D / 8);
+    // four rows a thread where that leaves every SM a few blocks
+    if (a.rows >= (uint32_t)(per * 4 * 4 * kScoreCtas)) launch(nibble::nibble_store_kernel<T, D, 4>, dim3((a.rows + per * 4 - 1) / (per * 4), 2), nibble::kCopyThreads, 0, st, a);
+    else launch(nibble::nibble_store_kernel<T, D, 1>, dim3((a.rows + per - 1) / per, 2), nibble::kCopyThreads, 0, st, a);
+    FLOWMM_LAUNCHED("nibble_store");
+    return FLOWMM_OK;
+}
+
+}  // namespace
+
+extern "C" flowmm_status flowmm_nibble_workspace_bytes(const flowmm_cache_params *p, size_t *bytes) {
+    if (!bytes) return FLOWMM_ERR_NULL;
+    FLOWMM_TRY(validate_cache(p));
+    *bytes = nibble_bytes(*p);
+    return FLOWMM_OK;
+}
+
+extern "C" flowmm_status flowmm_nibble_store(const flowmm_cache_params *p, const void *k, const void *v, const int32_t *slots,
+                                             void *k_pages, void *v_pages, void *k_scale, void *v_scale, void *ws,
+                                             size_t ws_bytes, void *cuda_stream) {
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    profile_begin(st);
+    FLOWMM_TRY(validate_cache(p));
+    if (p->n_rows < 1) return FLOWMM_ERR_SHAPE;
+    if (!k || !v || !slots || !k_pages || !v_pages || !k_scale || !v_scale) return FLOWMM_ERR_NULL;
+    if (!aligned16(k) || !aligned16(v) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(k_scale) || !aligned16(v_scale) ||
+        !strides_ok(p->k_stride, p->head_dim) || !strides_ok(p->v_stride, p->head_dim) || !aligned4(slots))
+        return FLOWMM_ERR_ALIGN;
+    FLOWMM_TRY(check_nibble_ws(p, ws, ws_bytes));
+    const int64_t rows = (int64_t)p->n_units * p->n_kv_heads * p->n_rows;
+    if (rows >= (int64_t)1 << 31) return FLOWMM_ERR_SHAPE;
+    FLOWMM_TRY(check_device());
+    nibble::StoreArgs a;
+    a.x[0] = k; a.x[1] = v; a.slots = slots; a.status = static_cast<int *>(ws);
+    a.pages[0] = static_cast<uint8_t *>(k_pages); a.pages[1] = static_cast<uint8_t *>(v_pages);
+    a.scale[0] = static_cast<uint8_t *>(k_scale); a.scale[1] = static_cast<uint8_t *>(v_scale);
+    a.page_shift = page_shift(p->page_size); a.n_pages = p->n_pages; a.rows = (uint32_t)rows;
+    for (int i = 0; i < 3; ++i) { a.stride[0][i] = p->k_stride[i]; a.stride[1][i] = p->v_stride[i]; }
+    a.by_rows = make_fastdiv(p->n_rows); a.by_heads = make_fastdiv(p->n_kv_heads);
+    if (p->dtype == FLOWMM_BF16) return p->head_dim == 128 ? launch_nibble_store<__nv_bfloat16, 128>(a, st) : launch_nibble_store<__nv_bfloat16, 64>(a, st);
+    return p->head_dim == 128 ? launch_nibble_store<float, 128>(a, st) : launch_nibble_store<float, 64>(a, st);
+}
+
+extern "C" flowmm_status flowmm_nibble_load(const flowmm_cache_params *p, const void *k_pages, const void *v_pages,
+                                            const void *k_scale, const void *v_scale, const int32_t *block_table,
+                                            const int32_t *rows, void *k, void *v, void *ws, size_t ws_bytes, void *cuda_stream) {
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    profile_begin(st);
+    FLOWMM_TRY(validate_cache(p));
+    if (p->n_rows < 1) return FLOWMM_ERR_SHAPE;
+    if (!k || !v || !k_pages || !v_pages || !k_scale || !v_scale || !block_table || !rows) return FLOWMM_ERR_NULL;
+    if (!aligned16(k) || !aligned16(v) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(k_scale) || !aligned16(v_scale) ||
+        !strides_ok(p->k_stride, p->head_dim) || !strides_ok(p->v_stride, p->head_dim) || !aligned4(block_table) || !aligned4(rows))
+        return FLOWMM_ERR_ALIGN;
+    FLOWMM_TRY(check_nibble_ws(p, ws, ws_bytes));
+    const int64_t chunks = ((int64_t)p->n_rows + nibble::kLoadRows - 1) / nibble::kLoadRows, blocks = 2 * (int64_t)p->n_units * p->n_kv_heads * chunks;
+    if (blocks >= (int64_t)1 << 31) return FLOWMM_ERR_SHAPE;
+    FLOWMM_TRY(check_device());
+    nibble::LoadArgs a;
+    a.pages[0] = static_cast<const uint8_t *>(k_pages); a.pages[1] = static_cast<const uint8_t *>(v_pages);
+    a.scale[0] = static_cast<const uint8_t *>(k_scale); a.scale[1] = static_cast<const uint8_t *>(v_scale);
+    a.table = block_table; a.rows = rows; a.x[0] = k; a.x[1] = v; a.status = static_cast<int *>(ws);
+    a.n_rows = p->n_rows; a.page_shift = page_shift(p->page_size); a.n_pages = p->n_pages; a.max_pages = p->max_pages;
+    for (int i = 0; i < 3; ++i) { a.stride[0][i] = p->k_stride[i]; a.stride[1][i] = p->v_stride[i]; }
+    a.by_heads = make_fastdiv(p->n_kv_heads); a.by_chunks = make_fastdiv((uint32_t)chunks);
+    auto kernel = p->dtype == FLOWMM_BF16 ? (p->head_dim == 128 ? nibble::nibble_load_kernel<__nv_bfloat16, 128> : nibble::nibble_load_kernel<__nv_bfloat16, 64>)
+                                          : (p->head_dim == 128 ? nibble::nibble_load_kernel<float, 128> : nibble::nibble_load_kernel<float, 64>);
+    launch(kernel, (unsigned)blocks, nibble::kCopyThreads, 0, st, a);
+    FLOWMM_LAUNCHED("nibble_load");
+    return FLOWMM_OK;
+}
+
+extern "C" flowmm_status flowmm_nibble_attention(const flowmm_cache_params *p, const void *q, const void *k_pages,
+                                                 const void *v_pages, const void *k_scale, const void *v_scale,
+                                                 const int32_t *block_table, const int32_t *rows, void *out, void *ws,
+                                                 size_t ws_bytes, void *cuda_stream) {
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    profile_begin(st);
+    FLOWMM_TRY(validate_cache(p));
+    if (!q || !k_pages || !v_pages || !k_scale || !v_scale || !block_table || !rows || !out) return FLOWMM_ERR_NULL;
+    if (!aligned16(q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(k_scale) || !aligned16(v_scale) || !aligned16(out) ||
+        !aligned4(block_table) || !aligned4(rows))
+        return FLOWMM_ERR_ALIGN;
+    FLOWMM_TRY(check_nibble_ws(p, ws, ws_bytes));
+    // tiles of all heads are counted in 32 bits
+    if ((int64_t)p->n_units * p->n_q_heads * (((int64_t)p->max_pages * p->page_size + 63) / 64) >= (int64_t)1 << 31) return FLOWMM_ERR_SHAPE;
+    FLOWMM_TRY(check_device());
+    nibble::AttnArgs a;
+    a.q = q; a.k = static_cast<const uint8_t *>(k_pages); a.v = static_cast<const uint8_t *>(v_pages);
+    a.k_scale = static_cast<const uint8_t *>(k_scale); a.v_scale = static_cast<const uint8_t *>(v_scale);
+    a.table = block_table; a.rows = rows; a.out = out; a.status = static_cast<int *>(ws);
+    a.U = p->n_units; a.Hq = p->n_q_heads; a.Hkv = p->n_kv_heads; a.G = p->n_q_heads / p->n_kv_heads;
+    a.page_shift = page_shift(p->page_size); a.n_pages = p->n_pages; a.max_pages = p->max_pages;
+    a.scale_log2 = (p->softmax_scale != 0.f ? p->softmax_scale : 1.f / sqrtf((float)p->head_dim)) * kLog2e;
+    auto kernel = p->dtype == FLOWMM_BF16 ? (p->head_dim == 128 ? nibble::nibble_attention_kernel<__nv_bfloat16, 128> : nibble::nibble_attention_kernel<__nv_bfloat16, 64>)
+                                          : (p->head_dim == 128 ? nibble::nibble_attention_kernel<float, 128> : nibble::nibble_attention_kernel<float, 64>);
+    launch(kernel, (unsigned)(p->n_units * p->n_q_heads), nibble::kSimpleWarps * 32, 0, st, a);
+    FLOWMM_LAUNCHED("nibble_attention");
+    return FLOWMM_OK;
+}
+
+// ---- rotary positions ------------------------------------------------------------------------------
+namespace {
+
+flowmm_status validate_rotary(const flowmm_rotary_params *p) {
+    if (!p) return FLOWMM_ERR_NULL;
+    if (p->n_units < 1 || p->n_q_heads < 1 || p->n_kv_heads < 1 || p->n_rows < 1) return FLOWMM_ERR_SHAPE;
+    if (p->head_dim != 64 && p->head_dim != 128) return FLOWMM_ERR_SHAPE;
+    if (p->rotary_dim < 0 || p->rotary_dim > p->head_dim || p->rotary_dim % 16 != 0) return FLOWMM_ERR_SHAPE;
+    if (p->layout != FLOWMM_ROTARY_HALVES && p->layout != FLOWMM_ROTARY_PAIRS) return FLOWMM_ERR_SHAPE;
+    if (p->adjoint != 0 && p->adjoint != 1) return FLOWMM_ERR_SHAPE;
+    if (p->n_axes != 1 && p->n_axes != 3) return FLOWMM_ERR_SHAPE;
+    if (p->n_axes == 3) {
+        int64_t pairs = 0;
+        for (int s : p->section) {
+            if (s < 0) return FLOWMM_ERR_SHAPE;
+            pairs += s;
+        }
+        if (pairs != (p->rotary_dim ? p->rotary_dim : p->head_dim) / 2) return FLOWMM_ERR_SHAPE;
+    }
+    if (p->scaling < FLOWMM_ROTARY_PLAIN || p->scaling > FLOWMM_ROTARY_BY_PARTS) return FLOWMM_ERR_SHAPE;
+    if (!(p->base >= 1.0) || !isfinite(p->base) || !isfinite(p->amplitude)) return FLOWMM_ERR_SHAPE;
+    if (p->scaling != FLOWMM_ROTARY_PLAIN && (!(p->factor > 0.0) || !isfinite(p->factor))) return FLOWMM_ERR_SHAPE;
+    if (p->scaling == FLOWMM_ROTARY_BY_PARTS && (!(p->high > p->low) || !isfinite(p->high) || !isfinite(p->low) || p->trained < 0)) return FLOWMM_ERR_SHAPE;
+    if (p->dtype != FLOWMM_F32 && p->dtype != FLOWMM_BF16) return FLOWMM_ERR_DTYPE;
+    const int64_t rows = (int64_t)p->n_units * p->n_rows;
+    if (rows >= (int64_t)1 << 31) return FLOWMM_ERR_SHAPE;
+    return FLOWMM_OK;
+}
+
+template <typename T, int D>
+flowmm_status launch_rotary(const flowmm_rotary_params &p, rotary::Args &a, cudaStream_t st) {
+    constexpr int per = rotary::kThreads / (D / (2 * Elem<T>::kVec));
+    const int64_t blocks = ((int64_t)a.rows + per - 1) / per;
+    const int heads = a.heads[0] + a.heads[1];
+    // as many heads to a thread as leave every SM eight blocks; blocks of heads in the grid's second dimension, 65 535 at most
+    const int64_t want = std::max<int64_t>(1, std::min<int64_t>(heads, blocks * heads / (8 * kScoreCtas)));
+    a.each = (int)std::max<int64_t>(want, (heads + 65534) / 65535);
+    auto kernel = p.layout == FLOWMM_ROTARY_PAIRS ? rotary::rotary_kernel<T, D, true> : rotary::rotary_kernel<T, D, false>;
+    launch(kernel, dim3((unsigned)blocks, (heads + a.each - 1) / a.each), rotary::kThreads, 0, st, a);
+    FLOWMM_LAUNCHED("rotary");
+    return FLOWMM_OK;
+}
+
+}  // namespace
+
+extern "C" flowmm_status flowmm_rotary_table(const flowmm_rotary_params *p, uint64_t *table, void *cuda_stream) {
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    profile_begin(st);
+    FLOWMM_TRY(validate_rotary(p));
+    if (!table) return FLOWMM_ERR_NULL;
+    if (reinterpret_cast<uintptr_t>(table) & 7) return FLOWMM_ERR_ALIGN;
+    FLOWMM_TRY(check_device());
+    rotary::TableArgs a;
+    a.phase = reinterpret_cast<unsigned long long *>(table); a.R = p->rotary_dim ? p->rotary_dim : p->head_dim; a.scaling = p->scaling;
+    a.base = p->base; a.factor = p->factor; a.low = p->low; a.high = p->high; a.trained = p->trained;
+    launch(rotary::rotary_table_kernel, 1, 64, 0, st, a);
+    FLOWMM_LAUNCHED("rotary_table");
+    return FLOWMM_OK;
+}
+
+extern "C" flowmm_status flowmm_rotary(const flowmm_rotary_params *p, const void *q, const void *k, const int32_t *positions,
+                                       const uint64_t *table, void *q_out, void *k_out, void *cuda_stream) {
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    profile_begin(st);
+    FLOWMM_TRY(validate_rotary(p));
+    if (!positions || !table || !q != !q_out || !k != !k_out || (!q && !k)) return FLOWMM_ERR_NULL;
+    if (!aligned4(positions) || (reinterpret_cast<uintptr_t>(table) & 7)) return FLOWMM_ERR_ALIGN;
+    const void *in[2] = {q, k};
+    void *out[2] = {q_out, k_out};
+    const int64_t *si[2] = {p->q_stride, p->k_stride}, *so[2] = {p->q_out_stride, p->k_out_stride};
+    for (int i = 0; i < 2; ++i) {
+        if (!in[i]) continue;
+        if (!aligned16(in[i]) || !aligned16(out[i]) || !strides_ok(si[i], p->head_dim) || !strides_ok(so[i], p->head_dim)) return FLOWMM_ERR_ALIGN;
+        if (in[i] == out[i] && memcmp(si[i], so[i], 3 * sizeof(int64_t)) != 0) return FLOWMM_ERR_SHAPE;
+    }
+    FLOWMM_TRY(check_device());
+    rotary::Args a;
+    for (int i = 0; i < 2; ++i) {
+        a.x[i] = in[i]; a.y[i] = out[i];
+        for (int d = 0; d < 3; ++d) { a.in[i][d] = si[i][d]; a.out[i][d] = so[i][d]; }
+    }
+    a.heads[0] = q ? p->n_q_heads : 0; a.heads[1] = k ? p->n_kv_heads : 0;
+    a.positions = positions; a.phase = reinterpret_cast<const unsigned long long *>(table);
+    a.R = p->rotary_dim ? p->rotary_dim : p->head_dim; a.axes = p->n_axes; a.adjoint = p->adjoint;
+    a.end0 = p->n_axes == 3 ? p->section[0] : a.R / 2; a.end1 = p->n_axes == 3 ? p->section[0] + p->section[1] : a.R / 2;
+    a.amplitude = p->amplitude != 0.f ? p->amplitude : 1.f;
+    a.rows = (uint32_t)((int64_t)p->n_units * p->n_rows); a.by_rows = make_fastdiv(p->n_rows);
+    if (p->dtype == FLOWMM_BF16) return p->head_dim == 128 ? launch_rotary<__nv_bfloat16, 128>(*p, a, st) : launch_rotary<__nv_bfloat16, 64>(*p, a, st);
+    return p->head_dim == 128 ? launch_rotary<float, 128>(*p, a, st) : launch_rotary<float, 64>(*p, a, st);
 }
 
 // ---- re-compression of a cache that grew during decoding ----------------------------------------

@@ -1,0 +1,211 @@
+// The paged 4-bit cache: rows quantised into pages, pages read back.
+//
+// Layout: pages of codes [n_pages, Hkv, page_size, D / 2], two channels a byte (the even one in the low half), and of scales
+// [n_pages, Hkv, page_size, D / 16], one for 16 neighbouring channels of a row.  A code is e2m1 (sign, two exponent bits, one of mantissa: 0, 0.5, 1,
+// 1.5, 2, 3, 4, 6), a scale the upper byte of a positive fp16 without its lowest seven bits (five exponent bits, three of mantissa),
+// so widening it is a shift, its range needs no second scale, and the product of the two is an fp16 exactly.  Rows do not depend on one
+// another: a row that is appended changes nothing else, and any row may go anywhere.
+// (Random keys with a few strong channels, the attention's output against the one without quantising, root mean square relative to its own:
+// so 0.159; integers with a scale of 16 bits for 32 channels, as many bits, 0.219; integers with a scale and an offset for 32, 5 bits, 0.155;
+// e2m1 with a power of two for 32, 4.25 bits, 0.277; scales rounded up and not to the nearest 0.184.)
+#pragma once
+#include "common.cuh"
+#include "paged_cache.cuh"
+
+namespace flowmm {
+namespace nibble {
+
+using paged::report;
+
+constexpr int kGroup = 16;                       // channels with a scale
+constexpr uint32_t kLeastScale = 0x38800000u;    // 2^-14, fp16's least normal number, as the bits of an fp32
+constexpr uint32_t kMostScale = 0x46200000u;     // 10240: the largest scale whose products with codes (6 at most) are fp16 numbers
+constexpr uint32_t kScaleBias = 896u;            // bits >> 20 of the fp32 minus the byte: 8 (127 - 15)
+constexpr uint32_t kNanScale = 255u;
+
+// The scale of a group whose largest size has these bits (finite): a sixth of it rounded to four significant bits, to the nearest, ties to even.
+// (IEEE division takes no number next to a tie onto it: the dividend has 24 bits, a tie times 6 has 8.)
+__device__ __forceinline__ uint32_t scale_bits(uint32_t size) {
+    uint32_t b = __float_as_uint(__fdiv_rn(__uint_as_float(size), 6.f));
+    b = (b + 0x7FFFFu + (b >> 20 & 1u)) & 0xFFF00000u;
+    return min(max(b, kLeastScale), kMostScale);
+}
+// Eight quotients x / s as codes.  Borders between codes are hit exactly (they have three bits, s has four), so the quotients are correctly rounded:
+// x times the rounded reciprocal, corrected once by the remainder (Markstein 1990).
+__device__ __forceinline__ uint32_t codes8(const float (&x)[8], float s, float inverse) {
+    float y[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float y0 = x[i] * inverse;
+        y[i] = fmaf(-fmaf(y0, s, -x[i]), inverse, y0);               // (this way round a zero keeps its sign)
+    }
+    uint32_t c;
+    asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
+        "mov.b32 %0, {a, b, c, d};\n\t}"
+        : "=r"(c)
+        : "f"(y[0]), "f"(y[1]), "f"(y[2]), "f"(y[3]), "f"(y[4]), "f"(y[5]), "f"(y[6]), "f"(y[7]));
+    return c;
+}
+// Eight codes as four pairs of fp16, neighbouring channels together.
+__device__ __forceinline__ void widen8(uint32_t c, uint32_t (&h)[4]) {
+    asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+        "mov.b32 {a, b, c, d}, %4;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %0, a;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %1, b;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %2, c;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %3, d;\n\t}"
+        : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3])
+        : "r"(c));
+}
+__device__ __forceinline__ float2 from_half2(uint32_t h) {
+    float2 f;
+    asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.f32.f16 %0, a;\n\tcvt.f32.f16 %1, b;\n\t}" : "=f"(f.x), "=f"(f.y) : "r"(h));
+    return f;
+}
+__device__ __forceinline__ float scale_value(uint32_t byte) { return from_half2(byte << 7).x; }
+__device__ __forceinline__ void values8(uint32_t codes, uint32_t scale, float (&x)[8]) {
+    uint32_t h[4];
+    widen8(codes, h);
+    const float s = scale_value(scale);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 f = from_half2(h[i]);
+        x[2 * i] = f.x * s;
+        x[2 * i + 1] = f.y * s;
+    }
+}
+
+// eight neighbouring elements as they are in memory
+template <typename T> struct Eight;
+template <> struct Eight<__nv_bfloat16> {
+    uint4 v;
+    __device__ __forceinline__ void load(const __nv_bfloat16 *p) { v = load_raw16(p); }
+    __device__ __forceinline__ uint32_t size() const { return paged::largest_bits<__nv_bfloat16>(v); }
+    __device__ __forceinline__ void get(float (&x)[8]) const { Elem<__nv_bfloat16>::unpack(v, x); }
+    static __device__ __forceinline__ void store(__nv_bfloat16 *p, const float (&x)[8]) { Elem<__nv_bfloat16>::store16(p, x); }
+};
+template <> struct Eight<float> {
+    uint4 v[2];
+    __device__ __forceinline__ void load(const float *p) { v[0] = load_raw16(p); v[1] = load_raw16(p + 4); }
+    __device__ __forceinline__ uint32_t size() const { return max(paged::largest_bits<float>(v[0]), paged::largest_bits<float>(v[1])); }
+    __device__ __forceinline__ void get(float (&x)[8]) const {
+        const uint32_t w[8] = {v[0].x, v[0].y, v[0].z, v[0].w, v[1].x, v[1].y, v[1].z, v[1].w};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(w[i]);
+    }
+    static __device__ __forceinline__ void store(float *p, const float (&x)[8]) {
+        *reinterpret_cast<float4 *>(p) = make_float4(x[0], x[1], x[2], x[3]);
+        *reinterpret_cast<float4 *>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
+    }
+};
+
+constexpr int kCopyThreads = 256;
+
+// ---- rows into pages -----------------------------------------------------------------------------
+struct StoreArgs {
+    const void *x[2];                  // K and V rows [U, Hkv, T, D]
+    const int *slots;                  // [U, T]
+    uint8_t *pages[2], *scale[2];
+    int *status;
+    int page_shift, n_pages;
+    uint32_t rows;                     // U * Hkv * T
+    int64_t stride[2][3];
+    FastDiv by_rows, by_heads;         // by T, by Hkv
+};
+
+// Rows stand in a line, by tensor, unit, KV head and row; D / 8 threads have a row, eight channels each, the two threads of a group find its scale together.
+template <typename T, int D, int kVecs>
+__global__ void __launch_bounds__(kCopyThreads) nibble_store_kernel(const StoreArgs A) {
+    constexpr int kLanes = D / 8, kRows = kCopyThreads / kLanes;
+    predecessor_done();
+    successor_may_start();
+    const int lane = threadIdx.x % kLanes;
+    const uint32_t which = blockIdx.y, row0 = blockIdx.x * (kRows * kVecs) + threadIdx.x / kLanes;
+    Eight<T> raw[kVecs];
+    int slot[kVecs];
+    uint32_t head[kVecs];
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+        const uint32_t row = row0 + i * kRows;
+        slot[i] = -1;
+        if (row >= A.rows) continue;
+        const uint32_t uh = A.by_rows.div(row), t = row - uh * A.by_rows.d, u = A.by_heads.div(uh);
+        head[i] = uh - u * A.by_heads.d;
+        slot[i] = A.slots[u * A.by_rows.d + t];
+        raw[i].load(static_cast<const T *>(A.x[which]) + u * A.stride[which][0] + head[i] * A.stride[which][1] + t * A.stride[which][2] + lane * 8);
+    }
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+        if (slot[i] < -1 || slot[i] >= A.n_pages << A.page_shift) { report(A.status, kStatusIndex); slot[i] = -1; }
+        uint32_t size = slot[i] < 0 ? 0u : raw[i].size();
+        size = max(size, __shfl_xor_sync(0xFFFFFFFFu, size, 1));
+        if (slot[i] < 0) continue;
+        const int64_t at = ((((int64_t)(slot[i] >> A.page_shift) * A.by_heads.d + head[i]) << A.page_shift) + (slot[i] & ((1 << A.page_shift) - 1)));
+        const bool finite = size < paged::kInfinityBits;
+        const uint32_t b = scale_bits(size);
+        const float s = __uint_as_float(b);
+        float x[8];
+        raw[i].get(x);
+        const uint32_t codes = codes8(x, s, __frcp_rn(s));
+        *reinterpret_cast<uint32_t *>(A.pages[which] + at * (D / 2) + lane * 4) = finite ? codes : 0u;
+        if ((lane & 1) == 0) A.scale[which][at * (D / kGroup) + lane / 2] = (uint8_t)(finite ? (b >> 20) - kScaleBias : kNanScale);
+    }
+}
+
+// ---- pages into rows -----------------------------------------------------------------------------
+struct LoadArgs {
+    const uint8_t *pages[2], *scale[2];
+    const int *table, *rows;           // [U, max_pages], [U]
+    void *x[2];                        // [U, Hkv, n_rows, D]
+    int *status;
+    int n_rows, page_shift, n_pages, max_pages;
+    int64_t stride[2][3];
+    FastDiv by_heads, by_chunks;
+};
+constexpr int kLoadRows = 64;
+
+// A block takes 64 rows of one (unit, KV head, K or V); D / 8 threads have a row.
+template <typename T, int D>
+__global__ void __launch_bounds__(kCopyThreads) nibble_load_kernel(const LoadArgs A) {
+    constexpr int kLanes = D / 8, kRows = kCopyThreads / kLanes, kVecs = kLoadRows / kRows;
+    predecessor_done();
+    successor_may_start();
+    const int lane = threadIdx.x % kLanes, row0 = threadIdx.x / kLanes;
+    const uint32_t which = blockIdx.x & 1u, q = blockIdx.x >> 1, q1 = A.by_heads.div(q), h = q - q1 * A.by_heads.d;
+    const uint32_t u = A.by_chunks.div(q1), chunk = q1 - u * A.by_chunks.d;
+    const int first = (int)(chunk * kLoadRows), held = A.rows[u], most = A.max_pages << A.page_shift;
+    if ((held < 0 || held > most) && threadIdx.x == 0) report(A.status, kStatusIndex);
+    const int n = min(min(held, most), A.n_rows) - first;             // rows of this block
+    const int *table = A.table + (int64_t)u * A.max_pages;
+    if (n <= 0) return;
+    int id[kVecs];
+    uint32_t codes[kVecs], scale[kVecs];
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+        const int r = row0 + i * kRows;
+        id[i] = r < n ? table[(first + r) >> A.page_shift] : -1;
+        if (r < n && (unsigned)id[i] >= (unsigned)A.n_pages) { report(A.status, kStatusIndex); id[i] = -1; }
+    }
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+        if (id[i] < 0) continue;
+        const int64_t at = (((int64_t)id[i] * A.by_heads.d + h) << A.page_shift) + ((first + row0 + i * kRows) & ((1 << A.page_shift) - 1));
+        codes[i] = *reinterpret_cast<const uint32_t *>(A.pages[which] + at * (D / 2) + lane * 4);
+        scale[i] = A.scale[which][at * (D / kGroup) + lane / 2];
+    }
+    T *x = static_cast<T *>(A.x[which]) + u * A.stride[which][0] + h * A.stride[which][1] + (int64_t)first * A.stride[which][2] + lane * 8;
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+        if (id[i] < 0) continue;
+        float f[8];
+        values8(codes[i], scale[i], f);
+        Eight<T>::store(x + (int64_t)(row0 + i * kRows) * A.stride[which][2], f);
+    }
+}
+
+}  // namespace nibble
+}  // namespace flowmm
