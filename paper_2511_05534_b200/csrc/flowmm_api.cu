@@ -1711,7 +1711,24 @@ extern "C" flowmm_status flowmm_cache_attention(const flowmm_cache_params *p, co
 // ---- paged 4-bit cache ----------------------------------------------------------------------------
 namespace {
 
-size_t nibble_bytes(const flowmm_cache_params &) { return 256; }
+// The attention's scratch: [status word, 256 bytes][cut heads][records], the last two where a head may be cut.
+struct NibblePlan {
+    bool joins;
+    int64_t blocks;
+    size_t part, total;
+};
+
+NibblePlan nibble_plan(const flowmm_cache_params &p) {
+    NibblePlan n;
+    const int64_t heads = (int64_t)p.n_units * p.n_kv_heads, tiles = ((int64_t)p.max_pages * p.page_size + nibble::kTile - 1) / nibble::kTile;
+    n.blocks = std::min<int64_t>(2 * kScoreCtas, heads * tiles);
+    n.joins = heads > n.blocks || tiles > nibble::kWholeTiles;
+    n.part = 256 + (n.joins ? align256((size_t)n.blocks * sizeof(int4)) : 0);
+    n.total = n.part + (n.joins ? align256((size_t)n.blocks * 2 * paged::record_floats(p.n_q_heads / p.n_kv_heads, p.head_dim) * sizeof(float)) : 0);
+    return n;
+}
+
+size_t nibble_bytes(const flowmm_cache_params &p) { return nibble_plan(p).total; }
 
 flowmm_status check_nibble_ws(const flowmm_cache_params *p, const void *ws, size_t ws_bytes) {
     if (!ws) return FLOWMM_ERR_NULL;
@@ -1726,6 +1743,25 @@ flowmm_status launch_nibble_store(const nibble::StoreArgs &a, cudaStream_t st) {
     if (a.rows >= (uint32_t)(per * 4 * 4 * kScoreCtas)) launch(nibble::nibble_store_kernel<T, D, 4>, dim3((a.rows + per * 4 - 1) / (per * 4), 2), nibble::kCopyThreads, 0, st, a);
     else launch(nibble::nibble_store_kernel<T, D, 1>, dim3((a.rows + per - 1) / per, 2), nibble::kCopyThreads, 0, st, a);
     FLOWMM_LAUNCHED("nibble_store");
+    return FLOWMM_OK;
+}
+
+template <typename T, int D>
+flowmm_status launch_nibble_attention(const nibble::AttnArgs &a, const NibblePlan &n, cudaStream_t st) {
+    auto kernel = nibble::nibble_attention_kernel<T, D>;
+    if (!allow_smem(kernel) || cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared) != cudaSuccess)
+        return FLOWMM_ERR_CUDA;
+    launch(kernel, (unsigned)n.blocks, nibble::kAttnThreads, nibble::Lay<D>::kBytes, st, a);
+    FLOWMM_LAUNCHED("nibble_attention");
+    if (!n.joins) return FLOWMM_OK;
+    paged::AttnArgs j = {};
+    j.out = static_cast<float *>(a.out); j.part = a.part; j.cut_heads = a.cut_heads; j.Hq = a.Hq;
+    const int record = paged::record_floats(a.G, D);
+    if (a.U * a.Hkv <= paged::kFewHeads)
+        launch(paged::cache_join_kernel<D, 4, T>, dim3((unsigned)n.blocks, (a.G + 1) / 2), paged::kJoinThreads, 0, st, j, record, 2, 1, 2);
+    else
+        launch(paged::cache_join_kernel<D, 1, T>, (unsigned)n.blocks, paged::kJoinThreads, 0, st, j, record, 2, 1, 2);
+    FLOWMM_LAUNCHED("nibble_join");
     return FLOWMM_OK;
 }
 
@@ -1809,17 +1845,17 @@ extern "C" flowmm_status flowmm_nibble_attention(const flowmm_cache_params *p, c
     if ((int64_t)p->n_units * p->n_q_heads * (((int64_t)p->max_pages * p->page_size + 63) / 64) >= (int64_t)1 << 31) return FLOWMM_ERR_SHAPE;
     FLOWMM_TRY(check_device());
     nibble::AttnArgs a;
-    a.q = q; a.k = static_cast<const uint8_t *>(k_pages); a.v = static_cast<const uint8_t *>(v_pages);
-    a.k_scale = static_cast<const uint8_t *>(k_scale); a.v_scale = static_cast<const uint8_t *>(v_scale);
+    const NibblePlan n = nibble_plan(*p);
+    a.q = q; a.pages[0] = static_cast<const uint8_t *>(k_pages); a.pages[1] = static_cast<const uint8_t *>(v_pages);
+    a.scale[0] = static_cast<const uint8_t *>(k_scale); a.scale[1] = static_cast<const uint8_t *>(v_scale);
     a.table = block_table; a.rows = rows; a.out = out; a.status = static_cast<int *>(ws);
+    a.part = at<float>(ws, n.part); a.cut_heads = n.joins ? at<int4>(ws, 256) : nullptr;
     a.U = p->n_units; a.Hq = p->n_q_heads; a.Hkv = p->n_kv_heads; a.G = p->n_q_heads / p->n_kv_heads;
     a.page_shift = page_shift(p->page_size); a.n_pages = p->n_pages; a.max_pages = p->max_pages;
     a.scale_log2 = (p->softmax_scale != 0.f ? p->softmax_scale : 1.f / sqrtf((float)p->head_dim)) * kLog2e;
-    auto kernel = p->dtype == FLOWMM_BF16 ? (p->head_dim == 128 ? nibble::nibble_attention_kernel<__nv_bfloat16, 128> : nibble::nibble_attention_kernel<__nv_bfloat16, 64>)
-                                          : (p->head_dim == 128 ? nibble::nibble_attention_kernel<float, 128> : nibble::nibble_attention_kernel<float, 64>);
-    launch(kernel, (unsigned)(p->n_units * p->n_q_heads), nibble::kSimpleWarps * 32, 0, st, a);
-    FLOWMM_LAUNCHED("nibble_attention");
-    return FLOWMM_OK;
+    if (p->dtype == FLOWMM_BF16)
+        return p->head_dim == 128 ? launch_nibble_attention<__nv_bfloat16, 128>(a, n, st) : launch_nibble_attention<__nv_bfloat16, 64>(a, n, st);
+    return p->head_dim == 128 ? launch_nibble_attention<float, 128>(a, n, st) : launch_nibble_attention<float, 64>(a, n, st);
 }
 
 // ---- rotary positions ------------------------------------------------------------------------------

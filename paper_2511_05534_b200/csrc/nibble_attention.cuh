@@ -1,8 +1,21 @@
 // Decode attention over the paged 4-bit cache: one new query per query head, lengths of their own for every unit.
 //   o = sum_j softmax_j(scale * q . k_j) v_j,   k_j, v_j: rows of e2m1 codes times their groups' scales
+//
+// One pass over K and V with a running maximum and sum.  A row of 128 channels is 72 bytes of K and 72 of V for 4 G 128 flops: memory bounds long calls as long
+// as a row takes an SM no more than 6.3 clocks, so the products go to the tensor cores and codes are widened in registers, by warps that feed their own matrix
+// instructions (mma.sync, fp16 operands, fp32 sums): a code times its scale is an fp16 number exactly, one conversion and one packed product for two of
+// them.  (tcgen05 takes its operands from shared or tensor memory: 256 bytes a row written and read there again for the 72 that came, 4 and 4 clocks of
+// the 6.3; and e2m1 operands with scales of their own, which it takes as they are, would want queries and weights in 4 or 8 bits.)
+//   S[key, head] = K Q^T:  16 keys on the wide side, eight query heads, the most there are, on the narrow one
+//   O^T[channel, head] = V^T W^T:  16 channels on the wide side; the weights go from the first product's layout to the second's by a transpose in registers
+// Which channel and which key stand at which place of an operand is free as long as both operands agree: a lane takes 16 neighbouring bytes of a K row and
+// 8 of a V row, one scale for all channels that it has of a V row, and ends with 16 neighbouring channels of two query heads.
+// bf16: a query is an fp16 number times a power of two exactly, a weight is rounded to fp16 (2^-12, where the output is rounded to 2^-9); fp32: both are the
+// sum of two fp16 numbers, each product is two.  Weights are 2^14 for the largest, so that fp16 holds them to full precision down to 2^-28 of that.
 #pragma once
 #include "common.cuh"
 #include "nibble_cache.cuh"
+#include "paged_attention.cuh"
 #include "tc_common.cuh"
 
 namespace flowmm {
@@ -10,80 +23,577 @@ namespace nibble {
 
 struct AttnArgs {
     const void *q;                     // [U, Hq, D] dense
-    const uint8_t *k, *v;              // pages [n_pages, Hkv, page, D / 2]
-    const uint8_t *k_scale, *v_scale;  // [n_pages, Hkv, page, D / 16]
+    const uint8_t *pages[2];           // of K and V [n_pages, Hkv, page, D / 2]
+    const uint8_t *scale[2];           // [n_pages, Hkv, page, D / 16]
     const int *table, *rows;           // [U, max_pages], [U]
     void *out;                         // [U, Hq, D]
+    float *part;                       // two records a block (paged::record_floats)
+    int4 *cut_heads;                   // [blocks], as paged::AttnArgs has it, or null: no head is cut
     int *status;
     int U, Hq, Hkv, G, page_shift, n_pages, max_pages;
     float scale_log2;
 };
 
-constexpr float kLowest = -3.402823466e38f;
+constexpr int kTile = 64, kWarps = 6, kAttnThreads = kWarps * 32, kHeads = 8;
+constexpr float kLowest = paged::kLowest;
+constexpr float kWeightExponent = 14.f;
 
-template <typename T> __device__ __forceinline__ float as_float(T x);
-template <> __device__ __forceinline__ float as_float<float>(float x) { return x; }
-template <> __device__ __forceinline__ float as_float<__nv_bfloat16>(__nv_bfloat16 x) { return __bfloat162float(x); }
+// What a warp has in shared memory: three half tiles (64 rows of K or of V: codes, then scales), K and V in turn, and a record.
+template <int D> struct Lay {
+    static constexpr uint32_t kCodes = kTile * D / 2, kScales = kTile * D / kGroup, kHalf = kCodes + kScales;
+    static constexpr uint32_t kRecord = kHeads * (D + 2) * 4;
+    static constexpr uint32_t kRecords = kWarps * 3 * kHalf, kBars = kRecords + kWarps * kRecord, kMeta = kBars + kWarps * 3 * 8;
+    static constexpr uint32_t kBytes = kMeta + kWarps * 32 + 16;
+    static_assert(kRecord <= 3 * kHalf && 2 * (kBytes + 1024) <= 228 * 1024, "two blocks to an SM");
+};
+
+// ---- how the work is shared out ------------------------------------------------------------------
+// The tiles of all heads stand in a line, by unit, head and key.  With at most as many heads as blocks a block has a range of one head, `per` tiles or what
+// remains of it; else an equal piece of the line.  A block's warps have equal parts of its tiles, one after the other.
+constexpr int kWholeTiles = 2 * kWarps, kJoinTiles = 2 * kWarps, kSwitchTiles = kWarps;
+
+__device__ __forceinline__ int unit_rows(const AttnArgs &A, int u) {
+    const int n = A.rows[u], most = A.max_pages << A.page_shift;
+    return n < 0 ? 0 : min(n, most);
+}
+__device__ __forceinline__ int tiles_of(int rows) { return (rows + kTile - 1) / kTile; }
+
+struct Cut {
+    int u0, u1;                          // this lane's units
+    uint32_t mine, upto;                 // their tiles, of one head; with all units before
+    uint32_t all, per, share;            // tiles of all heads; of a range, or 0; of a piece
+    uint32_t ranges, ranges_upto;        // ranges of a head of each of this lane's units; with all units before
+};
+__device__ __forceinline__ uint32_t sum_upto(uint32_t x) {
+    const int lane = lane_id();
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t y = __shfl_up_sync(0xFFFFFFFFu, x, o);
+        if (lane >= o) x += y;
+    }
+    return x;
+}
+__device__ __forceinline__ Cut make_cut(const AttnArgs &A) {
+    Cut c;
+    const int each = (A.U + 31) >> 5;
+    c.u0 = min(A.U, lane_id() * each);
+    c.u1 = min(A.U, c.u0 + each);
+    c.mine = 0;
+    int longest = 0;
+#pragma unroll 4
+    for (int u = c.u0; u < c.u1; ++u) {
+        const int t = tiles_of(unit_rows(A, u));
+        c.mine += t;
+        longest = max(longest, t);
+    }
+    c.upto = sum_upto(c.mine);
+    longest = __reduce_max_sync(0xFFFFFFFFu, longest);
+    c.all = __shfl_sync(0xFFFFFFFFu, c.upto, 31) * A.Hkv;
+    const uint32_t blocks = gridDim.x, heads = (uint32_t)A.U * A.Hkv;
+    c.share = max(1u, (c.all + blocks - 1) / blocks);
+    c.per = c.ranges = c.ranges_upto = 0;
+    if (heads > blocks) return c;
+    const uint32_t whole = max(1, longest);
+    for (uint32_t per = c.share; per <= c.share + kSwitchTiles || per == whole; ++per) {
+        if (whole <= kWholeTiles || whole <= per + kJoinTiles) per = whole;
+        uint32_t n = 0;
+#pragma unroll 2
+        for (int u = c.u0; u < c.u1; ++u) n += ((uint32_t)tiles_of(unit_rows(A, u)) + per - 1) / per;
+        if (__reduce_add_sync(0xFFFFFFFFu, n) * A.Hkv > blocks) continue;
+        c.per = per;
+        c.ranges = n;
+        c.ranges_upto = sum_upto(n);
+        break;
+    }
+    return c;
+}
+// Tile t of the head (u, h).
+struct Walk { int u, h, t, tiles, rows; };
+__device__ __forceinline__ void walk_on(const AttnArgs &A, Walk &w) {
+    if (++w.t < w.tiles) return;
+    w.t = 0;
+    if (++w.h < A.Hkv) return;
+    w.h = 0;
+    do { ++w.u; w.rows = w.u < A.U ? unit_rows(A, w.u) : 0; w.tiles = tiles_of(w.rows); } while (w.tiles == 0 && w.u < A.U);
+}
+// Where tile x is, x below c.all; base: the number of the unit's first tile.
+__device__ __forceinline__ Walk walk_to(const AttnArgs &A, const Cut &c, uint32_t x) {
+    const uint32_t H = A.Hkv;
+    const int owner = __ffs(__ballot_sync(0xFFFFFFFFu, x < c.upto * H)) - 1;
+    int u = 0;
+    uint32_t base = 0;
+    if (lane_id() == owner) {
+        base = c.upto - c.mine;
+        for (u = c.u0; u < c.u1 - 1; ++u) {
+            const int t = tiles_of(unit_rows(A, u));
+            if (x < (base + t) * H) break;
+            base += t;
+        }
+    }
+    Walk w;
+    w.u = __shfl_sync(0xFFFFFFFFu, u, owner);
+    base = __shfl_sync(0xFFFFFFFFu, base, owner) * H;
+    w.rows = unit_rows(A, w.u);
+    w.tiles = tiles_of(w.rows);
+    w.h = (x - base) / (uint32_t)w.tiles;
+    w.t = x - base - w.h * w.tiles;
+    return w;
+}
+// The block's tiles [x0, x1); none: x0 == x1.
+__device__ __forceinline__ void block_piece(const AttnArgs &A, const Cut &c, uint32_t &x0, uint32_t &x1) {
+    if (c.per == 0) {
+        x0 = min(c.all, blockIdx.x * c.share);
+        x1 = min(c.all, x0 + c.share);
+        return;
+    }
+    // ranges are numbered by unit, head and key
+    const uint32_t H = A.Hkv, i = blockIdx.x, hit = __ballot_sync(0xFFFFFFFFu, i < c.ranges_upto * H);
+    x0 = x1 = 0;
+    if (hit == 0) return;
+    const int owner = __ffs(hit) - 1;
+    if (lane_id() == owner) {
+        uint32_t ranges = (c.ranges_upto - c.ranges) * H, base = (c.upto - c.mine) * H;
+        for (int u = c.u0; u < c.u1; ++u) {
+            const uint32_t t = tiles_of(unit_rows(A, u)), n = (t + c.per - 1) / c.per;
+            if (i < ranges + n * H) {
+                const uint32_t in = i - ranges, h = in / n, first = (in - h * n) * c.per;
+                x0 = base + h * t + first;
+                x1 = x0 + min(c.per, t - first);
+                break;
+            }
+            ranges += n * H;
+            base += t * H;
+        }
+    }
+    x0 = __shfl_sync(0xFFFFFFFFu, x0, owner);
+    x1 = __shfl_sync(0xFFFFFFFFu, x1, owner);
+}
+
+// ---- matrix instructions -------------------------------------------------------------------------
+__device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// An 8 by 8 matrix of fp16, a row of it in four neighbouring lanes, transposed; by a whole warp.
+__device__ __forceinline__ uint32_t transposed(uint32_t x) {
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t half2_of(float lo, float hi) {
+    uint32_t h;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(h) : "f"(hi), "f"(lo));
+    return h;
+}
+__device__ __forceinline__ uint32_t times(uint32_t a, uint32_t b) {
+    uint32_t h;
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(h) : "r"(a), "r"(b));
+    return h;
+}
+__device__ __forceinline__ float max_over_rows(float x) {              // over the lanes with the same lane % 4
+#pragma unroll
+    for (int o = 4; o < 32; o <<= 1) x = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, o));
+    return x;
+}
+
+// The query operand of a head: a lane has query head lane / 4, the channels that it takes of a K row, and of every word of eight the pairs in order.
+template <int D, bool kTwo> struct Queries {
+    uint32_t hi[D / 8], lo[kTwo ? D / 8 : 1];      // [D / 32 words][4 pairs]
+    float factor[2];                               // of the logits of query heads 2 (lane % 4) and the next one
+};
+template <typename T, int D>
+__device__ __forceinline__ void load_queries(const AttnArgs &A, int u, int h, Queries<D, sizeof(T) == 4> &Q) {
+    constexpr bool kTwo = sizeof(T) == 4;
+    constexpr int kWords = D / 32;
+    const int lane = lane_id(), r = lane >> 2, t = lane & 3;
+    const T *q = static_cast<const T *>(A.q) + ((int64_t)u * A.Hq + h * A.G + r) * D + t * (D / 4);
+    Eight<T> raw[kWords];
+    uint32_t size = 0;
+    const bool on = r < A.G;
+#pragma unroll
+    for (int w = 0; w < kWords; ++w) {
+        if (on) {
+            raw[w].load(q + 8 * w);
+            size = max(size, raw[w].size());
+        }
+    }
+    size = max(size, __shfl_xor_sync(0xFFFFFFFFu, size, 1));
+    size = max(size, __shfl_xor_sync(0xFFFFFFFFu, size, 2));
+    const bool finite = size < paged::kInfinityBits;
+    const int ex = finite ? max(-100, (int)(size >> 23) - 127) - 14 : 0;          // the largest element to [2^14, 2^15)
+    const float f = paged::power_of_two(-ex);
+#pragma unroll
+    for (int w = 0; w < kWords; ++w) {
+        float x[8];
+        if (on) raw[w].get(x);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float a = on ? x[2 * i] * f : 0.f, b = on ? x[2 * i + 1] * f : 0.f;
+            const uint32_t hi = half2_of(a, b);
+            Q.hi[4 * w + i] = hi;
+            if constexpr (kTwo) {
+                const float2 g = from_half2(hi);
+                Q.lo[4 * w + i] = half2_of(a - g.x, b - g.y);
+            }
+        }
+    }
+    const float factor = finite ? paged::power_of_two(ex) * A.scale_log2 : __uint_as_float(0x7FC00000u);
+    Q.factor[0] = __shfl_sync(0xFFFFFFFFu, factor, 8 * t);
+    Q.factor[1] = __shfl_sync(0xFFFFFFFFu, factor, 8 * t + 4);
+}
+
+// ---- records -------------------------------------------------------------------------------------
+// [heads][D] outputs relative to the maximum, then maxima (log2), then sums of weights; 16 neighbouring channels of two query heads a lane (D = 64: eight).
+template <int D>
+__device__ __forceinline__ void put_record(float *rec, const float (&o)[D / 16][4], const float (&m)[2], const float (&l)[2]) {
+    const int lane = lane_id(), r = lane >> 2, t = lane & 3;
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        float4 *to = reinterpret_cast<float4 *>(rec + (2 * t + q) * D + r * (D / 8));
+#pragma unroll
+        for (int j = 0; j < D / 16; j += 2) to[j / 2] = make_float4(o[j][q], o[j][2 + q], o[j + 1][q], o[j + 1][2 + q]);
+        if (r == 0) { rec[kHeads * D + 2 * t + q] = m[q]; rec[kHeads * (D + 1) + 2 * t + q] = l[q]; }
+    }
+}
+__device__ __forceinline__ void put_four(float *to, const float (&x)[4]) { *reinterpret_cast<float4 *>(to) = make_float4(x[0], x[1], x[2], x[3]); }
+__device__ __forceinline__ void put_four(__nv_bfloat16 *to, const float (&x)[4]) {
+    const __nv_bfloat162 a = __floats2bfloat162_rn(x[0], x[1]), b = __floats2bfloat162_rn(x[2], x[3]);
+    *reinterpret_cast<uint2 *>(to) = make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&b));
+}
 template <typename T> __device__ __forceinline__ T from_float(float x);
 template <> __device__ __forceinline__ float from_float<float>(float x) { return x; }
 template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
 
-// A block has one (unit, query head), its warps every kWarps-th key, a lane D / 32 channels.
-constexpr int kSimpleWarps = 8;
+// What the parts of heads at both ends of a warp's tiles are.
+struct Meta {
+    int front, ends;                     // the first part's head began before the warp's tiles; and ends in them
+    int back;                            // the last part's head begins in them and goes on
+    int fu, fh, bu, bh;                  // the two heads
+    int blocks;                          // that have part in the back's head, should it go on behind this block
+};
+static_assert(sizeof(Meta) == 32, "as much as Lay::kMeta leaves");
+
 template <typename T, int D>
-__global__ void __launch_bounds__(kSimpleWarps * 32) nibble_attention_kernel(const AttnArgs A) {
-    constexpr int V = D / 32;
-    __shared__ float rec[kSimpleWarps][D + 2];
+__global__ void __launch_bounds__(kAttnThreads, 2) nibble_attention_kernel(const AttnArgs A) {
+    typedef Lay<D> L;
+    constexpr bool kTwo = sizeof(T) == 4;
+    constexpr int kWords = D / 32, kSubs = kTile / 16;               // words of a K row that a lane has; subtiles of 16 keys
+    extern __shared__ __align__(128) uint8_t smem[];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, r = lane >> 2, t = lane & 3;
+    uint8_t *ring = smem + warp * (3 * L::kHalf);
+    float *record = reinterpret_cast<float *>(smem + L::kRecords + warp * L::kRecord);
+    Meta *meta = reinterpret_cast<Meta *>(smem + L::kMeta);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + L::kMeta + kWarps * 32);
+    const uint32_t bars = tc::smem_u32(smem) + L::kBars + warp * 24;
+    if (lane == 0) {
+#pragma unroll
+        for (int i = 0; i < 3; ++i) tc::mbar_init(bars + 8 * i, 1);
+        tc::mbar_init_fence();
+    }
+    if (threadIdx.x == 0) *abort_flag = 0;
+    __syncthreads();
     predecessor_done();
     successor_may_start();
-    const int lane = lane_id(), warp = threadIdx.x >> 5, u = blockIdx.x / A.Hq, g = blockIdx.x - u * A.Hq, h = g / A.G;
-    int n = A.rows[u];
-    const int most = A.max_pages << A.page_shift;
-    if ((n < 0 || n > most) && threadIdx.x == 0) report(A.status, kStatusIndex);
-    n = max(0, min(n, most));
-    float q[V], acc[V], m = kLowest, l = 0.f;
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-        q[i] = A.scale_log2 * as_float(static_cast<const T *>(A.q)[((int64_t)blockIdx.x) * D + lane * V + i]);
-        acc[i] = 0.f;
-    }
-    for (int key = warp; key < n; key += kSimpleWarps) {
-        int id = A.table[(int64_t)u * A.max_pages + (key >> A.page_shift)];
-        if ((unsigned)id >= (unsigned)A.n_pages) { report(A.status, kStatusIndex); id = 0; }
-        const int64_t at = (((int64_t)id * A.Hkv + h) << A.page_shift) + (key & ((1 << A.page_shift) - 1));
-        const int word = lane * V / 8, first = lane * V % 8;
-        float k[8], v[8], z = 0.f;
-        values8(*reinterpret_cast<const uint32_t *>(A.k + at * (D / 2) + word * 4), A.k_scale[at * (D / kGroup) + word / 2], k);
-        values8(*reinterpret_cast<const uint32_t *>(A.v + at * (D / 2) + word * 4), A.v_scale[at * (D / kGroup) + word / 2], v);
-        float kk[V], vv[V];
-#pragma unroll
-        for (int c = 0; c < 8; c += V)
-            if (first == c)
-#pragma unroll
-                for (int i = 0; i < V; ++i) { kk[i] = k[c + i]; vv[i] = v[c + i]; }
-#pragma unroll
-        for (int i = 0; i < V; ++i) z = fmaf(q[i], kk[i], z);
-        z = warp_sum(z);
-        const float top = fmaxf(m, z), corr = tc::ex2(m - top), p = tc::ex2(z - top);
-        l = fmaf(l, corr, p);
-        m = top;
-#pragma unroll
-        for (int i = 0; i < V; ++i) acc[i] = fmaf(acc[i], corr, p * vv[i]);
-    }
-#pragma unroll
-    for (int i = 0; i < V; ++i) rec[warp][lane * V + i] = acc[i];
-    if (lane == 0) { rec[warp][D] = m; rec[warp][D + 1] = l; }
-    __syncthreads();
-    if (threadIdx.x < D) {
-        float top = kLowest, sum = 0.f, o = 0.f;
-        for (int w = 0; w < kSimpleWarps; ++w) top = fmaxf(top, rec[w][D]);
-        for (int w = 0; w < kSimpleWarps; ++w) {
-            const float c = tc::ex2(rec[w][D] - top);
-            sum = fmaf(rec[w][D + 1], c, sum);
-            o = fmaf(rec[w][threadIdx.x], c, o);
+    if (blockIdx.x == 0)
+        for (int u = threadIdx.x; u < A.U; u += kAttnThreads) {
+            const int n = A.rows[u];
+            if (n < 0 || n > A.max_pages << A.page_shift) report(A.status, kStatusIndex);
         }
-        static_cast<T *>(A.out)[(int64_t)blockIdx.x * D + threadIdx.x] = from_float<T>(n == 0 ? 0.f : o / sum);
+    // units without rows
+    for (int u = blockIdx.x * kWarps + warp; u < A.U; u += gridDim.x * kWarps)
+        if (unit_rows(A, u) == 0)
+            for (int i = lane; i < A.Hq * D / 4; i += 32) {
+                const float zero[4] = {0.f, 0.f, 0.f, 0.f};
+                put_four(static_cast<T *>(A.out) + (int64_t)u * A.Hq * D + 4 * i, zero);
+            }
+    const Cut cut = make_cut(A);
+    uint32_t x0, x1;
+    block_piece(A, cut, x0, x1);
+    const uint32_t each = (x1 - x0 + kWarps - 1) / kWarps;
+    const uint32_t w0 = min(x1, x0 + warp * each), w1 = min(x1, w0 + each);
+    const int count = (int)(w1 - w0);
+    Meta me = {0, 0, 0, 0, 0, 0, 0, 0};
+    bool fine = true;
+    if (count > 0) {
+        const int page = 1 << A.page_shift, in_page = min(page, kTile), shift = A.page_shift < 6 ? A.page_shift : 6, pieces = kTile >> shift;
+        // copies: lanes 2 i and 2 i + 1 have the codes and scales of the tile's i-th page, or part of one
+        const int piece = lane >> 1, row_bytes = lane & 1 ? D / kGroup : D / 2;
+        const uint32_t to = (lane & 1 ? L::kCodes : 0u) + piece * in_page * row_bytes;
+        const uint8_t *from[2] = {lane & 1 ? A.scale[0] : A.pages[0], lane & 1 ? A.scale[1] : A.pages[1]};
+        int ids = 0, ids_unit = -1, ids_base = 0;                    // 32 entries of the block table
+        struct Source { int64_t at; uint32_t bytes, all; } src = {0, 0, 0}, next = {0, 0, 0};
+        auto locate = [&](const Walk &w) {                           // where the tile's rows are
+            const int first = (w.t * kTile) >> A.page_shift;
+            if (w.u != ids_unit || (first & ~31) != ids_base) {
+                ids_unit = w.u;
+                ids_base = first & ~31;
+                const int p = ids_base + lane;
+                ids = p < (w.rows + page - 1) >> A.page_shift ? A.table[(int64_t)w.u * A.max_pages + p] : 0;
+                if ((unsigned)ids >= (unsigned)A.n_pages) { report(A.status, kStatusIndex); ids = 0; }
+            }
+            const int id = __shfl_sync(0xFFFFFFFFu, ids, (first - ids_base + piece) & 31);
+            const int valid = min(kTile, w.rows - w.t * kTile), rows = (valid + 3) & ~3;        // (four rows of scales are 16 bytes)
+            const int here = max(0, min(in_page, rows - piece * in_page));
+            Source s;
+            s.at = ((((int64_t)id * A.Hkv + w.h) << A.page_shift) + ((w.t * kTile) & (page - 1))) * row_bytes;
+            s.bytes = piece < pieces ? here * row_bytes : 0;
+            s.all = rows * (D / 2 + D / kGroup);
+            return s;
+        };
+        int put = 0;                                                 // the ring's next place
+        auto issue = [&](int which, const Source &s) {
+            const uint32_t bar = bars + 8 * put;
+            if (lane == 0) tc::mbar_expect_tx(bar, s.all);
+            __syncwarp();
+            if (s.bytes) tc::bulk_load(tc::smem_u32(ring) + put * L::kHalf + to, from[which] + s.at, s.bytes, bar);
+            put = put == 2 ? 0 : put + 1;
+        };
+        Walk cur = walk_to(A, cut, w0), far = cur;
+        int issued = 0, take = 0, phase = 0;
+        src = locate(far);
+        issue(0, src);
+        issue(1, src);
+        issued = 2;
+        if (count > 1) {
+            walk_on(A, far);
+            next = locate(far);
+            issue(0, next);
+            ++issued;
+        }
+        Queries<D, kTwo> Q;
+        float o[D / 16][4], m[2], l[2];
+        bool fresh = true;                                           // a part of a head begins
+        int part_first = cur.t;
+        for (int i = 0; i < count; ++i) {
+            if (fresh) {
+                load_queries<T, D>(A, cur.u, cur.h, Q);
+                part_first = cur.t;
+#pragma unroll
+                for (int j = 0; j < D / 16; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
+                m[0] = m[1] = kLowest;
+                l[0] = l[1] = 0.f;
+                fresh = false;
+            }
+            const int valid = min(kTile, cur.rows - cur.t * kTile);
+            if (!tc::mbar_wait_warp(bars + 8 * take, phase, abort_flag, A.status)) { fine = false; break; }
+            // logits: a lane's rows of a subtile are keys `key` and key + 8, its columns query heads 2 t and 2 t + 1
+            const int key = r ^ (r >> 1 & 1);
+            float z[kSubs][4];
+            {
+                const uint8_t *codes = ring + take * L::kHalf, *scales = codes + L::kCodes;
+#pragma unroll
+                for (int s = 0; s < kSubs; ++s) {
+                    float c[4] = {0.f, 0.f, 0.f, 0.f};
+                    uint32_t w[2][kWords], sc[2][2];
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) {
+                        const int row = 16 * s + 8 * b + key;
+                        if constexpr (D == 128) {
+                            const uint4 v = *reinterpret_cast<const uint4 *>(codes + row * 64 + t * 16);
+                            w[b][0] = v.x; w[b][1] = v.y; w[b][kWords - 2] = v.z; w[b][kWords - 1] = v.w;
+                            const uint32_t both = *reinterpret_cast<const unsigned short *>(scales + row * 8 + t * 2);
+                            sc[b][0] = (both & 255u) * 0x00800080u;
+                            sc[b][1] = (both >> 8) * 0x00800080u;
+                        } else {
+                            const uint2 v = *reinterpret_cast<const uint2 *>(codes + row * 32 + t * 8);
+                            w[b][0] = v.x; w[b][1] = v.y;
+                            sc[b][0] = sc[b][1] = scales[row * 4 + t] * 0x00800080u;
+                        }
+                    }
+#pragma unroll
+                    for (int j = 0; j < kWords; ++j) {
+                        uint32_t lo[4], hi[4];
+                        widen8(w[0][j], lo);
+                        widen8(w[1][j], hi);
+#pragma unroll
+                        for (int p = 0; p < 4; ++p) { lo[p] = times(lo[p], sc[0][j >> 1]); hi[p] = times(hi[p], sc[1][j >> 1]); }
+#pragma unroll
+                        for (int p = 0; p < 4; p += 2) {
+                            const uint32_t a[4] = {lo[p], hi[p], lo[p + 1], hi[p + 1]};
+                            mma(c, a, Q.hi[4 * j + p], Q.hi[4 * j + p + 1]);
+                            if constexpr (kTwo) mma(c, a, Q.lo[4 * j + p], Q.lo[4 * j + p + 1]);
+                        }
+                    }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) z[s][e] = c[e] * Q.factor[e & 1];
+                }
+            }
+            __syncwarp();
+            if (i + 1 < count) { issue(1, next); ++issued; }         // the next tile's V, where this one's K was
+            if (take == 2) { take = 0; phase ^= 1; } else ++take;
+            if (valid < kTile) {
+#pragma unroll
+                for (int s = 0; s < kSubs; ++s)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (16 * s + 8 * (e >> 1) + key >= valid) z[s][e] = __uint_as_float(0xFF800000u);
+            }
+            float top[2] = {m[0], m[1]};
+#pragma unroll
+            for (int s = 0; s < kSubs; ++s) {
+                top[0] = fmaxf(top[0], fmaxf(z[s][0], z[s][2]));
+                top[1] = fmaxf(top[1], fmaxf(z[s][1], z[s][3]));
+            }
+            top[0] = max_over_rows(top[0]);
+            top[1] = max_over_rows(top[1]);
+            if (__any_sync(0xFFFFFFFFu, top[0] > m[0] || top[1] > m[1])) {
+                const float c0 = tc::ex2(m[0] - top[0]), c1 = tc::ex2(m[1] - top[1]);
+                l[0] *= c0; l[1] *= c1;
+                m[0] = top[0]; m[1] = top[1];
+#pragma unroll
+                for (int j = 0; j < D / 16; ++j) { o[j][0] *= c0; o[j][1] *= c1; o[j][2] *= c0; o[j][3] *= c1; }
+            }
+            if (!tc::mbar_wait_warp(bars + 8 * take, phase, abort_flag, A.status)) { fine = false; break; }
+            {
+                const uint8_t *codes = ring + take * L::kHalf, *scales = codes + L::kCodes;
+                const int ka = 2 * t ^ (t & 1), kb = (2 * t + 1) ^ (t & 1);      // the keys at places 2 t and 2 t + 1
+#pragma unroll
+                for (int s = 0; s < kSubs; ++s) {
+                    uint32_t p[2], q[2];                             // weights of keys at places 0 to 7 and 8 to 15; their rests
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) {
+                        const float x = tc::ex2((z[s][2 * b] - m[0]) + kWeightExponent), y = tc::ex2((z[s][2 * b + 1] - m[1]) + kWeightExponent);
+                        l[0] += x;
+                        l[1] += y;
+                        p[b] = half2_of(x, y);
+                        if constexpr (kTwo) {
+                            const float2 h = from_half2(p[b]);
+                            q[b] = transposed(half2_of(x - h.x, y - h.y));
+                        }
+                        p[b] = transposed(p[b]);
+                    }
+                    // V's operand: lo, hi: even and odd channels, [place 2 t, 2 t + 1 | 8 further], each pair of keys in one register
+                    uint32_t w[2][2][D / 64], sc[2];                  // [8 further][key][words]
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) {
+                        const int a = 16 * s + 8 * b + ka, c = 16 * s + 8 * b + kb;
+                        uint32_t sa, sb;
+                        if constexpr (D == 128) {
+                            const uint2 va = *reinterpret_cast<const uint2 *>(codes + a * 64 + r * 8), vb = *reinterpret_cast<const uint2 *>(codes + c * 64 + r * 8);
+                            w[b][0][0] = va.x; w[b][0][D / 64 - 1] = va.y; w[b][1][0] = vb.x; w[b][1][D / 64 - 1] = vb.y;
+                            sa = scales[a * 8 + r]; sb = scales[c * 8 + r];
+                        } else {
+                            w[b][0][0] = *reinterpret_cast<const uint32_t *>(codes + a * 32 + r * 4);
+                            w[b][1][0] = *reinterpret_cast<const uint32_t *>(codes + c * 32 + r * 4);
+                            sa = scales[a * 4 + (r >> 1)]; sb = scales[c * 4 + (r >> 1)];
+                        }
+                        if (valid < kTile) {                          // (what stands behind the last row may be NaN)
+                            sa = a < valid ? sa : 0u;
+                            sb = c < valid ? sb : 0u;
+                        }
+                        sc[b] = (sa << 7) + sb * 0x00800000u;
+                    }
+#pragma unroll
+                    for (int j = 0; j < D / 64; ++j) {
+                        uint32_t even[2][4], odd[2][4];
+#pragma unroll
+                        for (int b = 0; b < 2; ++b) {
+                            const uint32_t x = w[b][0][j], y = w[b][1][j];
+                            widen8((x & 0x0F0F0F0Fu) | (y << 4 & 0xF0F0F0F0u), even[b]);
+                            widen8((x >> 4 & 0x0F0F0F0Fu) | (y & 0xF0F0F0F0u), odd[b]);
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) { even[b][k] = times(even[b][k], sc[b]); odd[b][k] = times(odd[b][k], sc[b]); }
+                        }
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const uint32_t a[4] = {even[0][k], odd[0][k], even[1][k], odd[1][k]};
+                            mma(o[4 * j + k], a, p[0], p[1]);
+                            if constexpr (kTwo) mma(o[4 * j + k], a, q[0], q[1]);
+                        }
+                    }
+                }
+            }
+            __syncwarp();
+            if (take == 2) { take = 0; phase ^= 1; } else ++take;
+            if (i + 2 < count) {                                     // K of the tile after the next one, where this one's V was
+                walk_on(A, far);
+                next = locate(far);
+                issue(0, next);
+                ++issued;
+            }
+            const bool last = cur.t + 1 == cur.tiles;
+            if (last || i + 1 == count) {                            // the part ends
+#pragma unroll
+                for (int q = 0; q < 2; ++q)
+#pragma unroll
+                    for (int k = 4; k < 32; k <<= 1) l[q] += __shfl_xor_sync(0xFFFFFFFFu, l[q], k);
+                if (part_first == 0 && last) {
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) {
+                        if (2 * t + q >= A.G) continue;
+                        const float inverse = 1.f / l[q];
+                        T *out = static_cast<T *>(A.out) + ((int64_t)cur.u * A.Hq + cur.h * A.G + 2 * t + q) * D + r * (D / 8);
+#pragma unroll
+                        for (int j = 0; j < D / 16; j += 2) {
+                            const float x[4] = {o[j][q] * inverse, o[j][2 + q] * inverse, o[j + 1][q] * inverse, o[j + 1][2 + q] * inverse};
+                            put_four(out + 2 * j, x);
+                        }
+                    }
+                } else if (part_first > 0) {
+                    me.front = 1; me.ends = last; me.fu = cur.u; me.fh = cur.h;
+                    put_record<D>(record, o, m, l);
+                } else {
+                    me.back = 1; me.bu = cur.u; me.bh = cur.h;
+                    me.blocks = cut.per ? (cur.tiles + cut.per - 1) / cut.per : (w0 + i - cur.t + cur.tiles - 1) / cut.share - blockIdx.x + 1;
+                    put_record<D>(reinterpret_cast<float *>(ring), o, m, l);       // (no copy is on its way any more)
+                }
+                fresh = true;
+            }
+            walk_on(A, cur);
+        }
+        if (!fine) tc::copies_land(bars, 8, 3, issued);
     }
+    if (lane == 0) meta[warp] = me;
+    fine = __syncthreads_and(fine);
+    int4 note = make_int4(0, 0, 0, 0);
+    if (fine && x1 > x0) {
+        // heads that several warps had part in: a chain of records, from a back, or from the block's first front, on to the front that ends; a warp for each
+        // query head of a chain in turn
+        int job = 0;
+        for (int first = 0; first < kWarps; ++first) {
+            const bool open = first == 0 && meta[0].front != 0;      // the block's first head began in a block before
+            for (int kind = open ? 0 : 1; kind < 2; ++kind) {
+                if (kind == 1 && !meta[first].back) continue;
+                const int u = kind == 0 ? meta[first].fu : meta[first].bu, h = kind == 0 ? meta[first].fh : meta[first].bh;
+                int end = kind == 0 ? first : first + 1;             // records: of warp `first`, then the fronts of those up to `end`
+                bool ends = false;
+                while (!ends && end < kWarps && meta[end].front) ends = meta[end++].ends;
+                const bool whole = kind == 1 && ends;
+                if (kind == 1 && !ends) note = make_int4(u, h * A.G, meta[first].blocks, A.G);      // (it goes on in the next block)
+                for (int g = 0; g < A.G; ++g, ++job) {
+                    if (job % kWarps != warp) continue;
+                    constexpr int V = D / 32;
+                    auto rec = [&](int w) {
+                        return reinterpret_cast<const float *>(kind == 1 && w == first ? smem + w * (3 * L::kHalf) : smem + L::kRecords + w * L::kRecord);
+                    };
+                    float top = kLowest, sum = 0.f, x[V];
+#pragma unroll
+                    for (int k = 0; k < V; ++k) x[k] = 0.f;
+                    for (int w = first; w < end; ++w) top = fmaxf(top, rec(w)[kHeads * D + g]);
+                    for (int w = first; w < end; ++w) {
+                        const float *from = rec(w);
+                        const float c = tc::ex2(from[kHeads * D + g] - top);
+                        sum = fmaf(from[kHeads * (D + 1) + g], c, sum);
+#pragma unroll
+                        for (int k = 0; k < V; ++k) x[k] = fmaf(from[g * D + lane + 32 * k], c, x[k]);
+                    }
+                    if (whole) {
+                        const float inverse = 1.f / sum;
+                        T *out = static_cast<T *>(A.out) + ((int64_t)u * A.Hq + h * A.G + g) * D;
+#pragma unroll
+                        for (int k = 0; k < V; ++k) out[lane + 32 * k] = from_float<T>(x[k] * inverse);
+                    } else {
+                        float *out = A.part + (int64_t)(2 * blockIdx.x + kind) * paged::record_floats(A.G, D);
+#pragma unroll
+                        for (int k = 0; k < V; ++k) out[g * D + lane + 32 * k] = x[k];
+                        if (lane == 0) { out[A.G * D + g] = top; out[A.G * (D + 1) + g] = sum; }
+                    }
+                }
+            }
+        }
+    }
+    if (A.cut_heads && threadIdx.x == 0) A.cut_heads[blockIdx.x] = note;
 }
 
 }  // namespace nibble

@@ -168,7 +168,9 @@ __device__ __forceinline__ Joined<D> join_part(const float *rec, int64_t ahead, 
 // 18.4, 72 heads 26.6 and 25.5; SIMT, 32 heads 13.2 and 14.3, 64 heads 19.6 and 20.1, 80 heads 24.0 and 23.9.  16 sequences of up to 33 792 rows,
 // 8 heads: 108.9 and 107.0.
 constexpr int kJoinThreads = 256, kFewHeads = 74;
-template <int D, int kWarps>
+__device__ __forceinline__ void put_output(float *out, float x) { *out = x; }
+__device__ __forceinline__ void put_output(__nv_bfloat16 *out, float x) { *out = __float2bfloat16_rn(x); }
+template <int D, int kWarps, typename Out = float>
 __global__ void __launch_bounds__(kJoinThreads) cache_join_kernel(const AttnArgs A, const int record, const int own, const int first, const int step) {
     constexpr int kTeams = kJoinThreads / 32 / kWarps, V = D / 32;
     predecessor_done();
@@ -177,10 +179,10 @@ __global__ void __launch_bounds__(kJoinThreads) cache_join_kernel(const AttnArgs
     const int lane = lane_id(), team = (threadIdx.x >> 5) / kWarps, p = (threadIdx.x >> 5) % kWarps, g = blockIdx.y * kTeams + team, G = cut.w;
     if (cut.z == 0 || g >= G) return;                                 // (whole teams)
     const Joined<D> j = join_part<D>(A.part + (int64_t)blockIdx.x * own * record, (int64_t)first * record, (int64_t)step * record, p, kWarps, cut.z, G, g);
-    float *out = A.out + ((int64_t)cut.x * A.Hq + cut.y + g) * D;
+    Out *out = static_cast<Out *>(static_cast<void *>(A.out)) + ((int64_t)cut.x * A.Hq + cut.y + g) * D;
     if constexpr (kWarps == 1) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) out[lane * V + i] = j.o[i] / j.sum;
+        for (int i = 0; i < V; ++i) put_output(out + lane * V + i, j.o[i] / j.sum);
     } else {
         __shared__ float parts[kTeams][kWarps][D], tops[kTeams][kWarps], sums[kTeams][kWarps];
 #pragma unroll
@@ -196,7 +198,7 @@ __global__ void __launch_bounds__(kJoinThreads) cache_join_kernel(const AttnArgs
             float o = 0.f;
 #pragma unroll
             for (int i = 0; i < kWarps; ++i) o = fmaf(parts[team][i][d], tc::ex2(tops[team][i] - top), o);
-            out[d] = o / sum;
+            put_output(out + d, o / sum);
         }
     }
 }
