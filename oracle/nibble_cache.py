@@ -63,7 +63,7 @@ def load(page_bytes, scale_bytes, table, n):
     return np.moveaxis(x, 1, 0).reshape(x.shape[1], -1, x.shape[3])[:, :n]
 
 
-def attention(q, pool, table, rows, softmax_scale=0.0, least=2.0 ** -28):
+def attention(q, pool, table, rows, softmax_scale=0.0, least=2.0 ** -18):
     """(out, size, logits): q [U, Hq, D], pool: pages and scales of K, then V, as bytes, in the order k, v, k scale, v scale.
     size[u, hq, d] = sum_j max(w_j, least * max_i w_i) |v_jd| / sum_j w_j, logits[u, hq] = the largest scale * sum_d |q_d k_jd|: by both of these the
     rounding errors go of an implementation that holds weights w with a relative error down to `least` of the largest, and with the absolute error that

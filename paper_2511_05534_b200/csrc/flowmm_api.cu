@@ -1748,7 +1748,7 @@ flowmm_status launch_nibble_store(const nibble::StoreArgs &a, cudaStream_t st) {
 
 template <typename T, int D>
 flowmm_status launch_nibble_attention(const nibble::AttnArgs &a, const NibblePlan &n, cudaStream_t st) {
-    auto kernel = nibble::nibble_attention_kernel<T, D>;
+    auto kernel = a.page_shift >= 6 ? nibble::nibble_attention_kernel<T, D, true> : nibble::nibble_attention_kernel<T, D, false>;
     if (!allow_smem(kernel) || cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared) != cudaSuccess)
         return FLOWMM_ERR_CUDA;
     launch(kernel, (unsigned)n.blocks, nibble::kAttnThreads, nibble::Lay<D>::kBytes, st, a);

@@ -11,7 +11,8 @@
 // Which channel and which key stand at which place of an operand is free as long as both operands agree: a lane takes 16 neighbouring bytes of a K row and
 // 8 of a V row, one scale for all channels that it has of a V row, and ends with 16 neighbouring channels of two query heads.
 // bf16: a query is an fp16 number times a power of two exactly, a weight is rounded to fp16 (2^-12, where the output is rounded to 2^-9); fp32: both are the
-// sum of two fp16 numbers, each product is two.  Weights are 2^14 for the largest, so that fp16 holds them to full precision down to 2^-28 of that.
+// sum of two fp16 numbers, each product is two.  The largest weight is 2^10 to 2^15 (fp32: 2^14), so that fp16 holds others to full precision down to 2^-24 of
+// it, and two of them to 2^-21 of themselves down to 2^-18 of it, both to 2^-35 (fp32: 2^-39) of it below.
 #pragma once
 #include "common.cuh"
 #include "nibble_cache.cuh"
@@ -36,14 +37,14 @@ struct AttnArgs {
 
 constexpr int kTile = 64, kWarps = 6, kAttnThreads = kWarps * 32, kHeads = 8;
 constexpr float kLowest = paged::kLowest;
-constexpr float kWeightExponent = 14.f;
+// Weights are 2^(logit - reference): the reference is set 10 below the maximum (log2; 14 for fp32 rows) and set again only when a weight would be above 2^15.
+constexpr float kMostExponent = 15.f;
 
 // What a warp has in shared memory: three half tiles (64 rows of K or of V: codes, then scales), K and V in turn, and a record.
 template <int D> struct Lay {
     static constexpr uint32_t kCodes = kTile * D / 2, kScales = kTile * D / kGroup, kHalf = kCodes + kScales;
     static constexpr uint32_t kRecord = kHeads * (D + 2) * 4;
-    static constexpr uint32_t kRecords = kWarps * 3 * kHalf, kBars = kRecords + kWarps * kRecord, kMeta = kBars + kWarps * 3 * 8;
-    static constexpr uint32_t kBytes = kMeta + kWarps * 32 + 16;
+    static constexpr uint32_t kRecords = kWarps * 3 * kHalf, kMeta = kRecords + kWarps * kRecord, kBytes = kMeta + kWarps * 32;
     static_assert(kRecord <= 3 * kHalf && 2 * (kBytes + 1024) <= 228 * 1024, "two blocks to an SM");
 };
 
@@ -107,21 +108,22 @@ __device__ __forceinline__ Cut make_cut(const AttnArgs &A) {
     }
     return c;
 }
-// Tile t of the head (u, h).
-struct Walk { int u, h, t, tiles, rows; };
+// A tile of the head (u, h): the unit's rows, and those from the tile's first one on.
+struct Walk { int u, h, rows, left; };
 __device__ __forceinline__ void walk_on(const AttnArgs &A, Walk &w) {
-    if (++w.t < w.tiles) return;
-    w.t = 0;
-    if (++w.h < A.Hkv) return;
-    w.h = 0;
-    do { ++w.u; w.rows = w.u < A.U ? unit_rows(A, w.u) : 0; w.tiles = tiles_of(w.rows); } while (w.tiles == 0 && w.u < A.U);
+    if ((w.left -= kTile) > 0) return;
+    if (++w.h >= A.Hkv) {
+        w.h = 0;
+        do { ++w.u; w.rows = w.u < A.U ? unit_rows(A, w.u) : 0; } while (w.rows == 0 && w.u < A.U);
+    }
+    w.left = w.rows;
 }
-// Where tile x is, x below c.all; base: the number of the unit's first tile.
+// Where tile x is, x below c.all.
 __device__ __forceinline__ Walk walk_to(const AttnArgs &A, const Cut &c, uint32_t x) {
     const uint32_t H = A.Hkv;
     const int owner = __ffs(__ballot_sync(0xFFFFFFFFu, x < c.upto * H)) - 1;
     int u = 0;
-    uint32_t base = 0;
+    uint32_t base = 0;                                                // tiles of a head of each of the units before
     if (lane_id() == owner) {
         base = c.upto - c.mine;
         for (u = c.u0; u < c.u1 - 1; ++u) {
@@ -134,9 +136,9 @@ __device__ __forceinline__ Walk walk_to(const AttnArgs &A, const Cut &c, uint32_
     w.u = __shfl_sync(0xFFFFFFFFu, u, owner);
     base = __shfl_sync(0xFFFFFFFFu, base, owner) * H;
     w.rows = unit_rows(A, w.u);
-    w.tiles = tiles_of(w.rows);
-    w.h = (x - base) / (uint32_t)w.tiles;
-    w.t = x - base - w.h * w.tiles;
+    const uint32_t tiles = tiles_of(w.rows);
+    w.h = (x - base) / tiles;
+    w.left = w.rows - (int)(x - base - w.h * tiles) * kTile;
     return w;
 }
 // The block's tiles [x0, x1); none: x0 == x1.
@@ -173,6 +175,12 @@ __device__ __forceinline__ void block_piece(const AttnArgs &A, const Cut &c, uin
 __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_first(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {      // onto zeros
+    asm("{\n\t.reg .f32 z;\n\tmov.f32 z, 0f00000000;\n\t"
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {z, z, z, z};\n\t}"
+        : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 // An 8 by 8 matrix of fp16, a row of it in four neighbouring lanes, transposed; by a whole warp.
@@ -238,7 +246,7 @@ __device__ __forceinline__ void load_queries(const AttnArgs &A, int u, int h, Qu
             }
         }
     }
-    const float factor = finite ? paged::power_of_two(ex) * A.scale_log2 : __uint_as_float(0x7FC00000u);
+    const float factor = finite ? fmaxf(paged::power_of_two(ex) * A.scale_log2, 1.175494351e-38f) : __uint_as_float(0x7FC00000u);     // (not zero: times -inf)
     Q.factor[0] = __shfl_sync(0xFFFFFFFFu, factor, 8 * t);
     Q.factor[1] = __shfl_sync(0xFFFFFFFFu, factor, 8 * t + 4);
 }
@@ -274,25 +282,18 @@ struct Meta {
 };
 static_assert(sizeof(Meta) == 32, "as much as Lay::kMeta leaves");
 
-template <typename T, int D>
+// kLong: pages of 64 rows and more, so that a tile is on one page.
+template <typename T, int D, bool kLong>
 __global__ void __launch_bounds__(kAttnThreads, 2) nibble_attention_kernel(const AttnArgs A) {
     typedef Lay<D> L;
     constexpr bool kTwo = sizeof(T) == 4;
+    constexpr float kWeightExponent = kTwo ? 14.f : 10.f;
     constexpr int kWords = D / 32, kSubs = kTile / 16;               // words of a K row that a lane has; subtiles of 16 keys
     extern __shared__ __align__(128) uint8_t smem[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, r = lane >> 2, t = lane & 3;
     uint8_t *ring = smem + warp * (3 * L::kHalf);
     float *record = reinterpret_cast<float *>(smem + L::kRecords + warp * L::kRecord);
     Meta *meta = reinterpret_cast<Meta *>(smem + L::kMeta);
-    volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + L::kMeta + kWarps * 32);
-    const uint32_t bars = tc::smem_u32(smem) + L::kBars + warp * 24;
-    if (lane == 0) {
-#pragma unroll
-        for (int i = 0; i < 3; ++i) tc::mbar_init(bars + 8 * i, 1);
-        tc::mbar_init_fence();
-    }
-    if (threadIdx.x == 0) *abort_flag = 0;
-    __syncthreads();
     predecessor_done();
     successor_may_start();
     if (blockIdx.x == 0)
@@ -314,17 +315,17 @@ __global__ void __launch_bounds__(kAttnThreads, 2) nibble_attention_kernel(const
     const uint32_t w0 = min(x1, x0 + warp * each), w1 = min(x1, w0 + each);
     const int count = (int)(w1 - w0);
     Meta me = {0, 0, 0, 0, 0, 0, 0, 0};
-    bool fine = true;
     if (count > 0) {
-        const int page = 1 << A.page_shift, in_page = min(page, kTile), shift = A.page_shift < 6 ? A.page_shift : 6, pieces = kTile >> shift;
-        // copies: lanes 2 i and 2 i + 1 have the codes and scales of the tile's i-th page, or part of one
-        const int piece = lane >> 1, row_bytes = lane & 1 ? D / kGroup : D / 2;
-        const uint32_t to = (lane & 1 ? L::kCodes : 0u) + piece * in_page * row_bytes;
-        const uint8_t *from[2] = {lane & 1 ? A.scale[0] : A.pages[0], lane & 1 ? A.scale[1] : A.pages[1]};
+        // Copies of 16 bytes, a lane the codes of row lane / kLanes of every kRows of the tile, and scales that lie side by side.  Sixteen rows are on one
+        // page and come or are left out together.
+        constexpr int kLanes = D / 32, kRows = 32 / kLanes, kScaleRows = 256 / D;
+        const int page = 1 << A.page_shift, scale_group = lane * kScaleRows >> 4;
+        const uint32_t to = tc::smem_u32(ring) + lane * 16, page_rows = (uint32_t)A.Hkv << A.page_shift;
         int ids = 0, ids_unit = -1, ids_base = 0;                    // 32 entries of the block table
-        struct Source { int64_t at; uint32_t bytes, all; } src = {0, 0, 0}, next = {0, 0, 0};
-        auto locate = [&](const Walk &w) {                           // where the tile's rows are
-            const int first = (w.t * kTile) >> A.page_shift;
+        // where the tile's codes are, from this lane's first sixteen bytes on, for every sixteen rows; the lane's scales; the tile's rows
+        struct Source { int64_t codes[kLong ? 1 : 4], scales; int left; } next;
+        auto locate = [&](const Walk &w) {
+            const int at = w.rows - w.left, first = at >> A.page_shift;
             if (w.u != ids_unit || (first & ~31) != ids_base) {
                 ids_unit = w.u;
                 ids_base = first & ~31;
@@ -332,73 +333,90 @@ __global__ void __launch_bounds__(kAttnThreads, 2) nibble_attention_kernel(const
                 ids = p < (w.rows + page - 1) >> A.page_shift ? A.table[(int64_t)w.u * A.max_pages + p] : 0;
                 if ((unsigned)ids >= (unsigned)A.n_pages) { report(A.status, kStatusIndex); ids = 0; }
             }
-            const int id = __shfl_sync(0xFFFFFFFFu, ids, (first - ids_base + piece) & 31);
-            const int valid = min(kTile, w.rows - w.t * kTile), rows = (valid + 3) & ~3;        // (four rows of scales are 16 bytes)
-            const int here = max(0, min(in_page, rows - piece * in_page));
-            Source s;
-            s.at = ((((int64_t)id * A.Hkv + w.h) << A.page_shift) + ((w.t * kTile) & (page - 1))) * row_bytes;
-            s.bytes = piece < pieces ? here * row_bytes : 0;
-            s.all = rows * (D / 2 + D / kGroup);
-            return s;
+            next.left = w.left;
+            auto row = [&](int of) {                                 // the number in the pool of the tile's row `of`
+                return (int64_t)((uint64_t)(uint32_t)__shfl_sync(0xFFFFFFFFu, ids, first + (of >> A.page_shift)) * page_rows) +
+                       (uint32_t)((w.h << A.page_shift) + ((at + of) & (page - 1)));
+            };
+            if constexpr (kLong) {
+                const int64_t r0 = row(0);
+                next.codes[0] = r0 * (D / 2) + lane * 16;
+                next.scales = r0 * (D / kGroup) + lane * 16;
+            } else {
+#pragma unroll
+                for (int g = 0; g < 4; ++g) next.codes[g] = row(16 * g) * (D / 2) + lane * 16;
+                next.scales = row(lane * kScaleRows) * (D / kGroup);
+            }
         };
-        int put = 0;                                                 // the ring's next place
-        auto issue = [&](int which, const Source &s) {
-            const uint32_t bar = bars + 8 * put;
-            if (lane == 0) tc::mbar_expect_tx(bar, s.all);
-            __syncwarp();
-            if (s.bytes) tc::bulk_load(tc::smem_u32(ring) + put * L::kHalf + to, from[which] + s.at, s.bytes, bar);
+        uint32_t put = 0;                                            // the ring's next place
+        auto issue = [&](int which, bool on) {
+            if (on) {
+                const uint32_t there = to + put * L::kHalf;
+                auto copy = [&](int g) {
+                    const uint8_t *codes = A.pages[which] + (kLong ? next.codes[0] + g * (8 * D) : next.codes[kLong ? 0 : g]);
+#pragma unroll
+                    for (int i = 0; i < 16 / kRows; ++i) tc::copy16_async(there + g * (8 * D) + i * 512, codes + i * 512);
+                };
+                if (next.left >= kTile) {
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) copy(g);
+                    if (D == 128 || lane < kTile / kScaleRows) tc::copy16_async(there + L::kCodes, A.scale[which] + next.scales);
+                } else {
+#pragma unroll
+                    for (int g = 0; g < 4; ++g)
+                        if (16 * g < next.left) copy(g);
+                    if (lane < kTile / kScaleRows && 16 * scale_group < next.left) tc::copy16_async(there + L::kCodes, A.scale[which] + next.scales);
+                }
+            }
+            tc::copies_commit();
             put = put == 2 ? 0 : put + 1;
         };
         Walk cur = walk_to(A, cut, w0), far = cur;
-        int issued = 0, take = 0, phase = 0;
-        src = locate(far);
-        issue(0, src);
-        issue(1, src);
-        issued = 2;
-        if (count > 1) {
-            walk_on(A, far);
-            next = locate(far);
-            issue(0, next);
-            ++issued;
-        }
+        uint32_t take = 0;
+        locate(far);
+        issue(0, true);
+        issue(1, true);
+        if (count > 1) { walk_on(A, far); locate(far); }
+        issue(0, count > 1);
         Queries<D, kTwo> Q;
-        float o[D / 16][4], m[2], l[2];
+        float o[D / 16][4], ref[2];
+        float2 l;                                                    // sums of weights, of this lane's keys
         bool fresh = true;                                           // a part of a head begins
-        int part_first = cur.t;
+        bool begins = true;                                          // ... with the head's first row
         for (int i = 0; i < count; ++i) {
             if (fresh) {
                 load_queries<T, D>(A, cur.u, cur.h, Q);
-                part_first = cur.t;
+                begins = cur.left == cur.rows;
 #pragma unroll
                 for (int j = 0; j < D / 16; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
-                m[0] = m[1] = kLowest;
-                l[0] = l[1] = 0.f;
+                ref[0] = ref[1] = kLowest;
+                l = make_float2(0.f, 0.f);
                 fresh = false;
             }
-            const int valid = min(kTile, cur.rows - cur.t * kTile);
-            if (!tc::mbar_wait_warp(bars + 8 * take, phase, abort_flag, A.status)) { fine = false; break; }
-            // logits: a lane's rows of a subtile are keys `key` and key + 8, its columns query heads 2 t and 2 t + 1
+            const int valid = cur.left;                              // rows, should they be fewer than a tile's
+            tc::copies_wait<2>();                                    // (of three half tiles on their way)
+            __syncwarp();
+            // products with keys: a lane's rows of a subtile are keys `key` and key + 8, its columns query heads 2 t and 2 t + 1
             const int key = r ^ (r >> 1 & 1);
             float z[kSubs][4];
             {
-                const uint8_t *codes = ring + take * L::kHalf, *scales = codes + L::kCodes;
+                const uint8_t *codes = ring + take * L::kHalf + key * (D / 2) + t * (D / 8), *scales = ring + take * L::kHalf + L::kCodes + key * (D / 16) + t * (D / 64);
 #pragma unroll
                 for (int s = 0; s < kSubs; ++s) {
-                    float c[4] = {0.f, 0.f, 0.f, 0.f};
                     uint32_t w[2][kWords], sc[2][2];
 #pragma unroll
                     for (int b = 0; b < 2; ++b) {
-                        const int row = 16 * s + 8 * b + key;
+                        const int row = 16 * s + 8 * b;
                         if constexpr (D == 128) {
-                            const uint4 v = *reinterpret_cast<const uint4 *>(codes + row * 64 + t * 16);
+                            const uint4 v = *reinterpret_cast<const uint4 *>(codes + row * 64);
                             w[b][0] = v.x; w[b][1] = v.y; w[b][kWords - 2] = v.z; w[b][kWords - 1] = v.w;
-                            const uint32_t both = *reinterpret_cast<const unsigned short *>(scales + row * 8 + t * 2);
+                            const uint32_t both = *reinterpret_cast<const unsigned short *>(scales + row * 8);
                             sc[b][0] = (both & 255u) * 0x00800080u;
                             sc[b][1] = (both >> 8) * 0x00800080u;
                         } else {
-                            const uint2 v = *reinterpret_cast<const uint2 *>(codes + row * 32 + t * 8);
+                            const uint2 v = *reinterpret_cast<const uint2 *>(codes + row * 32);
                             w[b][0] = v.x; w[b][1] = v.y;
-                            sc[b][0] = sc[b][1] = scales[row * 4 + t] * 0x00800080u;
+                            sc[b][0] = sc[b][1] = scales[row * 4] * 0x00800080u;
                         }
                     }
 #pragma unroll
@@ -411,17 +429,16 @@ __global__ void __launch_bounds__(kAttnThreads, 2) nibble_attention_kernel(const
 #pragma unroll
                         for (int p = 0; p < 4; p += 2) {
                             const uint32_t a[4] = {lo[p], hi[p], lo[p + 1], hi[p + 1]};
-                            mma(c, a, Q.hi[4 * j + p], Q.hi[4 * j + p + 1]);
-                            if constexpr (kTwo) mma(c, a, Q.lo[4 * j + p], Q.lo[4 * j + p + 1]);
+                            if (j == 0 && p == 0) mma_first(z[s], a, Q.hi[0], Q.hi[1]);
+                            else mma(z[s], a, Q.hi[4 * j + p], Q.hi[4 * j + p + 1]);
+                            if constexpr (kTwo) mma(z[s], a, Q.lo[4 * j + p], Q.lo[4 * j + p + 1]);
                         }
                     }
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) z[s][e] = c[e] * Q.factor[e & 1];
                 }
             }
             __syncwarp();
-            if (i + 1 < count) { issue(1, next); ++issued; }         // the next tile's V, where this one's K was
-            if (take == 2) { take = 0; phase ^= 1; } else ++take;
+            issue(1, i + 1 < count);                                 // the next tile's V, where this one's K was
+            take = take == 2 ? 0 : take + 1;
             if (valid < kTile) {
 #pragma unroll
                 for (int s = 0; s < kSubs; ++s)
@@ -429,60 +446,69 @@ __global__ void __launch_bounds__(kAttnThreads, 2) nibble_attention_kernel(const
                     for (int e = 0; e < 4; ++e)
                         if (16 * s + 8 * (e >> 1) + key >= valid) z[s][e] = __uint_as_float(0xFF800000u);
             }
-            float top[2] = {m[0], m[1]};
+            float top[2] = {fmaxf(z[0][0], z[0][2]), fmaxf(z[0][1], z[0][3])};
 #pragma unroll
-            for (int s = 0; s < kSubs; ++s) {
+            for (int s = 1; s < kSubs; ++s) {
                 top[0] = fmaxf(top[0], fmaxf(z[s][0], z[s][2]));
                 top[1] = fmaxf(top[1], fmaxf(z[s][1], z[s][3]));
             }
             top[0] = max_over_rows(top[0]);
             top[1] = max_over_rows(top[1]);
-            if (__any_sync(0xFFFFFFFFu, top[0] > m[0] || top[1] > m[1])) {
-                const float c0 = tc::ex2(m[0] - top[0]), c1 = tc::ex2(m[1] - top[1]);
-                l[0] *= c0; l[1] *= c1;
-                m[0] = top[0]; m[1] = top[1];
+            if (__any_sync(0xFFFFFFFFu, fmaf(top[0], Q.factor[0], -ref[0]) > kMostExponent || fmaf(top[1], Q.factor[1], -ref[1]) > kMostExponent)) {
+                float c[2];
 #pragma unroll
-                for (int j = 0; j < D / 16; ++j) { o[j][0] *= c0; o[j][1] *= c1; o[j][2] *= c0; o[j][3] *= c1; }
+                for (int q = 0; q < 2; ++q) {
+                    // (rounded up: however large the logits, no weight is above 2^15)
+                    const float next_ref = fmaxf(__fadd_ru(__fmul_ru(top[q], Q.factor[q]), -kWeightExponent), ref[q]);
+                    c[q] = tc::ex2(ref[q] - next_ref);
+                    ref[q] = next_ref;
+                }
+                l = tc::fmul2(l, make_float2(c[0], c[1]));
+#pragma unroll
+                for (int j = 0; j < D / 16; ++j) { o[j][0] *= c[0]; o[j][1] *= c[1]; o[j][2] *= c[0]; o[j][3] *= c[1]; }
             }
-            if (!tc::mbar_wait_warp(bars + 8 * take, phase, abort_flag, A.status)) { fine = false; break; }
+            tc::copies_wait<2>();                                    // (of three half tiles on their way)
+            __syncwarp();
+            if (valid < kTile) {                                     // what stands behind the last row counts for nothing, NaN neither
+                uint8_t *scales = ring + take * L::kHalf + L::kCodes;
+                for (int b = valid * (D / 16) + lane; b < (int)L::kScales; b += 32) scales[b] = 0;
+                __syncwarp();
+            }
             {
-                const uint8_t *codes = ring + take * L::kHalf, *scales = codes + L::kCodes;
                 const int ka = 2 * t ^ (t & 1), kb = (2 * t + 1) ^ (t & 1);      // the keys at places 2 t and 2 t + 1
+                const uint8_t *codes = ring + take * L::kHalf + r * (D / 16), *scales = ring + take * L::kHalf + L::kCodes + (D == 128 ? r : r >> 1);
+                const uint8_t *codes_of[2] = {codes + ka * (D / 2), codes + kb * (D / 2)}, *scales_of[2] = {scales + ka * (D / 16), scales + kb * (D / 16)};
+                const float2 factor = make_float2(Q.factor[0], Q.factor[1]), minus = make_float2(-ref[0], -ref[1]);
 #pragma unroll
                 for (int s = 0; s < kSubs; ++s) {
                     uint32_t p[2], q[2];                             // weights of keys at places 0 to 7 and 8 to 15; their rests
 #pragma unroll
                     for (int b = 0; b < 2; ++b) {
-                        const float x = tc::ex2((z[s][2 * b] - m[0]) + kWeightExponent), y = tc::ex2((z[s][2 * b + 1] - m[1]) + kWeightExponent);
-                        l[0] += x;
-                        l[1] += y;
-                        p[b] = half2_of(x, y);
+                        float2 x = tc::ffma2(make_float2(z[s][2 * b], z[s][2 * b + 1]), factor, minus);
+                        x = make_float2(tc::ex2(x.x), tc::ex2(x.y));
+                        l = tc::fadd2(l, x);
+                        p[b] = half2_of(x.x, x.y);
                         if constexpr (kTwo) {
                             const float2 h = from_half2(p[b]);
-                            q[b] = transposed(half2_of(x - h.x, y - h.y));
+                            q[b] = transposed(half2_of(x.x - h.x, x.y - h.y));
                         }
                         p[b] = transposed(p[b]);
                     }
-                    // V's operand: lo, hi: even and odd channels, [place 2 t, 2 t + 1 | 8 further], each pair of keys in one register
+                    // V's operand: even and odd channels, [places 2 t, 2 t + 1 | 8 further], a pair of keys in a register
                     uint32_t w[2][2][D / 64], sc[2];                  // [8 further][key][words]
 #pragma unroll
                     for (int b = 0; b < 2; ++b) {
-                        const int a = 16 * s + 8 * b + ka, c = 16 * s + 8 * b + kb;
-                        uint32_t sa, sb;
-                        if constexpr (D == 128) {
-                            const uint2 va = *reinterpret_cast<const uint2 *>(codes + a * 64 + r * 8), vb = *reinterpret_cast<const uint2 *>(codes + c * 64 + r * 8);
-                            w[b][0][0] = va.x; w[b][0][D / 64 - 1] = va.y; w[b][1][0] = vb.x; w[b][1][D / 64 - 1] = vb.y;
-                            sa = scales[a * 8 + r]; sb = scales[c * 8 + r];
-                        } else {
-                            w[b][0][0] = *reinterpret_cast<const uint32_t *>(codes + a * 32 + r * 4);
-                            w[b][1][0] = *reinterpret_cast<const uint32_t *>(codes + c * 32 + r * 4);
-                            sa = scales[a * 4 + (r >> 1)]; sb = scales[c * 4 + (r >> 1)];
+                        const int row = 16 * s + 8 * b;
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            if constexpr (D == 128) {
+                                const uint2 v = *reinterpret_cast<const uint2 *>(codes_of[k] + row * 64);
+                                w[b][k][0] = v.x; w[b][k][D / 64 - 1] = v.y;
+                            } else {
+                                w[b][k][0] = *reinterpret_cast<const uint32_t *>(codes_of[k] + row * 32);
+                            }
                         }
-                        if (valid < kTile) {                          // (what stands behind the last row may be NaN)
-                            sa = a < valid ? sa : 0u;
-                            sb = c < valid ? sb : 0u;
-                        }
-                        sc[b] = (sa << 7) + sb * 0x00800000u;
+                        sc[b] = scales_of[0][row * (D / 16)] * 0x00000080u + scales_of[1][row * (D / 16)] * 0x00800000u;
                     }
 #pragma unroll
                     for (int j = 0; j < D / 64; ++j) {
@@ -505,24 +531,21 @@ __global__ void __launch_bounds__(kAttnThreads, 2) nibble_attention_kernel(const
                 }
             }
             __syncwarp();
-            if (take == 2) { take = 0; phase ^= 1; } else ++take;
-            if (i + 2 < count) {                                     // K of the tile after the next one, where this one's V was
-                walk_on(A, far);
-                next = locate(far);
-                issue(0, next);
-                ++issued;
-            }
-            const bool last = cur.t + 1 == cur.tiles;
+            take = take == 2 ? 0 : take + 1;
+            if (i + 2 < count) { walk_on(A, far); locate(far); }
+            issue(0, i + 2 < count);                                 // K of the tile after the next one, where this one's V was
+            const bool last = cur.left <= kTile;
             if (last || i + 1 == count) {                            // the part ends
+                float sum[2] = {l.x, l.y};
 #pragma unroll
                 for (int q = 0; q < 2; ++q)
 #pragma unroll
-                    for (int k = 4; k < 32; k <<= 1) l[q] += __shfl_xor_sync(0xFFFFFFFFu, l[q], k);
-                if (part_first == 0 && last) {
+                    for (int k = 4; k < 32; k <<= 1) sum[q] += __shfl_xor_sync(0xFFFFFFFFu, sum[q], k);
+                if (begins && last) {
 #pragma unroll
                     for (int q = 0; q < 2; ++q) {
                         if (2 * t + q >= A.G) continue;
-                        const float inverse = 1.f / l[q];
+                        const float inverse = 1.f / sum[q];
                         T *out = static_cast<T *>(A.out) + ((int64_t)cur.u * A.Hq + cur.h * A.G + 2 * t + q) * D + r * (D / 8);
 #pragma unroll
                         for (int j = 0; j < D / 16; j += 2) {
@@ -530,24 +553,24 @@ __global__ void __launch_bounds__(kAttnThreads, 2) nibble_attention_kernel(const
                             put_four(out + 2 * j, x);
                         }
                     }
-                } else if (part_first > 0) {
+                } else if (!begins) {
                     me.front = 1; me.ends = last; me.fu = cur.u; me.fh = cur.h;
-                    put_record<D>(record, o, m, l);
+                    put_record<D>(record, o, ref, sum);
                 } else {
                     me.back = 1; me.bu = cur.u; me.bh = cur.h;
-                    me.blocks = cut.per ? (cur.tiles + cut.per - 1) / cut.per : (w0 + i - cur.t + cur.tiles - 1) / cut.share - blockIdx.x + 1;
-                    put_record<D>(reinterpret_cast<float *>(ring), o, m, l);       // (no copy is on its way any more)
+                    const uint32_t tiles = tiles_of(cur.rows), done = (cur.rows - cur.left) / kTile;
+                    me.blocks = cut.per ? (tiles + cut.per - 1) / cut.per : (w0 + i - done + tiles - 1) / cut.share - blockIdx.x + 1;
+                    put_record<D>(reinterpret_cast<float *>(ring), o, ref, sum);       // (no copy is on its way any more)
                 }
                 fresh = true;
             }
             walk_on(A, cur);
         }
-        if (!fine) tc::copies_land(bars, 8, 3, issued);
     }
     if (lane == 0) meta[warp] = me;
-    fine = __syncthreads_and(fine);
+    __syncthreads();
     int4 note = make_int4(0, 0, 0, 0);
-    if (fine && x1 > x0) {
+    if (x1 > x0) {
         // heads that several warps had part in: a chain of records, from a back, or from the block's first front, on to the front that ends; a warp for each
         // query head of a chain in turn
         int job = 0;

@@ -31,8 +31,10 @@ def attend(p, q, pool, table, rows, ws=None):
 def attention_bound(out, size, logits, n, D, dtype):
     """How far an implementation may be from the 64-bit one, per output.
     Logits: D products and their sum in fp32, the scale, each within 2^-23 (a tensor core that truncates); an fp32 query as two fp16 numbers,
-    2^-21 of its largest element (a bf16 one is an fp16 number exactly).  Weights: exp2 within 2^-21; as two fp16 numbers 2^-21 for fp32, as one 2^-11 for
-    bf16, both down to 2^-28 of the largest weight (2^14 in fp16, whose least normal number is 2^-14), as `size` counts them (oracle.nibble_cache.attention).
+    2^-21 of its largest element (a bf16 one is an fp16 number exactly).  Weights: exp2 within 2^-21; in fp16, whose least normal number is 2^-14 and whose
+    step below that is 2^-24, the largest weight is 2^10 at least for bf16 (2^14 for fp32).  bf16: one number, 2^-11 of itself down to 2^-14, 2^-24 of the
+    largest.  fp32: two numbers, the second within 2^-11 of itself, 2^-22 of the weight, or half a step, 2^-25, which is 2^-21 of a weight of 2^-4, 2^-18 of the
+    largest.  `size` counts weights as 2^-18 of the largest at least (oracle.nibble_cache.attention).
     Sums of n weights and products, each within 2^-23.  Numerator and denominator both carry the weights' error.  A bf16 output: half a step, 2^-8."""
     split = 2.0 ** -11 if dtype == F.BF16 else 2.0 ** -21
     rel = (D + 16) * 2.0 ** -23 * logits + 2.0 ** -21 * logits + split + 2.0 ** -21 + (n + 16) * 2.0 ** -23
