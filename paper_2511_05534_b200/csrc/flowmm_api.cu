@@ -1721,7 +1721,7 @@ struct NibblePlan {
 NibblePlan nibble_plan(const flowmm_cache_params &p) {
     NibblePlan n;
     const int64_t heads = (int64_t)p.n_units * p.n_kv_heads, tiles = ((int64_t)p.max_pages * p.page_size + nibble::kTile - 1) / nibble::kTile;
-    n.blocks = std::min<int64_t>(2 * kScoreCtas, heads * tiles);
+    n.blocks = std::min<int64_t>(nibble::kBlocks * kScoreCtas, heads * tiles);
     n.joins = heads > n.blocks || tiles > nibble::kWholeTiles;
     n.part = 256 + (n.joins ? align256((size_t)n.blocks * sizeof(int4)) : 0);
     n.total = n.part + (n.joins ? align256((size_t)n.blocks * 2 * paged::record_floats(p.n_q_heads / p.n_kv_heads, p.head_dim) * sizeof(float)) : 0);
@@ -1748,7 +1748,7 @@ flowmm_status launch_nibble_store(const nibble::StoreArgs &a, cudaStream_t st) {
 
 template <typename T, int D>
 flowmm_status launch_nibble_attention(const nibble::AttnArgs &a, const NibblePlan &n, cudaStream_t st) {
-    auto kernel = a.page_shift >= 6 ? nibble::nibble_attention_kernel<T, D, true> : nibble::nibble_attention_kernel<T, D, false>;
+    auto kernel = (1 << a.page_shift) >= nibble::kTile ? nibble::nibble_attention_kernel<T, D, true> : nibble::nibble_attention_kernel<T, D, false>;
     if (!allow_smem(kernel) || cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared) != cudaSuccess)
         return FLOWMM_ERR_CUDA;
     launch(kernel, (unsigned)n.blocks, nibble::kAttnThreads, nibble::Lay<D>::kBytes, st, a);

@@ -35,7 +35,7 @@ struct AttnArgs {
     float scale_log2;
 };
 
-constexpr int kTile = 64, kWarps = 6, kAttnThreads = kWarps * 32, kHeads = 8;
+constexpr int kTile = 64, kWarps = 6, kBlocks = 2, kAttnThreads = kWarps * 32, kHeads = 8;      // blocks of an SM
 constexpr float kLowest = paged::kLowest;
 // Weights are 2^(logit - reference): the reference is set 10 below the maximum (log2; 14 for fp32 rows) and set again only when a weight would be above 2^15.
 constexpr float kMostExponent = 15.f;
@@ -45,7 +45,7 @@ template <int D> struct Lay {
     static constexpr uint32_t kCodes = kTile * D / 2, kScales = kTile * D / kGroup, kHalf = kCodes + kScales;
     static constexpr uint32_t kRecord = kHeads * (D + 2) * 4;
     static constexpr uint32_t kRecords = kWarps * 3 * kHalf, kMeta = kRecords + kWarps * kRecord, kBytes = kMeta + kWarps * 32;
-    static_assert(kRecord <= 3 * kHalf && 2 * (kBytes + 1024) <= 228 * 1024, "two blocks to an SM");
+    static_assert(kRecord <= 3 * kHalf && kBlocks * (kBytes + 1024) <= 228 * 1024, "blocks of an SM");
 };
 
 // ---- how the work is shared out ------------------------------------------------------------------
@@ -60,10 +60,11 @@ __device__ __forceinline__ int unit_rows(const AttnArgs &A, int u) {
 __device__ __forceinline__ int tiles_of(int rows) { return (rows + kTile - 1) / kTile; }
 
 struct Cut {
-    int u0, u1;                          // this lane's units
+    int u0, u1, rows0, rows1;            // this lane's units, rows of the first two
     uint32_t mine, upto;                 // their tiles, of one head; with all units before
     uint32_t all, per, share;            // tiles of all heads; of a range, or 0; of a piece
     uint32_t ranges, ranges_upto;        // ranges of a head of each of this lane's units; with all units before
+    __device__ __forceinline__ int rows(const AttnArgs &A, int u) const { return u == u0 ? rows0 : u == u0 + 1 ? rows1 : unit_rows(A, u); }
 };
 __device__ __forceinline__ uint32_t sum_upto(uint32_t x) {
     const int lane = lane_id();
@@ -79,10 +80,12 @@ __device__ __forceinline__ Cut make_cut(const AttnArgs &A) {
     const int each = (A.U + 31) >> 5;
     c.u0 = min(A.U, lane_id() * each);
     c.u1 = min(A.U, c.u0 + each);
-    c.mine = 0;
-    int longest = 0;
+    c.rows0 = c.u0 < c.u1 ? unit_rows(A, c.u0) : 0;
+    c.rows1 = c.u0 + 1 < c.u1 ? unit_rows(A, c.u0 + 1) : 0;
+    c.mine = tiles_of(c.rows0) + tiles_of(c.rows1);
+    int longest = tiles_of(max(c.rows0, c.rows1));
 #pragma unroll 4
-    for (int u = c.u0; u < c.u1; ++u) {
+    for (int u = c.u0 + 2; u < c.u1; ++u) {
         const int t = tiles_of(unit_rows(A, u));
         c.mine += t;
         longest = max(longest, t);
@@ -99,7 +102,7 @@ __device__ __forceinline__ Cut make_cut(const AttnArgs &A) {
         if (whole <= kWholeTiles || whole <= per + kJoinTiles) per = whole;
         uint32_t n = 0;
 #pragma unroll 2
-        for (int u = c.u0; u < c.u1; ++u) n += ((uint32_t)tiles_of(unit_rows(A, u)) + per - 1) / per;
+        for (int u = c.u0; u < c.u1; ++u) n += ((uint32_t)tiles_of(c.rows(A, u)) + per - 1) / per;
         if (__reduce_add_sync(0xFFFFFFFFu, n) * A.Hkv > blocks) continue;
         c.per = per;
         c.ranges = n;
@@ -122,20 +125,21 @@ __device__ __forceinline__ void walk_on(const AttnArgs &A, Walk &w) {
 __device__ __forceinline__ Walk walk_to(const AttnArgs &A, const Cut &c, uint32_t x) {
     const uint32_t H = A.Hkv;
     const int owner = __ffs(__ballot_sync(0xFFFFFFFFu, x < c.upto * H)) - 1;
-    int u = 0;
+    int u = 0, rows = 0;
     uint32_t base = 0;                                                // tiles of a head of each of the units before
     if (lane_id() == owner) {
         base = c.upto - c.mine;
-        for (u = c.u0; u < c.u1 - 1; ++u) {
-            const int t = tiles_of(unit_rows(A, u));
-            if (x < (base + t) * H) break;
+        for (u = c.u0;; ++u) {
+            rows = c.rows(A, u);
+            const int t = tiles_of(rows);
+            if (u == c.u1 - 1 || x < (base + t) * H) break;
             base += t;
         }
     }
     Walk w;
     w.u = __shfl_sync(0xFFFFFFFFu, u, owner);
+    w.rows = __shfl_sync(0xFFFFFFFFu, rows, owner);
     base = __shfl_sync(0xFFFFFFFFu, base, owner) * H;
-    w.rows = unit_rows(A, w.u);
     const uint32_t tiles = tiles_of(w.rows);
     w.h = (x - base) / tiles;
     w.left = w.rows - (int)(x - base - w.h * tiles) * kTile;
@@ -156,7 +160,7 @@ __device__ __forceinline__ void block_piece(const AttnArgs &A, const Cut &c, uin
     if (lane_id() == owner) {
         uint32_t ranges = (c.ranges_upto - c.ranges) * H, base = (c.upto - c.mine) * H;
         for (int u = c.u0; u < c.u1; ++u) {
-            const uint32_t t = tiles_of(unit_rows(A, u)), n = (t + c.per - 1) / c.per;
+            const uint32_t t = tiles_of(c.rows(A, u)), n = (t + c.per - 1) / c.per;
             if (i < ranges + n * H) {
                 const uint32_t in = i - ranges, h = in / n, first = (in - h * n) * c.per;
                 x0 = base + h * t + first;
@@ -269,10 +273,6 @@ __device__ __forceinline__ void put_four(__nv_bfloat16 *to, const float (&x)[4])
     const __nv_bfloat162 a = __floats2bfloat162_rn(x[0], x[1]), b = __floats2bfloat162_rn(x[2], x[3]);
     *reinterpret_cast<uint2 *>(to) = make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&b));
 }
-template <typename T> __device__ __forceinline__ T from_float(float x);
-template <> __device__ __forceinline__ float from_float<float>(float x) { return x; }
-template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
-
 // What the parts of heads at both ends of a warp's tiles are.
 struct Meta {
     int front, ends;                     // the first part's head began before the warp's tiles; and ends in them
@@ -282,9 +282,9 @@ struct Meta {
 };
 static_assert(sizeof(Meta) == 32, "as much as Lay::kMeta leaves");
 
-// kLong: pages of 64 rows and more, so that a tile is on one page.
+// kLong: pages of kTile rows and more, so that a tile is on one page.
 template <typename T, int D, bool kLong>
-__global__ void __launch_bounds__(kAttnThreads, 2) nibble_attention_kernel(const AttnArgs A) {
+__global__ void __launch_bounds__(kAttnThreads, kBlocks) nibble_attention_kernel(const AttnArgs A) {
     typedef Lay<D> L;
     constexpr bool kTwo = sizeof(T) == 4;
     constexpr float kWeightExponent = kTwo ? 14.f : 10.f;
@@ -296,18 +296,20 @@ __global__ void __launch_bounds__(kAttnThreads, 2) nibble_attention_kernel(const
     Meta *meta = reinterpret_cast<Meta *>(smem + L::kMeta);
     predecessor_done();
     successor_may_start();
-    if (blockIdx.x == 0)
-        for (int u = threadIdx.x; u < A.U; u += kAttnThreads) {
-            const int n = A.rows[u];
-            if (n < 0 || n > A.max_pages << A.page_shift) report(A.status, kStatusIndex);
-        }
-    // units without rows
-    for (int u = blockIdx.x * kWarps + warp; u < A.U; u += gridDim.x * kWarps)
-        if (unit_rows(A, u) == 0)
-            for (int i = lane; i < A.Hq * D / 4; i += 32) {
-                const float zero[4] = {0.f, 0.f, 0.f, 0.f};
-                put_four(static_cast<T *>(A.out) + (int64_t)u * A.Hq * D + 4 * i, zero);
+    // lengths out of range, units without rows (while the first tiles are on their way)
+    auto aside = [&]() {
+        if (blockIdx.x == 0)
+            for (int u = threadIdx.x; u < A.U; u += kAttnThreads) {
+                const int n = A.rows[u];
+                if (n < 0 || n > A.max_pages << A.page_shift) report(A.status, kStatusIndex);
             }
+        for (int u = blockIdx.x * kWarps + warp; u < A.U; u += gridDim.x * kWarps)
+            if (unit_rows(A, u) == 0)
+                for (int i = lane; i < A.Hq * D / 4; i += 32) {
+                    const float zero[4] = {0.f, 0.f, 0.f, 0.f};
+                    put_four(static_cast<T *>(A.out) + (int64_t)u * A.Hq * D + 4 * i, zero);
+                }
+    };
     const Cut cut = make_cut(A);
     uint32_t x0, x1;
     block_piece(A, cut, x0, x1);
@@ -323,7 +325,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) nibble_attention_kernel(const
         const uint32_t to = tc::smem_u32(ring) + lane * 16, page_rows = (uint32_t)A.Hkv << A.page_shift;
         int ids = 0, ids_unit = -1, ids_base = 0;                    // 32 entries of the block table
         // where the tile's codes are, from this lane's first sixteen bytes on, for every sixteen rows; the lane's scales; the tile's rows
-        struct Source { int64_t codes[kLong ? 1 : 4], scales; int left; } next;
+        struct Source { int64_t codes[kLong ? 1 : kTile / 16], scales; int left; } next;
         auto locate = [&](const Walk &w) {
             const int at = w.rows - w.left, first = at >> A.page_shift;
             if (w.u != ids_unit || (first & ~31) != ids_base) {
@@ -344,7 +346,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) nibble_attention_kernel(const
                 next.scales = r0 * (D / kGroup) + lane * 16;
             } else {
 #pragma unroll
-                for (int g = 0; g < 4; ++g) next.codes[g] = row(16 * g) * (D / 2) + lane * 16;
+                for (int g = 0; g < kTile / 16; ++g) next.codes[g] = row(16 * g) * (D / 2) + lane * 16;
                 next.scales = row(lane * kScaleRows) * (D / kGroup);
             }
         };
@@ -359,11 +361,11 @@ __global__ void __launch_bounds__(kAttnThreads, 2) nibble_attention_kernel(const
                 };
                 if (next.left >= kTile) {
 #pragma unroll
-                    for (int g = 0; g < 4; ++g) copy(g);
-                    if (D == 128 || lane < kTile / kScaleRows) tc::copy16_async(there + L::kCodes, A.scale[which] + next.scales);
+                    for (int g = 0; g < kTile / 16; ++g) copy(g);
+                    if (kTile == 32 * kScaleRows || lane < kTile / kScaleRows) tc::copy16_async(there + L::kCodes, A.scale[which] + next.scales);
                 } else {
 #pragma unroll
-                    for (int g = 0; g < 4; ++g)
+                    for (int g = 0; g < kTile / 16; ++g)
                         if (16 * g < next.left) copy(g);
                     if (lane < kTile / kScaleRows && 16 * scale_group < next.left) tc::copy16_async(there + L::kCodes, A.scale[which] + next.scales);
                 }
@@ -378,6 +380,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) nibble_attention_kernel(const
         issue(1, true);
         if (count > 1) { walk_on(A, far); locate(far); }
         issue(0, count > 1);
+        aside();
         Queries<D, kTwo> Q;
         float o[D / 16][4], ref[2];
         float2 l;                                                    // sums of weights, of this lane's keys
@@ -567,13 +570,13 @@ __global__ void __launch_bounds__(kAttnThreads, 2) nibble_attention_kernel(const
             walk_on(A, cur);
         }
     }
+    if (count == 0) aside();
     if (lane == 0) meta[warp] = me;
     __syncthreads();
     int4 note = make_int4(0, 0, 0, 0);
     if (x1 > x0) {
-        // heads that several warps had part in: a chain of records, from a back, or from the block's first front, on to the front that ends; a warp for each
-        // query head of a chain in turn
-        int job = 0;
+        // Heads that several warps had part in: a chain of records, from a back, or from the block's first front, on to the front that ends.  A thread has
+        // four channels of a query head, and all their records on their way at once.
         for (int first = 0; first < kWarps; ++first) {
             const bool open = first == 0 && meta[0].front != 0;      // the block's first head began in a block before
             for (int kind = open ? 0 : 1; kind < 2; ++kind) {
@@ -584,33 +587,36 @@ __global__ void __launch_bounds__(kAttnThreads, 2) nibble_attention_kernel(const
                 while (!ends && end < kWarps && meta[end].front) ends = meta[end++].ends;
                 const bool whole = kind == 1 && ends;
                 if (kind == 1 && !ends) note = make_int4(u, h * A.G, meta[first].blocks, A.G);      // (it goes on in the next block)
-                for (int g = 0; g < A.G; ++g, ++job) {
-                    if (job % kWarps != warp) continue;
-                    constexpr int V = D / 32;
-                    auto rec = [&](int w) {
-                        return reinterpret_cast<const float *>(kind == 1 && w == first ? smem + w * (3 * L::kHalf) : smem + L::kRecords + w * L::kRecord);
-                    };
-                    float top = kLowest, sum = 0.f, x[V];
+                for (int item = threadIdx.x; item < A.G * (D / 4); item += kAttnThreads) {
+                    const int g = item / (D / 4), d = item % (D / 4) * 4;
+                    float tops[kWarps], sums[kWarps], top = kLowest, sum = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
+                    float4 part[kWarps];
 #pragma unroll
-                    for (int k = 0; k < V; ++k) x[k] = 0.f;
-                    for (int w = first; w < end; ++w) top = fmaxf(top, rec(w)[kHeads * D + g]);
-                    for (int w = first; w < end; ++w) {
-                        const float *from = rec(w);
-                        const float c = tc::ex2(from[kHeads * D + g] - top);
-                        sum = fmaf(from[kHeads * (D + 1) + g], c, sum);
+                    for (int w = 0; w < kWarps; ++w) {
+                        const float *rec = reinterpret_cast<const float *>(kind == 1 && w == first ? smem + w * (3 * L::kHalf) : smem + L::kRecords + w * L::kRecord);
+                        const bool on = w >= first && w < end;
+                        tops[w] = on ? rec[kHeads * D + g] : kLowest;
+                        sums[w] = on ? rec[kHeads * (D + 1) + g] : 0.f;
+                        part[w] = on ? *reinterpret_cast<const float4 *>(rec + g * D + d) : make_float4(0.f, 0.f, 0.f, 0.f);
+                    }
 #pragma unroll
-                        for (int k = 0; k < V; ++k) x[k] = fmaf(from[g * D + lane + 32 * k], c, x[k]);
+                    for (int w = 0; w < kWarps; ++w) top = fmaxf(top, tops[w]);
+#pragma unroll
+                    for (int w = 0; w < kWarps; ++w) {
+                        const float c = tc::ex2(tops[w] - top);
+                        sum = fmaf(sums[w], c, sum);
+                        x[0] = fmaf(part[w].x, c, x[0]); x[1] = fmaf(part[w].y, c, x[1]);
+                        x[2] = fmaf(part[w].z, c, x[2]); x[3] = fmaf(part[w].w, c, x[3]);
                     }
                     if (whole) {
                         const float inverse = 1.f / sum;
-                        T *out = static_cast<T *>(A.out) + ((int64_t)u * A.Hq + h * A.G + g) * D;
 #pragma unroll
-                        for (int k = 0; k < V; ++k) out[lane + 32 * k] = from_float<T>(x[k] * inverse);
+                        for (int k = 0; k < 4; ++k) x[k] *= inverse;
+                        put_four(static_cast<T *>(A.out) + ((int64_t)u * A.Hq + h * A.G + g) * D + d, x);
                     } else {
                         float *out = A.part + (int64_t)(2 * blockIdx.x + kind) * paged::record_floats(A.G, D);
-#pragma unroll
-                        for (int k = 0; k < V; ++k) out[g * D + lane + 32 * k] = x[k];
-                        if (lane == 0) { out[A.G * D + g] = top; out[A.G * (D + 1) + g] = sum; }
+                        put_four(out + g * D + d, x);
+                        if (d == 0) { out[A.G * D + g] = top; out[A.G * (D + 1) + g] = sum; }
                     }
                 }
             }
