@@ -84,7 +84,7 @@ __device__ __forceinline__ Cut make_cut(const AttnArgs &A) {
     c.rows1 = c.u0 + 1 < c.u1 ? unit_rows(A, c.u0 + 1) : 0;
     c.mine = tiles_of(c.rows0) + tiles_of(c.rows1);
     int longest = tiles_of(max(c.rows0, c.rows1));
-#pragma unroll 4
+#pragma unroll 1
     for (int u = c.u0 + 2; u < c.u1; ++u) {
         const int t = tiles_of(unit_rows(A, u));
         c.mine += t;
@@ -98,10 +98,11 @@ __device__ __forceinline__ Cut make_cut(const AttnArgs &A) {
     c.per = c.ranges = c.ranges_upto = 0;
     if (heads > blocks) return c;
     const uint32_t whole = max(1, longest);
+#pragma unroll 1
     for (uint32_t per = c.share; per <= c.share + kSwitchTiles || per == whole; ++per) {
         if (whole <= kWholeTiles || whole <= per + kJoinTiles) per = whole;
         uint32_t n = 0;
-#pragma unroll 2
+#pragma unroll 1
         for (int u = c.u0; u < c.u1; ++u) n += ((uint32_t)tiles_of(c.rows(A, u)) + per - 1) / per;
         if (__reduce_add_sync(0xFFFFFFFFu, n) * A.Hkv > blocks) continue;
         c.per = per;
@@ -129,6 +130,7 @@ __device__ __forceinline__ Walk walk_to(const AttnArgs &A, const Cut &c, uint32_
     uint32_t base = 0;                                                // tiles of a head of each of the units before
     if (lane_id() == owner) {
         base = c.upto - c.mine;
+#pragma unroll 1
         for (u = c.u0;; ++u) {
             rows = c.rows(A, u);
             const int t = tiles_of(rows);
@@ -159,6 +161,7 @@ __device__ __forceinline__ void block_piece(const AttnArgs &A, const Cut &c, uin
     const int owner = __ffs(hit) - 1;
     if (lane_id() == owner) {
         uint32_t ranges = (c.ranges_upto - c.ranges) * H, base = (c.upto - c.mine) * H;
+#pragma unroll 1
         for (int u = c.u0; u < c.u1; ++u) {
             const uint32_t t = tiles_of(c.rows(A, u)), n = (t + c.per - 1) / c.per;
             if (i < ranges + n * H) {
@@ -299,12 +302,15 @@ __global__ void __launch_bounds__(kAttnThreads, kBlocks) nibble_attention_kernel
     // lengths out of range, units without rows (while the first tiles are on their way)
     auto aside = [&]() {
         if (blockIdx.x == 0)
+#pragma unroll 1
             for (int u = threadIdx.x; u < A.U; u += kAttnThreads) {
                 const int n = A.rows[u];
                 if (n < 0 || n > A.max_pages << A.page_shift) report(A.status, kStatusIndex);
             }
+#pragma unroll 1
         for (int u = blockIdx.x * kWarps + warp; u < A.U; u += gridDim.x * kWarps)
             if (unit_rows(A, u) == 0)
+#pragma unroll 1
                 for (int i = lane; i < A.Hq * D / 4; i += 32) {
                     const float zero[4] = {0.f, 0.f, 0.f, 0.f};
                     put_four(static_cast<T *>(A.out) + (int64_t)u * A.Hq * D + 4 * i, zero);
@@ -474,6 +480,7 @@ __global__ void __launch_bounds__(kAttnThreads, kBlocks) nibble_attention_kernel
             __syncwarp();
             if (valid < kTile) {                                     // what stands behind the last row counts for nothing, NaN neither
                 uint8_t *scales = ring + take * L::kHalf + L::kCodes;
+#pragma unroll 1
                 for (int b = valid * (D / 16) + lane; b < (int)L::kScales; b += 32) scales[b] = 0;
                 __syncwarp();
             }
@@ -577,16 +584,20 @@ __global__ void __launch_bounds__(kAttnThreads, kBlocks) nibble_attention_kernel
     if (x1 > x0) {
         // Heads that several warps had part in: a chain of records, from a back, or from the block's first front, on to the front that ends.  A thread has
         // four channels of a query head, and all their records on their way at once.
+#pragma unroll 1
         for (int first = 0; first < kWarps; ++first) {
             const bool open = first == 0 && meta[0].front != 0;      // the block's first head began in a block before
+#pragma unroll 1
             for (int kind = open ? 0 : 1; kind < 2; ++kind) {
                 if (kind == 1 && !meta[first].back) continue;
                 const int u = kind == 0 ? meta[first].fu : meta[first].bu, h = kind == 0 ? meta[first].fh : meta[first].bh;
                 int end = kind == 0 ? first : first + 1;             // records: of warp `first`, then the fronts of those up to `end`
                 bool ends = false;
+#pragma unroll 1
                 while (!ends && end < kWarps && meta[end].front) ends = meta[end++].ends;
                 const bool whole = kind == 1 && ends;
                 if (kind == 1 && !ends) note = make_int4(u, h * A.G, meta[first].blocks, A.G);      // (it goes on in the next block)
+#pragma unroll 1
                 for (int item = threadIdx.x; item < A.G * (D / 4); item += kAttnThreads) {
                     const int g = item / (D / 4), d = item % (D / 4) * 4;
                     float tops[kWarps], sums[kWarps], top = kLowest, sum = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
