@@ -1737,11 +1737,16 @@ flowmm_status check_nibble_ws(const flowmm_cache_params *p, const void *ws, size
 }
 
 template <typename T, int D>
-flowmm_status launch_nibble_store(const nibble::StoreArgs &a, cudaStream_t st) {
-    constexpr int per = nibble::kCopyThreads / (D / 8);
-    // four rows a thread where that leaves every SM a few blocks
-    if (a.rows >= (uint32_t)(per * 4 * 4 * kScoreCtas)) launch(nibble::nibble_store_kernel<T, D, 4>, dim3((a.rows + per * 4 - 1) / (per * 4), 2), nibble::kCopyThreads, 0, st, a);
-    else launch(nibble::nibble_store_kernel<T, D, 1>, dim3((a.rows + per - 1) / per, 2), nibble::kCopyThreads, 0, st, a);
+flowmm_status launch_nibble_store(const flowmm_cache_params &p, nibble::StoreArgs &a, cudaStream_t st) {
+    constexpr int rows = nibble::kCopyThreads / (D / nibble::kGroup), vecs = 2;
+    if (p.n_rows < rows) {
+        a.by_rows = make_fastdiv(p.n_rows);
+        launch(nibble::nibble_store_kernel<T, D, 1, true>, dim3((a.rows + rows - 1) / rows, 2), nibble::kCopyThreads, 0, st, a);
+    } else {
+        const uint32_t parts = ((uint32_t)p.n_rows + rows * vecs - 1) / (rows * vecs);
+        a.by_rows = make_fastdiv(parts);
+        launch(nibble::nibble_store_kernel<T, D, vecs, false>, dim3((uint32_t)p.n_units * p.n_kv_heads * parts, 2), nibble::kCopyThreads, 0, st, a);
+    }
     FLOWMM_LAUNCHED("nibble_store");
     return FLOWMM_OK;
 }
@@ -1793,11 +1798,11 @@ extern "C" flowmm_status flowmm_nibble_store(const flowmm_cache_params *p, const
     a.x[0] = k; a.x[1] = v; a.slots = slots; a.status = static_cast<int *>(ws);
     a.pages[0] = static_cast<uint8_t *>(k_pages); a.pages[1] = static_cast<uint8_t *>(v_pages);
     a.scale[0] = static_cast<uint8_t *>(k_scale); a.scale[1] = static_cast<uint8_t *>(v_scale);
-    a.page_shift = page_shift(p->page_size); a.n_pages = p->n_pages; a.rows = (uint32_t)rows;
+    a.T = p->n_rows; a.Hkv = p->n_kv_heads; a.page_shift = page_shift(p->page_size); a.n_pages = p->n_pages; a.rows = (uint32_t)rows;
     for (int i = 0; i < 3; ++i) { a.stride[0][i] = p->k_stride[i]; a.stride[1][i] = p->v_stride[i]; }
-    a.by_rows = make_fastdiv(p->n_rows); a.by_heads = make_fastdiv(p->n_kv_heads);
-    if (p->dtype == FLOWMM_BF16) return p->head_dim == 128 ? launch_nibble_store<__nv_bfloat16, 128>(a, st) : launch_nibble_store<__nv_bfloat16, 64>(a, st);
-    return p->head_dim == 128 ? launch_nibble_store<float, 128>(a, st) : launch_nibble_store<float, 64>(a, st);
+    a.by_heads = make_fastdiv(p->n_kv_heads);
+    if (p->dtype == FLOWMM_BF16) return p->head_dim == 128 ? launch_nibble_store<__nv_bfloat16, 128>(*p, a, st) : launch_nibble_store<__nv_bfloat16, 64>(*p, a, st);
+    return p->head_dim == 128 ? launch_nibble_store<float, 128>(*p, a, st) : launch_nibble_store<float, 64>(*p, a, st);
 }
 
 extern "C" flowmm_status flowmm_nibble_load(const flowmm_cache_params *p, const void *k_pages, const void *v_pages,

@@ -11,6 +11,7 @@
 #pragma once
 #include "common.cuh"
 #include "paged_cache.cuh"
+#include "tc_common.cuh"
 
 namespace flowmm {
 namespace nibble {
@@ -24,20 +25,30 @@ constexpr uint32_t kScaleBias = 896u;            // bits >> 20 of the fp32 minus
 constexpr uint32_t kNanScale = 255u;
 
 // The scale of a group whose largest size has these bits (finite): a sixth of it rounded to four significant bits, to the nearest, ties to even.
-// (IEEE division takes no number next to a tie onto it: the dividend has 24 bits, a tie times 6 has 8.)
+// `low` is a sixth cut off, or, where the product was rounded onto the next number, that: what lies half way to the one above it is compared exactly,
+// as six times that has eight bits at most.
 __device__ __forceinline__ uint32_t scale_bits(uint32_t size) {
-    uint32_t b = __float_as_uint(__fdiv_rn(__uint_as_float(size), 6.f));
-    b = (b + 0x7FFFFu + (b >> 20 & 1u)) & 0xFFF00000u;
+    const uint32_t low = __float_as_uint(__uint_as_float(size) * (1.f / 6.f)) & 0xFFF00000u;
+    const uint32_t half = __float_as_uint(6.f * __uint_as_float(low + 0x00080000u));
+    const uint32_t b = size > half - (low >> 20 & 1u) ? low + 0x00100000u : low;      // (positive numbers are ordered as their bits are)
     return min(max(b, kLeastScale), kMostScale);
 }
-// Eight quotients x / s as codes.  Borders between codes are hit exactly (they have three bits, s has four), so the quotients are correctly rounded:
-// x times the rounded reciprocal, corrected once by the remainder (Markstein 1990).
+__device__ __forceinline__ float reciprocal(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// Eight quotients x / s as codes, all signs turned (to be turned back with 0x88888888).  Borders between codes are hit exactly - they have three bits, s has
+// four - and what is next to a border must not be taken onto it, so a product with the reciprocal (within 2^-22) is corrected once by its exact
+// remainder: then it is within 2^-44 of the quotient before its rounding, and a quotient next to a border is 0.53 of a step or more away from it, as
+// s's significand is 15 / 8 at most.  (Two at a time; signs turned because x - s y keeps the sign of zeros then.)
 __device__ __forceinline__ uint32_t codes8(const float (&x)[8], float s, float inverse) {
-    float y[8];
+    const float2 step = make_float2(s, s), minus = make_float2(-inverse, -inverse);
+    float2 y[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float y0 = x[i] * inverse;
-        y[i] = fmaf(-fmaf(y0, s, -x[i]), inverse, y0);               // (this way round a zero keeps its sign)
+    for (int i = 0; i < 4; ++i) {
+        const float2 v = make_float2(x[2 * i], x[2 * i + 1]), y0 = tc::fmul2(v, minus);
+        y[i] = tc::ffma2(tc::ffma2(y0, step, v), minus, y0);
     }
     uint32_t c;
     asm("{\n\t.reg .b8 a, b, c, d;\n\t"
@@ -47,7 +58,7 @@ __device__ __forceinline__ uint32_t codes8(const float (&x)[8], float s, float i
         "cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
         "mov.b32 %0, {a, b, c, d};\n\t}"
         : "=r"(c)
-        : "f"(y[0]), "f"(y[1]), "f"(y[2]), "f"(y[3]), "f"(y[4]), "f"(y[5]), "f"(y[6]), "f"(y[7]));
+        : "f"(y[0].x), "f"(y[0].y), "f"(y[1].x), "f"(y[1].y), "f"(y[2].x), "f"(y[2].y), "f"(y[3].x), "f"(y[3].y));
     return c;
 }
 // Eight codes as four pairs of fp16, neighbouring channels together.
@@ -111,48 +122,75 @@ struct StoreArgs {
     const int *slots;                  // [U, T]
     uint8_t *pages[2], *scale[2];
     int *status;
-    int page_shift, n_pages;
-    uint32_t rows;                     // U * Hkv * T
+    int T, Hkv, page_shift, n_pages;
+    uint32_t rows;                     // of few: U * Hkv * T
     int64_t stride[2][3];
-    FastDiv by_rows, by_heads;         // by T, by Hkv
+    FastDiv by_heads, by_rows;         // by Hkv; by T, or by the parts that a unit's rows make
 };
 
-// Rows stand in a line, by tensor, unit, KV head and row; D / 8 threads have a row, eight channels each, the two threads of a group find its scale together.
-template <typename T, int D, int kVecs>
+// A thread has a group, 16 channels of a row, and kVecs rows on their way at once.  kFew: calls of few rows a unit; rows stand in a line, by unit, KV head and
+// row.  Else a block takes kRows * kVecs rows of one unit and head, so that what addresses need is found once.  Memory bounds it as long as a
+// group takes no more than about 200 instructions: so sizes are compared as integers, two bf16 at a time, and quotients are formed in pairs.
+template <typename T, int D, int kVecs, bool kFew>
 __global__ void __launch_bounds__(kCopyThreads) nibble_store_kernel(const StoreArgs A) {
-    constexpr int kLanes = D / 8, kRows = kCopyThreads / kLanes;
+    constexpr int kLanes = D / kGroup, kRows = kCopyThreads / kLanes;
     predecessor_done();
     successor_may_start();
-    const int lane = threadIdx.x % kLanes;
-    const uint32_t which = blockIdx.y, row0 = blockIdx.x * (kRows * kVecs) + threadIdx.x / kLanes;
-    Eight<T> raw[kVecs];
+    const int lane = threadIdx.x % kLanes, row0 = threadIdx.x / kLanes;
+    const uint32_t which = blockIdx.y;
+    uint32_t u = 0, h = 0, first = blockIdx.x * (kRows * kVecs), end = A.rows;
+    if (!kFew) {
+        const uint32_t uh = A.by_rows.div(blockIdx.x);
+        first = (blockIdx.x - uh * A.by_rows.d) * (kRows * kVecs);
+        end = A.T;
+        u = A.by_heads.div(uh);
+        h = uh - u * A.by_heads.d;
+    }
+    const int *slots = A.slots + (int64_t)u * A.T;
+    const T *x = static_cast<const T *>(A.x[which]) + u * A.stride[which][0] + h * A.stride[which][1] + lane * kGroup;
+    Eight<T> raw[kVecs][2];
     int slot[kVecs];
     uint32_t head[kVecs];
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
-        const uint32_t row = row0 + i * kRows;
+        const uint32_t r = first + row0 + i * kRows;
         slot[i] = -1;
-        if (row >= A.rows) continue;
-        const uint32_t uh = A.by_rows.div(row), t = row - uh * A.by_rows.d, u = A.by_heads.div(uh);
-        head[i] = uh - u * A.by_heads.d;
-        slot[i] = A.slots[u * A.by_rows.d + t];
-        raw[i].load(static_cast<const T *>(A.x[which]) + u * A.stride[which][0] + head[i] * A.stride[which][1] + t * A.stride[which][2] + lane * 8);
+        head[i] = h;
+        if (r >= end) continue;
+        const T *from = x;
+        if (kFew) {
+            const uint32_t uh = A.by_rows.div(r), t = r - uh * A.by_rows.d, unit = A.by_heads.div(uh);
+            head[i] = uh - unit * A.by_heads.d;
+            slot[i] = slots[(int64_t)unit * A.T + t];
+            from += unit * A.stride[which][0] + head[i] * A.stride[which][1] + t * A.stride[which][2];
+        } else {
+            slot[i] = slots[r];
+            from += r * A.stride[which][2];
+        }
+        raw[i][0].load(from);
+        raw[i][1].load(from + 8);
     }
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
-        if (slot[i] < -1 || slot[i] >= A.n_pages << A.page_shift) { report(A.status, kStatusIndex); slot[i] = -1; }
-        uint32_t size = slot[i] < 0 ? 0u : raw[i].size();
-        size = max(size, __shfl_xor_sync(0xFFFFFFFFu, size, 1));
-        if (slot[i] < 0) continue;
-        const int64_t at = ((((int64_t)(slot[i] >> A.page_shift) * A.by_heads.d + head[i]) << A.page_shift) + (slot[i] & ((1 << A.page_shift) - 1)));
-        const bool finite = size < paged::kInfinityBits;
+        if (slot[i] < 0 || slot[i] >= A.n_pages << A.page_shift) {
+            if (slot[i] != -1) report(A.status, kStatusIndex);
+            continue;
+        }
+        const uint32_t size = max(raw[i][0].size(), raw[i][1].size());
+        const int64_t at = ((int64_t)((uint64_t)((uint32_t)slot[i] >> A.page_shift) * ((uint32_t)A.Hkv << A.page_shift))) +
+                           ((head[i] << A.page_shift) + ((uint32_t)slot[i] & ((1u << A.page_shift) - 1u)));
         const uint32_t b = scale_bits(size);
-        const float s = __uint_as_float(b);
-        float x[8];
-        raw[i].get(x);
-        const uint32_t codes = codes8(x, s, __frcp_rn(s));
-        *reinterpret_cast<uint32_t *>(A.pages[which] + at * (D / 2) + lane * 4) = finite ? codes : 0u;
-        if ((lane & 1) == 0) A.scale[which][at * (D / kGroup) + lane / 2] = (uint8_t)(finite ? (b >> 20) - kScaleBias : kNanScale);
+        const float s = __uint_as_float(b), inverse = reciprocal(s);
+        float f[8];
+        uint2 codes;
+        raw[i][0].get(f);
+        codes.x = codes8(f, s, inverse) ^ 0x88888888u;
+        raw[i][1].get(f);
+        codes.y = codes8(f, s, inverse) ^ 0x88888888u;
+        uint32_t byte = (b >> 20) - kScaleBias;
+        if (size >= paged::kInfinityBits) { codes = make_uint2(0u, 0u); byte = kNanScale; }
+        *reinterpret_cast<uint2 *>(A.pages[which] + at * (D / 2) + lane * 8) = codes;
+        A.scale[which][at * (D / kGroup) + lane] = (uint8_t)byte;
     }
 }
 
