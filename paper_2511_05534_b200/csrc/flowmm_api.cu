@@ -1752,6 +1752,11 @@ flowmm_status launch_nibble_store(const flowmm_cache_params &p, nibble::StoreArg
 }
 
 template <typename T, int D>
+auto nibble_load(const flowmm_cache_params &p) {
+    return p.page_size >= nibble::kLoadRows ? nibble::nibble_load_kernel<T, D, true> : nibble::nibble_load_kernel<T, D, false>;
+}
+
+template <typename T, int D>
 flowmm_status launch_nibble_attention(const nibble::AttnArgs &a, const NibblePlan &n, cudaStream_t st) {
     auto kernel = (1 << a.page_shift) >= nibble::kTile ? nibble::nibble_attention_kernel<T, D, true> : nibble::nibble_attention_kernel<T, D, false>;
     if (!allow_smem(kernel) || cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared) != cudaSuccess)
@@ -1827,9 +1832,9 @@ extern "C" flowmm_status flowmm_nibble_load(const flowmm_cache_params *p, const 
     a.n_rows = p->n_rows; a.page_shift = page_shift(p->page_size); a.n_pages = p->n_pages; a.max_pages = p->max_pages;
     for (int i = 0; i < 3; ++i) { a.stride[0][i] = p->k_stride[i]; a.stride[1][i] = p->v_stride[i]; }
     a.by_heads = make_fastdiv(p->n_kv_heads); a.by_chunks = make_fastdiv((uint32_t)chunks);
-    auto kernel = p->dtype == FLOWMM_BF16 ? (p->head_dim == 128 ? nibble::nibble_load_kernel<__nv_bfloat16, 128> : nibble::nibble_load_kernel<__nv_bfloat16, 64>)
-                                          : (p->head_dim == 128 ? nibble::nibble_load_kernel<float, 128> : nibble::nibble_load_kernel<float, 64>);
-    launch(kernel, (unsigned)blocks, nibble::kCopyThreads, 0, st, a);
+    auto kernel = p->dtype == FLOWMM_BF16 ? (p->head_dim == 128 ? nibble_load<__nv_bfloat16, 128>(*p) : nibble_load<__nv_bfloat16, 64>(*p))
+                                          : (p->head_dim == 128 ? nibble_load<float, 128>(*p) : nibble_load<float, 64>(*p));
+    launch(kernel, (unsigned)blocks, nibble::kLoadThreads, 0, st, a);
     FLOWMM_LAUNCHED("nibble_load");
     return FLOWMM_OK;
 }

@@ -97,7 +97,6 @@ template <> struct Eight<__nv_bfloat16> {
     __device__ __forceinline__ void load(const __nv_bfloat16 *p) { v = load_raw16(p); }
     __device__ __forceinline__ uint32_t size() const { return paged::largest_bits<__nv_bfloat16>(v); }
     __device__ __forceinline__ void get(float (&x)[8]) const { Elem<__nv_bfloat16>::unpack(v, x); }
-    static __device__ __forceinline__ void store(__nv_bfloat16 *p, const float (&x)[8]) { Elem<__nv_bfloat16>::store16(p, x); }
 };
 template <> struct Eight<float> {
     uint4 v[2];
@@ -107,10 +106,6 @@ template <> struct Eight<float> {
         const uint32_t w[8] = {v[0].x, v[0].y, v[0].z, v[0].w, v[1].x, v[1].y, v[1].z, v[1].w};
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(w[i]);
-    }
-    static __device__ __forceinline__ void store(float *p, const float (&x)[8]) {
-        *reinterpret_cast<float4 *>(p) = make_float4(x[0], x[1], x[2], x[3]);
-        *reinterpret_cast<float4 *>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
     }
 };
 
@@ -204,44 +199,94 @@ struct LoadArgs {
     int64_t stride[2][3];
     FastDiv by_heads, by_chunks;
 };
-constexpr int kLoadRows = 64;
+constexpr int kLoadRows = 64, kLoadThreads = 128;
 
-// A block takes 64 rows of one (unit, KV head, K or V); D / 8 threads have a row.
-template <typename T, int D>
-__global__ void __launch_bounds__(kCopyThreads) nibble_load_kernel(const LoadArgs A) {
-    constexpr int kLanes = D / 8, kRows = kCopyThreads / kLanes, kVecs = kLoadRows / kRows;
+// The codes of 16 bytes of output, and what they stand for.
+template <typename T> struct Codes;
+template <> struct Codes<__nv_bfloat16> {
+    typedef uint32_t Word;
+    static __device__ __forceinline__ void store(__nv_bfloat16 *to, Word c, uint32_t scale) {
+        float x[8];
+        values8(c, scale, x);
+        Elem<__nv_bfloat16>::store16(to, x);
+    }
+};
+template <> struct Codes<float> {
+    typedef unsigned short Word;
+    static __device__ __forceinline__ void store(float *to, Word c, uint32_t scale) {
+        uint32_t h[2];
+        asm("{\n\t.reg .b8 a, b;\n\tmov.b16 {a, b}, %2;\n\tcvt.rn.f16x2.e2m1x2 %0, a;\n\tcvt.rn.f16x2.e2m1x2 %1, b;\n\t}" : "=r"(h[0]), "=r"(h[1]) : "h"(c));
+        const float2 a = from_half2(h[0]), b = from_half2(h[1]);
+        const float s = scale_value(scale);
+        *reinterpret_cast<float4 *>(to) = make_float4(a.x * s, a.y * s, b.x * s, b.y * s);
+    }
+};
+
+// A block takes 64 rows of one (unit, KV head, K or V); a thread has 16 bytes of output of every kRows-th row, neighbours side by side, eight rows' codes
+// and scales on their way at once.  Writing bounds it, next to it the instructions for each 16 bytes, so that addresses are formed once where all
+// rows are on one page (kOnePage: pages of 64 rows and more).
+template <typename T, int D, bool kOnePage>
+__global__ void __launch_bounds__(kLoadThreads) nibble_load_kernel(const LoadArgs A) {
+    constexpr int kN = Elem<T>::kVec, kLanes = D / kN, kRows = kLoadThreads / kLanes, kVecs = kLoadRows / kRows < 8 ? kLoadRows / kRows : 8;
+    typedef typename Codes<T>::Word Word;
     predecessor_done();
     successor_may_start();
-    const int lane = threadIdx.x % kLanes, row0 = threadIdx.x / kLanes;
+    const int lane = threadIdx.x % kLanes, row0 = threadIdx.x / kLanes, page = 1 << A.page_shift;
     const uint32_t which = blockIdx.x & 1u, q = blockIdx.x >> 1, q1 = A.by_heads.div(q), h = q - q1 * A.by_heads.d;
     const uint32_t u = A.by_chunks.div(q1), chunk = q1 - u * A.by_chunks.d;
     const int first = (int)(chunk * kLoadRows), held = A.rows[u], most = A.max_pages << A.page_shift;
+    const int *table = A.table + (int64_t)u * A.max_pages + (first >> A.page_shift);
     if ((held < 0 || held > most) && threadIdx.x == 0) report(A.status, kStatusIndex);
-    const int n = min(min(held, most), A.n_rows) - first;             // rows of this block
-    const int *table = A.table + (int64_t)u * A.max_pages;
+    const int n = min(kLoadRows, min(min(held, most), A.n_rows) - first);             // rows of this block
     if (n <= 0) return;
-    int id[kVecs];
-    uint32_t codes[kVecs], scale[kVecs];
-#pragma unroll
-    for (int i = 0; i < kVecs; ++i) {
-        const int r = row0 + i * kRows;
-        id[i] = r < n ? table[(first + r) >> A.page_shift] : -1;
-        if (r < n && (unsigned)id[i] >= (unsigned)A.n_pages) { report(A.status, kStatusIndex); id[i] = -1; }
+    const uint8_t *codes = A.pages[which] + lane * kN / 2, *scales = A.scale[which] + lane * kN / kGroup;
+    const uint32_t page_rows = A.by_heads.d << A.page_shift;
+    if (kOnePage) {
+        int id = table[0];
+        if ((unsigned)id >= (unsigned)A.n_pages) { if (threadIdx.x == 0) report(A.status, kStatusIndex); return; }
+        const int64_t row = (int64_t)((uint64_t)(uint32_t)id * page_rows) + ((h << A.page_shift) + (first & (page - 1)) + row0);
+        codes += row * (D / 2);
+        scales += row * (D / kGroup);
     }
+    T *x = static_cast<T *>(A.x[which]) + u * A.stride[which][0] + h * A.stride[which][1] + (int64_t)(first + row0) * A.stride[which][2] + lane * kN;
+    const int64_t step = kRows * A.stride[which][2];
+#pragma unroll 1
+    for (int r0 = 0; r0 < n; r0 += kVecs * kRows) {
+        Word c[kVecs];
+        uint8_t s[kVecs];
+        if (kOnePage && r0 + kVecs * kRows <= n) {
 #pragma unroll
-    for (int i = 0; i < kVecs; ++i) {
-        if (id[i] < 0) continue;
-        const int64_t at = (((int64_t)id[i] * A.by_heads.d + h) << A.page_shift) + ((first + row0 + i * kRows) & ((1 << A.page_shift) - 1));
-        codes[i] = *reinterpret_cast<const uint32_t *>(A.pages[which] + at * (D / 2) + lane * 4);
-        scale[i] = A.scale[which][at * (D / kGroup) + lane / 2];
-    }
-    T *x = static_cast<T *>(A.x[which]) + u * A.stride[which][0] + h * A.stride[which][1] + (int64_t)first * A.stride[which][2] + lane * 8;
+            for (int i = 0; i < kVecs; ++i) {
+                c[i] = *reinterpret_cast<const Word *>(codes + (r0 + i * kRows) * (D / 2));
+                s[i] = scales[(r0 + i * kRows) * (D / kGroup)];
+            }
 #pragma unroll
-    for (int i = 0; i < kVecs; ++i) {
-        if (id[i] < 0) continue;
-        float f[8];
-        values8(codes[i], scale[i], f);
-        Eight<T>::store(x + (int64_t)(row0 + i * kRows) * A.stride[which][2], f);
+            for (int i = 0; i < kVecs; ++i) {
+                Codes<T>::store(x, c[i], s[i]);
+                x += step;
+            }
+            continue;
+        }
+        int id[kVecs];
+#pragma unroll
+        for (int i = 0; i < kVecs; ++i) {
+            const int r = row0 + r0 + i * kRows;
+            id[i] = r < n ? (kOnePage ? 0 : table[r >> A.page_shift]) : -1;            // (first is the first row of a page)
+            if (r < n && (unsigned)id[i] >= (unsigned)A.n_pages) { report(A.status, kStatusIndex); id[i] = -1; }
+        }
+#pragma unroll
+        for (int i = 0; i < kVecs; ++i) {
+            if (id[i] < 0) continue;
+            const int64_t row = kOnePage ? r0 + i * kRows
+                                         : (int64_t)((uint64_t)(uint32_t)id[i] * page_rows) + ((h << A.page_shift) + ((row0 + r0 + i * kRows) & (page - 1)));
+            c[i] = *reinterpret_cast<const Word *>(codes + row * (D / 2));
+            s[i] = scales[row * (D / kGroup)];
+        }
+#pragma unroll
+        for (int i = 0; i < kVecs; ++i) {
+            if (id[i] >= 0) Codes<T>::store(x, c[i], s[i]);
+            x += step;
+        }
     }
 }
 
