@@ -434,7 +434,7 @@ def _cache_call(p: CacheParams, what: str):
     codes, scales, table, own = (p.n_pages, p.n_kv_heads, p.page_size, p.head_dim), (p.n_pages, p.n_kv_heads), (U, p.max_pages), (torch_dtype(p.dtype),)
     pool = (("k_pages", codes, _CODE_TYPES, 0, False), ("v_pages", codes, _CODE_TYPES, 0, False),
             ("k_scale", scales, _FLOAT, 0, False), ("v_scale", scales, _FLOAT, 0, False))
-    dense = (("k", rows, own, 1, False), ("v", rows, own, 2, False))
+    dense = (("k", rows, own, _CCacheParams.k_stride.offset, False), ("v", rows, own, _CCacheParams.v_stride.offset, False))
     held = (("block_table", table, _INT32, 0, False), ("rows", (U,), _INT32, 0, False))
     heads = (U, p.n_q_heads, p.head_dim)
     pairs, groups = codes[:3] + (p.head_dim // 2,), codes[:3] + (p.head_dim // 16,)       # of the 4-bit cache: bytes of two codes, scales
@@ -452,9 +452,12 @@ def _cache_call(p: CacheParams, what: str):
         "flowmm_nibble_load": nibbles + held + dense,
         "flowmm_nibble_attention": (("q", heads, own, 0, False),) + nibbles + held + (("out", heads, own, 0, False),),
     }[what] + (("ws", (-1,), _BYTES, 0, False),)
+    return _keep_call(p, what, p.c(), True, arguments)
+
+
+def _keep_call(p, what: str, cp, workspace: bool, arguments):
     function = ctypes.cast(getattr(load(), what), ctypes.c_void_p).value
-    cp = p.c()
-    handle = _load_marshal().make(what, function, ctypes.addressof(cp), arguments)
+    handle = _load_marshal().make(what, function, ctypes.addressof(cp), ctypes.sizeof(cp), workspace, arguments)
     p.calls[what] = handle = (_lib, _marshal.run, handle)
     return handle
 
@@ -547,7 +550,7 @@ class _CRotaryParams(ctypes.Structure):
 @dataclass
 class RotaryParams:
     """Mirror of flowmm_rotary_params; rotary_dim 0: the whole head; sections: pairs that go by each of three positions, None: one position a row.
-    The strides are taken from the tensors each call receives."""
+    The strides are taken from the tensors each call receives.  Keeps the handle of the call made with it until a field changes."""
     n_units: int
     n_q_heads: int
     n_kv_heads: int
@@ -566,28 +569,40 @@ class RotaryParams:
     trained: int = 0
     amplitude: float = 1.0
 
+    def __setattr__(self, name, value):
+        object.__setattr__(self, name, tuple(value) if name == "sections" and value is not None else value)
+        object.__setattr__(self, "calls", {})
+
+    def __reduce__(self):                    # (copies and pickles: the fields alone, a handle is an address of this process)
+        return type(self), _ROTARY_FIELDS(self)
+
     @property
     def pairs(self) -> int:
         return (self.rotary_dim or self.head_dim) // 2
 
-    def c(self, *tensors) -> _CRotaryParams:
-        """tensors: q, k, q_out, k_out, each may be None or missing."""
-        section = (0, 0, 0) if self.sections is None else tuple(self.sections)
+    def c(self) -> _CRotaryParams:
+        section = self.sections or (0, 0, 0)
         if len(section) != 3:
             raise ValueError("sections must be three numbers of pairs")
         cp = _CRotaryParams(self.n_units, self.n_q_heads, self.n_kv_heads, self.head_dim, self.n_rows, self.dtype, self.rotary_dim, self.layout,
                             int(self.adjoint), 1 if self.sections is None else 3, (ctypes.c_int32 * 3)(*section), self.scaling, self.amplitude, self.trained,
                             self.base, self.factor, self.low, self.high)
-        for name, heads, t in zip(("q_stride", "k_stride", "q_out_stride", "k_out_stride"), (self.n_q_heads, self.n_kv_heads) * 2, tensors + (None,) * 4):
-            if t is None:
-                dense = (heads * self.n_rows * self.head_dim, self.n_rows * self.head_dim, self.head_dim)
-                setattr(cp, name, (ctypes.c_int64 * 3)(*dense))
-                continue
-            if t.shape != (self.n_units, heads, self.n_rows, self.head_dim) or t.stride(3) != 1 or t.dtype != torch_dtype(self.dtype):
-                raise ValueError("flowmm_rotary: expected a %s tensor of shape %s with contiguous head_dim"
-                                 % (torch_dtype(self.dtype), (self.n_units, heads, self.n_rows, self.head_dim)))
-            setattr(cp, name, (ctypes.c_int64 * 3)(*t.stride()[:3]))
+        for name, heads in (("q_stride", self.n_q_heads), ("k_stride", self.n_kv_heads), ("q_out_stride", self.n_q_heads), ("k_out_stride", self.n_kv_heads)):
+            setattr(cp, name, (ctypes.c_int64 * 3)(heads * self.n_rows * self.head_dim, self.n_rows * self.head_dim, self.head_dim))
         return cp
+
+
+_ROTARY_FIELDS = operator.attrgetter("n_units", "n_q_heads", "n_kv_heads", "head_dim", "n_rows", "dtype", "rotary_dim", "layout", "adjoint", "sections",
+                                     "scaling", "base", "factor", "low", "high", "trained", "amplitude")
+
+
+def _rotary_call(p: RotaryParams):
+    q, k = ((p.n_units, heads, p.n_rows, p.head_dim) for heads in (p.n_q_heads, p.n_kv_heads))
+    own, at = (torch_dtype(p.dtype),), _CRotaryParams
+    return _keep_call(p, "flowmm_rotary", p.c(), False, (
+        ("q", q, own, at.q_stride.offset, True), ("k", k, own, at.k_stride.offset, True),
+        ("positions", (p.n_units, 1 if p.sections is None else 3, p.n_rows), _INT32, 0, False), ("table", (p.pairs,), (torch.int64,), 0, False),
+        ("q_out", q, own, at.q_out_stride.offset, True), ("k_out", k, own, at.k_out_stride.offset, True)))
 
 
 def alloc_rotary_table(p: RotaryParams, device="cuda") -> torch.Tensor:
@@ -608,13 +623,12 @@ def flowmm_rotary_table(p: RotaryParams, table):
 def flowmm_rotary(p: RotaryParams, q, k, positions, table, q_out, k_out):
     """Queries q [units, q_heads, n_rows, head_dim] and keys k turned by positions [units, n_rows] ([units, 3, n_rows] with sections);
     q and q_out, or k and k_out, may be None, an output may be its input."""
-    cp = p.c(q, k, q_out, k_out)
-    want = (p.n_units, p.n_rows) if p.sections is None else (p.n_units, 3, p.n_rows)
-    if positions.dtype != torch.int32 or positions.numel() != math.prod(want) or positions.shape[-1] != p.n_rows or not positions.is_contiguous():
-        raise ValueError("flowmm_rotary: positions must be a contiguous int32 tensor of shape %s" % (want,))
-    if table.dtype != torch.int64 or table.shape != (p.pairs,) or not table.is_contiguous():
-        raise ValueError("flowmm_rotary: table must be a contiguous int64 tensor of %d elements" % p.pairs)
-    _check(load().flowmm_rotary(ctypes.byref(cp), _p(q), _p(k), _p(positions), _p(table), _p(q_out), _p(k_out), _stream()), "flowmm_rotary")
+    call = p.calls.get("flowmm_rotary")
+    if call is None or call[0] is not _lib:
+        call = _rotary_call(p)
+    code = call[1](call[2], q, k, positions, table, q_out, k_out)
+    if code != 0:
+        raise FlowmmError(code, "flowmm_rotary")
 
 
 def flowmm_selftest_wait_timeout(ws):

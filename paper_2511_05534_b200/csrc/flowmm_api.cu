@@ -1897,18 +1897,23 @@ flowmm_status validate_rotary(const flowmm_rotary_params *p) {
     return FLOWMM_OK;
 }
 
-template <typename T, int D>
-flowmm_status launch_rotary(const flowmm_rotary_params &p, rotary::Args &a, cudaStream_t st) {
-    constexpr int per = rotary::kThreads / (D / (2 * Elem<T>::kVec));
-    const int64_t blocks = ((int64_t)a.rows + per - 1) / per;
+template <typename T, int D, int kRows>
+flowmm_status launch_rotary_rows(const flowmm_rotary_params &p, rotary::Args &a, cudaStream_t st) {
+    constexpr int at_once = rotary::kThreads / (D / (2 * Elem<T>::kVec) * kRows);      // heads
+    const int64_t blocks = ((int64_t)a.rows + kRows - 1) / kRows;
     const int heads = a.heads[0] + a.heads[1];
-    // as many heads to a thread as leave every SM eight blocks; blocks of heads in the grid's second dimension, 65 535 at most
-    const int64_t want = std::max<int64_t>(1, std::min<int64_t>(heads, blocks * heads / (8 * kScoreCtas)));
-    a.each = (int)std::max<int64_t>(want, (heads + 65534) / 65535);
-    auto kernel = p.layout == FLOWMM_ROTARY_PAIRS ? rotary::rotary_kernel<T, D, true> : rotary::rotary_kernel<T, D, false>;
+    // all heads to a block, or as few as make four blocks an SM; 65 535 parts of the heads at most
+    const int64_t most = (heads + at_once - 1) / at_once, parts = std::min<int64_t>({most, (4 * kScoreCtas + blocks - 1) / blocks, 65535});
+    a.each = (int)((most + parts - 1) / parts * at_once);
+    auto kernel = p.layout == FLOWMM_ROTARY_PAIRS ? rotary::rotary_kernel<T, D, true, kRows> : rotary::rotary_kernel<T, D, false, kRows>;
     launch(kernel, dim3((unsigned)blocks, (heads + a.each - 1) / a.each), rotary::kThreads, 0, st, a);
     FLOWMM_LAUNCHED("rotary");
     return FLOWMM_OK;
+}
+template <typename T, int D>
+flowmm_status launch_rotary(const flowmm_rotary_params &p, rotary::Args &a, cudaStream_t st) {
+    constexpr int many = rotary::kManyBytes / (D * (int)sizeof(T));
+    return a.rows >= 4u * kScoreCtas * many ? launch_rotary_rows<T, D, many>(p, a, st) : launch_rotary_rows<T, D, rotary::kFewRows>(p, a, st);
 }
 
 }  // namespace
@@ -1951,9 +1956,10 @@ extern "C" flowmm_status flowmm_rotary(const flowmm_rotary_params *p, const void
     }
     a.heads[0] = q ? p->n_q_heads : 0; a.heads[1] = k ? p->n_kv_heads : 0;
     a.positions = positions; a.phase = reinterpret_cast<const unsigned long long *>(table);
-    a.R = p->rotary_dim ? p->rotary_dim : p->head_dim; a.axes = p->n_axes; a.adjoint = p->adjoint;
+    a.R = p->rotary_dim ? p->rotary_dim : p->head_dim; a.axes = p->n_axes;
     a.end0 = p->n_axes == 3 ? p->section[0] : a.R / 2; a.end1 = p->n_axes == 3 ? p->section[0] + p->section[1] : a.R / 2;
     a.amplitude = p->amplitude != 0.f ? p->amplitude : 1.f;
+    a.sine = p->adjoint ? -a.amplitude : a.amplitude;
     a.rows = (uint32_t)((int64_t)p->n_units * p->n_rows); a.by_rows = make_fastdiv(p->n_rows);
     if (p->dtype == FLOWMM_BF16) return p->head_dim == 128 ? launch_rotary<__nv_bfloat16, 128>(*p, a, st) : launch_rotary<__nv_bfloat16, 64>(*p, a, st);
     return p->head_dim == 128 ? launch_rotary<float, 128>(*p, a, st) : launch_rotary<float, 64>(*p, a, st);

@@ -1,4 +1,4 @@
-// Argument marshalling of the paged cache's calls for Python: looks at the tensors of a call (shapes, types, devices, strides) and
+// Argument marshalling of the paged caches' calls and of rotary positions for Python: looks at the tensors of a call (shapes, types, devices, strides) and
 // passes their addresses on.  The same in Python took longer than the kernels of a decode step: ten tensors' attributes 4 us.
 #include <Python.h>
 
@@ -8,6 +8,7 @@
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <cstring>
 #include <exception>
 #include <string>
 #include <vector>
@@ -16,34 +17,45 @@
 
 namespace {
 
+union Params {
+    flowmm_cache_params cache;
+    flowmm_rotary_params rotary;
+    char bytes[1];
+};
+
 struct Argument {
     std::string name;
     std::vector<int64_t> shape;              // -1: any size
     std::vector<c10::ScalarType> types;
-    int dense;                               // 1, 2: the rows of K, of V, by strides; else 0: contiguous
+    int dense;                               // where in the params the strides of a tensor of rows are, in bytes; else 0: contiguous
     bool optional;                           // may be None
 };
-// One entry point with one set of params: what its tensors have to look like, in the order of its pointers, `ws` last.
+// One entry point with one set of params: what its tensors have to look like, in the order of its pointers; should it have a workspace, that is the last one.
 struct Call {
     std::string what;
     void *function;
-    flowmm_cache_params params;
+    Params params;
+    bool workspace;
     std::vector<Argument> arguments;
 };
 
 constexpr const char *kCapsule = "flowmm_call";
-constexpr int kMostPointers = 9;
+constexpr size_t kFewestPointers = 6, kMostPointers = 9;
 
 void drop(PyObject *capsule) { delete static_cast<Call *>(PyCapsule_GetPointer(capsule, kCapsule)); }
 
-// make(what, function's address, params' address, ((name, shape, types, dense, optional), ...)) -> the call's handle
+// make(what, function's address, params' address and size, workspace, ((name, shape, types, dense, optional), ...)) -> the call's handle
 PyObject *make(PyObject *, PyObject *args) {
     const char *what;
     unsigned long long function, params;
+    Py_ssize_t size;
+    int workspace;
     PyObject *list;
-    if (!PyArg_ParseTuple(args, "sKKO!", &what, &function, &params, &PyTuple_Type, &list)) return nullptr;
+    if (!PyArg_ParseTuple(args, "sKKnpO!", &what, &function, &params, &size, &workspace, &PyTuple_Type, &list)) return nullptr;
+    if (size < 0 || (size_t)size > sizeof(Params)) { PyErr_SetString(PyExc_ValueError, "unknown params"); return nullptr; }
     try {
-        Call *call = new Call{what, reinterpret_cast<void *>(function), *reinterpret_cast<const flowmm_cache_params *>(params), {}};
+        Call *call = new Call{what, reinterpret_cast<void *>(function), {}, workspace != 0, {}};
+        std::memcpy(call->params.bytes, reinterpret_cast<const void *>(params), (size_t)size);
         PyObject *capsule = PyCapsule_New(call, kCapsule, drop);
         if (!capsule) { delete call; return nullptr; }
         for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(list); ++i) {
@@ -82,9 +94,9 @@ PyObject *run(PyObject *, PyObject *const *args, Py_ssize_t n) {
     const Call *call = static_cast<const Call *>(PyCapsule_GetPointer(args[0], kCapsule));
     if (!call) return nullptr;
     const size_t count = call->arguments.size();
-    if ((size_t)(n - 1) != count || count < 2 || count > kMostPointers) { PyErr_SetString(PyExc_TypeError, "wrong number of tensors"); return nullptr; }
+    if ((size_t)(n - 1) != count || count < kFewestPointers || count > kMostPointers) { PyErr_SetString(PyExc_TypeError, "wrong number of tensors"); return nullptr; }
     try {
-        flowmm_cache_params params = call->params;
+        Params params = call->params;
         void *at[kMostPointers] = {};
         int64_t ws_bytes = 0;
         c10::DeviceIndex device = -1;
@@ -99,6 +111,7 @@ PyObject *run(PyObject *, PyObject *const *args, Py_ssize_t n) {
             const auto sizes = t.sizes(), strides = t.strides();
             bool same = sizes.size() == a.shape.size();
             for (size_t d = 0; same && d < sizes.size(); ++d) same = a.shape[d] < 0 || sizes[d] == a.shape[d];
+            if (!same && a.shape.size() == 3 && a.shape[1] == 1 && sizes.size() == 2) same = sizes[0] == a.shape[0] && sizes[1] == a.shape[2];
             bool type = false;
             for (c10::ScalarType s : a.types) type = type || t.scalar_type() == s;
             if (!same || !type) {
@@ -110,21 +123,25 @@ PyObject *run(PyObject *, PyObject *const *args, Py_ssize_t n) {
             }
             if (a.dense) {
                 if (strides[3] != 1) return refuse(*call, a, "must have contiguous head_dim");
-                for (int d = 0; d < 3; ++d) (a.dense == 1 ? params.k_stride : params.v_stride)[d] = strides[d];
+                int64_t three[3] = {strides[0], strides[1], strides[2]};
+                std::memcpy(params.bytes + a.dense, three, sizeof(three));
             } else if (!t.is_contiguous()) {
                 return refuse(*call, a, "must be contiguous");
             }
             at[i] = t.data_ptr();
-            if (i == count - 1) ws_bytes = t.numel();
+            if (call->workspace && i == count - 1) ws_bytes = t.numel();
         }
         void *stream = c10::cuda::getCurrentCUDAStream(device).stream();
-        typedef flowmm_status (*Seven)(const flowmm_cache_params *, void *, void *, void *, void *, void *, void *, void *, void *, size_t, void *);
-        typedef flowmm_status (*Eight)(const flowmm_cache_params *, void *, void *, void *, void *, void *, void *, void *, void *, void *, size_t, void *);
+        typedef flowmm_status (*Six)(const void *, void *, void *, void *, void *, void *, void *, void *);
+        typedef flowmm_status (*Seven)(const void *, void *, void *, void *, void *, void *, void *, void *, void *, size_t, void *);
+        typedef flowmm_status (*Eight)(const void *, void *, void *, void *, void *, void *, void *, void *, void *, void *, size_t, void *);
         int status = -1;
         Py_BEGIN_ALLOW_THREADS
-        if (count == 8)
+        if (count == 6 && !call->workspace)
+            status = reinterpret_cast<Six>(call->function)(&params, at[0], at[1], at[2], at[3], at[4], at[5], stream);
+        else if (count == 8 && call->workspace)
             status = reinterpret_cast<Seven>(call->function)(&params, at[0], at[1], at[2], at[3], at[4], at[5], at[6], at[7], (size_t)ws_bytes, stream);
-        else if (count == 9)
+        else if (count == 9 && call->workspace)
             status = reinterpret_cast<Eight>(call->function)(&params, at[0], at[1], at[2], at[3], at[4], at[5], at[6], at[7], at[8], (size_t)ws_bytes, stream);
         Py_END_ALLOW_THREADS
         return PyLong_FromLong(status);

@@ -37,81 +37,97 @@ struct Args {
     const int *positions;              // [U, axes, T]
     const unsigned long long *phase;
     int heads[2];
-    int each;                          // heads of a thread
+    int each;                          // heads of a block
     int R, axes, end0, end1;           // the first pairs that go by the second and the third position
-    float amplitude;
+    float amplitude, sine;             // of cos, of sin: turned for the adjoint
     uint32_t rows;                     // U * T
     int64_t in[2][3], out[2][3];
     FastDiv by_rows;                   // by T
-    int adjoint;
 };
-constexpr int kThreads = 256;
+constexpr int kThreads = 256, kFewRows = 4, kManyBytes = 4096;
 
-// cos and sin of a phase, a 32-bit fraction of a turn: the nearest quarter apart, what is left (an eighth at most) to fp32, where it has 25 bits and more
-__device__ __forceinline__ void turn(uint32_t phase, float &c, float &s) {
+// cos and sin of a phase, a 32-bit fraction of a turn: the nearest quarter apart; of what is left, an eighth of a turn at most, their Taylor series to the tenth and
+// ninth power, which leave 2^-32 and 2^-29 of it.
+__device__ __forceinline__ float2 turn(uint32_t phase) {
     const uint32_t quarter = (phase + 0x20000000u) >> 30;
-    const float rest = (float)(int)(phase - (quarter << 30)) * 4.656612873077393e-10f;      // of half a turn: 2^-31
-    float c0, s0;
-    sincospif(rest, &s0, &c0);
-    c = quarter & 1u ? s0 : c0;
-    s = quarter & 1u ? c0 : s0;
-    if (quarter == 1u || quarter == 2u) c = -c;
-    if (quarter & 2u) s = -s;
+    const float x = (float)(int)(phase - (quarter << 30)) * 1.4629180792671596e-9f;      // 2 pi 2^-32
+    const float y = x * x;
+    float s = fmaf(y, 1.f / 362880.f, -1.f / 5040.f), c = fmaf(y, -1.f / 3628800.f, 1.f / 40320.f);
+    s = fmaf(y, s, 1.f / 120.f); c = fmaf(y, c, -1.f / 720.f);
+    s = fmaf(y, s, -1.f / 6.f); c = fmaf(y, c, 1.f / 24.f);
+    c = fmaf(y, c, -0.5f);
+    s = fmaf(y * s, x, x); c = fmaf(y, c, 1.f);
+    const float2 r = quarter & 1u ? make_float2(s, c) : make_float2(c, s);
+    return make_float2(quarter == 1u || quarter == 2u ? -r.x : r.x, quarter & 2u ? -r.y : r.y);
 }
 
-// A thread has two vectors of a row, so kN pairs: channels i and i + R / 2, or neighbours; the angles once for `each` heads.
-template <typename T, int D, bool kPairs>
+// A block takes four rows, or where that leaves blocks enough so many as make 4 KB of a head on end, of all or `each` heads: the angles once for all of
+// them, a pair and row a thread, then a thread two vectors of a row, so kN pairs (channels i and i + R / 2, or neighbours), of every kHeads-th
+// head.  Memory bounds it: each element is read and written once, 16 bytes at a time.  (33 792 rows, 72 heads of 128, 195 us for 193 of memory; with
+// 1 KB on end 209, 2 KB 207; two heads on their way at once, by more registers a thread, 204; with 4 KB fp32 rows 61.6 for 61.0, with 8 KB 65.)
+template <typename T, int D, bool kPairs, int kRows>
 __global__ void __launch_bounds__(kThreads) rotary_kernel(const Args A) {
-    constexpr int kN = Elem<T>::kVec, kLanes = D / (2 * kN), kRows = kThreads / kLanes;
+    constexpr int kN = Elem<T>::kVec, kLanes = D / (2 * kN), kHeads = kThreads / (kLanes * kRows);
+    __shared__ float cosine[kRows][D / 2], sine[kRows][D / 2];
     predecessor_done();
     successor_may_start();
-    const int lane = threadIdx.x % kLanes, pair = lane * kN, half = A.R / 2;
-    const uint32_t row = blockIdx.x * kRows + threadIdx.x / kLanes;
+    const uint32_t base = blockIdx.x * kRows;
+    const int half = A.R / 2;
+#pragma unroll
+    for (int i = 0; i < (kRows * D / 2 + kThreads - 1) / kThreads; ++i) {
+        const int p = (threadIdx.x + i * kThreads) % (D / 2), r = (threadIdx.x + i * kThreads) / (D / 2);
+        const uint32_t row = base + r;
+        if (r < kRows && p < half && row < A.rows) {
+            const uint32_t u = A.by_rows.div(row), t = row - u * A.by_rows.d;
+            const int axis = p < A.end0 ? 0 : p < A.end1 ? 1 : 2;
+            const int at = A.positions[((int64_t)u * A.axes + axis) * A.by_rows.d + t];
+            const float2 v = turn((uint32_t)((A.phase[p] * (unsigned long long)(long long)at) >> 32));
+            cosine[r][p] = v.x * A.amplitude;
+            sine[r][p] = v.y * A.sine;
+        }
+    }
+    __syncthreads();
+    const int lane = threadIdx.x % kLanes, r = threadIdx.x / kLanes % kRows, pair = lane * kN;
+    const uint32_t row = base + r;
     if (row >= A.rows) return;
     const uint32_t u = A.by_rows.div(row), t = row - u * A.by_rows.d;
     const bool turns = pair < half;
     const int first = kPairs || !turns ? 2 * pair : pair, second = kPairs || !turns ? first + kN : pair + half;
     float c[kN], s[kN];
-    if (turns) {
-        int pos[3];
 #pragma unroll
-        for (int a = 0; a < 3; ++a) pos[a] = a < A.axes ? A.positions[((int64_t)u * A.axes + a) * A.by_rows.d + t] : 0;
-#pragma unroll
-        for (int i = 0; i < kN; ++i) {
-            const int p = pair + i, at = p < A.end0 ? pos[0] : p < A.end1 ? pos[1] : pos[2];
-            turn((uint32_t)((A.phase[p] * (unsigned long long)(long long)at) >> 32), c[i], s[i]);
-            c[i] *= A.amplitude;
-            s[i] *= A.adjoint ? -A.amplitude : A.amplitude;
-        }
+    for (int i = 0; i < kN; ++i) {
+        c[i] = turns ? cosine[r][pair + i] : 1.f;
+        s[i] = turns ? sine[r][pair + i] : 0.f;
     }
-    const int all = A.heads[0] + A.heads[1], g0 = blockIdx.y * A.each, g1 = min(all, g0 + A.each);
-    for (int g = g0; g < g1; ++g) {
+    const int all = A.heads[0] + A.heads[1], end = min(all, ((int)blockIdx.y + 1) * A.each);
+#pragma unroll 1
+    for (int g = blockIdx.y * A.each + threadIdx.x / (kLanes * kRows); g < end; g += kHeads) {
         const int which = g >= A.heads[0], h = g - (which ? A.heads[0] : 0);
         const T *x = static_cast<const T *>(A.x[which]) + u * A.in[which][0] + h * A.in[which][1] + t * A.in[which][2];
         T *y = static_cast<T *>(A.y[which]) + u * A.out[which][0] + h * A.out[which][1] + t * A.out[which][2];
-        float a[kN], b[kN];
-        Elem<T>::load16(x + first, a);
-        Elem<T>::load16(x + second, b);
-        if (turns) {
-            float p[kN], q[kN];
-            if (kPairs) {
-#pragma unroll
-                for (int i = 0; i < kN; i += 2) {
-                    p[i] = a[i] * c[i / 2] - a[i + 1] * s[i / 2];
-                    p[i + 1] = a[i + 1] * c[i / 2] + a[i] * s[i / 2];
-                    q[i] = b[i] * c[kN / 2 + i / 2] - b[i + 1] * s[kN / 2 + i / 2];
-                    q[i + 1] = b[i + 1] * c[kN / 2 + i / 2] + b[i] * s[kN / 2 + i / 2];
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < kN; ++i) { p[i] = a[i] * c[i] - b[i] * s[i]; q[i] = b[i] * c[i] + a[i] * s[i]; }
-            }
-            Elem<T>::store16(y + first, p);
-            Elem<T>::store16(y + second, q);
-        } else {
-            Elem<T>::store16(y + first, a);
-            Elem<T>::store16(y + second, b);
+        const uint4 raw[2] = {load_raw16(x + first), load_raw16(x + second)};
+        if (!turns) {                                                 // (as it is: not a product with one, which a NaN's bits need not survive)
+            *reinterpret_cast<uint4 *>(y + first) = raw[0];
+            *reinterpret_cast<uint4 *>(y + second) = raw[1];
+            continue;
         }
+        float a[kN], b[kN], p[kN], q[kN];
+        Elem<T>::unpack(raw[0], a);
+        Elem<T>::unpack(raw[1], b);
+        if (kPairs) {
+#pragma unroll
+            for (int i = 0; i < kN; i += 2) {
+                p[i] = a[i] * c[i / 2] - a[i + 1] * s[i / 2];
+                p[i + 1] = a[i + 1] * c[i / 2] + a[i] * s[i / 2];
+                q[i] = b[i] * c[kN / 2 + i / 2] - b[i + 1] * s[kN / 2 + i / 2];
+                q[i + 1] = b[i + 1] * c[kN / 2 + i / 2] + b[i] * s[kN / 2 + i / 2];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kN; ++i) { p[i] = a[i] * c[i] - b[i] * s[i]; q[i] = b[i] * c[i] + a[i] * s[i]; }
+        }
+        Elem<T>::store16(y + first, p);
+        Elem<T>::store16(y + second, q);
     }
 }
 
