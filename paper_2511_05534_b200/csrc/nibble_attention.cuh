@@ -14,6 +14,8 @@
 // sum of two fp16 numbers, each product is two.  The largest weight is 2^10 to 2^15 (fp32: 2^14), so that fp16 holds others to full precision down to 2^-24 of
 // it, and two of them to 2^-21 of themselves down to 2^-18 of it, both to 2^-35 (fp32: 2^-39) of it below.
 #pragma once
+#include <cuda_fp16.h>
+
 #include "common.cuh"
 #include "nibble_cache.cuh"
 #include "paged_attention.cuh"
@@ -205,6 +207,11 @@ __device__ __forceinline__ uint32_t times(uint32_t a, uint32_t b) {
     uint32_t h;
     asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(h) : "r"(a), "r"(b));
     return h;
+}
+// both halves times one half of b (which the instruction picks by itself)
+__device__ __forceinline__ uint32_t times_one(uint32_t a, uint32_t b, int upper) {
+    const __half2 x = *reinterpret_cast<const __half2 *>(&a), y = *reinterpret_cast<const __half2 *>(&b), z = __hmul2_rn(x, upper ? __high2half2(y) : __low2half2(y));
+    return *reinterpret_cast<const uint32_t *>(&z);
 }
 __device__ __forceinline__ float max_over_rows(float x) {              // over the lanes with the same lane % 4
 #pragma unroll
@@ -412,7 +419,7 @@ __global__ void __launch_bounds__(kAttnThreads, kBlocks) nibble_attention_kernel
                 const uint8_t *codes = ring + take * L::kHalf + key * (D / 2) + t * (D / 8), *scales = ring + take * L::kHalf + L::kCodes + key * (D / 16) + t * (D / 64);
 #pragma unroll
                 for (int s = 0; s < kSubs; ++s) {
-                    uint32_t w[2][kWords], sc[2][2];
+                    uint32_t w[2][kWords], sc[2];                    // [8 further], scales of the first two words and the next
 #pragma unroll
                     for (int b = 0; b < 2; ++b) {
                         const int row = 16 * s + 8 * b;
@@ -420,12 +427,11 @@ __global__ void __launch_bounds__(kAttnThreads, kBlocks) nibble_attention_kernel
                             const uint4 v = *reinterpret_cast<const uint4 *>(codes + row * 64);
                             w[b][0] = v.x; w[b][1] = v.y; w[b][kWords - 2] = v.z; w[b][kWords - 1] = v.w;
                             const uint32_t both = *reinterpret_cast<const unsigned short *>(scales + row * 8);
-                            sc[b][0] = (both & 255u) * 0x00800080u;
-                            sc[b][1] = (both >> 8) * 0x00800080u;
+                            sc[b] = __byte_perm(both, 0, 0x4140) << 7;
                         } else {
                             const uint2 v = *reinterpret_cast<const uint2 *>(codes + row * 32);
                             w[b][0] = v.x; w[b][1] = v.y;
-                            sc[b][0] = sc[b][1] = scales[row * 4] * 0x00800080u;
+                            sc[b] = (uint32_t)scales[row * 4] << 7;
                         }
                     }
 #pragma unroll
@@ -434,7 +440,7 @@ __global__ void __launch_bounds__(kAttnThreads, kBlocks) nibble_attention_kernel
                         widen8(w[0][j], lo);
                         widen8(w[1][j], hi);
 #pragma unroll
-                        for (int p = 0; p < 4; ++p) { lo[p] = times(lo[p], sc[0][j >> 1]); hi[p] = times(hi[p], sc[1][j >> 1]); }
+                        for (int p = 0; p < 4; ++p) { lo[p] = times_one(lo[p], sc[0], j >> 1); hi[p] = times_one(hi[p], sc[1], j >> 1); }
 #pragma unroll
                         for (int p = 0; p < 4; p += 2) {
                             const uint32_t a[4] = {lo[p], hi[p], lo[p + 1], hi[p + 1]};
