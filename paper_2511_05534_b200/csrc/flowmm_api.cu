@@ -1721,8 +1721,9 @@ struct NibblePlan {
 NibblePlan nibble_plan(const flowmm_cache_params &p) {
     NibblePlan n;
     const int64_t heads = (int64_t)p.n_units * p.n_kv_heads, tiles = ((int64_t)p.max_pages * p.page_size + nibble::kTile - 1) / nibble::kTile;
-    n.blocks = std::min<int64_t>(nibble::kBlocks * kScoreCtas, heads * tiles);
-    n.joins = heads > n.blocks || tiles > nibble::kWholeTiles;
+    constexpr int64_t blocks = nibble::kBlocks * kScoreCtas;
+    n.joins = heads > blocks || tiles > nibble::kWholeTiles;
+    n.blocks = n.joins ? std::min(blocks, heads * tiles) : heads;
     n.part = 256 + (n.joins ? align256((size_t)n.blocks * sizeof(int4)) : 0);
     n.total = n.part + (n.joins ? align256((size_t)n.blocks * 2 * paged::record_floats(p.n_q_heads / p.n_kv_heads, p.head_dim) * sizeof(float)) : 0);
     return n;
@@ -1861,7 +1862,7 @@ extern "C" flowmm_status flowmm_nibble_attention(const flowmm_cache_params *p, c
     a.table = block_table; a.rows = rows; a.out = out; a.status = static_cast<int *>(ws);
     a.part = at<float>(ws, n.part); a.cut_heads = n.joins ? at<int4>(ws, 256) : nullptr;
     a.U = p->n_units; a.Hq = p->n_q_heads; a.Hkv = p->n_kv_heads; a.G = p->n_q_heads / p->n_kv_heads;
-    a.page_shift = page_shift(p->page_size); a.n_pages = p->n_pages; a.max_pages = p->max_pages;
+    a.page_shift = page_shift(p->page_size); a.n_pages = p->n_pages; a.max_pages = p->max_pages; a.by_heads = make_fastdiv(p->n_kv_heads);
     a.scale_log2 = (p->softmax_scale != 0.f ? p->softmax_scale : 1.f / sqrtf((float)p->head_dim)) * kLog2e;
     if (p->dtype == FLOWMM_BF16)
         return p->head_dim == 128 ? launch_nibble_attention<__nv_bfloat16, 128>(a, n, st) : launch_nibble_attention<__nv_bfloat16, 64>(a, n, st);

@@ -31,10 +31,11 @@ struct AttnArgs {
     const int *table, *rows;           // [U, max_pages], [U]
     void *out;                         // [U, Hq, D]
     float *part;                       // two records a block (paged::record_floats)
-    int4 *cut_heads;                   // [blocks], as paged::AttnArgs has it, or null: no head is cut
+    int4 *cut_heads;                   // [blocks], as paged::AttnArgs has it, or null: no head is cut, a block for each
     int *status;
     int U, Hq, Hkv, G, page_shift, n_pages, max_pages;
     float scale_log2;
+    FastDiv by_heads;                  // by Hkv
 };
 
 constexpr int kTile = 64, kWarps = 6, kBlocks = 2, kAttnThreads = kWarps * 32, kHeads = 8;      // blocks of an SM
@@ -283,14 +284,21 @@ __device__ __forceinline__ void put_four(__nv_bfloat16 *to, const float (&x)[4])
     const __nv_bfloat162 a = __floats2bfloat162_rn(x[0], x[1]), b = __floats2bfloat162_rn(x[2], x[3]);
     *reinterpret_cast<uint2 *>(to) = make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&b));
 }
-// What the parts of heads at both ends of a warp's tiles are.
+__device__ __forceinline__ void put_eight(float *to, const float (&x)[8]) {
+    reinterpret_cast<float4 *>(to)[0] = make_float4(x[0], x[1], x[2], x[3]);
+    reinterpret_cast<float4 *>(to)[1] = make_float4(x[4], x[5], x[6], x[7]);
+}
+__device__ __forceinline__ void put_eight(__nv_bfloat16 *to, const float (&x)[8]) { Elem<__nv_bfloat16>::store16(to, x); }
+
+// What the parts of heads at both ends of a warp's tiles are: the first part's head began before them (a front), and ends in them; the last part's head
+// begins in them and goes on (a back).
+constexpr int kFront = 1, kEnds = 2, kBack = 4;
 struct Meta {
-    int front, ends;                     // the first part's head began before the warp's tiles; and ends in them
-    int back;                            // the last part's head begins in them and goes on
-    int fu, fh, bu, bh;                  // the two heads
+    int flags;
+    int fu, fh, bu, bh;                  // the heads of front and back
     int blocks;                          // that have part in the back's head, should it go on behind this block
 };
-static_assert(sizeof(Meta) == 32, "as much as Lay::kMeta leaves");
+static_assert(sizeof(Meta) <= 32, "as much as Lay::kMeta leaves");
 
 // kLong: pages of kTile rows and more, so that a tile is on one page.
 template <typename T, int D, bool kLong>
@@ -323,20 +331,33 @@ __global__ void __launch_bounds__(kAttnThreads, kBlocks) nibble_attention_kernel
                     put_four(static_cast<T *>(A.out) + (int64_t)u * A.Hq * D + 4 * i, zero);
                 }
     };
-    const Cut cut = make_cut(A);
-    uint32_t x0, x1;
-    block_piece(A, cut, x0, x1);
+    // No head is cut: block i has the i-th one, and the table is read together with the lengths.  Else the lengths say what the block has.
+    Cut cut;
+    Walk cur;
+    uint32_t x0 = 0, x1;
+    int ids = 0, ids_unit = -1, ids_base = 0;                        // 32 entries of the block table
+    if (A.cut_heads == nullptr) {
+        cur.u = ids_unit = A.by_heads.div(blockIdx.x);
+        cur.h = blockIdx.x - cur.u * A.Hkv;
+        cur.rows = unit_rows(A, cur.u);
+        ids = lane < A.max_pages ? A.table[(int64_t)cur.u * A.max_pages + lane] : 0;
+        x1 = tiles_of(cur.rows);
+        if (lane >= (cur.rows + (1 << A.page_shift) - 1) >> A.page_shift) ids = 0;
+        if ((unsigned)ids >= (unsigned)A.n_pages) { report(A.status, kStatusIndex); ids = 0; }
+    } else {
+        cut = make_cut(A);
+        block_piece(A, cut, x0, x1);
+    }
     const uint32_t each = (x1 - x0 + kWarps - 1) / kWarps;
     const uint32_t w0 = min(x1, x0 + warp * each), w1 = min(x1, w0 + each);
     const int count = (int)(w1 - w0);
-    Meta me = {0, 0, 0, 0, 0, 0, 0, 0};
+    Meta me = {0, 0, 0, 0, 0, 0};
     if (count > 0) {
         // Copies of 16 bytes, a lane the codes of row lane / kLanes of every kRows of the tile, and scales that lie side by side.  Sixteen rows are on one
         // page and come or are left out together.
         constexpr int kLanes = D / 32, kRows = 32 / kLanes, kScaleRows = 256 / D;
         const int page = 1 << A.page_shift, scale_group = lane * kScaleRows >> 4;
         const uint32_t to = tc::smem_u32(ring) + lane * 16, page_rows = (uint32_t)A.Hkv << A.page_shift;
-        int ids = 0, ids_unit = -1, ids_base = 0;                    // 32 entries of the block table
         // where the tile's codes are, from this lane's first sixteen bytes on, for every sixteen rows; the lane's scales; the tile's rows
         struct Source { int64_t codes[kLong ? 1 : kTile / 16], scales; int left; } next;
         auto locate = [&](const Walk &w) {
@@ -386,7 +407,9 @@ __global__ void __launch_bounds__(kAttnThreads, kBlocks) nibble_attention_kernel
             tc::copies_commit();
             put = put == 2 ? 0 : put + 1;
         };
-        Walk cur = walk_to(A, cut, w0), far = cur;
+        if (A.cut_heads == nullptr) cur.left = cur.rows - (int)w0 * kTile;
+        else cur = walk_to(A, cut, w0);
+        Walk far = cur;
         uint32_t take = 0;
         locate(far);
         issue(0, true);
@@ -561,7 +584,7 @@ __global__ void __launch_bounds__(kAttnThreads, kBlocks) nibble_attention_kernel
 #pragma unroll
                     for (int q = 0; q < 2; ++q) {
                         if (2 * t + q >= A.G) continue;
-                        const float inverse = 1.f / sum[q];
+                        const float inverse = reciprocal(sum[q]);
                         T *out = static_cast<T *>(A.out) + ((int64_t)cur.u * A.Hq + cur.h * A.G + 2 * t + q) * D + r * (D / 8);
 #pragma unroll
                         for (int j = 0; j < D / 16; j += 2) {
@@ -570,12 +593,12 @@ __global__ void __launch_bounds__(kAttnThreads, kBlocks) nibble_attention_kernel
                         }
                     }
                 } else if (!begins) {
-                    me.front = 1; me.ends = last; me.fu = cur.u; me.fh = cur.h;
+                    me.flags |= last ? kFront | kEnds : kFront; me.fu = cur.u; me.fh = cur.h;
                     put_record<D>(record, o, ref, sum);
                 } else {
-                    me.back = 1; me.bu = cur.u; me.bh = cur.h;
+                    me.flags |= kBack; me.bu = cur.u; me.bh = cur.h;
                     const uint32_t tiles = tiles_of(cur.rows), done = (cur.rows - cur.left) / kTile;
-                    me.blocks = cut.per ? (tiles + cut.per - 1) / cut.per : (w0 + i - done + tiles - 1) / cut.share - blockIdx.x + 1;
+                    if (A.cut_heads) me.blocks = cut.per ? (tiles + cut.per - 1) / cut.per : (w0 + i - done + tiles - 1) / cut.share - blockIdx.x + 1;
                     put_record<D>(reinterpret_cast<float *>(ring), o, ref, sum);       // (no copy is on its way any more)
                 }
                 fresh = true;
@@ -589,53 +612,52 @@ __global__ void __launch_bounds__(kAttnThreads, kBlocks) nibble_attention_kernel
     int4 note = make_int4(0, 0, 0, 0);
     if (x1 > x0) {
         // Heads that several warps had part in: a chain of records, from a back, or from the block's first front, on to the front that ends.  A thread has
-        // four channels of a query head, and all their records on their way at once.
+        // eight channels of a query head, and all their records on their way at once.
+        const int flags = lane < kWarps ? meta[lane].flags : 0;
+        const uint32_t fronts = __ballot_sync(0xFFFFFFFFu, flags & kFront), ending = __ballot_sync(0xFFFFFFFFu, flags & kEnds),
+                       backs = __ballot_sync(0xFFFFFFFFu, flags & kBack);
 #pragma unroll 1
-        for (int first = 0; first < kWarps; ++first) {
-            const bool open = first == 0 && meta[0].front != 0;      // the block's first head began in a block before
-#pragma unroll 1
-            for (int kind = open ? 0 : 1; kind < 2; ++kind) {
-                if (kind == 1 && !meta[first].back) continue;
-                const int u = kind == 0 ? meta[first].fu : meta[first].bu, h = kind == 0 ? meta[first].fh : meta[first].bh;
-                int end = kind == 0 ? first : first + 1;             // records: of warp `first`, then the fronts of those up to `end`
-                bool ends = false;
-#pragma unroll 1
-                while (!ends && end < kWarps && meta[end].front) ends = meta[end++].ends;
-                const bool whole = kind == 1 && ends;
-                if (kind == 1 && !ends) note = make_int4(u, h * A.G, meta[first].blocks, A.G);      // (it goes on in the next block)
-#pragma unroll 1
-                for (int item = threadIdx.x; item < A.G * (D / 4); item += kAttnThreads) {
-                    const int g = item / (D / 4), d = item % (D / 4) * 4;
-                    float tops[kWarps], sums[kWarps], top = kLowest, sum = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
-                    float4 part[kWarps];
+        for (uint32_t starts = (fronts & 1u) | backs << 1; starts; starts &= starts - 1u) {
+            const int from = __ffs(starts) - 1, back = from - 1;     // the chain's first front; the warp that has its back, -1: none, it began in a block before
+            const int end = from + __ffs((~fronts | (ending << 1 & ~1u << from)) >> from) - 1;      // fronts: of warps from, ..., end - 1
+            const bool ends = end > from && (ending >> (end - 1) & 1u);
+            const int u = back < 0 ? meta[0].fu : meta[back].bu, h = back < 0 ? meta[0].fh : meta[back].bh;
+            if (back >= 0 && !ends) note = make_int4(u, h * A.G, meta[back].blocks, A.G);            // (it goes on in the next block)
+            const int g = threadIdx.x / (D / 8), d = threadIdx.x % (D / 8) * 8;
+            static_assert(kHeads * (D / 8) <= kAttnThreads, "eight channels a thread");
+            if (g >= A.G) continue;
+            float tops[kWarps], sums[kWarps], top = kLowest, sum = 0.f, x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            float4 part[kWarps][2];
 #pragma unroll
-                    for (int w = 0; w < kWarps; ++w) {
-                        const float *rec = reinterpret_cast<const float *>(kind == 1 && w == first ? smem + w * (3 * L::kHalf) : smem + L::kRecords + w * L::kRecord);
-                        const bool on = w >= first && w < end;
-                        tops[w] = on ? rec[kHeads * D + g] : kLowest;
-                        sums[w] = on ? rec[kHeads * (D + 1) + g] : 0.f;
-                        part[w] = on ? *reinterpret_cast<const float4 *>(rec + g * D + d) : make_float4(0.f, 0.f, 0.f, 0.f);
-                    }
+            for (int w = 0; w < kWarps; ++w) {
+                const float *rec = reinterpret_cast<const float *>(w == back ? smem + w * (3 * L::kHalf) : smem + L::kRecords + w * L::kRecord);
+                const bool on = w == back || (w >= from && w < end);
+                tops[w] = on ? rec[kHeads * D + g] : kLowest;
+                sums[w] = on ? rec[kHeads * (D + 1) + g] : 0.f;
 #pragma unroll
-                    for (int w = 0; w < kWarps; ++w) top = fmaxf(top, tops[w]);
+                for (int k = 0; k < 2; ++k) part[w][k] = on ? *reinterpret_cast<const float4 *>(rec + g * D + d + 4 * k) : make_float4(0.f, 0.f, 0.f, 0.f);
+            }
 #pragma unroll
-                    for (int w = 0; w < kWarps; ++w) {
-                        const float c = tc::ex2(tops[w] - top);
-                        sum = fmaf(sums[w], c, sum);
-                        x[0] = fmaf(part[w].x, c, x[0]); x[1] = fmaf(part[w].y, c, x[1]);
-                        x[2] = fmaf(part[w].z, c, x[2]); x[3] = fmaf(part[w].w, c, x[3]);
-                    }
-                    if (whole) {
-                        const float inverse = 1.f / sum;
+            for (int w = 0; w < kWarps; ++w) top = fmaxf(top, tops[w]);
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) x[k] *= inverse;
-                        put_four(static_cast<T *>(A.out) + ((int64_t)u * A.Hq + h * A.G + g) * D + d, x);
-                    } else {
-                        float *out = A.part + (int64_t)(2 * blockIdx.x + kind) * paged::record_floats(A.G, D);
-                        put_four(out + g * D + d, x);
-                        if (d == 0) { out[A.G * D + g] = top; out[A.G * (D + 1) + g] = sum; }
-                    }
+            for (int w = 0; w < kWarps; ++w) {
+                const float c = tc::ex2(tops[w] - top);
+                sum = fmaf(sums[w], c, sum);
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    x[4 * k] = fmaf(part[w][k].x, c, x[4 * k]); x[4 * k + 1] = fmaf(part[w][k].y, c, x[4 * k + 1]);
+                    x[4 * k + 2] = fmaf(part[w][k].z, c, x[4 * k + 2]); x[4 * k + 3] = fmaf(part[w][k].w, c, x[4 * k + 3]);
                 }
+            }
+            if (back >= 0 && ends) {
+                const float inverse = reciprocal(sum);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) x[k] *= inverse;
+                put_eight(static_cast<T *>(A.out) + ((int64_t)u * A.Hq + h * A.G + g) * D + d, x);
+            } else {
+                float *out = A.part + (int64_t)(2 * blockIdx.x + (back >= 0)) * paged::record_floats(A.G, D);
+                put_eight(out + g * D + d, x);
+                if (d == 0) { out[A.G * D + g] = top; out[A.G * (D + 1) + g] = sum; }
             }
         }
     }
