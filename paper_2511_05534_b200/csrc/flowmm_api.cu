@@ -1722,10 +1722,12 @@ NibblePlan nibble_plan(const flowmm_cache_params &p) {
     NibblePlan n;
     const int64_t heads = (int64_t)p.n_units * p.n_kv_heads, tiles = ((int64_t)p.max_pages * p.page_size + nibble::kTile - 1) / nibble::kTile;
     constexpr int64_t blocks = nibble::kBlocks * kScoreCtas;
-    n.joins = heads > blocks || tiles > nibble::kWholeTiles;
-    n.blocks = n.joins ? std::min(blocks, heads * tiles) : heads;
-    n.part = 256 + (n.joins ? align256((size_t)n.blocks * sizeof(int4)) : 0);
-    n.total = n.part + (n.joins ? align256((size_t)n.blocks * 2 * paged::record_floats(p.n_q_heads / p.n_kv_heads, p.head_dim) * sizeof(float)) : 0);
+    n.joins = heads <= blocks ? tiles > nibble::kWholeTiles : tiles > nibble::kPairTiles || heads > 2 * blocks || p.n_units > nibble::kMostSorted;
+    n.blocks = std::min(blocks, n.joins ? heads * tiles : heads);
+    // (room also where more units need none: it is not to shrink with their number)
+    const bool room = n.joins || tiles > nibble::kWholeTiles;
+    n.part = 256 + (room ? align256((size_t)n.blocks * sizeof(int4)) : 0);
+    n.total = n.part + (room ? align256((size_t)n.blocks * 2 * paged::record_floats(p.n_q_heads / p.n_kv_heads, p.head_dim) * sizeof(float)) : 0);
     return n;
 }
 

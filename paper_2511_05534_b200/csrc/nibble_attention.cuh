@@ -54,7 +54,11 @@ template <int D> struct Lay {
 // ---- how the work is shared out ------------------------------------------------------------------
 // The tiles of all heads stand in a line, by unit, head and key.  With at most as many heads as blocks a block has a range of one head, `per` tiles or what
 // remains of it; else an equal piece of the line.  A block's warps have equal parts of its tiles, one after the other.
-constexpr int kWholeTiles = 2 * kWarps, kJoinTiles = 2 * kWarps, kSwitchTiles = kWarps;
+// Where the table has room for few tiles no head is cut, and the second kernel, which joins what several blocks had part in, not launched: it takes 4 us.
+// A block has one head of kWholeTiles at most (one head of 1000 rows of four 9.4 us, cut 10.0; 128 heads of up to 1500 11.9 and 12.8; 16 heads of up to
+// 2000 15.6 and 11.0), or, of kMostSorted units, kPairTiles and twice as many heads as blocks at most, the i-th longest and the i-th last (64 units of up to
+// 1690 rows, 8 heads, 24.8, cut 29.4).
+constexpr int kWholeTiles = 24, kPairTiles = 32, kJoinTiles = 2 * kWarps, kSwitchTiles = kWarps, kMostSorted = 64;
 
 __device__ __forceinline__ int unit_rows(const AttnArgs &A, int u) {
     const int n = A.rows[u], most = A.max_pages << A.page_shift;
@@ -117,13 +121,56 @@ __device__ __forceinline__ Cut make_cut(const AttnArgs &A) {
 }
 // A tile of the head (u, h): the unit's rows, and those from the tile's first one on.
 struct Walk { int u, h, rows, left; };
-__device__ __forceinline__ void walk_on(const AttnArgs &A, Walk &w) {
+struct Head { int u, h, rows; };
+// On to the next tile; behind a block's first whole head comes its second one.
+__device__ __forceinline__ void walk_on(const AttnArgs &A, Walk &w, const Head &second) {
     if ((w.left -= kTile) > 0) return;
+    if (A.cut_heads == nullptr) {
+        w.u = second.u; w.h = second.h;
+        w.rows = w.left = second.rows;
+        return;
+    }
     if (++w.h >= A.Hkv) {
         w.h = 0;
         do { ++w.u; w.rows = w.u < A.U ? unit_rows(A, w.u) : 0; } while (w.rows == 0 && w.u < A.U);
     }
     w.left = w.rows;
+}
+// A block's two whole heads, rows zero where there is none.  A unit's place is the number of units with more tiles, or with as many and a lower
+// number, counted bit by bit over the warp: `same` are the units that are alike so far.
+__device__ __forceinline__ void two_heads(const AttnArgs &A, Head &first, Head &second) {
+    const int lane = lane_id();
+    int rows[2], place[2] = {0, 0};
+    uint32_t same[2][2] = {{~0u, ~0u}, {~0u, ~0u}};
+#pragma unroll
+    for (int i = 0; i < 2; ++i) rows[i] = lane + 32 * i < A.U ? unit_rows(A, lane + 32 * i) : 0;
+    const int tiles[2] = {tiles_of(rows[0]), tiles_of(rows[1])};
+    static_assert(kPairTiles < 64, "six bits");
+#pragma unroll
+    for (int b = 5; b >= 0; --b) {
+        const uint32_t has[2] = {__ballot_sync(0xFFFFFFFFu, tiles[0] >> b & 1), __ballot_sync(0xFFFFFFFFu, tiles[1] >> b & 1)};
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t turn = tiles[i] >> b & 1 ? 0u : ~0u;      // units with the bit are before one without it; then alike are those with the same
+            place[i] += __popc(same[i][0] & has[0] & turn) + __popc(same[i][1] & has[1] & turn);
+            same[i][0] &= has[0] ^ turn;
+            same[i][1] &= has[1] ^ turn;
+        }
+    }
+    place[0] += __popc(same[0][0] & lanemask_lt());
+    place[1] += __popc(same[1][0]) + __popc(same[1][1] & lanemask_lt());
+    auto find = [&](uint32_t number, Head &head) {
+        head = {0, 0, 0};
+        if (number >= (uint32_t)A.U * A.Hkv) return;
+        const int at = A.by_heads.div(number);
+        const uint32_t low = __ballot_sync(0xFFFFFFFFu, place[0] == at), high = __ballot_sync(0xFFFFFFFFu, place[1] == at);
+        const int owner = __ffs(low ? low : high) - 1;
+        head.u = low ? owner : owner + 32;
+        head.h = number - at * A.Hkv;
+        head.rows = __shfl_sync(0xFFFFFFFFu, low ? rows[0] : rows[1], owner);
+    };
+    find(blockIdx.x, first);
+    find(2 * gridDim.x - 1 - blockIdx.x, second);
 }
 // Where tile x is, x below c.all.
 __device__ __forceinline__ Walk walk_to(const AttnArgs &A, const Cut &c, uint32_t x) {
@@ -331,19 +378,24 @@ __global__ void __launch_bounds__(kAttnThreads, kBlocks) nibble_attention_kernel
                     put_four(static_cast<T *>(A.out) + (int64_t)u * A.Hq * D + 4 * i, zero);
                 }
     };
-    // No head is cut: block i has the i-th one, and the table is read together with the lengths.  Else the lengths say what the block has.
+    // No head is cut: block i has the i-th one, and the table is read together with the lengths, or two.  Else the lengths say what the block has.
     Cut cut;
     Walk cur;
+    Head whole, second = {0, 0, 0};
     uint32_t x0 = 0, x1;
     int ids = 0, ids_unit = -1, ids_base = 0;                        // 32 entries of the block table
     if (A.cut_heads == nullptr) {
-        cur.u = ids_unit = A.by_heads.div(blockIdx.x);
-        cur.h = blockIdx.x - cur.u * A.Hkv;
-        cur.rows = unit_rows(A, cur.u);
-        ids = lane < A.max_pages ? A.table[(int64_t)cur.u * A.max_pages + lane] : 0;
-        x1 = tiles_of(cur.rows);
-        if (lane >= (cur.rows + (1 << A.page_shift) - 1) >> A.page_shift) ids = 0;
-        if ((unsigned)ids >= (unsigned)A.n_pages) { report(A.status, kStatusIndex); ids = 0; }
+        if ((uint32_t)A.U * A.Hkv > gridDim.x) {
+            two_heads(A, whole, second);
+        } else {
+            whole.u = ids_unit = A.by_heads.div(blockIdx.x);
+            whole.h = blockIdx.x - whole.u * A.Hkv;
+            whole.rows = unit_rows(A, whole.u);
+            ids = lane < A.max_pages ? A.table[(int64_t)whole.u * A.max_pages + lane] : 0;
+            if (lane >= (whole.rows + (1 << A.page_shift) - 1) >> A.page_shift) ids = 0;
+            if ((unsigned)ids >= (unsigned)A.n_pages) { report(A.status, kStatusIndex); ids = 0; }
+        }
+        x1 = tiles_of(whole.rows) + tiles_of(second.rows);
     } else {
         cut = make_cut(A);
         block_piece(A, cut, x0, x1);
@@ -407,14 +459,19 @@ __global__ void __launch_bounds__(kAttnThreads, kBlocks) nibble_attention_kernel
             tc::copies_commit();
             put = put == 2 ? 0 : put + 1;
         };
-        if (A.cut_heads == nullptr) cur.left = cur.rows - (int)w0 * kTile;
-        else cur = walk_to(A, cut, w0);
+        if (A.cut_heads == nullptr) {
+            const int at = (int)w0 - tiles_of(whole.rows);            // in the second head
+            const Head &of = at < 0 ? whole : second;
+            cur = {of.u, of.h, of.rows, of.rows - (at < 0 ? (int)w0 : at) * kTile};
+        } else {
+            cur = walk_to(A, cut, w0);
+        }
         Walk far = cur;
         uint32_t take = 0;
         locate(far);
         issue(0, true);
         issue(1, true);
-        if (count > 1) { walk_on(A, far); locate(far); }
+        if (count > 1) { walk_on(A, far, second); locate(far); }
         issue(0, count > 1);
         aside();
         Queries<D, kTwo> Q;
@@ -571,7 +628,7 @@ __global__ void __launch_bounds__(kAttnThreads, kBlocks) nibble_attention_kernel
             }
             __syncwarp();
             take = take == 2 ? 0 : take + 1;
-            if (i + 2 < count) { walk_on(A, far); locate(far); }
+            if (i + 2 < count) { walk_on(A, far, second); locate(far); }
             issue(0, i + 2 < count);                                 // K of the tile after the next one, where this one's V was
             const bool last = cur.left <= kTile;
             if (last || i + 1 == count) {                            // the part ends
@@ -603,7 +660,7 @@ __global__ void __launch_bounds__(kAttnThreads, kBlocks) nibble_attention_kernel
                 }
                 fresh = true;
             }
-            walk_on(A, cur);
+            walk_on(A, cur, second);
         }
     }
     if (count == 0) aside();

@@ -401,3 +401,13 @@ def test_rows_read_back_can_be_compressed_again(U, H, B):
     F.flowmm_recompress(fp, q, k, v, torch.zeros((U, H, B), dtype=torch.uint8, device="cuda"), ko, vo, mo, wsr)
     assert F.flowmm_last_device_status(wsr) == 0 and F.flowmm_last_device_status(ws) == 0
     assert torch.isfinite(ko).all() and torch.isfinite(vo).all()
+
+
+@pytest.mark.parametrize("dtype", [F.BF16, F.F32])
+@pytest.mark.parametrize("U,H,most", [(64, 8, 1690), (64, 8, 2048), (37, 8, 64), (64, 5, 700), (40, 9, 1500), (38, 8, 1), (60, 8, 2049), (65, 8, 300)])
+def test_attention_of_two_whole_heads_a_block(dtype, U, H, most):
+    """More heads than blocks, twice as many at most, and on both sides of that: lengths that differ, that are all the same, and none."""
+    rng = np.random.default_rng(U + most)
+    rows = rng.integers(0, most + 1, U)
+    rows[rng.integers(0, U, U // 3)] = most
+    _check(rng, U, H, 2, 64, 64, rows, dtype, wide=(most + 63) // 64)

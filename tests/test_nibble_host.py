@@ -186,6 +186,6 @@ def test_workspace_never_shrinks(lib, D, dtype):
         for U in (1, 3, 40, 300):
             sizes = [size(U, wide, 64, G) for wide in range(1, 700)]
             assert sizes == sorted(sizes)
-        for wide in (1, 10, 500):
+        for wide in (1, 10, 95, 97, 110, 128, 129, 500):
             sizes = [size(U, wide, 16, G) for U in range(1, 700)]
             assert sizes == sorted(sizes)
