@@ -441,7 +441,7 @@ flowmm_status flowmm_nibble_attention(const flowmm_cache_params *p, const void *
  *   positions [U, n_axes, T] int32
  * rotary_dim is a multiple of 16 up to head_dim (0: head_dim).  n_axes is 1, or 3: then section[a] pairs go by position a, in order, R / 2 in all.
  * base at least 1, factor above 0, high above low, trained at least 0 are asked for where `scaling` uses them; amplitude 0 selects 1.
- * U * T is below 2^31.  No workspace: nothing on the device can fail.
+ * U * T is below 2^31, Hq + Hkv below 2^30.  No workspace: nothing on the device can fail.
  */
 typedef enum { FLOWMM_ROTARY_HALVES = 0,        /* channels i and i + R / 2 are pair i */
                FLOWMM_ROTARY_PAIRS = 1          /* channels 2 i and 2 i + 1 are pair i */

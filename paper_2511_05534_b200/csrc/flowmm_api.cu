@@ -1895,8 +1895,8 @@ flowmm_status validate_rotary(const flowmm_rotary_params *p) {
     if (p->scaling != FLOWMM_ROTARY_PLAIN && (!(p->factor > 0.0) || !isfinite(p->factor))) return FLOWMM_ERR_SHAPE;
     if (p->scaling == FLOWMM_ROTARY_BY_PARTS && (!(p->high > p->low) || !isfinite(p->high) || !isfinite(p->low) || p->trained < 0)) return FLOWMM_ERR_SHAPE;
     if (p->dtype != FLOWMM_F32 && p->dtype != FLOWMM_BF16) return FLOWMM_ERR_DTYPE;
-    const int64_t rows = (int64_t)p->n_units * p->n_rows;
-    if (rows >= (int64_t)1 << 31) return FLOWMM_ERR_SHAPE;
+    constexpr int64_t limit = (int64_t)1 << 31;
+    if ((int64_t)p->n_units * p->n_rows >= limit || (int64_t)p->n_q_heads + p->n_kv_heads >= limit / 2) return FLOWMM_ERR_SHAPE;
     return FLOWMM_OK;
 }
 

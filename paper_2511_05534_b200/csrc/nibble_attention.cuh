@@ -1,11 +1,11 @@
 // Decode attention over the paged 4-bit cache: one new query per query head, lengths of their own for every unit.
 //   o = sum_j softmax_j(scale * q . k_j) v_j,   k_j, v_j: rows of e2m1 codes times their groups' scales
 //
-// One pass over K and V with a running maximum and sum.  A row of 128 channels is 72 bytes of K and 72 of V for 4 G 128 flops: memory bounds long calls as long
-// as a row takes an SM no more than 6.3 clocks, so the products go to the tensor cores and codes are widened in registers, by warps that feed their own matrix
-// instructions (mma.sync, fp16 operands, fp32 sums): a code times its scale is an fp16 number exactly, one conversion and one packed product for two of
-// them.  (tcgen05 takes its operands from shared or tensor memory: 256 bytes a row written and read there again for the 72 that came, 4 and 4 clocks of
-// the 6.3; and e2m1 operands with scales of their own, which it takes as they are, would want queries and weights in 4 or 8 bits.)
+// One pass over K and V with a running maximum and sum.  A row of 128 channels is 72 bytes of K and 72 of V for 4 G 128 flops: memory has one for an SM every
+// 6.3 clocks.  The products go to the tensor cores, the codes are widened in registers, by warps that feed their own matrix instructions (mma.sync, fp16
+// operands, fp32 sums): a code times its scale is an fp16 number exactly, one conversion and one packed product for two of them.
+// (tcgen05 takes its operands from shared or tensor memory: 256 bytes a row written and read there for the 72 that came, 4 clocks of the 6.3; and e2m1 operands
+// with scales of their own, which it takes as they are, would want queries and weights in 4 or 8 bits.)
 //   S[key, head] = K Q^T:  16 keys on the wide side, eight query heads, the most there are, on the narrow one
 //   O^T[channel, head] = V^T W^T:  16 channels on the wide side; the weights go from the first product's layout to the second's by a transpose in registers
 // Which channel and which key stand at which place of an operand is free as long as both operands agree: a lane takes 16 neighbouring bytes of a K row and
@@ -13,6 +13,15 @@
 // bf16: a query is an fp16 number times a power of two exactly, a weight is rounded to fp16 (2^-12, where the output is rounded to 2^-9); fp32: both are the
 // sum of two fp16 numbers, each product is two.  The largest weight is 2^10 to 2^15 (fp32: 2^14), so that fp16 holds others to full precision down to 2^-24 of
 // it, and two of them to 2^-21 of themselves down to 2^-18 of it, both to 2^-35 (fp32: 2^-39) of it below.
+//
+// A warp works by itself: tiles of 64 rows come into its own ring of three half tiles (K and V in turn), 16 bytes a lane and copy, two ahead; it keeps the
+// maximum, the sum and the output of the head that it is at.  Twelve warps are on an SM, as many as 168 registers and 18 KB of shared memory each allow.
+// (32 rows a tile and sixteen warps of 128 registers spilled: 101 us where this took 84; ten warps 94.)  What it costs is instructions: 1000 for a tile of
+// 128 channels, of which 860 widen and multiply, so addresses are formed from one page number for a tile where pages have 64 rows (bulk copies by one thread
+// took 40 instructions each), and outputs are rescaled only where fp16 asks for it.
+// Measured: 16 sequences of up to 33 792 rows, 8 heads of 8 query heads, 386 MB, 80 us, 60 of memory: 5.5 TB/s while all blocks run, 6 us from the launch to the first
+// tile, and an end of 14 us in which blocks finish one after the other, since equal pieces take SMs 76 to 90 us.  64 sequences of up to 1690 rows, 74 MB, 24.8 us, 11.5
+// of memory.  One sequence of 218 rows 5.0 us: lengths and table 0.6, the first tile 0.9, its products 1.2, joining the warps' records 0.9, the launch.
 #pragma once
 #include <cuda_fp16.h>
 
@@ -53,7 +62,8 @@ template <int D> struct Lay {
 
 // ---- how the work is shared out ------------------------------------------------------------------
 // The tiles of all heads stand in a line, by unit, head and key.  With at most as many heads as blocks a block has a range of one head, `per` tiles or what
-// remains of it; else an equal piece of the line.  A block's warps have equal parts of its tiles, one after the other.
+// remains of it (ranges no longer than kSwitchTiles above an even share); else an equal piece of the line.  A block's warps have equal parts of its tiles, one
+// after the other.  Heads are not cut for a range kJoinTiles longer.
 // Where the table has room for few tiles no head is cut, and the second kernel, which joins what several blocks had part in, not launched: it takes 4 us.
 // A block has one head of kWholeTiles at most (one head of 1000 rows of four 9.4 us, cut 10.0; 128 heads of up to 1500 11.9 and 12.8; 16 heads of up to
 // 2000 15.6 and 11.0), or, of kMostSorted units, kPairTiles and twice as many heads as blocks at most, the i-th longest and the i-th last (64 units of up to
@@ -260,6 +270,11 @@ __device__ __forceinline__ uint32_t times(uint32_t a, uint32_t b) {
 __device__ __forceinline__ uint32_t times_one(uint32_t a, uint32_t b, int upper) {
     const __half2 x = *reinterpret_cast<const __half2 *>(&a), y = *reinterpret_cast<const __half2 *>(&b), z = __hmul2_rn(x, upper ? __high2half2(y) : __low2half2(y));
     return *reinterpret_cast<const uint32_t *>(&z);
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
 }
 __device__ __forceinline__ float max_over_rows(float x) {              // over the lanes with the same lane % 4
 #pragma unroll
@@ -544,12 +559,12 @@ __global__ void __launch_bounds__(kAttnThreads, kBlocks) nibble_attention_kernel
             float top[2] = {fmaxf(z[0][0], z[0][2]), fmaxf(z[0][1], z[0][3])};
 #pragma unroll
             for (int s = 1; s < kSubs; ++s) {
-                top[0] = fmaxf(top[0], fmaxf(z[s][0], z[s][2]));
-                top[1] = fmaxf(top[1], fmaxf(z[s][1], z[s][3]));
+                top[0] = max3(top[0], z[s][0], z[s][2]);
+                top[1] = max3(top[1], z[s][1], z[s][3]);
             }
-            top[0] = max_over_rows(top[0]);
-            top[1] = max_over_rows(top[1]);
             if (__any_sync(0xFFFFFFFFu, fmaf(top[0], Q.factor[0], -ref[0]) > kMostExponent || fmaf(top[1], Q.factor[1], -ref[1]) > kMostExponent)) {
+                top[0] = max_over_rows(top[0]);
+                top[1] = max_over_rows(top[1]);
                 float c[2];
 #pragma unroll
                 for (int q = 0; q < 2; ++q) {
