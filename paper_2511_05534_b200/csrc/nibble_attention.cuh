@@ -116,7 +116,7 @@ __device__ __forceinline__ Cut make_cut(const AttnArgs &A) {
     if (heads > blocks) return c;
     const uint32_t whole = max(1, longest);
 #pragma unroll 1
-    for (uint32_t per = c.share; per <= c.share + kSwitchTiles || per == whole; ++per) {
+    for (uint32_t per = c.share; per <= c.share + kSwitchTiles || per == whole; per += 2) {
         if (whole <= kWholeTiles || whole <= per + kJoinTiles) per = whole;
         uint32_t n = 0;
 #pragma unroll 1
