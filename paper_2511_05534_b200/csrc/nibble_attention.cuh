@@ -68,7 +68,7 @@ template <int D> struct Lay {
 // A block has one head of kWholeTiles at most (one head of 1000 rows of four 9.4 us, cut 10.0; 128 heads of up to 1500 11.9 and 12.8; 16 heads of up to
 // 2000 15.6 and 11.0), or, of kMostSorted units, kPairTiles and twice as many heads as blocks at most, the i-th longest and the i-th last (64 units of up to
 // 1690 rows, 8 heads, 24.8, cut 29.4).
-constexpr int kWholeTiles = 24, kPairTiles = 32, kJoinTiles = 2 * kWarps, kSwitchTiles = kWarps, kMostSorted = 64;
+constexpr int kWholeTiles = 24, kPairTiles = 32, kJoinTiles = 2 * kWarps, kSwitchTiles = kWarps, kMostSorted = 160;
 
 __device__ __forceinline__ int unit_rows(const AttnArgs &A, int u) {
     const int n = A.rows[u], most = A.max_pages << A.page_shift;
@@ -146,38 +146,53 @@ __device__ __forceinline__ void walk_on(const AttnArgs &A, Walk &w, const Head &
     }
     w.left = w.rows;
 }
-// A block's two whole heads, rows zero where there is none.  A unit's place is the number of units with more tiles, or with as many and a lower
-// number, counted bit by bit over the warp: `same` are the units that are alike so far.
+// A block's two whole heads, rows zero where there is none; kEach units a lane.  A unit's place is the number of units with more tiles, or with as many and a
+// lower number, counted bit by bit over the warp: `same` are the units that are alike so far.
+template <int kEach>
 __device__ __forceinline__ void two_heads(const AttnArgs &A, Head &first, Head &second) {
     const int lane = lane_id();
-    int rows[2], place[2] = {0, 0};
-    uint32_t same[2][2] = {{~0u, ~0u}, {~0u, ~0u}};
+    int rows[kEach], place[kEach];
+    uint32_t same[kEach][kEach];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) rows[i] = lane + 32 * i < A.U ? unit_rows(A, lane + 32 * i) : 0;
-    const int tiles[2] = {tiles_of(rows[0]), tiles_of(rows[1])};
+    for (int i = 0; i < kEach; ++i) {
+        rows[i] = lane + 32 * i < A.U ? unit_rows(A, lane + 32 * i) : 0;
+        place[i] = 0;
+#pragma unroll
+        for (int k = 0; k < kEach; ++k) same[i][k] = ~0u;
+    }
     static_assert(kPairTiles < 64, "six bits");
-#pragma unroll
+#pragma unroll 1
     for (int b = 5; b >= 0; --b) {
-        const uint32_t has[2] = {__ballot_sync(0xFFFFFFFFu, tiles[0] >> b & 1), __ballot_sync(0xFFFFFFFFu, tiles[1] >> b & 1)};
+        uint32_t has[kEach];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const uint32_t turn = tiles[i] >> b & 1 ? 0u : ~0u;      // units with the bit are before one without it; then alike are those with the same
-            place[i] += __popc(same[i][0] & has[0] & turn) + __popc(same[i][1] & has[1] & turn);
-            same[i][0] &= has[0] ^ turn;
-            same[i][1] &= has[1] ^ turn;
+        for (int k = 0; k < kEach; ++k) has[k] = __ballot_sync(0xFFFFFFFFu, tiles_of(rows[k]) >> b & 1);
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const uint32_t turn = tiles_of(rows[i]) >> b & 1 ? 0u : ~0u;      // units with the bit are before one without it; then alike are those with the same
+#pragma unroll
+            for (int k = 0; k < kEach; ++k) {
+                place[i] += __popc(same[i][k] & has[k] & turn);
+                same[i][k] &= has[k] ^ turn;
+            }
         }
     }
-    place[0] += __popc(same[0][0] & lanemask_lt());
-    place[1] += __popc(same[1][0]) + __popc(same[1][1] & lanemask_lt());
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+#pragma unroll
+        for (int k = 0; k < i; ++k) place[i] += __popc(same[i][k]);
+        place[i] += __popc(same[i][i] & lanemask_lt());
+    }
     auto find = [&](uint32_t number, Head &head) {
         head = {0, 0, 0};
         if (number >= (uint32_t)A.U * A.Hkv) return;
         const int at = A.by_heads.div(number);
-        const uint32_t low = __ballot_sync(0xFFFFFFFFu, place[0] == at), high = __ballot_sync(0xFFFFFFFFu, place[1] == at);
-        const int owner = __ffs(low ? low : high) - 1;
-        head.u = low ? owner : owner + 32;
         head.h = number - at * A.Hkv;
-        head.rows = __shfl_sync(0xFFFFFFFFu, low ? rows[0] : rows[1], owner);
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const uint32_t here = __ballot_sync(0xFFFFFFFFu, place[i] == at);
+            const int owner = __ffs(here) - 1, n = __shfl_sync(0xFFFFFFFFu, rows[i], owner & 31);
+            if (here) { head.u = owner + 32 * i; head.rows = n; }
+        }
     };
     find(blockIdx.x, first);
     find(2 * gridDim.x - 1 - blockIdx.x, second);
@@ -401,7 +416,8 @@ __global__ void __launch_bounds__(kAttnThreads, kBlocks) nibble_attention_kernel
     int ids = 0, ids_unit = -1, ids_base = 0;                        // 32 entries of the block table
     if (A.cut_heads == nullptr) {
         if ((uint32_t)A.U * A.Hkv > gridDim.x) {
-            two_heads(A, whole, second);
+            if (A.U <= 64) two_heads<2>(A, whole, second);
+            else two_heads<kMostSorted / 32>(A, whole, second);
         } else {
             whole.u = ids_unit = A.by_heads.div(blockIdx.x);
             whole.h = blockIdx.x - whole.u * A.Hkv;

@@ -404,7 +404,8 @@ def test_rows_read_back_can_be_compressed_again(U, H, B):
 
 
 @pytest.mark.parametrize("dtype", [F.BF16, F.F32])
-@pytest.mark.parametrize("U,H,most", [(64, 8, 1690), (64, 8, 2048), (37, 8, 64), (64, 5, 700), (40, 9, 1500), (38, 8, 1), (60, 8, 2049), (65, 8, 300)])
+@pytest.mark.parametrize("U,H,most", [(64, 8, 1690), (64, 8, 2048), (37, 8, 64), (64, 5, 700), (40, 9, 1500), (38, 8, 1), (60, 8, 2049), (65, 8, 300),
+                                        (128, 4, 900), (160, 3, 500), (161, 3, 100), (148, 4, 64)])
 def test_attention_of_two_whole_heads_a_block(dtype, U, H, most):
     """More heads than blocks, twice as many at most, and on both sides of that: lengths that differ, that are all the same, and none."""
     rng = np.random.default_rng(U + most)
