@@ -1713,7 +1713,7 @@ namespace {
 
 // The attention's scratch: [status word, 256 bytes][cut heads][records], the last two where a head may be cut.
 struct NibblePlan {
-    bool joins;
+    nibble::Share share;
     int64_t blocks;
     size_t part, total;
 };
@@ -1722,10 +1722,12 @@ NibblePlan nibble_plan(const flowmm_cache_params &p) {
     NibblePlan n;
     const int64_t heads = (int64_t)p.n_units * p.n_kv_heads, tiles = ((int64_t)p.max_pages * p.page_size + nibble::kTile - 1) / nibble::kTile;
     constexpr int64_t blocks = nibble::kBlocks * kScoreCtas;
-    n.joins = heads <= blocks ? tiles > nibble::kWholeTiles : tiles > nibble::kPairTiles || heads > 2 * blocks || p.n_units > nibble::kMostSorted;
-    n.blocks = std::min(blocks, n.joins ? heads * tiles : heads);
+    if (heads <= blocks) n.share = tiles <= nibble::kWholeTiles ? nibble::kOneHead : nibble::kCutHeads;
+    else if (tiles <= nibble::kPairTiles && heads <= 2 * blocks && p.n_units <= nibble::kMostSorted) n.share = nibble::kTwoHeads;
+    else n.share = tiles <= nibble::kLineTiles ? nibble::kHeadsInLine : nibble::kCutHeads;
+    n.blocks = std::min(blocks, n.share == nibble::kCutHeads ? heads * tiles : heads);
     // (room also where more units need none: it is not to shrink with their number)
-    const bool room = n.joins || tiles > nibble::kWholeTiles;
+    const bool room = n.share == nibble::kCutHeads || tiles > nibble::kLineTiles;
     n.part = 256 + (room ? align256((size_t)n.blocks * sizeof(int4)) : 0);
     n.total = n.part + (room ? align256((size_t)n.blocks * 2 * paged::record_floats(p.n_q_heads / p.n_kv_heads, p.head_dim) * sizeof(float)) : 0);
     return n;
@@ -1766,7 +1768,7 @@ flowmm_status launch_nibble_attention(const nibble::AttnArgs &a, const NibblePla
         return FLOWMM_ERR_CUDA;
     launch(kernel, (unsigned)n.blocks, nibble::kAttnThreads, nibble::Lay<D>::kBytes, st, a);
     FLOWMM_LAUNCHED("nibble_attention");
-    if (!n.joins) return FLOWMM_OK;
+    if (n.share != nibble::kCutHeads) return FLOWMM_OK;
     paged::AttnArgs j = {};
     j.out = static_cast<float *>(a.out); j.part = a.part; j.cut_heads = a.cut_heads; j.Hq = a.Hq;
     const int record = paged::record_floats(a.G, D);
@@ -1862,7 +1864,7 @@ extern "C" flowmm_status flowmm_nibble_attention(const flowmm_cache_params *p, c
     a.q = q; a.pages[0] = static_cast<const uint8_t *>(k_pages); a.pages[1] = static_cast<const uint8_t *>(v_pages);
     a.scale[0] = static_cast<const uint8_t *>(k_scale); a.scale[1] = static_cast<const uint8_t *>(v_scale);
     a.table = block_table; a.rows = rows; a.out = out; a.status = static_cast<int *>(ws);
-    a.part = at<float>(ws, n.part); a.cut_heads = n.joins ? at<int4>(ws, 256) : nullptr;
+    a.part = at<float>(ws, n.part); a.cut_heads = n.share == nibble::kCutHeads ? at<int4>(ws, 256) : nullptr; a.share = n.share;
     a.U = p->n_units; a.Hq = p->n_q_heads; a.Hkv = p->n_kv_heads; a.G = p->n_q_heads / p->n_kv_heads;
     a.page_shift = page_shift(p->page_size); a.n_pages = p->n_pages; a.max_pages = p->max_pages; a.by_heads = make_fastdiv(p->n_kv_heads);
     a.scale_log2 = (p->softmax_scale != 0.f ? p->softmax_scale : 1.f / sqrtf((float)p->head_dim)) * kLog2e;

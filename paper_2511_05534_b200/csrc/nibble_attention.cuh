@@ -40,13 +40,15 @@ struct AttnArgs {
     const int *table, *rows;           // [U, max_pages], [U]
     void *out;                         // [U, Hq, D]
     float *part;                       // two records a block (paged::record_floats)
-    int4 *cut_heads;                   // [blocks], as paged::AttnArgs has it, or null: no head is cut, a block for each
+    int4 *cut_heads;                   // [blocks], as paged::AttnArgs has it; null: no head is cut
     int *status;
+    int share;                         // Share
     int U, Hq, Hkv, G, page_shift, n_pages, max_pages;
     float scale_log2;
     FastDiv by_heads;                  // by Hkv
 };
 
+enum Share { kOneHead, kTwoHeads, kHeadsInLine, kCutHeads };          // what a block has
 constexpr int kTile = 64, kWarps = 6, kBlocks = 2, kAttnThreads = kWarps * 32, kHeads = 8;      // blocks of an SM
 constexpr float kLowest = paged::kLowest;
 // Weights are 2^(logit - reference): the reference is set 10 below the maximum (log2; 14 for fp32 rows) and set again only when a weight would be above 2^15.
@@ -65,10 +67,11 @@ template <int D> struct Lay {
 // remains of it (ranges no longer than kSwitchTiles above an even share); else an equal piece of the line.  A block's warps have equal parts of its tiles, one
 // after the other.  Heads are not cut for a range kJoinTiles longer.
 // Where the table has room for few tiles no head is cut, and the second kernel, which joins what several blocks had part in, not launched: it takes 4 us.
-// A block has one head of kWholeTiles at most (one head of 1000 rows of four 9.4 us, cut 10.0; 128 heads of up to 1500 11.9 and 12.8; 16 heads of up to
-// 2000 15.6 and 11.0), or, of kMostSorted units, kPairTiles and twice as many heads as blocks at most, the i-th longest and the i-th last (64 units of up to
-// 1690 rows, 8 heads, 24.8, cut 29.4).
-constexpr int kWholeTiles = 24, kPairTiles = 32, kJoinTiles = 2 * kWarps, kSwitchTiles = kWarps, kMostSorted = 160;
+// kOneHead: one head of kWholeTiles at most (one head of 1000 rows of four 9.4 us, cut 10.0; 128 heads of up to 1500 11.9 and 12.8; 16 heads of up to 2000
+// 15.6 and 11.0).  kTwoHeads: the i-th longest and the i-th last, of kMostSorted units, kPairTiles and twice as many heads as blocks at most (64 units of up to
+// 1690 rows, 8 heads, 24.8, cut 29.4).  kHeadsInLine: more heads, of kLineTiles at most; a block has those that begin in its piece (320 units of up to 100 rows, 8
+// heads, 18.2, cut 19.8).
+constexpr int kWholeTiles = 24, kPairTiles = 32, kJoinTiles = 2 * kWarps, kSwitchTiles = kWarps, kMostSorted = 160, kLineTiles = 8;
 
 __device__ __forceinline__ int unit_rows(const AttnArgs &A, int u) {
     const int n = A.rows[u], most = A.max_pages << A.page_shift;
@@ -135,7 +138,7 @@ struct Head { int u, h, rows; };
 // On to the next tile; behind a block's first whole head comes its second one.
 __device__ __forceinline__ void walk_on(const AttnArgs &A, Walk &w, const Head &second) {
     if ((w.left -= kTile) > 0) return;
-    if (A.cut_heads == nullptr) {
+    if (A.share == kTwoHeads) {
         w.u = second.u; w.h = second.h;
         w.rows = w.left = second.rows;
         return;
@@ -227,6 +230,16 @@ __device__ __forceinline__ void block_piece(const AttnArgs &A, const Cut &c, uin
     if (c.per == 0) {
         x0 = min(c.all, blockIdx.x * c.share);
         x1 = min(c.all, x0 + c.share);
+        if (A.share == kHeadsInLine) {
+            auto head = [&](uint32_t x) {                            // the first head's tile from x on
+                if (x >= c.all) return x;
+                const Walk w = walk_to(A, c, x);
+                const int done = (w.rows - w.left) / kTile;
+                return done ? x + tiles_of(w.rows) - done : x;
+            };
+            x0 = head(x0);
+            x1 = head(x1);
+        }
         return;
     }
     // ranges are numbered by unit, head and key
@@ -408,14 +421,14 @@ __global__ void __launch_bounds__(kAttnThreads, kBlocks) nibble_attention_kernel
                     put_four(static_cast<T *>(A.out) + (int64_t)u * A.Hq * D + 4 * i, zero);
                 }
     };
-    // No head is cut: block i has the i-th one, and the table is read together with the lengths, or two.  Else the lengths say what the block has.
+    // One head: the table is read together with the length.  Two, or a piece of the line: the lengths say what the block has.
     Cut cut;
     Walk cur;
     Head whole, second = {0, 0, 0};
     uint32_t x0 = 0, x1;
     int ids = 0, ids_unit = -1, ids_base = 0;                        // 32 entries of the block table
-    if (A.cut_heads == nullptr) {
-        if ((uint32_t)A.U * A.Hkv > gridDim.x) {
+    if (A.share <= kTwoHeads) {
+        if (A.share == kTwoHeads) {
             if (A.U <= 64) two_heads<2>(A, whole, second);
             else two_heads<kMostSorted / 32>(A, whole, second);
         } else {
@@ -490,7 +503,7 @@ __global__ void __launch_bounds__(kAttnThreads, kBlocks) nibble_attention_kernel
             tc::copies_commit();
             put = put == 2 ? 0 : put + 1;
         };
-        if (A.cut_heads == nullptr) {
+        if (A.share <= kTwoHeads) {
             const int at = (int)w0 - tiles_of(whole.rows);            // in the second head
             const Head &of = at < 0 ? whole : second;
             cur = {of.u, of.h, of.rows, of.rows - (at < 0 ? (int)w0 : at) * kTile};
@@ -686,7 +699,7 @@ __global__ void __launch_bounds__(kAttnThreads, kBlocks) nibble_attention_kernel
                 } else {
                     me.flags |= kBack; me.bu = cur.u; me.bh = cur.h;
                     const uint32_t tiles = tiles_of(cur.rows), done = (cur.rows - cur.left) / kTile;
-                    if (A.cut_heads) me.blocks = cut.per ? (tiles + cut.per - 1) / cut.per : (w0 + i - done + tiles - 1) / cut.share - blockIdx.x + 1;
+                    if (A.share == kCutHeads) me.blocks = cut.per ? (tiles + cut.per - 1) / cut.per : (w0 + i - done + tiles - 1) / cut.share - blockIdx.x + 1;
                     put_record<D>(reinterpret_cast<float *>(ring), o, ref, sum);       // (no copy is on its way any more)
                 }
                 fresh = true;

@@ -412,3 +412,14 @@ def test_attention_of_two_whole_heads_a_block(dtype, U, H, most):
     rows = rng.integers(0, most + 1, U)
     rows[rng.integers(0, U, U // 3)] = most
     _check(rng, U, H, 2, 64, 64, rows, dtype, wide=(most + 63) // 64)
+
+
+@pytest.mark.parametrize("dtype", [F.BF16, F.F32])
+@pytest.mark.parametrize("U,H,most", [(320, 8, 100), (200, 4, 512), (200, 4, 513), (700, 1, 64), (75, 8, 512), (1000, 2, 1), (90, 16, 130)])
+def test_attention_of_many_short_heads(dtype, U, H, most):
+    """More heads than two for a block: whole ones of a line that is cut between heads, of up to eight tiles, and cut ones beyond."""
+    rng = np.random.default_rng(U + most)
+    rows = rng.integers(0, most + 1, U)
+    rows[rng.integers(0, U, U // 3)] = most
+    rows[rng.integers(0, U, U // 9)] = 0
+    _check(rng, U, H, 2, 64, 16, rows, dtype, wide=(most + 15) // 16)
