@@ -423,3 +423,76 @@ def test_attention_of_many_short_heads(dtype, U, H, most):
     rows[rng.integers(0, U, U // 3)] = most
     rows[rng.integers(0, U, U // 9)] = 0
     _check(rng, U, H, 2, 64, 16, rows, dtype, wide=(most + 15) // 16)
+
+
+@pytest.mark.parametrize("dtype", [F.BF16, F.F32])
+@pytest.mark.parametrize("U,H,wide", [(3, 2, 4), (3, 2, 100), (64, 8, 20), (400, 2, 3), (400, 2, 40)])
+def test_attention_of_units_without_rows(dtype, U, H, wide):
+    """No unit has any, and one has."""
+    rng = np.random.default_rng(U + wide)
+    for some in (0, 1):
+        rows = np.zeros(U, np.int32)
+        rows[U - 1] = some * wide * 64
+        got = _check(rng, U, H, 3, 128, 64, rows, dtype, wide=wide)
+        assert (got[:U - 1] == 0).all() and (got[U - 1] != 0).any() == bool(some)
+
+
+@pytest.mark.parametrize("dtype", [F.BF16, F.F32])
+def test_attention_over_the_smallest_scales(dtype):
+    """Scales that no store writes: the steps below fp16's least normal number, and zero."""
+    rng = np.random.default_rng(51)
+    _check(rng, 2, 2, 4, 128, 64, [300, 129], dtype, scales=(0, 12), q=2.0 ** 14 * rng.standard_normal((2, 8, 128)))
+
+
+@pytest.mark.parametrize("dtype", [F.BF16, F.F32])
+def test_pools_beyond_32_bits(dtype):
+    """Pages whose bytes lie more than 2^32 behind the pool's first ones: stored, read back and attended to."""
+    rng = np.random.default_rng(61)
+    U, H, D, page, n, n_pages = 2, 8, 128, 128, 300, 70000
+    table = (n_pages - 1 - rng.permutation(6)).reshape(U, 3).astype(np.int32)
+    table[0, 0] = 1
+    slots = np.stack([table[u, np.arange(n) // page] * page + np.arange(n) % page for u in range(U)]).astype(np.int32)
+    x = [rows_like_a_cache(rng, (U, H, n, D), dtype) for _ in "kv"]
+    p = T.params(U, H, H, D, page, n_pages, 3, n, dtype=dtype)
+    pool = [torch.empty((n_pages, H, page, D // w), dtype=torch.uint8, device="cuda") for w in (2, 2, 16, 16)]
+    assert pool[0].numel() > 1 << 32
+    ws, t, r = F.alloc_nibble_workspace(p), T.dev(table), T.dev(np.full(U, n, np.int32))
+    F.flowmm_nibble_store(p, *(T.dev(v, dtype) for v in x), T.dev(slots), *pool, ws)
+    back = [torch.empty((U, H, n, D), device="cuda", dtype=F.torch_dtype(dtype)) for _ in "kv"]
+    F.flowmm_nibble_load(p, *pool, t, r, *back, ws)
+    q = rounded(rng.standard_normal((U, H, D)), dtype)
+    out = torch.empty((U, H, D), device="cuda", dtype=F.torch_dtype(dtype))
+    F.flowmm_nibble_attention(p, T.dev(q, dtype), *pool, t, r, out, ws)
+    assert F.flowmm_last_device_status(ws) == 0
+    low = [b[torch.from_numpy(table.ravel()).long().cuda()].cpu().numpy() for b in pool]
+    near = np.arange(6, dtype=np.int32).reshape(U, 3)
+    for i in range(2):
+        codes, scale = N.quantise(x[i])
+        assert np.array_equal(back[i].double().cpu().numpy(), N.E2M1[codes] * np.repeat(N.SCALE[scale], 16, -1))
+    want, size, logits = N.attention(q, low, near, np.full(U, n))
+    assert (np.abs(out.double().cpu().numpy() - want) <= T.attention_bound(want, size, logits, n, D, dtype)).all()
+
+
+def test_two_calls_at_once():
+    """Two streams, a workspace each, the same pages: each gives what it gives alone; a call in between on a third changes nothing."""
+    rng = np.random.default_rng(71)
+    U, H, G, D, page = 6, 4, 8, 128, 32
+    rows = rng.integers(1, 4000, U).astype(np.int32)
+    table, n_pages = T.random_table(rng, rows, page)
+    pool = [T.dev(x) for x in T.random_pool(rng, n_pages, H, page, D, rows, table)]
+    p = T.params(U, H * G, H, D, page, n_pages, table.shape[1])
+    t, r = T.dev(table), T.dev(rows)
+    q = [T.dev(rng.standard_normal((U, H * G, D)), F.BF16) for _ in range(3)]
+    ws = [F.alloc_nibble_workspace(p) for _ in q]
+    alone = [torch.empty_like(x) for x in q]
+    for x, o, w in zip(q, alone, ws):
+        F.flowmm_nibble_attention(p, x, *pool, t, r, o, w)
+    torch.cuda.synchronize()
+    streams, outs = [torch.cuda.Stream() for _ in q], [torch.empty_like(x) for x in q]
+    for _ in range(20):
+        for x, o, w, s in zip(q, outs, ws, streams):
+            with torch.cuda.stream(s):
+                F.flowmm_nibble_attention(p, x, *pool, t, r, o, w)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(alone, outs))
+    assert [F.flowmm_last_device_status(w) for w in ws] == [0, 0, 0]
