@@ -496,3 +496,35 @@ def test_two_calls_at_once():
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(alone, outs))
     assert [F.flowmm_last_device_status(w) for w in ws] == [0, 0, 0]
+
+
+def test_two_graphs_share_a_workspace():
+    """Calls of different units, lengths and ways of sharing the work out, replayed in turn on one workspace."""
+    rng = np.random.default_rng(81)
+    shapes = [(2, 8, 8, 6000), (64, 8, 4, 1500), (3, 4, 7, 200), (200, 4, 2, 300), (90, 8, 2, 2500)]
+    calls = []
+    for U, H, G, most in shapes:
+        rows = rng.integers(0, most + 1, U).astype(np.int32)
+        table, n_pages = T.random_table(rng, rows, 64, wide=(most + 63) // 64)
+        pool = [T.dev(x) for x in T.random_pool(rng, n_pages, H, 64, 64, rows, table)]
+        p = T.params(U, H * G, H, 64, 64, n_pages, table.shape[1])
+        q = T.dev(rng.standard_normal((U, H * G, 64)), F.BF16)
+        calls.append((p, q, pool, T.dev(table), T.dev(rows), torch.empty_like(q)))
+    ws = max((F.alloc_nibble_workspace(c[0]) for c in calls), key=torch.Tensor.numel)
+    graphs, want = [], []
+    for p, q, pool, t, r, out in calls:
+        F.flowmm_nibble_attention(p, q, *pool, t, r, out, F.alloc_nibble_workspace(p))
+        torch.cuda.synchronize()
+        want.append(out.clone())
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            F.flowmm_nibble_attention(p, q, *pool, t, r, out, ws)
+        graphs.append(graph)
+    for order in (range(5), (4, 0, 3, 0, 1, 2), (2, 1, 0, 4, 3)):
+        for c in calls:
+            c[5].fill_(7.0)
+        for i in order:
+            graphs[i].replay()
+        torch.cuda.synchronize()
+        assert F.flowmm_last_device_status(ws) == 0
+        assert all(torch.equal(calls[i][5], want[i]) for i in order)

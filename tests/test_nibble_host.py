@@ -189,3 +189,15 @@ def test_workspace_never_shrinks(lib, D, dtype):
         for wide in (1, 10, 95, 97, 110, 128, 129, 500):
             sizes = [size(U, wide, 16, G) for U in range(1, 700)]
             assert sizes == sorted(sizes)
+
+
+def test_rotary_params_can_be_copied_and_pickled():
+    """Also with the handle of a call in them, which is an address of this process and gone when a field changes."""
+    import copy
+    import pickle
+    p = F.RotaryParams(**ROTARY, sections=[16, 24, 24], scaling=F.ROTARY_BY_PARTS, factor=4.0, trained=100, adjoint=True, amplitude=1.5)
+    p.calls["flowmm_rotary"] = object()
+    for q in (copy.copy(p), copy.deepcopy(p), pickle.loads(pickle.dumps(p))):
+        assert q == p and q.calls == {} and q.sections == (16, 24, 24) and bytes(q.c()) == bytes(p.c())
+    p.base = 5.0
+    assert p.calls == {} and p.c().base == 5.0
