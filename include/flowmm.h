@@ -417,7 +417,7 @@ flowmm_status flowmm_nibble_load(const flowmm_cache_params *p, const void *k_pag
 /*
  * flowmm_decode_attention over the paged 4-bit cache: o = softmax(scale * q . K^T) V over the rows[u] rows of each unit, zero for a unit without rows.  What
  * stands behind a unit's last row (scales of NaN too) has no influence.  Several new queries of a sequence are units that share a row of the block table
- * and differ in rows.
+ * and differ in rows.  Logits may be as large as fp32 holds them (2^127 in units of log 2; beyond, outputs may be NaN).
  *   q, out [U, Hq, D] dense, element type `dtype`
  */
 flowmm_status flowmm_nibble_attention(const flowmm_cache_params *p, const void *q, const void *k_pages, const void *v_pages,

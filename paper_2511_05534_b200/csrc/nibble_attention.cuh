@@ -52,7 +52,9 @@ struct AttnArgs {
 enum Share { kOneHead, kTwoHeads, kHeadsInLine, kCutHeads };          // what a block has
 constexpr int kTile = 64, kWarps = 6, kBlocks = 2, kAttnThreads = kWarps * 32, kHeads = 8;      // blocks of an SM
 constexpr float kLowest = paged::kLowest;
-// Weights are 2^(logit - reference): the reference is set 10 below the maximum (log2; 14 for fp32 rows) and set again only when a weight would be above 2^15.
+// Weights are 2^(10 + (product - reference) factor) (fp32 rows: 14): the reference is a maximum of the products q . k as they come from the matrix instructions, and set
+// again only when a weight would be above 2^15.  Differences are formed before they are scaled, so the largest product's weight is 2^10 however large the logits are
+// (2^(logit - reference) by one multiply-add lost it where a step of fp32 at the logit is above 10: zeros and NaN from 2^28 on).
 constexpr float kMostExponent = 15.f;
 
 // What a warp has in shared memory: three half tiles (64 rows of K or of V: codes, then scales), K and V in turn, and a record.
@@ -520,8 +522,8 @@ __global__ void __launch_bounds__(kAttnThreads, kBlocks) nibble_attention_kernel
         issue(0, count > 1);
         aside();
         Queries<D, kTwo> Q;
-        float o[D / 16][4], ref[2];
-        float2 l;                                                    // sums of weights, of this lane's keys
+        float o[D / 16][4];
+        float2 l, minus;                                             // sums of weights, of this lane's keys; the references, their signs turned
         bool fresh = true;                                           // a part of a head begins
         bool begins = true;                                          // ... with the head's first row
         for (int i = 0; i < count; ++i) {
@@ -530,7 +532,7 @@ __global__ void __launch_bounds__(kAttnThreads, kBlocks) nibble_attention_kernel
                 begins = cur.left == cur.rows;
 #pragma unroll
                 for (int j = 0; j < D / 16; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
-                ref[0] = ref[1] = kLowest;
+                minus.x = minus.y = __uint_as_float(0x7F800000u);    // (the first product is above it)
                 l = make_float2(0.f, 0.f);
                 fresh = false;
             }
@@ -592,17 +594,11 @@ __global__ void __launch_bounds__(kAttnThreads, kBlocks) nibble_attention_kernel
                 top[0] = max3(top[0], z[s][0], z[s][2]);
                 top[1] = max3(top[1], z[s][1], z[s][3]);
             }
-            if (__any_sync(0xFFFFFFFFu, fmaf(top[0], Q.factor[0], -ref[0]) > kMostExponent || fmaf(top[1], Q.factor[1], -ref[1]) > kMostExponent)) {
-                top[0] = max_over_rows(top[0]);
-                top[1] = max_over_rows(top[1]);
-                float c[2];
-#pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    // (rounded up: however large the logits, no weight is above 2^15)
-                    const float next_ref = fmaxf(__fadd_ru(__fmul_ru(top[q], Q.factor[q]), -kWeightExponent), ref[q]);
-                    c[q] = tc::ex2(ref[q] - next_ref);
-                    ref[q] = next_ref;
-                }
+            constexpr float kRoom = kMostExponent - kWeightExponent;
+            if (__any_sync(0xFFFFFFFFu, (top[0] + minus.x) * Q.factor[0] > kRoom || (top[1] + minus.y) * Q.factor[1] > kRoom)) {
+                const float2 next = make_float2(fminf(-max_over_rows(top[0]), minus.x), fminf(-max_over_rows(top[1]), minus.y));
+                const float c[2] = {tc::ex2((next.x - minus.x) * Q.factor[0]), tc::ex2((next.y - minus.y) * Q.factor[1])};
+                minus = next;
                 l = tc::fmul2(l, make_float2(c[0], c[1]));
 #pragma unroll
                 for (int j = 0; j < D / 16; ++j) { o[j][0] *= c[0]; o[j][1] *= c[1]; o[j][2] *= c[0]; o[j][3] *= c[1]; }
@@ -619,13 +615,13 @@ __global__ void __launch_bounds__(kAttnThreads, kBlocks) nibble_attention_kernel
                 const int ka = 2 * t ^ (t & 1), kb = (2 * t + 1) ^ (t & 1);      // the keys at places 2 t and 2 t + 1
                 const uint8_t *codes = ring + take * L::kHalf + r * (D / 16), *scales = ring + take * L::kHalf + L::kCodes + (D == 128 ? r : r >> 1);
                 const uint8_t *codes_of[2] = {codes + ka * (D / 2), codes + kb * (D / 2)}, *scales_of[2] = {scales + ka * (D / 16), scales + kb * (D / 16)};
-                const float2 factor = make_float2(Q.factor[0], Q.factor[1]), minus = make_float2(-ref[0], -ref[1]);
+                const float2 factor = make_float2(Q.factor[0], Q.factor[1]), most = make_float2(kWeightExponent, kWeightExponent);
 #pragma unroll
                 for (int s = 0; s < kSubs; ++s) {
                     uint32_t p[2], q[2];                             // weights of keys at places 0 to 7 and 8 to 15; their rests
 #pragma unroll
                     for (int b = 0; b < 2; ++b) {
-                        float2 x = tc::ffma2(make_float2(z[s][2 * b], z[s][2 * b + 1]), factor, minus);
+                        float2 x = tc::ffma2(tc::fadd2(make_float2(z[s][2 * b], z[s][2 * b + 1]), minus), factor, most);
                         x = make_float2(tc::ex2(x.x), tc::ex2(x.y));
                         l = tc::fadd2(l, x);
                         p[b] = half2_of(x.x, x.y);
@@ -682,6 +678,8 @@ __global__ void __launch_bounds__(kAttnThreads, kBlocks) nibble_attention_kernel
                 for (int q = 0; q < 2; ++q)
 #pragma unroll
                     for (int k = 4; k < 32; k <<= 1) sum[q] += __shfl_xor_sync(0xFFFFFFFFu, sum[q], k);
+                // (a record's maximum: all weights of a head are 2^10 for a logit at it, or all 2^14; equal products have equal ones)
+                const float most[2] = {-minus.x * Q.factor[0], -minus.y * Q.factor[1]};
                 if (begins && last) {
 #pragma unroll
                     for (int q = 0; q < 2; ++q) {
@@ -696,12 +694,12 @@ __global__ void __launch_bounds__(kAttnThreads, kBlocks) nibble_attention_kernel
                     }
                 } else if (!begins) {
                     me.flags |= last ? kFront | kEnds : kFront; me.fu = cur.u; me.fh = cur.h;
-                    put_record<D>(record, o, ref, sum);
+                    put_record<D>(record, o, most, sum);
                 } else {
                     me.flags |= kBack; me.bu = cur.u; me.bh = cur.h;
                     const uint32_t tiles = tiles_of(cur.rows), done = (cur.rows - cur.left) / kTile;
                     if (A.share == kCutHeads) me.blocks = cut.per ? (tiles + cut.per - 1) / cut.per : (w0 + i - done + tiles - 1) / cut.share - blockIdx.x + 1;
-                    put_record<D>(reinterpret_cast<float *>(ring), o, ref, sum);       // (no copy is on its way any more)
+                    put_record<D>(reinterpret_cast<float *>(ring), o, most, sum);       // (no copy is on its way any more)
                 }
                 fresh = true;
             }
