@@ -434,7 +434,8 @@ flowmm_status flowmm_nibble_attention(const flowmm_cache_params *p, const void *
  * adjoint = 1 turns by -t: the gradient's way back, and for amplitude 1 the inverse (keys taken out of a cache and put to other positions).
  *
  * flowmm_rotary_table writes what the call needs of the frequencies, once for a model: table [R / 2] uint64, pair i's f_i / (2 pi) as a 64-bit fraction of a
- * turn.  Positions are multiplied with it modulo whole turns, so any int32 position has its angle within 2^-31 turns; cos and sin and the products are fp32.
+ * turn, within 2^-63.  Positions are multiplied with it modulo whole turns, so any int32 position has its angle within 2^-31 turns (a factor below 1 divides both of
+ * these); cos and sin and the products are fp32.
  *
  *   q, q_out [U, Hq, T, D], k, k_out [U, Hkv, T, D] with the element strides given, T = n_rows; q with q_out, or k with k_out, may be NULL (not both).
  *   q_out may be q (the same strides), k_out may be k; otherwise outputs must not overlap inputs.

@@ -1930,10 +1930,11 @@ extern "C" flowmm_status flowmm_rotary_table(const flowmm_rotary_params *p, uint
     if (!table) return FLOWMM_ERR_NULL;
     if (reinterpret_cast<uintptr_t>(table) & 7) return FLOWMM_ERR_ALIGN;
     FLOWMM_TRY(check_device());
-    rotary::TableArgs a;
-    a.phase = reinterpret_cast<unsigned long long *>(table); a.R = p->rotary_dim ? p->rotary_dim : p->head_dim; a.scaling = p->scaling;
-    a.base = p->base; a.factor = p->factor; a.low = p->low; a.high = p->high; a.trained = p->trained;
-    launch(rotary::rotary_table_kernel, 1, 64, 0, st, a);
+    rotary::TableArgs a = {};
+    const int R = p->rotary_dim ? p->rotary_dim : p->head_dim;
+    a.to = reinterpret_cast<unsigned long long *>(table); a.pairs = R / 2;
+    for (int i = 0; i < a.pairs; ++i) a.phase[i] = rotary::phase_of(i, R, p->scaling, p->base, p->factor, p->low, p->high, p->trained);
+    launch(rotary::rotary_table_kernel, 1, rotary::kMostPairs, 0, st, a);
     FLOWMM_LAUNCHED("rotary_table");
     return FLOWMM_OK;
 }

@@ -2,33 +2,44 @@
 //   (a, b) -> m (a cos - b sin, b cos + a sin),   angle = position * frequency of the pair
 //
 // A pair's frequency is held as what a position adds to its phase, in turns, as a 64-bit fraction: position times that, modulo 2^64, is the phase,
-// whole turns gone by themselves and nothing lost at far positions (an angle formed in fp32 is off by 0.03 at position 10^6).
+// whole turns gone by themselves (an angle formed in fp32 is off by 0.03 at position 10^6).  The fraction is within 2^-63 of the true one (factors of one and more), so
+// any 32-bit position has its phase, 32 bits of it, within 2^-31 turns.
 #pragma once
+#include <cfloat>
+#include <cmath>
+
 #include "common.cuh"
+#include "flowmm.h"
 
 namespace flowmm {
 namespace rotary {
 
+constexpr int kMostPairs = 64;         // heads of 128
 struct TableArgs {
-    unsigned long long *phase;         // [R / 2]
-    int R, scaling;                    // flowmm_rotary_scaling
-    double base, factor, low, high, trained;
+    unsigned long long *to;            // [pairs]
+    unsigned long long phase[kMostPairs];
+    int pairs;
 };
+
+// The fractions, on the host: a double has 53 bits, 2^-56 of a turn, which position 2^31 makes 2^-25; numbers of 64 significant bits have what is asked for.  (A factor
+// below one makes more turns, and the fraction's last bits go by that.)
+static_assert(LDBL_MANT_DIG >= 64, "64 significant bits");
+inline unsigned long long phase_of(int i, int R, int scaling, double base, double factor, double low, double high, int trained) {
+    constexpr long double kTurn = 6.283185307179586476925286766559005768394L;
+    long double f = powl(base, -2.0L * i / R);
+    if (scaling == FLOWMM_ROTARY_LINEAR) {
+        f /= factor;
+    } else if (scaling == FLOWMM_ROTARY_BY_PARTS) {
+        const long double kept = fminl(1.0L, fmaxl(0.0L, (trained * f / kTurn - low) / ((long double)high - low)));
+        f = kept * f + (1.0L - kept) * (f / factor);
+    }
+    const long double turns = f / kTurn, fraction = rintl(ldexpl(turns - floorl(turns), 64));
+    return fraction < 18446744073709551616.0L ? (unsigned long long)fraction : 0ull;
+}
 
 __global__ void rotary_table_kernel(const TableArgs A) {
     predecessor_done();
-    const int i = blockIdx.x * blockDim.x + threadIdx.x;
-    if (i >= A.R / 2) return;
-    constexpr double kTurn = 6.283185307179586476925;
-    double f = pow(A.base, -2.0 * i / A.R);
-    if (A.scaling == 1) {
-        f /= A.factor;
-    } else if (A.scaling == 2) {
-        const double kept = fmin(1.0, fmax(0.0, (A.trained * f / kTurn - A.low) / (A.high - A.low)));
-        f = kept * f + (1.0 - kept) * (f / A.factor);
-    }
-    const double turns = f / kTurn;
-    A.phase[i] = (unsigned long long)ldexp(turns - floor(turns), 64);
+    if ((int)threadIdx.x < A.pairs) A.to[threadIdx.x] = A.phase[threadIdx.x];
 }
 
 struct Args {
