@@ -601,7 +601,7 @@ def _rotary_call(p: RotaryParams):
     own, at = (torch_dtype(p.dtype),), _CRotaryParams
     return _keep_call(p, "flowmm_rotary", p.c(), False, (
         ("q", q, own, at.q_stride.offset, True), ("k", k, own, at.k_stride.offset, True),
-        ("positions", (p.n_units, 1 if p.sections is None else 3, p.n_rows), _INT32, 0, False), ("table", (p.pairs,), (torch.int64,), 0, False),
+        ("positions", (p.n_units, 1 if p.sections is None else 3, p.n_rows), _INT32, 0, False, p.sections is None), ("table", (p.pairs,), (torch.int64,), 0, False),
         ("q_out", q, own, at.q_out_stride.offset, True), ("k_out", k, own, at.k_out_stride.offset, True)))
 
 

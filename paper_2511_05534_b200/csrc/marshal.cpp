@@ -29,6 +29,7 @@ struct Argument {
     std::vector<c10::ScalarType> types;
     int dense;                               // where in the params the strides of a tensor of rows are, in bytes; else 0: contiguous
     bool optional;                           // may be None
+    bool no_middle;                          // the middle one of three sizes, 1, may be left out
 };
 // One entry point with one set of params: what its tensors have to look like, in the order of its pointers; should it have a workspace, that is the last one.
 struct Call {
@@ -44,7 +45,7 @@ constexpr size_t kFewestPointers = 6, kMostPointers = 9;
 
 void drop(PyObject *capsule) { delete static_cast<Call *>(PyCapsule_GetPointer(capsule, kCapsule)); }
 
-// make(what, function's address, params' address and size, workspace, ((name, shape, types, dense, optional), ...)) -> the call's handle
+// make(what, function's address, params' address and size, workspace, ((name, shape, types, dense, optional[, no_middle]), ...)) -> the call's handle
 PyObject *make(PyObject *, PyObject *args) {
     const char *what;
     unsigned long long function, params;
@@ -61,18 +62,19 @@ PyObject *make(PyObject *, PyObject *args) {
         for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(list); ++i) {
             const char *name;
             PyObject *shape, *types;
-            int dense, optional;
-            if (!PyArg_ParseTuple(PyTuple_GET_ITEM(list, i), "sO!O!ip", &name, &PyTuple_Type, &shape, &PyTuple_Type, &types, &dense, &optional)) {
+            int dense, optional, no_middle = 0;
+            if (!PyArg_ParseTuple(PyTuple_GET_ITEM(list, i), "sO!O!ip|p", &name, &PyTuple_Type, &shape, &PyTuple_Type, &types, &dense, &optional, &no_middle)) {
                 Py_DECREF(capsule);
                 return nullptr;
             }
-            Argument a{name, {}, {}, dense, optional != 0};
+            Argument a{name, {}, {}, dense, optional != 0, no_middle != 0};
             for (Py_ssize_t j = 0; j < PyTuple_GET_SIZE(shape); ++j) a.shape.push_back(PyLong_AsLongLong(PyTuple_GET_ITEM(shape, j)));
             for (Py_ssize_t j = 0; j < PyTuple_GET_SIZE(types); ++j) {
                 PyObject *type = PyTuple_GET_ITEM(types, j);
                 if (!THPDtype_Check(type)) PyErr_SetString(PyExc_TypeError, "types must be torch dtypes");
                 else a.types.push_back(reinterpret_cast<THPDtype *>(type)->scalar_type);
             }
+            if (!PyErr_Occurred() && no_middle && a.shape.size() != 3) PyErr_SetString(PyExc_ValueError, "no_middle wants three sizes");
             if (PyErr_Occurred()) { Py_DECREF(capsule); return nullptr; }
             call->arguments.push_back(std::move(a));
         }
@@ -111,7 +113,7 @@ PyObject *run(PyObject *, PyObject *const *args, Py_ssize_t n) {
             const auto sizes = t.sizes(), strides = t.strides();
             bool same = sizes.size() == a.shape.size();
             for (size_t d = 0; same && d < sizes.size(); ++d) same = a.shape[d] < 0 || sizes[d] == a.shape[d];
-            if (!same && a.shape.size() == 3 && a.shape[1] == 1 && sizes.size() == 2) same = sizes[0] == a.shape[0] && sizes[1] == a.shape[2];
+            if (!same && a.no_middle && sizes.size() == 2) same = sizes[0] == a.shape[0] && sizes[1] == a.shape[2];
             bool type = false;
             for (c10::ScalarType s : a.types) type = type || t.scalar_type() == s;
             if (!same || !type) {
