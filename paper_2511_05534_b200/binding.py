@@ -607,15 +607,18 @@ def _rotary_call(p: RotaryParams):
 
 def alloc_rotary_table(p: RotaryParams, device="cuda") -> torch.Tensor:
     """The phases of the pairs, written by flowmm_rotary_table; once for a model."""
-    table = torch.empty(p.pairs, dtype=torch.int64, device=device)
-    flowmm_rotary_table(p, table)
+    with torch.cuda.device(device):          # (the table's, which need not be the current one)
+        table = torch.empty(p.pairs, dtype=torch.int64, device=device)
+        flowmm_rotary_table(p, table)
     return table
 
 
 def flowmm_rotary_table(p: RotaryParams, table):
-    """table [pairs] int64: 64-bit fractions of a turn."""
+    """table [pairs] int64, on the current device: 64-bit fractions of a turn."""
     if table.dtype != torch.int64 or table.shape != (p.pairs,) or not table.is_contiguous():
         raise ValueError("flowmm_rotary_table: table must be a contiguous int64 tensor of %d elements" % p.pairs)
+    if table.is_cuda and table.device.index != torch.cuda.current_device():
+        raise ValueError("flowmm_rotary_table: table is not on the current device")
     cp = p.c()
     _check(load().flowmm_rotary_table(ctypes.byref(cp), _p(table), _stream()), "flowmm_rotary_table")
 
