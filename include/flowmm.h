@@ -418,6 +418,11 @@ flowmm_status flowmm_nibble_load(const flowmm_cache_params *p, const void *k_pag
  * flowmm_decode_attention over the paged 4-bit cache: o = softmax(scale * q . K^T) V over the rows[u] rows of each unit, zero for a unit without rows.  What
  * stands behind a unit's last row (scales of NaN too) has no influence.  Several new queries of a sequence are units that share a row of the block table
  * and differ in rows.  Logits may be as large as fp32 holds them (2^127 in units of log 2; beyond, outputs may be NaN).
+ * Accuracy: sums and the softmax are fp32, both products go to the tensor cores as fp16 numbers.  K and V are that exactly.  A bf16 query is, down to 2^-31 of its
+ * head's largest element; an fp32 one is two such numbers, within 2^-22 of itself or 2^-39 of the largest.  A weight is rounded to one fp16 number for bf16 rows,
+ * within 2^-11 of itself down to 2^-24 of the largest weight, and to two for fp32, within 2^-21 down to 2^-18 of the largest; below that an error stays what it is
+ * there.  The sum that weights are divided by takes them unrounded.  Random keys and values, root mean square of the error relative to the output's: bf16 1.7e-3, its
+ * own last rounding; fp32 2.5e-7 to 2.9e-7, where sums in fp32 throughout have 1.0e-7.
  *   q, out [U, Hq, D] dense, element type `dtype`
  */
 flowmm_status flowmm_nibble_attention(const flowmm_cache_params *p, const void *q, const void *k_pages, const void *v_pages,
@@ -430,12 +435,15 @@ flowmm_status flowmm_nibble_attention(const flowmm_cache_params *p, const void *
  * The first R = rotary_dim channels of a head are R / 2 pairs (a, b), pair i at angle t = position * f_i:
  *   (a, b) -> amplitude * (a cos t - b sin t, b cos t + a sin t);   the other D - R channels are copied
  *   f_i = base^(-2 i / R), by `scaling`: PLAIN as it is; LINEAR f_i / factor; BY_PARTS g f_i + (1 - g) f_i / factor with
- *         g = min(1, max(0, (trained * f_i / (2 pi) - low) / (high - low))): by how many turns the pair makes over the context that was trained on
+ *         g = min(1, max(0, (trained * f_i / (2 pi) - low) / (high - low))): by how many turns the pair makes over the context that was trained on.
+ *         Models whose g is a ramp over the pair's number i, between two rounded numbers, are not these: with a factor of 4, 1, 32 and 32 768 trained positions a middle
+ *         frequency is up to 1.7 times the other.  For them, and for any other frequencies, the caller writes the table.
  * adjoint = 1 turns by -t: the gradient's way back, and for amplitude 1 the inverse (keys taken out of a cache and put to other positions).
  *
  * flowmm_rotary_table writes what the call needs of the frequencies, once for a model: table [R / 2] uint64, pair i's f_i / (2 pi) as a 64-bit fraction of a
  * turn, within 2^-63.  Positions are multiplied with it modulo whole turns, so any int32 position has its angle within 2^-31 turns (a factor below 1 divides both of
- * these); cos and sin and the products are fp32.
+ * these); cos and sin and the products are fp32.  A table of the caller's own is as good: round(2^64 (f_i / (2 pi) mod 1)) for each pair; flowmm_rotary looks at
+ * the table alone, not at base, scaling and what goes with it (which have to be valid all the same).
  *
  *   q, q_out [U, Hq, T, D], k, k_out [U, Hkv, T, D] with the element strides given, T = n_rows; q with q_out, or k with k_out, may be NULL (not both).
  *   q_out may be q (the same strides), k_out may be k; otherwise outputs must not overlap inputs.

@@ -10,8 +10,8 @@
 //   O^T[channel, head] = V^T W^T:  16 channels on the wide side; the weights go from the first product's layout to the second's by a transpose in registers
 // Which channel and which key stand at which place of an operand is free as long as both operands agree: a lane takes 16 neighbouring bytes of a K row and
 // 8 of a V row, one scale for all channels that it has of a V row, and ends with 16 neighbouring channels of two query heads.
-// bf16: a query is an fp16 number times a power of two exactly, a weight is rounded to fp16 (2^-12, where the output is rounded to 2^-9); fp32: both are the
-// sum of two fp16 numbers, each product is two.  The largest weight is 2^10 to 2^15 (fp32: 2^14), so that fp16 holds others to full precision down to 2^-24 of
+// bf16: a query is an fp16 number times a power of two exactly, a weight is rounded to fp16 (2^-11, where the output is rounded to 2^-8: one element in 70 to 700 becomes
+// its neighbour by that; the sum that divides takes weights unrounded, as it has them in fp32); fp32: both are the sum of two fp16 numbers, each product is two.  The largest weight is 2^10 to 2^15 (fp32: 2^14), so that fp16 holds others to full precision down to 2^-24 of
 // it, and two of them to 2^-21 of themselves down to 2^-18 of it, both to 2^-35 (fp32: 2^-39) of it below.
 //
 // A warp works by itself: tiles of 64 rows come into its own ring of three half tiles (K and V in turn), 16 bytes a lane and copy, two ahead; it keeps the
