@@ -17,10 +17,10 @@
 // A warp works by itself: tiles of 64 rows come into its own ring of three half tiles (K and V in turn), 16 bytes a lane and copy, two ahead; it keeps the
 // maximum, the sum and the output of the head that it is at.  Twelve warps are on an SM, as many as 168 registers and 18 KB of shared memory each allow.
 // (32 rows a tile and sixteen warps of 128 registers spilled: 101 us where this took 84; ten warps 94; a tile's V together with the next one's K, in a ring of four,
-// 85 where this took 79; loops over the 16 keys not unrolled 87.)  What it costs is instructions: 1000 for a tile of
+// 85 where this took 79; loops over the 16 keys not unrolled 87.)  What it costs is instructions: 1040 for a tile of
 // 128 channels, of which 860 widen and multiply, so addresses are formed from one page number for a tile where pages have 64 rows (bulk copies by one thread
 // took 40 instructions each), and outputs are rescaled only where fp16 asks for it.
-// Measured: 16 sequences of up to 33 792 rows, 8 heads of 8 query heads, 386 MB, 80 us, 60 of memory: 5.5 TB/s while all blocks run, 6 us from the launch to the first
+// Measured: 16 sequences of up to 33 792 rows, 8 heads of 8 query heads, 386 MB, 79 us, 60 of memory: 5.5 TB/s while all blocks run, 6 us from the launch to the first
 // tile, and an end of 14 us in which blocks finish one after the other, since equal pieces take SMs 76 to 90 us.  64 sequences of up to 1690 rows, 74 MB, 24.8 us, 11.5
 // of memory.  One sequence of 218 rows 5.0 us: lengths and table 0.6, the first tile 0.9, its products 1.2, joining the warps' records 0.9, the launch.
 #pragma once
