@@ -421,8 +421,9 @@ flowmm_status flowmm_nibble_load(const flowmm_cache_params *p, const void *k_pag
  * Accuracy: sums and the softmax are fp32, both products go to the tensor cores as fp16 numbers.  K and V are that exactly.  A bf16 query is, down to 2^-31 of its
  * head's largest element; an fp32 one is two such numbers, within 2^-22 of itself or 2^-39 of the largest.  A weight is rounded to one fp16 number for bf16 rows,
  * within 2^-11 of itself down to 2^-24 of the largest weight, and to two for fp32, within 2^-21 down to 2^-18 of the largest; below that an error stays what it is
- * there.  The sum that weights are divided by takes them unrounded.  Random keys and values, root mean square of the error relative to the output's: bf16 1.7e-3, its
- * own last rounding; fp32 2.5e-7 to 2.9e-7, where sums in fp32 throughout have 1.0e-7.
+ * there.  The sum that weights are divided by takes them unrounded.  Matrix instructions cut their sums off: for fp32 rows these are 16 keys long and added to the
+ * nearest, for bf16 as long as what a warp has of a sequence, 2^-23 of them at most for 16 keys (half a million rows of one warp to reach the output's rounding).  Random
+ * keys and values, root mean square of the error relative to the output's: bf16 1.7e-3, its own last rounding; fp32 0.7e-7 to 2.5e-7, as with sums in fp32 throughout.
  *   q, out [U, Hq, D] dense, element type `dtype`
  */
 flowmm_status flowmm_nibble_attention(const flowmm_cache_params *p, const void *q, const void *k_pages, const void *v_pages,
